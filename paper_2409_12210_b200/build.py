@@ -16,7 +16,7 @@ LIB = os.path.join(PKG, "libmodse.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "-shared",
-         "-Xcompiler", "-fPIC"]
+         "-Xcompiler", "-fPIC", "--threads", "0"]
 
 
 def sources():
