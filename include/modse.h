@@ -306,6 +306,43 @@ modse_status_t modse_stage_timing_begin(modse_layer_t *layer, int max_calls);
 modse_status_t modse_stage_timing_end(modse_layer_t *layer, float *ms_out, int *calls_out);
 const char *modse_stage_name(int stage);
 
+/* ---- operators around the layer ------------------------------------------
+ * What a transformer block needs on either side of modse_forward/backward.
+ * None of them uses a layer object; tensors are row-major and contiguous unless
+ * said otherwise, every pointer 16-byte aligned unless said otherwise, every
+ * workspace 256-byte aligned and in use by one call at a time (two calls that may
+ * overlap, or two captured graphs that may, need one each).  Results do not
+ * depend on the order in which blocks run.  (The paper fixes none of them: its
+ * blocks are Llama-2's, Sec. 4.1, whose pre-norm residual form this is.)      */
+
+/* Residual addition and root-mean-square norm, the step that makes a sub-layer's
+ * input (x of modse_forward) out of the residual stream and the previous
+ * sub-layer's output:
+ *   s = x + residual,  y = s / sqrt(mean_c(s_c^2) + eps) * weight,
+ *   y_scale[t] = max_c |y_tc| / 448,  y_e4m3 = e4m3(y / y_scale).
+ * x, residual, sum, y [T, d] and weight [d] in `dtype`; d a multiple of 8, at most
+ * 32768 (else MODSE_ERR_UNSUPPORTED).  residual NULL: s = x; weight NULL: ones.
+ * Outputs, each of them optional, at least one: sum (may be x or residual
+ * itself), y, and y_e4m3 [T, d] bytes together with y_scale [T].  The norm is
+ * taken from the fp32 sum, not from its rounding into `sum`; each output is
+ * rounded once.  A row of zeros has scale 0 and zero bytes; a row that holds a NaN
+ * has scale NaN.                                                             */
+modse_status_t modse_add_rms_norm(modse_dtype_t dtype, int n_tokens, int d_model, const void *x, const void *residual,
+                                  const void *weight, float eps, void *sum, void *y, void *y_e4m3, float *y_scale,
+                                  void *cuda_stream);
+
+/* Gradient of the above as a function of `sum` (as forward wrote it): dy [T, d] is
+ * the gradient of y, dsum [T, d] (may be NULL) the one that reaches s past the
+ * norm, along the residual stream;
+ *   dx = rstd (u - s rstd^2 mean_c(u_c s_c)) + dsum,  u = dy weight,
+ * is the gradient of x and of residual alike (dx may be dy or dsum itself);
+ * dweight [d] fp32 (may be NULL, then no workspace is needed) = sum_t dy s rstd,
+ * overwritten, summed in a fixed order.                                      */
+size_t modse_add_rms_norm_backward_workspace_bytes(int n_tokens, int d_model);
+modse_status_t modse_add_rms_norm_backward(modse_dtype_t dtype, int n_tokens, int d_model, const void *sum,
+                                           const void *weight, float eps, const void *dy, const void *dsum, void *dx,
+                                           float *dweight, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 /* Debugging aid, process-wide: when on, bf16 layers run their grouped GEMMs on
  * the fp32-FMA kernels of the fp32 type (with bf16 storage) instead of the
  * tensor-core kernels - slow, meant for cross-checking.  Such a forward must

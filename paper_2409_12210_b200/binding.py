@@ -134,6 +134,13 @@ def load():
     lib.modse_set_fusion.argtypes = [vp, ci]
     lib.modse_get_fusion.restype = ci
     lib.modse_get_fusion.argtypes = [vp]
+    cf = ctypes.c_float
+    lib.modse_add_rms_norm.restype = ci
+    lib.modse_add_rms_norm.argtypes = [ci, ci, ci, vp, vp, vp, cf, vp, vp, vp, vp, vp]
+    lib.modse_add_rms_norm_backward_workspace_bytes.restype = sz
+    lib.modse_add_rms_norm_backward_workspace_bytes.argtypes = [ci, ci]
+    lib.modse_add_rms_norm_backward.restype = ci
+    lib.modse_add_rms_norm_backward.argtypes = [ci, ci, ci, vp, vp, cf, vp, vp, vp, vp, vp, sz, vp]
     lib.modse_debug_use_fma_path.restype = None
     lib.modse_debug_use_fma_path.argtypes = [ci]
     _lib = lib
@@ -220,6 +227,78 @@ def _dtype_code(t):
     if t.dtype == torch.bfloat16:
         return MODSE_BF16
     raise TypeError(f"unsupported dtype {t.dtype}")
+
+
+# ---- operators around the layer ---------------------------------------------
+def _buffer(name, t, shape, dtype, device):
+    """Device address of a tensor that has to have this shape, type and device (None: a null pointer)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+    return t.data_ptr()
+
+
+def _current_stream(name, t):
+    """Raw current stream of t's device, which has to be the current CUDA device."""
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: expected a tensor on the current CUDA device, got one on {t.device}")
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _rows(name, t):
+    if t.dim() != 2:
+        raise ValueError(f"{name}: expected two dimensions, got shape {tuple(t.shape)}")
+    return t.shape
+
+
+def add_rms_norm(x, residual, weight, eps: float, *, sum_out=None, y=None, y8=None, y_scale=None) -> None:
+    """modse_add_rms_norm on the current stream: ``sum_out = x + residual`` and its root-mean-square norm times
+    ``weight`` into ``y`` and, in 8 bits (torch.float8_e4m3fn) with one fp32 scale a row, into ``y8`` and ``y_scale``.
+    ``residual`` and ``weight`` may be None, and so may any output the caller does not want."""
+    import torch
+    T, d = shape = _rows("x", x)
+    dt, dev = x.dtype, x.device
+    code = _dtype_code(x)
+    stream = _current_stream("x", x)
+    st = load().modse_add_rms_norm(
+        code, T, d, _buffer("x", x, shape, dt, dev), _buffer("residual", residual, shape, dt, dev),
+        _buffer("weight", weight, (d,), dt, dev), eps, _buffer("sum_out", sum_out, shape, dt, dev),
+        _buffer("y", y, shape, dt, dev), _buffer("y8", y8, shape, torch.float8_e4m3fn, dev),
+        _buffer("y_scale", y_scale, (T,), torch.float32, dev), stream)
+    if st != MODSE_OK:
+        raise ModseError(st, "modse_add_rms_norm")
+
+
+def add_rms_norm_backward_workspace_bytes(n_tokens: int, d_model: int) -> int:
+    return int(load().modse_add_rms_norm_backward_workspace_bytes(n_tokens, d_model))
+
+
+def add_rms_norm_backward(s, weight, eps: float, dy, dsum, dx, dweight=None, workspace=None) -> None:
+    """modse_add_rms_norm_backward: ``s`` is the sum forward wrote, ``dsum`` (or None) the gradient that reaches it past
+    the norm; ``dx`` receives the gradient of x and of the residual alike, ``dweight`` (fp32, or None) the weight's."""
+    import torch
+    T, d = shape = _rows("s", s)
+    dt, dev = s.dtype, s.device
+    code = _dtype_code(s)
+    stream = _current_stream("s", s)
+    st = load().modse_add_rms_norm_backward(
+        code, T, d, _buffer("s", s, shape, dt, dev), _buffer("weight", weight, (d,), dt, dev), eps,
+        _buffer("dy", dy, shape, dt, dev), _buffer("dsum", dsum, shape, dt, dev), _buffer("dx", dx, shape, dt, dev),
+        _buffer("dweight", dweight, (d,), torch.float32, dev), *_workspace(workspace, dev), stream)
+    if st != MODSE_OK:
+        raise ModseError(st, "modse_add_rms_norm_backward")
+
+
+def _workspace(t, device):
+    """(address, bytes) of a workspace tensor."""
+    if t is None:
+        return None, 0
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on {device}, got one on {t.device}")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 class ModseLayer:

@@ -108,6 +108,11 @@ cudaError_t launch_canaries(void *ws, const WsLayout &L, bool check, int *status
 cudaError_t launch_aux_loss(const LayerMeta &m, int T, int nblk_bwd, const WsPtrs &p, float alpha, float *loss,
                             float *f, float *P, cudaStream_t s, int *launches);
 
+// ---- shared by the operators around the layer (norm_kernels.cu) ----
+int device_sms();      // SMs of the current device (148 where the question fails)
+// out[c] = sum over r of part[r][c], in a fixed order
+cudaError_t launch_column_sum(const float *part, int n_rows, int d, float *out, cudaStream_t s);
+
 // ---- fp32-FMA grouped GEMMs and SwiGLU elementwise (simt_gemm.cu) ----
 enum GemmKind : int {
     kUpGate = 0,      // C[cp_e, h_e]  = xp_e  . W_e^T          (W = w_gate or w_up)

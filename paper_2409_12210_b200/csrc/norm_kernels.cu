@@ -1,0 +1,508 @@
+// Residual addition with root-mean-square norm, forward (16/32-bit rows and 8-bit rows with a scale a row) and backward.
+//
+//   s = x + r;  rstd = 1 / sqrt(mean_c s_c^2 + eps);  y_c = s_c rstd w_c;  scale = max_c |y_c| / 448;  q_c = e4m3(y_c / scale)
+//   backward, with u = dy w:  dx = rstd (u - s rstd^2 mean_c(u_c s_c)) + dsum;   dw_c = sum_t dy_tc s_tc rstd_t
+//
+// Both passes are bound by HBM: a row is read once, held in registers while its sums are formed, and written once.
+// "Vector" below: 8 consecutive elements of a row (16 bytes of bf16, 32 of fp32).  A row belongs to TPR threads of a
+// block, VPT vectors each; the choice of (TPR, VPT) is in pick_shape.  All sums are fp32 of fp32 terms.
+#include <cuda_fp8.h>
+
+#include "modse_internal.h"
+
+namespace modse {
+namespace {
+
+constexpr float kE4m3Max = 448.f;
+constexpr int kNormBlock = 256;
+constexpr int kNormMaxD = 32768;
+
+template <typename T> struct Vec;                      // 8 elements as they lie in memory
+template <> struct Vec<__nv_bfloat16> { uint4 a; };
+template <> struct Vec<float> { float4 a, b; };
+
+__device__ __forceinline__ void load_vec(Vec<__nv_bfloat16> &v, const __nv_bfloat16 *p) { v.a = *reinterpret_cast<const uint4 *>(p); }
+__device__ __forceinline__ void load_vec(Vec<float> &v, const float *p)
+{
+    v.a = *reinterpret_cast<const float4 *>(p);
+    v.b = *reinterpret_cast<const float4 *>(p + 4);
+}
+__device__ __forceinline__ void zero_vec(Vec<__nv_bfloat16> &v) { v.a = make_uint4(0, 0, 0, 0); }
+__device__ __forceinline__ void zero_vec(Vec<float> &v) { v.a = v.b = make_float4(0, 0, 0, 0); }
+__device__ __forceinline__ void unpack(const Vec<__nv_bfloat16> &v, float (&f)[8])
+{
+    const uint32_t w[4] = {v.a.x, v.a.y, v.a.z, v.a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(w[i] << 16);
+        f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void unpack(const Vec<float> &v, float (&f)[8])
+{
+    f[0] = v.a.x; f[1] = v.a.y; f[2] = v.a.z; f[3] = v.a.w;
+    f[4] = v.b.x; f[5] = v.b.y; f[6] = v.b.z; f[7] = v.b.w;
+}
+__device__ __forceinline__ void store_vec(__nv_bfloat16 *p, const float (&f)[8])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __nv_bfloat162 t = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+        w[i] = *reinterpret_cast<uint32_t *>(&t);
+    }
+    *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void store_vec(float *p, const float (&f)[8])
+{
+    *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    *reinterpret_cast<float4 *>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+
+// Sum over the TPR threads of a row (every one of them gets it; fixed order).  `slot`: this row's TPR / 32 words.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float *slot)
+{
+    v = warp_sum(v);
+    if constexpr (TPR == 32) return v;
+    constexpr int W = TPR / 32;
+    const int w = (threadIdx.x % TPR) >> 5;
+    if ((threadIdx.x & 31) == 0) slot[w] = v;
+    __syncthreads();
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) s += slot[i];
+    return s;
+}
+template <int TPR>
+__device__ __forceinline__ unsigned row_max(unsigned v, unsigned *slot)
+{
+    v = __reduce_max_sync(0xFFFFFFFFu, v);
+    if constexpr (TPR == 32) return v;
+    constexpr int W = TPR / 32;
+    const int w = (threadIdx.x % TPR) >> 5;
+    if ((threadIdx.x & 31) == 0) slot[w] = v;
+    __syncthreads();
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) m = max(m, slot[i]);
+    return m;
+}
+
+struct NormArgs {
+    const void *x, *residual, *weight;
+    void *sum, *y;
+    unsigned char *q;
+    float *q_scale;
+    int T, d;
+    float eps;
+};
+
+template <typename T, int TPR, int VPT>
+__global__ void __launch_bounds__(TPR < kNormBlock ? kNormBlock : TPR)
+add_rms_norm_kernel(const NormArgs a)
+{
+    constexpr int kThreads = TPR < kNormBlock ? kNormBlock : TPR;
+    constexpr int kRows = kThreads / TPR;
+    __shared__ float sums[kThreads / 32];
+    __shared__ unsigned maxs[kThreads / 32];
+    const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR;
+    const int row = blockIdx.x * kRows + group;
+    const bool live = row < a.T;                  // rows past the end take part in the barriers and touch no memory
+    const int nv = a.d / 8;
+    const size_t base = (size_t)(live ? row : 0) * a.d;
+    Vec<T> xv[VPT], rv[VPT];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        const int v = lane + i * TPR;
+        if (live && v < nv) {
+            load_vec(xv[i], (const T *)a.x + base + 8 * (size_t)v);
+            if (a.residual) load_vec(rv[i], (const T *)a.residual + base + 8 * (size_t)v);
+            else zero_vec(rv[i]);
+        } else {
+            zero_vec(xv[i]);
+            zero_vec(rv[i]);
+        }
+    }
+    float s[VPT][8];
+    float acc = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        float f[8];
+        unpack(xv[i], s[i]);
+        unpack(rv[i], f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (a.residual) s[i][j] += f[j];      // (-0) + (+0) would lose the sign of a zero where there is no residual
+            acc = fmaf(s[i][j], s[i][j], acc);
+        }
+        const int v = lane + i * TPR;
+        if (a.sum && live && v < nv) store_vec((T *)a.sum + base + 8 * (size_t)v, s[i]);
+    }
+    if (a.y == nullptr && a.q == nullptr) return;
+    const float total = row_sum<TPR>(acc, sums + group * (TPR / 32));
+    const float rstd = 1.f / sqrtf(total / (float)a.d + a.eps);
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        const int v = lane + i * TPR;
+        if (v >= nv) continue;
+        float w[8];
+        Vec<T> wv;
+        if (a.weight) load_vec(wv, (const T *)a.weight + 8 * v);
+        if (a.weight) unpack(wv, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s[i][j] = a.weight ? s[i][j] * rstd * w[j] : s[i][j] * rstd;
+            top = max(top, __float_as_uint(s[i][j]) & 0x7FFFFFFFu);   // ordered like |y|, a NaN above all numbers
+        }
+        if (a.y && live) store_vec((T *)a.y + base + 8 * (size_t)v, s[i]);
+    }
+    if (a.q == nullptr) return;
+    const float scale = __uint_as_float(row_max<TPR>(top, maxs + group * (TPR / 32))) / kE4m3Max;
+    // one reciprocal a row; where it would overflow (a scale below the normal range) the division itself is used
+    const bool tiny = scale < 1.17549435e-38f;
+    const float inv = tiny ? 0.f : 1.f / scale;
+    if (live && lane == 0) a.q_scale[row] = scale;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        const int v = lane + i * TPR;
+        if (!live || v >= nv) continue;
+        uint32_t w[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float t[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t[j] = tiny ? (scale > 0.f ? s[i][4 * h + j] / scale : 0.f) : s[i][4 * h + j] * inv;
+            const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(t[0], t[1]), __NV_SATFINITE, __NV_E4M3);
+            const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(t[2], t[3]), __NV_SATFINITE, __NV_E4M3);
+            w[h] = lo | (hi << 16);
+        }
+        *reinterpret_cast<uint2 *>(a.q + base + 8 * (size_t)v) = make_uint2(w[0], w[1]);
+    }
+}
+
+struct NormBwdArgs {
+    const void *s, *weight, *dy, *dsum;
+    void *dx;
+    float *dw_part;          // [blocks][d]
+    int T, d;
+    float eps;
+};
+
+// One block walks over its rows and keeps the columns' dweight sums in registers; kRowsAt rows are loaded together so
+// that enough bytes are in flight and the block meets once for all of them.
+template <typename T, int TPR, int VPT, int RA>
+__global__ void __launch_bounds__(TPR < kNormBlock ? kNormBlock : TPR)
+add_rms_norm_bwd_kernel(const NormBwdArgs a)
+{
+    constexpr int kThreads = TPR < kNormBlock ? kNormBlock : TPR;
+    constexpr int kRows = kThreads / TPR, W = TPR / 32;
+    __shared__ float part[2][kThreads / 32][2 * RA];
+    __shared__ float dw_sh[kRows > 1 ? kThreads * VPT * 8 : 1];
+    const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR, wid = threadIdx.x >> 5;
+    const int nv = a.d / 8;
+    float dw[VPT][8];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dw[i][j] = 0.f;
+    int buf = 0;
+    for (int row0 = (blockIdx.x * kRows) * RA; row0 < a.T; row0 += gridDim.x * kRows * RA, buf ^= 1) {
+        Vec<T> sv[RA][VPT], yv[RA][VPT], av[RA][VPT];
+#pragma unroll
+        for (int r = 0; r < RA; ++r) {
+            const int row = row0 + group * RA + r;
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int v = lane + i * TPR;
+                const bool in = row < a.T && v < nv;
+                const size_t at = (size_t)row * a.d + 8 * (size_t)v;
+                if (in) {
+                    load_vec(sv[r][i], (const T *)a.s + at);
+                    load_vec(yv[r][i], (const T *)a.dy + at);
+                } else {
+                    zero_vec(sv[r][i]);
+                    zero_vec(yv[r][i]);
+                }
+                if (in && a.dsum) load_vec(av[r][i], (const T *)a.dsum + at);
+                else zero_vec(av[r][i]);
+            }
+        }
+        float ss[RA], us[RA];
+#pragma unroll
+        for (int r = 0; r < RA; ++r) {
+            ss[r] = us[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int v = lane + i * TPR;
+                float f[8], g[8], w[8];
+                unpack(sv[r][i], f);
+                unpack(yv[r][i], g);
+                if (a.weight && v < nv) {
+                    Vec<T> wv;
+                    load_vec(wv, (const T *)a.weight + 8 * v);
+                    unpack(wv, w);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float u = (a.weight && v < nv) ? g[j] * w[j] : g[j];
+                    ss[r] = fmaf(f[j], f[j], ss[r]);
+                    us[r] = fmaf(u, f[j], us[r]);
+                }
+            }
+            ss[r] = warp_sum(ss[r]);
+            us[r] = warp_sum(us[r]);
+        }
+        if constexpr (TPR > 32) {
+            if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+                for (int r = 0; r < RA; ++r) {
+                    part[buf][wid][2 * r] = ss[r];
+                    part[buf][wid][2 * r + 1] = us[r];
+                }
+            }
+            __syncthreads();      // the two buffers alternate: one barrier per step separates reads from the next writes
+#pragma unroll
+            for (int r = 0; r < RA; ++r) {
+                ss[r] = us[r] = 0.f;
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    ss[r] += part[buf][group * W + i][2 * r];
+                    us[r] += part[buf][group * W + i][2 * r + 1];
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < RA; ++r) {
+            const int row = row0 + group * RA + r;
+            if (row >= a.T) break;
+            const float rstd = 1.f / sqrtf(ss[r] / (float)a.d + a.eps);
+            const float c = rstd * rstd * (us[r] / (float)a.d);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int v = lane + i * TPR;
+                if (v >= nv) continue;
+                float f[8], g[8], w[8], o[8], add[8];
+                unpack(sv[r][i], f);
+                unpack(yv[r][i], g);
+                unpack(av[r][i], add);
+                if (a.weight) {
+                    Vec<T> wv;
+                    load_vec(wv, (const T *)a.weight + 8 * v);
+                    unpack(wv, w);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float u = a.weight ? g[j] * w[j] : g[j];
+                    o[j] = rstd * (u - f[j] * c) + add[j];
+                    dw[i][j] = fmaf(g[j], f[j] * rstd, dw[i][j]);
+                }
+                store_vec((T *)a.dx + (size_t)row * a.d + 8 * (size_t)v, o);
+            }
+        }
+    }
+    if (a.dw_part == nullptr) return;
+    float *out = a.dw_part + (size_t)blockIdx.x * a.d;
+    if constexpr (kRows == 1) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int v = lane + i * TPR;
+            if (v < nv) store_vec(out + 8 * v, dw[i]);
+        }
+    } else {
+        // the row groups' sums meet in shared memory and are added in group order
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) dw_sh[group * (TPR * VPT * 8) + 8 * (lane + i * TPR) + j] = dw[i][j];
+        __syncthreads();
+        for (int c = threadIdx.x; c < a.d; c += kThreads) {
+            float t = 0.f;
+#pragma unroll
+            for (int g = 0; g < kRows; ++g) t += dw_sh[g * (TPR * VPT * 8) + c];
+            out[c] = t;
+        }
+    }
+}
+
+// out[c] = sum over the blocks' partial rows, in block order within 32 interleaved runs that are added in order.
+__global__ void __launch_bounds__(1024) column_sum_kernel(const float *__restrict__ part, int n_rows, int d, float *__restrict__ out)
+{
+    __shared__ float sh[32][33];
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31), run = threadIdx.x >> 5;
+    float acc = 0.f;
+    if (c < d)
+#pragma unroll 8
+        for (int r = run; r < n_rows; r += 32) acc += part[(size_t)r * d + c];
+    sh[run][threadIdx.x & 31] = acc;
+    __syncthreads();
+    if (run == 0 && c < d) {
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t += sh[i][threadIdx.x];
+        out[c] = t;
+    }
+}
+
+template <typename T, int TPR, int VPT>
+cudaError_t launch_norm(const NormArgs &a, cudaStream_t s)
+{
+    constexpr int threads = TPR < kNormBlock ? kNormBlock : TPR;
+    constexpr int rows = threads / TPR;
+    add_rms_norm_kernel<T, TPR, VPT><<<(a.T + rows - 1) / rows, threads, 0, s>>>(a);
+    return cudaGetLastError();
+}
+
+// Few rows: a row's latency counts, so it is spread over a block with one vector a thread where that holds it.
+// Many rows: a warp a row as long as it fits in registers (no barrier in the row's sums).
+template <typename T>
+cudaError_t dispatch_norm(const NormArgs &a, int sms, cudaStream_t s)
+{
+    const int nv = a.d / 8;
+    if (nv <= 32) return launch_norm<T, 32, 1>(a, s);
+    if (a.T <= 2 * sms && nv <= 256) return launch_norm<T, 256, 1>(a, s);
+    if (nv <= 64) return launch_norm<T, 32, 2>(a, s);
+    if (nv <= 128) return launch_norm<T, 32, 4>(a, s);
+    if (nv <= 256) return launch_norm<T, 32, 8>(a, s);
+    if (nv <= 512) return launch_norm<T, 256, 2>(a, s);
+    if (nv <= 1024) return launch_norm<T, 256, 4>(a, s);
+    if (nv <= 2048) return launch_norm<T, 256, 8>(a, s);
+    return launch_norm<T, 1024, 4>(a, s);
+}
+
+// Blocks of the backward kernel for a batch: the partial dweight rows they write are part of the workspace, whose size
+// is asked for without a device, so the count goes by the batch alone.
+constexpr int kBwdBlocks = 592;      // four for each of 148 SMs
+struct BwdShape { int tpr, vpt, rows_at; };
+BwdShape bwd_shape(int d)
+{
+    const int nv = d / 8;
+    if (nv <= 32) return {32, 1, 2};
+    if (nv <= 64) return {32, 2, 2};
+    if (nv <= 128) return {128, 1, 4};
+    if (nv <= 256) return {256, 1, 4};
+    if (nv <= 512) return {256, 2, 2};
+    if (nv <= 1024) return {256, 4, 1};
+    if (nv <= 2048) return {256, 8, 1};
+    return {1024, 4, 1};
+}
+int bwd_blocks(int T, int d)
+{
+    const BwdShape b = bwd_shape(d);
+    const int rows = (b.tpr < kNormBlock ? kNormBlock / b.tpr : 1) * b.rows_at;
+    const long long need = ((long long)T + rows - 1) / rows;
+    return (int)(need < kBwdBlocks ? need : kBwdBlocks);
+}
+
+template <typename T, int TPR, int VPT, int RA>
+cudaError_t launch_bwd(const NormBwdArgs &a, int blocks, cudaStream_t s)
+{
+    add_rms_norm_bwd_kernel<T, TPR, VPT, RA><<<blocks, TPR < kNormBlock ? kNormBlock : TPR, 0, s>>>(a);
+    return cudaGetLastError();
+}
+template <typename T>
+cudaError_t dispatch_bwd(const NormBwdArgs &a, int blocks, cudaStream_t s)
+{
+    const int nv = a.d / 8;
+    if (nv <= 32) return launch_bwd<T, 32, 1, 2>(a, blocks, s);
+    if (nv <= 64) return launch_bwd<T, 32, 2, 2>(a, blocks, s);
+    if (nv <= 128) return launch_bwd<T, 128, 1, 4>(a, blocks, s);
+    if (nv <= 256) return launch_bwd<T, 256, 1, 4>(a, blocks, s);
+    if (nv <= 512) return launch_bwd<T, 256, 2, 2>(a, blocks, s);
+    if (nv <= 1024) return launch_bwd<T, 256, 4, 1>(a, blocks, s);
+    if (nv <= 2048) return launch_bwd<T, 256, 8, 1>(a, blocks, s);
+    return launch_bwd<T, 1024, 4, 1>(a, blocks, s);
+}
+
+bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+bool norm_shape_ok(int T, int d) { return T >= 0 && T <= (1 << 30) && d >= 8 && d % 8 == 0; }
+
+}  // namespace
+
+int device_sms()
+{
+    static int cached[64];                         // by device ordinal; a lost race writes the same value
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 148;
+    if (dev >= 0 && dev < 64 && cached[dev] > 0) return cached[dev];
+    int n = 0;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 148;
+    if (dev >= 0 && dev < 64) cached[dev] = n;
+    return n;
+}
+
+cudaError_t launch_column_sum(const float *part, int n_rows, int d, float *out, cudaStream_t s)
+{
+    column_sum_kernel<<<(d + 31) / 32, 1024, 0, s>>>(part, n_rows, d, out);
+    return cudaGetLastError();
+}
+
+}  // namespace modse
+
+using namespace modse;
+
+extern "C" {
+
+modse_status_t modse_add_rms_norm(modse_dtype_t dtype, int n_tokens, int d_model, const void *x, const void *residual,
+                                  const void *weight, float eps, void *sum, void *y, void *y_e4m3, float *y_scale,
+                                  void *cuda_stream)
+{
+    if ((dtype != MODSE_F32 && dtype != MODSE_BF16) || !norm_shape_ok(n_tokens, d_model) || !(eps >= 0.f) || eps > 3e38f)
+        return MODSE_ERR_INVALID_ARG;
+    if (d_model > kNormMaxD) return MODSE_ERR_UNSUPPORTED;
+    if (n_tokens == 0) return MODSE_OK;
+    if (sum == nullptr && y == nullptr && y_e4m3 == nullptr) return MODSE_ERR_INVALID_ARG;
+    if ((y_e4m3 == nullptr) != (y_scale == nullptr)) return MODSE_ERR_INVALID_ARG;
+    if (x == nullptr || !aligned(x, 16) || !aligned(residual, 16) || !aligned(weight, 16) || !aligned(sum, 16) ||
+        !aligned(y, 16) || !aligned(y_e4m3, 16) || !aligned(y_scale, 4))
+        return MODSE_ERR_INVALID_ARG;
+    const NormArgs a{x, residual, weight, sum, y, (unsigned char *)y_e4m3, y_scale, n_tokens, d_model, eps};
+    const cudaStream_t s = (cudaStream_t)cuda_stream;
+    const cudaError_t e = dtype == MODSE_F32 ? dispatch_norm<float>(a, device_sms(), s)
+                                             : dispatch_norm<__nv_bfloat16>(a, device_sms(), s);
+    return e == cudaSuccess ? MODSE_OK : MODSE_ERR_CUDA;
+}
+
+size_t modse_add_rms_norm_backward_workspace_bytes(int n_tokens, int d_model)
+{
+    if (!norm_shape_ok(n_tokens, d_model) || d_model > kNormMaxD) return 0;
+    return (size_t)bwd_blocks(n_tokens > 0 ? n_tokens : 1, d_model) * d_model * sizeof(float);
+}
+
+modse_status_t modse_add_rms_norm_backward(modse_dtype_t dtype, int n_tokens, int d_model, const void *sum,
+                                           const void *weight, float eps, const void *dy, const void *dsum, void *dx,
+                                           float *dweight, void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    if ((dtype != MODSE_F32 && dtype != MODSE_BF16) || !norm_shape_ok(n_tokens, d_model) || !(eps >= 0.f) || eps > 3e38f)
+        return MODSE_ERR_INVALID_ARG;
+    if (d_model > kNormMaxD) return MODSE_ERR_UNSUPPORTED;
+    if (!aligned(dweight, 16)) return MODSE_ERR_INVALID_ARG;
+    const cudaStream_t s = (cudaStream_t)cuda_stream;
+    if (n_tokens == 0) {
+        if (dweight && cudaMemsetAsync(dweight, 0, (size_t)d_model * sizeof(float), s) != cudaSuccess) return MODSE_ERR_CUDA;
+        return MODSE_OK;
+    }
+    if (sum == nullptr || dy == nullptr || dx == nullptr || !aligned(sum, 16) || !aligned(weight, 16) || !aligned(dy, 16) ||
+        !aligned(dsum, 16) || !aligned(dx, 16))
+        return MODSE_ERR_INVALID_ARG;
+    if (dweight != nullptr) {
+        if (workspace == nullptr || !aligned(workspace, 256)) return MODSE_ERR_INVALID_ARG;
+        if (workspace_bytes < modse_add_rms_norm_backward_workspace_bytes(n_tokens, d_model))
+            return MODSE_ERR_WORKSPACE_TOO_SMALL;
+    }
+    const int blocks = bwd_blocks(n_tokens, d_model);
+    const NormBwdArgs a{sum, weight, dy, dsum, dx, dweight ? (float *)workspace : nullptr, n_tokens, d_model, eps};
+    cudaError_t e = dtype == MODSE_F32 ? dispatch_bwd<float>(a, blocks, s) : dispatch_bwd<__nv_bfloat16>(a, blocks, s);
+    if (e == cudaSuccess && dweight) e = launch_column_sum(a.dw_part, blocks, d_model, dweight, s);
+    return e == cudaSuccess ? MODSE_OK : MODSE_ERR_CUDA;
+}
+
+}  // extern "C"
