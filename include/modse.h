@@ -43,7 +43,8 @@ typedef enum {
 
 typedef enum {
     MODSE_F32 = 0, /* fp32 storage, fp32 FMA arithmetic                                   */
-    MODSE_BF16 = 1 /* bf16 storage, tensor-core products with fp32 accumulation           */
+    MODSE_BF16 = 1, /* bf16 storage, tensor-core products with fp32 accumulation          */
+    MODSE_E4M3 = 2  /* 8-bit operands of modse_linear (e4m3 with a scale a row); no layer */
 } modse_dtype_t;
 
 /* ---- layer object ------------------------------------------------------- */
@@ -342,6 +343,60 @@ size_t modse_add_rms_norm_backward_workspace_bytes(int n_tokens, int d_model);
 modse_status_t modse_add_rms_norm_backward(modse_dtype_t dtype, int n_tokens, int d_model, const void *sum,
                                            const void *weight, float eps, const void *dy, const void *dsum, void *dx,
                                            float *dweight, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Dense product with bias, activation and residual in its epilogue, for the
+ * projections of the block the layer sits in:
+ *   z = x w^T + bias,  y = act(z) + residual.
+ * x [T, d_in], w [d_out, d_in], bias [d_out], residual and y [T, d_out], z [T, d_out].
+ * MODSE_BF16: everything bf16.  MODSE_E4M3: x and w are e4m3 bytes with one fp32
+ * scale a row each (x_scale [T], w_scale [d_out], e.g. from modse_add_rms_norm):
+ * z = (x w^T) x_scale w_scale + bias; bias, residual, z and y are bf16.  MODSE_F32
+ * is MODSE_ERR_UNSUPPORTED.  d_in a multiple of 8 (e4m3: 16), d_out of 8.
+ * bias, residual and z may be NULL; y may be residual itself, otherwise outputs do
+ * not overlap inputs.  z, what
+ * modse_linear_backward reads, is rounded once from the fp32 value, and y, from
+ * the unrounded z, once.  Products are accumulated in fp32.
+ * relu, gelu (z Phi(z), Phi the normal distribution function), silu (z / (1 + e^-z)).
+ * The workspace's first bytes hold a status word that modse_check_workspace_status
+ * reads (a bounded wait inside a kernel may expire, as in modse_forward).     */
+typedef enum {
+    MODSE_ACT_NONE = 0,
+    MODSE_ACT_RELU = 1,
+    MODSE_ACT_GELU = 2,
+    MODSE_ACT_SILU = 3
+} modse_activation_t;
+typedef struct {
+    const void *x, *w;
+    const float *x_scale, *w_scale; /* MODSE_E4M3 only, else NULL */
+    const void *bias, *residual;
+    void *z, *y;
+} modse_linear_t;
+size_t modse_linear_workspace_bytes(modse_dtype_t dtype, int n_tokens, int d_in, int d_out);
+modse_status_t modse_linear(modse_dtype_t dtype, int n_tokens, int d_in, int d_out, modse_activation_t activation,
+                            const modse_linear_t *args, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Gradient of the bf16 product, from dy [T, d_out] and the z that forward saved (may
+ * be NULL for MODSE_ACT_NONE):
+ *   dz = dy act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum_t dz
+ * (the residual's gradient is dy itself; relu'(0) = 0).  dx [T, d_in] and
+ * dw [d_out, d_in] bf16, dbias [d_out] fp32; each may be NULL, all overwritten, none
+ * overlaps an input.  At most 4194240 tokens.
+ * dz enters the products rounded to bf16 once (they read 16-bit operands) and
+ * dbias unrounded.                                                           */
+typedef struct {
+    const void *x, *w, *dy, *z;
+    void *dx, *dw;
+    float *dbias;
+} modse_linear_grads_t;
+size_t modse_linear_backward_workspace_bytes(int n_tokens, int d_in, int d_out);
+modse_status_t modse_linear_backward(int n_tokens, int d_in, int d_out, modse_activation_t activation,
+                                     const modse_linear_grads_t *args, void *workspace, size_t workspace_bytes,
+                                     void *cuda_stream);
+
+/* Synchronises the stream and reads the status word of the last call that used this
+ * workspace (modse_linear, modse_linear_backward, modse_orthogonalize): MODSE_OK or
+ * MODSE_ERR_DEVICE_TIMEOUT.                                                  */
+modse_status_t modse_check_workspace_status(const void *workspace, void *cuda_stream);
 
 /* Debugging aid, process-wide: when on, bf16 layers run their grouped GEMMs on
  * the fp32-FMA kernels of the fp32 type (with bf16 storage) instead of the

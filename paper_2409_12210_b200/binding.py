@@ -23,6 +23,8 @@ MODSE_ERR_DEVICE_TIMEOUT = 6
 MODSE_ERR_DEVICE_BOUNDS = 7
 MODSE_F32 = 0
 MODSE_BF16 = 1
+MODSE_E4M3 = 2
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 N_STAGES = 12
 MODSE_FUSE_GATHER = 1
 MODSE_FUSE_DG_ROWDOT = 2
@@ -45,6 +47,14 @@ class _Weights(ctypes.Structure):
 class _WGrads(ctypes.Structure):
     _fields_ = [("dw_router", ctypes.c_void_p), ("dw_gate", ctypes.c_void_p), ("dw_up", ctypes.c_void_p),
                 ("dw_down", ctypes.c_void_p)]
+
+
+class _Linear(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "w", "x_scale", "w_scale", "bias", "residual", "z", "y")]
+
+
+class _LinearGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "w", "dy", "z", "dx", "dw", "dbias")]
 
 
 _lib = None
@@ -141,6 +151,16 @@ def load():
     lib.modse_add_rms_norm_backward_workspace_bytes.argtypes = [ci, ci]
     lib.modse_add_rms_norm_backward.restype = ci
     lib.modse_add_rms_norm_backward.argtypes = [ci, ci, ci, vp, vp, cf, vp, vp, vp, vp, vp, sz, vp]
+    lib.modse_linear_workspace_bytes.restype = sz
+    lib.modse_linear_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    lib.modse_linear.restype = ci
+    lib.modse_linear.argtypes = [ci, ci, ci, ci, ci, ctypes.POINTER(_Linear), vp, sz, vp]
+    lib.modse_linear_backward_workspace_bytes.restype = sz
+    lib.modse_linear_backward_workspace_bytes.argtypes = [ci, ci, ci]
+    lib.modse_linear_backward.restype = ci
+    lib.modse_linear_backward.argtypes = [ci, ci, ci, ci, ctypes.POINTER(_LinearGrads), vp, sz, vp]
+    lib.modse_check_workspace_status.restype = ci
+    lib.modse_check_workspace_status.argtypes = [vp, vp]
     lib.modse_debug_use_fma_path.restype = None
     lib.modse_debug_use_fma_path.argtypes = [ci]
     _lib = lib
@@ -290,6 +310,66 @@ def add_rms_norm_backward(s, weight, eps: float, dy, dsum, dx, dweight=None, wor
         _buffer("dweight", dweight, (d,), torch.float32, dev), *_workspace(workspace, dev), stream)
     if st != MODSE_OK:
         raise ModseError(st, "modse_add_rms_norm_backward")
+
+
+def _linear_code(dtype):
+    import torch
+    if dtype == torch.bfloat16:
+        return MODSE_BF16
+    if dtype == torch.float8_e4m3fn:
+        return MODSE_E4M3
+    raise TypeError(f"unsupported dtype {dtype}")
+
+
+def linear_workspace_bytes(dtype, n_tokens: int, d_in: int, d_out: int) -> int:
+    return int(load().modse_linear_workspace_bytes(_linear_code(dtype), n_tokens, d_in, d_out))
+
+
+def linear(x, w, y, workspace, *, bias=None, residual=None, activation: str = "none", z=None, x_scale=None,
+           w_scale=None) -> None:
+    """modse_linear on the current stream: ``y = act(x w^T + bias) + residual``, the pre-activation into ``z`` if given.
+    x [T, d_in] and w [d_out, d_in] are bf16, or torch.float8_e4m3fn with one fp32 scale a row (``x_scale``,
+    ``w_scale``); everything else is bf16."""
+    import torch
+    T, k = _rows("x", x)
+    n = _rows("w", w)[0]
+    bf, dev, code = torch.bfloat16, x.device, _linear_code(x.dtype)
+    stream = _current_stream("x", x)
+    f32, out = torch.float32, (T, n)
+    args = _Linear(_buffer("x", x, (T, k), x.dtype, dev), _buffer("w", w, (n, k), x.dtype, dev),
+                   _buffer("x_scale", x_scale, (T,), f32, dev), _buffer("w_scale", w_scale, (n,), f32, dev),
+                   _buffer("bias", bias, (n,), bf, dev), _buffer("residual", residual, out, bf, dev),
+                   _buffer("z", z, out, bf, dev), _buffer("y", y, out, bf, dev))
+    st = load().modse_linear(code, T, k, n, ACTIVATIONS[activation], args, *_workspace(workspace, dev), stream)
+    if st != MODSE_OK:
+        raise ModseError(st, "modse_linear")
+
+
+def linear_backward_workspace_bytes(n_tokens: int, d_in: int, d_out: int) -> int:
+    return int(load().modse_linear_backward_workspace_bytes(n_tokens, d_in, d_out))
+
+
+def linear_backward(x, w, dy, z, activation: str, dx, dw, dbias, workspace) -> None:
+    """modse_linear_backward: the gradients of :func:`linear` on bf16 operands from ``dy`` and the saved ``z`` (None where
+    there is no activation) into ``dx``, ``dw`` (bf16) and ``dbias`` (fp32); any of the three may be None."""
+    import torch
+    T, k = _rows("x", x)
+    n = _rows("w", w)[0]
+    bf, dev = torch.bfloat16, x.device
+    stream = _current_stream("x", x)
+    args = _LinearGrads(_buffer("x", x, (T, k), bf, dev), _buffer("w", w, (n, k), bf, dev),
+                        _buffer("dy", dy, (T, n), bf, dev), _buffer("z", z, (T, n), bf, dev),
+                        _buffer("dx", dx, (T, k), bf, dev), _buffer("dw", dw, (n, k), bf, dev),
+                        _buffer("dbias", dbias, (n,), torch.float32, dev))
+    st = load().modse_linear_backward(T, k, n, ACTIVATIONS[activation], args, *_workspace(workspace, dev), stream)
+    if st != MODSE_OK:
+        raise ModseError(st, "modse_linear_backward")
+
+
+def check_workspace_status(workspace) -> int:
+    """Status the last operator call on this workspace left (synchronises the current stream)."""
+    import torch
+    return int(load().modse_check_workspace_status(workspace.data_ptr(), torch.cuda.current_stream().cuda_stream))
 
 
 def _workspace(t, device):

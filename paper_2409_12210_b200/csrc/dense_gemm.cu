@@ -1,0 +1,721 @@
+// Dense products on Blackwell tensor cores: a persistent kernel in which a pair of CTAs on neighbouring SMs computes
+// 256 x 256 (or 256 x 128) output tiles with tcgen05.mma.cta_group::2.
+//
+// Each CTA of a pair stages its own 128 rows of the row operand and half of the column operand by TMA (six stages of
+// 32 KB) and holds the accumulator rows of its half in tensor memory; two accumulators fit, so the epilogue of one
+// tile overlaps the main loop of the next.  Operands are read K-major or MN-major straight from where they lie.
+// What bounds the main loop is the rate at which shared memory fills from L2 (32 KB a k-block of 128 bytes against 512
+// clocks of MMA), as for the layer's grouped products; a 128-column tile is for outputs with too few tiles to fill the GPU.
+//
+// Tail: the tiles left over after the last full round over the CTA pairs would leave most pairs idle for a whole
+// tile.  They are cut along the contraction instead, into as many pieces as there are pairs for them; every piece
+// writes its fp32 accumulator to the workspace, and the epilogue warp that arrives last at a 32-row strip adds the
+// pieces of that strip in order (so the sum does not depend on who was last) and runs the epilogue on it.
+//
+// Every wait is bounded; one that expires records kDevTimeout in the status word and the CTAs drain and leave.
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "dense_gemm.h"
+#include "tc_device.h"
+#include "tc_gemm.h"
+
+namespace modse {
+namespace {
+
+constexpr int kDenseStages = 6;
+constexpr int kDenseStageBytes = 32768;          // 16 KB of rows, up to 16 KB of columns
+constexpr uint32_t kDenseRows = 16384;           // a CTA's 128 rows of 128 bytes
+constexpr int kDenseEpiWarps = 8;
+constexpr int kDenseFirstEpi = 4;                // warps 0-1: TMA, MMA; 2-3 idle so that the epilogue starts on a warpgroup
+constexpr int kDenseThreads = 32 * (kDenseFirstEpi + kDenseEpiWarps);
+constexpr int kDenseAccCols = 256;
+constexpr int kDenseTmemCols = 512;
+constexpr int kDenseGroupRows = 8;               // row tiles whose column tiles are walked before the next group's
+
+struct DenseTail {
+    unsigned long long full[kDenseStages], empty[kDenseStages], tmem_full[2], tmem_empty[2];
+    unsigned int tmem_base;
+    int abort_flag;
+};
+constexpr size_t kDenseSmem = 1024 + (size_t)kDenseStages * kDenseStageBytes + kDenseEpiWarps * kEpiBufBytes + sizeof(DenseTail);
+static_assert(kDenseSmem <= 232448, "shared memory per CTA");
+
+template <int P> struct DenseParams {
+    CUtensorMap a[P], b[P];
+    DenseProblem prob[P];
+    LinearEpilogue lin;
+    int n_prob, tiles, full_tiles, splits, items;   // tiles [0, full_tiles) are whole, the others cut into `splits` pieces
+    int *status, *counters;
+    float *partial;
+    unsigned long long wait_limit_ns;
+};
+
+struct DenseTile {
+    int p, m0, n0, kb0, kb1;
+    int tail;        // index among the cut tiles, -1: a whole tile
+    int split;
+    bool mirror;     // symmetric output: also write the transposed tile
+};
+
+template <int TN, int P>
+__device__ __forceinline__ DenseTile dense_decode(const DenseParams<P> &prm, int item, int &cursor)
+{
+    DenseTile t;
+    int tile = item;
+    t.tail = -1;
+    t.split = 0;
+    if (item >= prm.full_tiles) {
+        const int r = item - prm.full_tiles;
+        t.tail = r / prm.splits;
+        t.split = r - t.tail * prm.splits;
+        tile = prm.full_tiles + t.tail;
+        if (prm.splits == 1) t.tail = -1;
+    }
+    if constexpr (P > 1)
+        while (cursor + 1 < prm.n_prob && tile >= prm.prob[cursor + 1].tile0) ++cursor;
+    t.p = cursor;
+    const DenseProblem &q = prm.prob[cursor];
+    int local = tile - q.tile0, mb, nb;
+    t.mirror = false;
+    if (q.flags & kDenseSym) {
+        mb = 0;                              // row by row of the upper triangle (square tiles)
+        while (local >= q.nt - mb) { local -= q.nt - mb; ++mb; }
+        nb = mb + local;
+        t.mirror = nb > mb;
+    } else {
+        const int per = kDenseGroupRows * q.nt, g = local / per, rem = local - g * per;
+        const int rows = min(kDenseGroupRows, q.mt - g * kDenseGroupRows);
+        nb = rem / rows;
+        mb = g * kDenseGroupRows + rem - nb * rows;
+    }
+    t.m0 = mb * 256;
+    t.n0 = nb * TN;
+    t.kb0 = 0;
+    t.kb1 = q.nk;
+    if (t.tail >= 0) {
+        t.kb0 = (int)((long long)q.nk * t.split / prm.splits);
+        t.kb1 = (int)((long long)q.nk * (t.split + 1) / prm.splits);
+    }
+    return t;
+}
+
+// ---- epilogue pieces: a warp holds 32 rows x 32 columns, one row a lane ----
+
+// 32 rows x 64 bytes between global memory and the lanes' rows, by way of the staging buffer, so that four neighbouring
+// lanes move the 64 bytes of one row.  `at` points at (first row of the warp, first column of the chunk); only pieces of
+// 16 bytes that start at a valid column and row are touched.
+__device__ __forceinline__ void rows_out(unsigned char *stg, int lane, unsigned char *at, long long row_bytes, int rows_valid,
+                                         int pieces_valid, const uint4 (&w)[4])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4 *>(stg + epi_piece(lane, q)) = w[q];
+    __syncwarp();
+    const int q = lane & 3;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int rr = 8 * j + (lane >> 2);
+        const uint4 v = *reinterpret_cast<const uint4 *>(stg + epi_piece(rr, q));
+        if (rr < rows_valid && q < pieces_valid) *reinterpret_cast<uint4 *>(at + rr * row_bytes + q * 16) = v;
+    }
+    __syncwarp();
+}
+__device__ __forceinline__ void rows_load(int lane, const unsigned char *at, long long row_bytes, int rows_valid,
+                                          int pieces_valid, uint4 (&raw)[4])
+{
+    const int q = lane & 3;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int rr = 8 * j + (lane >> 2);
+        raw[j] = make_uint4(0, 0, 0, 0);
+        if (rr < rows_valid && q < pieces_valid) raw[j] = *reinterpret_cast<const uint4 *>(at + rr * row_bytes + q * 16);
+    }
+}
+__device__ __forceinline__ void rows_hand(unsigned char *stg, int lane, const uint4 (&raw)[4], uint4 (&own)[4])
+{
+    const int q = lane & 3;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4 *>(stg + epi_piece(8 * j + (lane >> 2), q)) = raw[j];
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) own[k] = *reinterpret_cast<const uint4 *>(stg + epi_piece(lane, k));
+    __syncwarp();
+}
+
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
+{
+    __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&t);
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi)
+{
+    __half2 t = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&t);
+}
+__device__ __forceinline__ float2 from_f16x2(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+__device__ __forceinline__ float2 from_bf16x2(uint32_t w)
+{
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+__device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+__device__ __forceinline__ void pack_bf16(const float (&v)[32], uint4 (&w)[4])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        w[q] = make_uint4(bf16x2(v[8 * q], v[8 * q + 1]), bf16x2(v[8 * q + 2], v[8 * q + 3]),
+                          bf16x2(v[8 * q + 4], v[8 * q + 5]), bf16x2(v[8 * q + 6], v[8 * q + 7]));
+}
+__device__ __forceinline__ void pack_f16(const float (&v)[32], uint4 (&w)[4])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        w[q] = make_uint4(f16x2(v[8 * q], v[8 * q + 1]), f16x2(v[8 * q + 2], v[8 * q + 3]),
+                          f16x2(v[8 * q + 4], v[8 * q + 5]), f16x2(v[8 * q + 6], v[8 * q + 7]));
+}
+
+template <int ACT>
+__device__ __forceinline__ float activate(float z)
+{
+    if constexpr (ACT == MODSE_ACT_RELU) return z < 0.f ? 0.f : z;       // a NaN stays
+    if constexpr (ACT == MODSE_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if constexpr (ACT == MODSE_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
+    return z;
+}
+__device__ __forceinline__ void activate_all(float (&v)[32], int act)
+{
+    if (act == MODSE_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = activate<MODSE_ACT_RELU>(v[i]);
+    } else if (act == MODSE_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = activate<MODSE_ACT_GELU>(v[i]);
+    } else if (act == MODSE_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = activate<MODSE_ACT_SILU>(v[i]);
+    }
+}
+
+// Finishes 32 rows (from row r0) x 32 columns (from c0) of problem q; v: this lane's row.
+template <int MODE>
+__device__ __forceinline__ void dense_finish(const DenseProblem &q, const LinearEpilogue &lin, bool mirror, int r0, int c0,
+                                             int lane, unsigned char *stg, float (&v)[32])
+{
+    const int rows = min(32, q.M - r0), cols = min(32, q.N - c0);
+    if (rows <= 0 || cols <= 0) return;
+    const int pieces = (cols + 7) >> 3;      // 16-byte pieces of 2-byte elements; a last partial piece ends in a row's padding
+    if constexpr (MODE == DenseLinear) {
+        const long long at = (long long)r0 * q.N + c0;
+        uint4 raw[4];
+        if (lin.residual) rows_load(lane, (const unsigned char *)(lin.residual + at), 2ll * q.N, rows, pieces, raw);
+        if (lin.sx) {
+            const float s = lane < rows ? __ldg(lin.sx + r0 + lane) : 0.f;
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+                if (p < 2 * pieces) {
+                    const float4 w = __ldg(reinterpret_cast<const float4 *>(lin.sw + c0) + p);
+                    v[4 * p] *= s * w.x; v[4 * p + 1] *= s * w.y; v[4 * p + 2] *= s * w.z; v[4 * p + 3] *= s * w.w;
+                }
+        }
+        if (lin.bias) {
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+                if (p < pieces) {
+                    const uint4 w = __ldg(reinterpret_cast<const uint4 *>(lin.bias + c0) + p);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 f = from_bf16x2(word_of(w, i));
+                        v[8 * p + 2 * i] += f.x;
+                        v[8 * p + 2 * i + 1] += f.y;
+                    }
+                }
+        }
+        uint4 w[4];
+        if (lin.z) {
+            pack_bf16(v, w);
+            rows_out(stg, lane, (unsigned char *)(lin.z + at), 2ll * q.N, rows, pieces, w);
+        }
+        activate_all(v, lin.act);
+        if (lin.residual) {
+            uint4 own[4];
+            rows_hand(stg, lane, raw, own);
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = from_bf16x2(word_of(own[p], i));
+                    v[8 * p + 2 * i] += f.x;
+                    v[8 * p + 2 * i + 1] += f.y;
+                }
+        }
+        pack_bf16(v, w);
+        rows_out(stg, lane, (unsigned char *)(lin.y + at), 2ll * q.N, rows, pieces, w);
+    } else if constexpr (MODE == DensePlain) {
+        const long long at = (long long)r0 * q.ld_out + c0;
+        if (q.flags & kDenseF32) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint4 w[4];
+#pragma unroll
+                for (int p = 0; p < 4; ++p)
+                    w[p] = make_uint4(__float_as_uint(v[16 * h + 4 * p]), __float_as_uint(v[16 * h + 4 * p + 1]),
+                                      __float_as_uint(v[16 * h + 4 * p + 2]), __float_as_uint(v[16 * h + 4 * p + 3]));
+                rows_out(stg, lane, (unsigned char *)((float *)q.out0 + at + 16 * h), 4 * q.ld_out, rows,
+                         2 * pieces - 4 * h, w);
+            }
+        } else {
+            uint4 w[4];
+            pack_bf16(v, w);
+            rows_out(stg, lane, (unsigned char *)((__nv_bfloat16 *)q.out0 + at), 2 * q.ld_out, rows, pieces, w);
+        }
+    } else if constexpr (MODE == DenseGram || MODE == DensePoly) {
+        __half *out = (__half *)q.out0;
+        const long long at = (long long)r0 * q.ld_out + c0;
+        if constexpr (MODE == DensePoly) {
+            uint4 raw[4], own[4];
+            rows_load(lane, (const unsigned char *)((const __half *)q.in0 + at), 2 * q.ld_out, rows, pieces, raw);
+            rows_hand(stg, lane, raw, own);
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = from_f16x2(word_of(own[p], i));
+                    v[8 * p + 2 * i] = fmaf(q.beta, f.x, q.alpha * v[8 * p + 2 * i]);
+                    v[8 * p + 2 * i + 1] = fmaf(q.beta, f.y, q.alpha * v[8 * p + 2 * i + 1]);
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= q.alpha;
+        }
+        uint4 w[4];
+        pack_f16(v, w);
+        rows_out(stg, lane, (unsigned char *)(out + at), 2 * q.ld_out, rows, pieces, w);
+        if (mirror && lane < rows) {
+            // the transposed block: a lane's values lie one output row apart, a warp's lanes side by side
+            __half *t = out + (long long)c0 * q.ld_out + r0 + lane;
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (i < cols) t[(long long)i * q.ld_out] = __float2half_rn(v[i]);
+        }
+    } else {
+        const long long at = (long long)r0 * q.ld_in + c0;
+        uint4 raw[4], own[4], raw2[4];
+        rows_load(lane, (const unsigned char *)((const __half *)q.in0 + at), 2 * q.ld_in, rows, pieces, raw);
+        rows_load(lane, (const unsigned char *)((const __half *)q.in1 + at), 2 * q.ld_in, rows, pieces, raw2);
+        rows_hand(stg, lane, raw, own);
+        float lo[32];
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = from_f16x2(word_of(own[p], i));
+                lo[8 * p + 2 * i] = f.x;
+                lo[8 * p + 2 * i + 1] = f.y;
+            }
+        rows_hand(stg, lane, raw2, own);
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = from_f16x2(word_of(own[p], i));
+                const int k = 8 * p + 2 * i;
+                v[k] = fmaf(q.beta, lo[k] + f.x, q.alpha * v[k]);
+                v[k + 1] = fmaf(q.beta, lo[k + 1] + f.y, q.alpha * v[k + 1]);
+            }
+        uint4 w[4];
+        if (q.flags & kDenseLast) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= q.scale;
+            __nv_bfloat16 *out = (__nv_bfloat16 *)q.out0 + (long long)r0 * q.ld_out + c0;
+            const bool wide = ((q.ld_out | q.N) & 7) == 0 && (reinterpret_cast<uintptr_t>(q.out0) & 15) == 0;
+            if (wide) {
+                pack_bf16(v, w);
+                rows_out(stg, lane, (unsigned char *)out, 2 * q.ld_out, rows, pieces, w);
+            } else if (lane < rows) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i < cols) out[lane * q.ld_out + i] = __float2bfloat16_rn(v[i]);
+            }
+        } else {
+            pack_f16(v, w);
+            rows_out(stg, lane, (unsigned char *)((__half *)q.out0 + at), 2 * q.ld_in, rows, pieces, w);
+#pragma unroll
+            for (int p = 0; p < 4; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = from_f16x2(word_of(w[p], i));
+                    v[8 * p + 2 * i] -= f.x;
+                    v[8 * p + 2 * i + 1] -= f.y;
+                }
+            pack_f16(v, w);
+            rows_out(stg, lane, (unsigned char *)((__half *)q.out1 + at), 2 * q.ld_in, rows, pieces, w);
+        }
+    }
+}
+
+__device__ __forceinline__ void umma_f8_pair(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accum)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accum)
+        : "memory");
+}
+
+// fp32 accumulator; operand format bits: f16 0, bf16 1 (kind::f16), e4m3 0 (kind::f8f6f4); M = 256.
+template <int TYPE>
+__device__ __forceinline__ uint32_t dense_idesc(bool a_mn, bool b_mn, int n)
+{
+    constexpr uint32_t fmt = TYPE == DenseBf16 ? 1u : 0u;
+    return (1u << 4) | (fmt << 7) | (fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+           ((uint32_t)(n >> 3) << 17) | (16u << 24);
+}
+
+template <int MODE, int TYPE, int TN, int P>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kDenseThreads, 1)
+dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
+{
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t pad = ((raw + 1023u) & ~1023u) - raw;
+    unsigned char *smem = smem_raw + pad;
+    const uint32_t stage_base = raw + pad;
+    unsigned char *epi_bufs = smem + (size_t)kDenseStages * kDenseStageBytes;
+    DenseTail *st = reinterpret_cast<DenseTail *>(epi_bufs + kDenseEpiWarps * kEpiBufBytes);
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = (int)cluster_ctarank();
+    const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+    constexpr int kElems = TYPE == DenseE4m3 ? 128 : 64;       // elements in 128 bytes
+    constexpr int kHalf = TN / 2;                              // column-operand rows staged by each CTA
+    constexpr uint32_t kTx = 2u * (kDenseRows + kHalf * 128u); // bytes of both CTAs a stage
+
+    if (tid == 0) {
+        for (int s = 0; s < kDenseStages; ++s) {
+            mbar_init(smem_u32(&st->full[s]), 1);
+            mbar_init(smem_u32(&st->empty[s]), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(smem_u32(&st->tmem_full[a]), 1);
+            mbar_init(smem_u32(&st->tmem_empty[a]), 2 * kDenseEpiWarps);
+        }
+        st->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                     ::"r"(smem_u32(&st->tmem_base)), "r"(kDenseTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                 // both CTAs' barriers exist before any remote arrival or copy completion
+    tc_fence_after();
+    const uint32_t tmem_base = st->tmem_base;
+    const WaitCtx wc{&st->abort_flag, prm.status, prm.wait_limit_ns};
+
+    if (warp == 0) {
+        // ===================== TMA producer (both CTAs) =====================
+        if (lane == 0) {
+            int stage = 0, cursor = 0;
+            uint32_t phase = 0;
+            long long issued = 0;
+            bool ok = true;
+            for (int item = cluster_id; ok && item < prm.items; item += n_clusters) {
+                const DenseTile t = dense_decode<TN, P>(prm, item, cursor);
+                const int flags = prm.prob[t.p].flags;
+                const CUtensorMap *am = &prm.a[t.p], *bm = &prm.b[t.p];
+                const int ar = t.m0 + rank * 128, br = t.n0 + rank * kHalf;
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    if (!mbar_wait(smem_u32(&st->empty[stage]), phase ^ 1u, wc)) { ok = false; break; }
+                    const uint32_t bar = map_to_cta(smem_u32(&st->full[stage]), 0);
+                    if (rank == 0) mbar_arrive_expect_tx(smem_u32(&st->full[stage]), kTx);
+                    const uint32_t dst = stage_base + stage * kDenseStageBytes;
+                    if (flags & kDenseAMn) {
+                        tma_load_2d_pair(dst, am, bar, ar, kb * 64);
+                        tma_load_2d_pair(dst + kBoxBytes, am, bar, ar + 64, kb * 64);
+                    } else {
+                        tma_load_2d_pair(dst, am, bar, kb * kElems, ar);
+                    }
+                    if (flags & kDenseBMn) {
+#pragma unroll
+                        for (int i = 0; i < kHalf / 64; ++i)
+                            tma_load_2d_pair(dst + kDenseRows + i * kBoxBytes, bm, bar, br + 64 * i, kb * 64);
+                    } else {
+                        tma_load_2d_pair(dst + kDenseRows, bm, bar, kb * kElems, br);
+                    }
+                    ++issued;
+                    if (++stage == kDenseStages) { stage = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok && rank == 0) {
+                // the copies of both CTAs complete on the leader's barriers: it lets those in flight land
+                const int n = issued < kDenseStages ? (int)issued : kDenseStages;
+                for (int i = 1; i <= n; ++i) {
+                    int s2 = stage - i;
+                    uint32_t ph = phase;
+                    if (s2 < 0) { s2 += kDenseStages; ph ^= 1u; }
+                    const unsigned long long tb = global_ns();
+                    while (!mbar_try_wait(smem_u32(&st->full[s2]), ph) && global_ns() - tb < prm.wait_limit_ns) {}
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ===================== MMA issuer (leader only) =====================
+        if (lane == 0 && rank == 0) {
+            int stage = 0, cursor = 0, it = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int item = cluster_id; ok && item < prm.items; item += n_clusters, ++it) {
+                const DenseTile t = dense_decode<TN, P>(prm, item, cursor);
+                const int flags = prm.prob[t.p].flags;
+                const bool a_mn = (flags & kDenseAMn) != 0, b_mn = (flags & kDenseBMn) != 0;
+                const uint32_t a_step = a_mn ? (2048u >> 4) : (32u >> 4), b_step = b_mn ? (2048u >> 4) : (32u >> 4);
+                const uint32_t idesc = dense_idesc<TYPE>(a_mn, b_mn, TN);
+                const int acc = it & 1;
+                if (!mbar_wait(smem_u32(&st->tmem_empty[acc]), ((uint32_t)(it >> 1) & 1u) ^ 1u, wc)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t tacc = tmem_base + (uint32_t)(acc * kDenseAccCols);
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    if (!mbar_wait(smem_u32(&st->full[stage]), phase, wc)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t addr = stage_base + stage * kDenseStageBytes;
+                    const uint64_t adesc = make_desc(addr, a_mn), bdesc = make_desc(addr + kDenseRows, b_mn);
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks) {
+                        const uint32_t more = (kb > t.kb0 || ks > 0) ? 1u : 0u;
+                        if constexpr (TYPE == DenseE4m3)
+                            umma_f8_pair(tacc, adesc + (uint64_t)(ks * a_step), bdesc + (uint64_t)(ks * b_step), idesc, more);
+                        else
+                            umma_bf16_pair(tacc, adesc + (uint64_t)(ks * a_step), bdesc + (uint64_t)(ks * b_step), idesc, more);
+                    }
+                    umma_commit_pair(smem_u32(&st->empty[stage]));
+                    if (++stage == kDenseStages) { stage = 0; phase ^= 1u; }
+                }
+                if (!ok) break;
+                umma_commit_pair(smem_u32(&st->tmem_full[acc]));
+            }
+        }
+    } else if (warp >= kDenseFirstEpi) {
+        // ===================== epilogue (both CTAs) =====================
+        const int quad = warp & 3;                          // tensor-memory lanes this warp may read
+        const int cq = (warp - kDenseFirstEpi) >> 2;        // which half of the tile's columns
+        unsigned char *stg = epi_bufs + (warp - kDenseFirstEpi) * kEpiBufBytes;
+        const uint32_t leader_empty0 = map_to_cta(smem_u32(&st->tmem_empty[0]), 0);
+        const uint32_t leader_empty1 = map_to_cta(smem_u32(&st->tmem_empty[1]), 0);
+        constexpr int kChunks = TN / 64;                    // 32-column chunks a warp owns
+        int cursor = 0, it = 0;
+        for (int item = cluster_id; item < prm.items; item += n_clusters, ++it) {
+            const DenseTile t = dense_decode<TN, P>(prm, item, cursor);
+            const DenseProblem &q = prm.prob[t.p];
+            const int acc = it & 1;
+            if (!mbar_wait(smem_u32(&st->tmem_full[acc]), (uint32_t)(it >> 1) & 1u, wc)) break;
+            tc_fence_after();
+            const uint32_t tacc = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * kDenseAccCols + cq * kHalf);
+            const int r0 = t.m0 + rank * 128 + quad * 32, c0 = t.n0 + cq * kHalf;
+            // a cut tile's strip: 32 rows x kHalf columns, float4 j of all lanes side by side
+            float4 *strip = nullptr;
+            if (t.tail >= 0)
+                strip = reinterpret_cast<float4 *>(prm.partial) +
+                        ((size_t)(t.tail * prm.splits) * 16 + rank * 8 + cq * 4 + quad) * (32 * kHalf / 4) + lane;
+            constexpr size_t kPieceStride = (size_t)16 * (32 * kHalf / 4);
+            if (r0 < q.M) {
+#pragma unroll 1
+                for (int c = 0; c < kChunks; ++c) {
+                    if (c0 + 32 * c >= q.N) break;
+                    uint32_t w[32];
+                    tmem_ld32(tacc + 32 * c, w);
+                    tmem_ld_wait();
+                    float v[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
+                    if (t.tail < 0) {
+                        dense_finish<MODE>(q, prm.lin, t.mirror, r0, c0 + 32 * c, lane, stg, v);
+                    } else {
+                        float4 *dst = strip + (size_t)t.split * kPieceStride + (size_t)c * 256;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) __stcg(dst + 32 * j, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(acc ? leader_empty1 : leader_empty0);
+            if (t.tail >= 0 && r0 < q.M && c0 < q.N) {
+                __threadfence();
+                __syncwarp();
+                int seen = 0;
+                if (lane == 0) seen = atomicAdd(prm.counters + t.tail * 16 + rank * 8 + cq * 4 + quad, 1);
+                seen = __shfl_sync(0xFFFFFFFFu, seen, 0);
+                if (seen == prm.splits - 1) {
+                    __threadfence();
+                    if (lane == 0) prm.counters[t.tail * 16 + rank * 8 + cq * 4 + quad] = 0;   // for the next launch
+#pragma unroll 1
+                    for (int c = 0; c < kChunks; ++c) {
+                        if (c0 + 32 * c >= q.N) break;
+                        float v[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = 0.f;
+#pragma unroll 1
+                        for (int s = 0; s < prm.splits; ++s) {
+                            const float4 *src = strip + (size_t)s * kPieceStride + (size_t)c * 256;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const float4 f = __ldcg(src + 32 * j);
+                                v[4 * j] += f.x; v[4 * j + 1] += f.y; v[4 * j + 2] += f.z; v[4 * j + 3] += f.w;
+                            }
+                        }
+                        dense_finish<MODE>(q, prm.lin, t.mirror, r0, c0 + 32 * c, lane, stg, v);
+                    }
+                }
+            }
+        }
+    }
+
+    // ---- teardown: neither CTA leaves while its partner may still touch its shared or tensor memory ----
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kDenseTmemCols) : "memory");
+    }
+}
+
+// A 2-D tensor map: `cols` contiguous elements a row, boxes of 128 bytes x box_rows rows, 128-byte swizzle.
+bool encode_operand(CUtensorMap *map, const DenseOperand &o, int type, int box_rows)
+{
+    EncodeTiledFn fn = get_encode();
+    if (fn == nullptr) return false;
+    const int esz = type == DenseE4m3 ? 1 : 2;
+    const cuuint64_t dims[2] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)(o.ld * esz)};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / esz), (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUtensorMapDataType dt = type == DenseE4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                   : type == DenseF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    return fn(map, dt, 2, const_cast<void *>(o.base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// How a launch is cut: tile width, whole tiles, pieces of the rest.
+struct DensePlan { int tn, tiles, full, splits, items; };
+
+int dense_nk(DenseType type, long long k) { return (int)((k + (type == DenseE4m3 ? 127 : 63)) / (type == DenseE4m3 ? 128 : 64)); }
+
+DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int n, int sms, size_t partial_capacity)
+{
+    const int pairs = std::max(1, sms / 2);
+    auto count = [&](int tn) {
+        long long tiles = 0;
+        for (int i = 0; i < n; ++i) {
+            const long long mt = (items[i].p.M + 255) / 256, nt = (items[i].p.N + tn - 1) / tn;
+            tiles += (items[i].p.flags & kDenseSym) ? nt * (nt + 1) / 2 : mt * nt;
+        }
+        return tiles;
+    };
+    DensePlan pl;
+    // 256-column tiles unless the whole output has less than half a tile for each CTA pair: then 128-column tiles
+    // (symmetric outputs have square tiles)
+    pl.tn = (mode != DenseGram && mode != DensePoly && count(256) * 2 <= pairs) ? 128 : 256;
+    pl.tiles = (int)count(pl.tn);
+    pl.full = pl.tiles / pairs * pairs;
+    const int left = pl.tiles - pl.full;
+    pl.splits = 1;
+    if (left > 0) {
+        int min_nk = 1 << 30;
+        for (int i = 0; i < n; ++i) min_nk = std::min(min_nk, dense_nk(type, items[i].k));
+        // pieces of at least four k-blocks, one round over the pairs, as many as the workspace holds
+        const long long held = (long long)(partial_capacity / ((size_t)256 * pl.tn * 4));
+        const long long sp = std::min<long long>({std::min(pairs, kDenseMaxSplitItems) / left, min_nk / 4, 16, held / left});
+        pl.splits = (int)std::max<long long>(1, sp);
+    }
+    pl.items = pl.full + left * pl.splits;
+    return pl;
+}
+
+template <int MODE, int TYPE, int TN, int P>
+cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const LinearEpilogue *lin, void *ws, cudaStream_t s)
+{
+    DenseParams<P> prm;
+    int tiles = 0;
+    for (int i = 0; i < n; ++i) {
+        const DenseItem &it = items[i];
+        DenseProblem &q = prm.prob[i];
+        q = it.p;
+        q.nk = dense_nk((DenseType)TYPE, it.k);
+        q.mt = (q.M + 255) / 256;
+        q.nt = (q.N + TN - 1) / TN;
+        q.tile0 = tiles;
+        tiles += (q.flags & kDenseSym) ? q.nt * (q.nt + 1) / 2 : q.mt * q.nt;
+        if (!encode_operand(&prm.a[i], it.a, TYPE, (q.flags & kDenseAMn) ? 64 : 128) ||
+            !encode_operand(&prm.b[i], it.b, TYPE, (q.flags & kDenseBMn) ? 64 : TN / 2))
+            return cudaErrorInvalidValue;
+    }
+    const int pairs = std::max(1, device_sms() / 2);
+    prm.lin = lin ? *lin : LinearEpilogue{};
+    prm.n_prob = n;
+    prm.tiles = tiles;
+    prm.full_tiles = pl.full;
+    prm.splits = pl.splits;
+    prm.items = pl.items;
+    prm.status = (int *)ws;
+    prm.counters = (int *)((unsigned char *)ws + kDenseCounterOffset);
+    prm.partial = (float *)((unsigned char *)ws + kDenseHead);
+    prm.wait_limit_ns = tc_wait_limit_ns();
+
+    auto kern = dense_gemm_pair<MODE, TYPE, TN, P>;
+    static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev > 63 || !((attr_done >> dev) & 1ull)) {
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDenseSmem);
+        if (e != cudaSuccess) return e;
+        if (dev <= 63) attr_done |= 1ull << dev;
+    }
+    kern<<<2 * std::min(pairs, prm.items), kDenseThreads, kDenseSmem, s>>>(prm);
+    return cudaGetLastError();
+}
+
+template <int MODE, int TYPE, int P>
+cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin, void *ws, size_t cap, cudaStream_t s)
+{
+    if (n > P) return cudaErrorInvalidValue;
+    const DensePlan pl = dense_plan((DenseMode)MODE, (DenseType)TYPE, items, n, device_sms(), cap);
+    if constexpr (MODE == DenseGram || MODE == DensePoly) {
+        return launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, ws, s);
+    } else {
+        return pl.tn == 128 ? launch_tn<MODE, TYPE, 128, P>(pl, items, n, lin, ws, s)
+                            : launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, ws, s);
+    }
+}
+
+}  // namespace
+
+size_t dense_partial_bytes(DenseMode mode, DenseType type, const DenseItem *items, int n)
+{
+    const DensePlan pl = dense_plan(mode, type, items, n, kDenseSms, ~(size_t)0 >> 1);
+    return pl.splits > 1 ? (size_t)(pl.items - pl.full) * 256 * pl.tn * 4 : 0;
+}
+
+cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *items, int n, const LinearEpilogue *lin, void *ws,
+                         size_t partial_capacity, cudaStream_t s)
+{
+    if (n < 1 || n > kDenseMaxProblems) return cudaErrorInvalidValue;
+    switch (mode) {
+    case DenseLinear:
+        return type == DenseE4m3 ? launch_mode<DenseLinear, DenseE4m3, 1>(items, n, lin, ws, partial_capacity, s)
+                                 : launch_mode<DenseLinear, DenseBf16, 1>(items, n, lin, ws, partial_capacity, s);
+    case DensePlain: return launch_mode<DensePlain, DenseBf16, 2>(items, n, lin, ws, partial_capacity, s);
+    case DenseGram: return launch_mode<DenseGram, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, s);
+    case DensePoly: return launch_mode<DensePoly, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, s);
+    case DenseStep: return launch_mode<DenseStep, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, s);
+    }
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace modse

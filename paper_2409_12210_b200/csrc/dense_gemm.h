@@ -1,0 +1,74 @@
+// Dense matrix products on CTA pairs (tcgen05, cta_group::2) with fused epilogues: the products of modse_linear, its
+// gradients and modse_orthogonalize.
+#pragma once
+
+#include <cuda.h>
+
+#include "modse_internal.h"
+
+namespace modse {
+
+// What happens to an accumulator on its way out.
+enum DenseMode : int {
+    DenseLinear = 0,   // y = act(acc * sx * sw + bias) + residual, z beside it
+    DensePlain = 1,    // out = acc (bf16 or fp32)
+    DenseGram = 2,     // out = alpha acc (fp16), symmetric
+    DensePoly = 3,     // out = alpha acc + beta in0 (fp16), symmetric
+    DenseStep = 4      // x = alpha acc + beta (hi + lo): hi, lo (fp16), or the final bf16 result
+};
+enum DenseType : int { DenseBf16 = 0, DenseF16 = 1, DenseE4m3 = 2 };
+enum : int {
+    kDenseAMn = 1,     // the row operand lies with its rows along the contiguous axis ([K, M]), not [M, K]
+    kDenseBMn = 2,     // same for the column operand ([K, N], not [N, K])
+    kDenseSym = 4,     // out is symmetric: tiles below the diagonal are not computed but mirrored
+    kDenseLast = 8,    // DenseStep: write the final result
+    kDenseF32 = 16     // DensePlain: out is fp32
+};
+
+// One product out[M, N] = sum_k A[m, k] B[n, k] of a launch.
+struct DenseProblem {
+    int M, N, nk;            // output extents, k-blocks (128 bytes of the contraction axis each)
+    int mt, nt;              // row and column tiles
+    int tile0;               // this problem's first tile in the launch's list
+    int flags;
+    float alpha, beta, scale;
+    const void *in0, *in1;
+    void *out0, *out1;
+    long long ld_in, ld_out; // elements
+};
+
+struct LinearEpilogue {
+    const float *sx, *sw;
+    const __nv_bfloat16 *bias, *residual;
+    __nv_bfloat16 *z, *y;
+    int act;
+};
+
+constexpr int kDenseMaxProblems = 16;
+// An operand as it lies in memory: rows x cols elements, ld elements from row to row (a multiple of 16 bytes).
+struct DenseOperand {
+    const void *base;
+    long long rows, cols, ld;
+};
+struct DenseItem {
+    DenseOperand a, b;
+    DenseProblem p;          // mt, nt, nk, tile0 are filled in by the launch
+    long long k;             // length of the contraction in elements
+};
+
+// Workspace of a call that launches dense products: the status word, the arrival counters of cut tiles (both zeroed by
+// the call before its first launch; a launch leaves the counters zero), then the fp32 pieces of cut tiles.
+constexpr int kDenseSms = 148;                         // workspace sizes are asked for without a device
+constexpr int kDenseMaxSplitItems = 128;               // pieces of one launch: at most one for each CTA pair
+constexpr size_t kDenseCounterOffset = 64;
+constexpr size_t kDenseZeroBytes = kDenseCounterOffset + (size_t)kDenseMaxSplitItems * 16 * 4;
+constexpr size_t kDenseHead = (kDenseZeroBytes + 255) / 256 * 256;
+
+// Bytes behind the head that a launch of these products (extents and flags of p, k) can use for pieces.
+size_t dense_partial_bytes(DenseMode mode, DenseType type, const DenseItem *items, int n);
+
+// Launches n products of one mode and type as one kernel on a workspace whose head is `ws`.
+cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *items, int n, const LinearEpilogue *lin, void *ws,
+                         size_t partial_capacity, cudaStream_t s);
+
+}  // namespace modse

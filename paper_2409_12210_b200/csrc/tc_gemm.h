@@ -77,6 +77,7 @@ void tc_set_default_plan(int mask);   // tile plan used by layers that have none
 int tc_default_plan();
 void tc_set_dynamic_tiles(int on);    // 1 (default): CTAs take tiles from a shared counter; 0: tiles are dealt statically
 void tc_set_wait_limit_ms(int ms);    // limit of every bounded wait inside the kernels (default 2000)
+unsigned long long tc_wait_limit_ns();
 // bit per product: sixteen epilogue warps on 128-row tiles / one-CTA 256-row tiles / CTA-pair tiles
 void tc_set_epilogue_warps16(int narrow_mask, int wide_mask, int pair_mask);
 void tc_set_skip_tile(int kind, int tile);   // the producer of the CTA that gets `tile` of product `kind` stops there (-1: off)

@@ -1,0 +1,304 @@
+"""The dense product with bias, activation and residual (modse_linear and its gradient) against a plain implementation
+in 64 bits, element by element.
+
+Bounds.  Products of 16- or 8-bit numbers are exact in fp32; K of them are added in fp32, each addition off by at most
+2^-23 of the running magnitude (tensor cores may truncate), which stays below S = sum_k |x w|: K 2^-23 S, and a few more
+roundings for scales, bias and residual: ACC = (K + 64) 2^-23 times the sum of all magnitudes.  An activation changes an
+error by at most 1.13 (the largest slope of gelu and silu is below that) and adds its own arithmetic, 2^-20 of |z|.  An
+output is rounded once, to bf16: 2^-8 of its value.  In backward dz is rounded to bf16 before it enters a product: 2^-8
+of every term."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+ACTS = ["none", "relu", "gelu", "silu"]
+BF, U = 2.0 ** -8, 2.0 ** -23
+# (T, d_in, d_out): one token, few, ragged tiles, one tile over, several tiles with a tail, many tiles
+SHAPES = [(1, 8, 8), (1, 2048, 2048), (3, 136, 264), (17, 4096, 24), (32, 512, 1000), (33, 64, 136), (64, 1024, 4096),
+          (127, 200, 72), (129, 80, 520), (257, 648, 1032), (300, 2816, 2048), (1000, 256, 384), (2500, 512, 2048)]
+
+
+def f64(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def phi(z):
+    return 0.5 * (1 + np.vectorize(math.erf)(z / math.sqrt(2)))
+
+
+def act64(z, name):
+    return {"none": lambda: z, "relu": lambda: np.maximum(z, 0), "gelu": lambda: z * phi(z),
+            "silu": lambda: z / (1 + np.exp(-z))}[name]()
+
+
+def slope64(z, name):
+    if name == "none":
+        return np.ones_like(z)
+    if name == "relu":
+        return (z > 0).astype(np.float64)
+    if name == "gelu":
+        return phi(z) + z * np.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    s = 1 / (1 + np.exp(-z))
+    return s * (1 + z * (1 - s))
+
+
+def rand(rng, *shape, std=1.0):
+    return torch.from_numpy((rng.standard_normal(shape) * std).astype(np.float32)).cuda()
+
+
+def guarded(shape, dtype=torch.bfloat16):
+    """A buffer with a filled margin behind it."""
+    n = int(np.prod(shape))
+    base = torch.full((n + 512,), 3.0, dtype=dtype, device="cuda")
+    return base[:n].view(shape), base[n:]
+
+
+def workspace(n):
+    ws = torch.full((n + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    return ws[:n], ws[n:]
+
+
+def check_forward(T, k, n, f8, act, bias, residual, save, seed=0):
+    from paper_2409_12210_b200 import binding as B
+    rng = np.random.default_rng(seed)
+    x, w = rand(rng, T, k), rand(rng, n, k, std=k ** -0.5)
+    sx = sw = None
+    if f8:
+        sx, sw = rand(rng, T).abs() + 0.1, rand(rng, n).abs() + 0.1
+        x, w = x.to(torch.float8_e4m3fn), (w * math.sqrt(k)).to(torch.float8_e4m3fn)
+        sw *= k ** -0.5
+    else:
+        x, w = x.bfloat16(), w.bfloat16()
+    b = rand(rng, n).bfloat16() if bias else None
+    r = rand(rng, T, n).bfloat16() if residual else None
+    y, y_margin = guarded((T, n))
+    z, z_margin = guarded((T, n))
+    ws, ws_margin = workspace(B.linear_workspace_bytes(x.dtype, T, k, n))
+    B.linear(x, w, y, ws, bias=b, residual=r, activation=act, z=z if save else None, x_scale=sx, w_scale=sw)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    X, W = f64(x), f64(w)
+    if f8:
+        X, W = X * f64(sx)[:, None], W * f64(sw)[:, None]
+    zz, mag = X @ W.T, np.abs(X) @ np.abs(W).T
+    if bias:
+        zz, mag = zz + f64(b), mag + np.abs(f64(b))
+    rr = f64(r) if residual else 0.0
+    yy = act64(zz, act) + rr
+    acc = (k + 64) * U * mag
+    if save:
+        assert np.all(np.abs(f64(z) - zz) <= BF * np.abs(zz) + acc * (1 + BF))
+    tol = BF * np.abs(yy) + (1.13 * acc + 2.0 ** -20 * np.abs(zz) + U * np.abs(rr)) * (1 + BF)
+    bad = np.abs(f64(y) - yy) > tol
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist())
+    for m in (y_margin, z_margin):
+        assert bool((m == 3).all())
+    assert bool((ws_margin == 0xA5).all())
+    again = torch.empty_like(y)
+    B.linear(x, w, again, ws, bias=b, residual=r, activation=act, x_scale=sx, w_scale=sw)
+    assert torch.equal(again, y)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("act,bias,residual,save", [("none", False, False, False), ("gelu", True, False, True),
+                                                    ("silu", True, True, True), ("relu", False, True, False)])
+def test_forward_bf16(shape, act, bias, residual, save):
+    check_forward(*shape, False, act, bias, residual, save)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(T, (k + 15) // 16 * 16, n) for T, k, n in SHAPES])
+@pytest.mark.parametrize("act,bias,residual,save", [("none", False, True, False), ("silu", True, False, True)])
+def test_forward_e4m3(shape, act, bias, residual, save):
+    check_forward(*shape, True, act, bias, residual, save)
+
+
+def run_backward(T, k, n, act, want=("dx", "dw", "db"), seed=1):
+    from paper_2409_12210_b200 import binding as B
+    rng = np.random.default_rng(seed)
+    x, w, dy = rand(rng, T, k).bfloat16(), rand(rng, n, k, std=k ** -0.5).bfloat16(), rand(rng, T, n).bfloat16()
+    z = rand(rng, T, n).bfloat16()
+    z.view(-1)[::7] = 0
+    dx, m1 = guarded((T, k))
+    dw, m2 = guarded((n, k))
+    db, m3 = guarded((n,), torch.float32)
+    ws, m4 = workspace(B.linear_backward_workspace_bytes(T, k, n))
+    B.linear_backward(x, w, dy, z if act != "none" else None, act, dx if "dx" in want else None,
+                      dw if "dw" in want else None, db if "db" in want else None, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    for m in (m1, m2, m3):
+        assert bool((m == 3).all())
+    assert bool((m4 == 0xA5).all())
+    return x, w, dy, z, dx, dw, db
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("act", ACTS)
+def test_backward(shape, act):
+    T, k, n = shape
+    x, w, dy, z, dx, dw, db = run_backward(T, k, n, act)
+    X, W, G, Z = f64(x), f64(w), f64(dy), f64(z)
+    dz = G * slope64(Z, act)
+    # dz carries its own arithmetic (2^-19 of dy; slopes are at most 1.13) and, inside the products, one rounding to bf16
+    own = 2.0 ** -19 * np.abs(G)
+    term = np.abs(dz) * BF + own * (1 + BF) if act != "none" else 0 * np.abs(dz)
+    for got, ref, err, mag, terms in ((dx, dz @ W, term @ np.abs(W), np.abs(dz) @ np.abs(W), n),
+                                      (dw, dz.T @ X, term.T @ np.abs(X), np.abs(dz).T @ np.abs(X), T)):
+        tol = BF * np.abs(ref) + (err + (terms + 64) * U * (mag + err)) * (1 + BF)
+        bad = np.abs(f64(got) - ref) > tol
+        assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist())
+    tol = own.sum(0) + (T / 8 + 200) * U * (np.abs(dz) + own).sum(0)
+    assert np.all(np.abs(f64(db) - dz.sum(0)) <= tol)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("want", [("dx",), ("dw",), ("db",), ("dx", "db")])
+def test_backward_outputs_that_are_not_wanted_are_left_alone(want):
+    full = run_backward(257, 648, 1032, "silu")
+    part = run_backward(257, 648, 1032, "silu", want)
+    for name, a, b in (("dx", full[4], part[4]), ("dw", full[5], part[5]), ("db", full[6], part[6])):
+        if name in want:
+            # which pieces a cut tile is summed from depends on the products of the launch: one bf16 step at most
+            assert torch.allclose(a.float(), b.float(), rtol=2.0 ** -7, atol=1e-5)
+        else:
+            assert bool((b == 3).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_slopes_against_differences(act):
+    """dbias of a batch of one token is the slope itself (dy = 1): central differences of the 64-bit activation."""
+    from paper_2409_12210_b200 import binding as B
+    z = torch.linspace(-6, 6, 1024).bfloat16().cuda().view(1, 1024)
+    z[0, 512] = 0.25                                       # away from relu's corner
+    dy, db = torch.ones_like(z), torch.empty(1024, device="cuda")
+    ws = torch.empty(B.linear_backward_workspace_bytes(1, 8, 1024), dtype=torch.uint8, device="cuda")
+    x, w = torch.zeros(1, 8, device="cuda").bfloat16(), torch.zeros(1024, 8, device="cuda").bfloat16()
+    B.linear_backward(x, w, dy, z, act, None, None, db, ws)
+    Z, h = f64(z)[0], 1e-6
+    keep = np.abs(Z) > 1e-4
+    num = (act64(Z + h, act) - act64(Z - h, act)) / (2 * h)
+    assert np.all(np.abs(f64(db) - num)[keep] <= 1e-6)
+
+
+@pytest.mark.gpu
+def test_far_activations_and_special_values():
+    """The activations' ends: no NaN from exp overflowing, NaN and infinities pass through a row and stay in it."""
+    from paper_2409_12210_b200 import binding as B
+    x = torch.zeros(5, 64, device="cuda").bfloat16()
+    x[0, 0], x[1, 0], x[2, 0], x[3, 1] = 3e4, -3e4, float("nan"), 1.0
+    w = torch.zeros(16, 64, device="cuda").bfloat16()
+    w[:, 0] = 1
+    ws = torch.empty(B.linear_workspace_bytes(x.dtype, 5, 64, 16), dtype=torch.uint8, device="cuda")
+    y = torch.empty(5, 16, device="cuda").bfloat16()
+    for act in ACTS:
+        B.linear(x, w, y, ws, activation=act)
+        assert bool((y[0] == x[0, 0]).all()) and bool(torch.isnan(y[2]).all())
+        assert bool((y[1] == (x[1, 0] if act == "none" else 0)).all())
+        assert bool((y[3:] == 0).all())
+
+
+@pytest.mark.gpu
+def test_in_place_residual_replay_and_two_streams():
+    from paper_2409_12210_b200 import binding as B
+    rng = np.random.default_rng(5)
+    x, w, r = rand(rng, 300, 512).bfloat16(), rand(rng, 512, 512, std=0.05).bfloat16(), rand(rng, 300, 512).bfloat16()
+    n = B.linear_workspace_bytes(x.dtype, 300, 512, 512)
+    wss = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    ref = torch.empty_like(r)
+    B.linear(x, w, ref, wss[0], residual=r, activation="silu")
+    stream = r.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.linear(x, w, stream, wss[0], residual=stream, activation="silu")
+    for _ in range(3):
+        stream.copy_(r)
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(stream, ref)
+    # two calls at once, a workspace each
+    outs = [torch.empty_like(r) for _ in range(2)]
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for side, out, ws in zip(sides, outs, wss):
+            with torch.cuda.stream(side):
+                B.linear(x, w, out, ws, residual=r, activation="silu")
+    torch.cuda.synchronize()
+    for out in outs:
+        assert torch.equal(out, ref)
+
+
+@pytest.mark.gpu
+def test_empty_batch_and_binding_refusals():
+    from paper_2409_12210_b200 import binding as B
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    x, w, y = torch.empty(0, 64, **bf), torch.zeros(32, 64, **bf), torch.empty(0, 32, **bf)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    B.linear(x, w, y, ws)
+    dw, db = torch.ones(32, 64, **bf), torch.ones(32, device="cuda")
+    B.linear_backward(x, w, y, y, "gelu", x, dw, db, ws)
+    assert bool((dw == 0).all()) and bool((db == 0).all())
+    x, y = torch.zeros(4, 64, **bf), torch.empty(4, 32, **bf)
+    with pytest.raises(ValueError):
+        B.linear(x, w.t().contiguous().t(), y, ws)
+    with pytest.raises(ValueError):
+        B.linear(x, w, y, ws, bias=torch.zeros(32, device="cuda"))
+    with pytest.raises(ValueError):
+        B.linear(x, w, y, ws, z=torch.empty(4, 31, **bf))
+    with pytest.raises(B.ModseError):
+        B.linear(x, w, y, ws[:64])
+    with pytest.raises(KeyError):
+        B.linear(x, w, y, ws, activation="tanh")
+    with pytest.raises(TypeError):
+        B.linear(x.float(), w.float(), y, ws)
+
+
+def test_refusals_need_no_gpu():
+    from paper_2409_12210_b200 import binding as B
+    from paper_2409_12210_b200 import build
+    build.build()
+    lib = B.load()
+    p = 0x10000
+    need = lib.modse_linear_workspace_bytes(B.MODSE_BF16, 4, 64, 32)
+    assert need > 0 and need % 256 == 0
+    for bad in [(B.MODSE_F32, 4, 64, 32), (9, 4, 64, 32), (B.MODSE_BF16, -1, 64, 32), (B.MODSE_BF16, 4, 60, 32),
+                (B.MODSE_BF16, 4, 64, 36), (B.MODSE_BF16, 4, 0, 32), (B.MODSE_BF16, 4, 64, 0), (B.MODSE_E4M3, 4, 72, 32),
+                (B.MODSE_BF16, 1 << 30, 64, 1 << 26)]:
+        assert lib.modse_linear_workspace_bytes(*bad) == 0, bad
+
+    def call(dtype=B.MODSE_BF16, T=4, k=64, n=32, act=0, ws=p, size=None, x=p, w=p, x_scale=None, w_scale=None, bias=p,
+             residual=p, z=p, y=p, none=False):
+        args = B._Linear(x, w, x_scale, w_scale, bias, residual, z, y)
+        return lib.modse_linear(dtype, T, k, n, act, None if none else args, ws, need if size is None else size, None)
+
+    inv = B.MODSE_ERR_INVALID_ARG
+    assert call(T=0) == B.MODSE_OK
+    assert call(dtype=B.MODSE_F32) == B.MODSE_ERR_UNSUPPORTED
+    assert call(size=need - 1) == B.MODSE_ERR_WORKSPACE_TOO_SMALL
+    for bad in [dict(none=True), dict(act=-1), dict(act=4), dict(dtype=5), dict(T=-1), dict(k=60), dict(n=12), dict(x=None),
+                dict(w=None), dict(y=None), dict(x=p + 8), dict(w=p + 8), dict(bias=p + 2), dict(residual=p + 8),
+                dict(z=p + 4), dict(y=p + 8), dict(ws=None), dict(ws=p + 64), dict(x_scale=p), dict(w_scale=p),
+                dict(dtype=B.MODSE_E4M3), dict(dtype=B.MODSE_E4M3, x_scale=p), dict(dtype=B.MODSE_E4M3, w_scale=p),
+                dict(dtype=B.MODSE_E4M3, x_scale=p + 2, w_scale=p), dict(dtype=B.MODSE_E4M3, x_scale=p, w_scale=p + 4)]:
+        assert call(**bad) == inv, bad
+
+    need_b = lib.modse_linear_backward_workspace_bytes(4, 64, 32)
+    assert need_b > 0
+    for bad in [(-1, 64, 32), (4, 60, 32), (4, 64, 33), (4194241, 64, 32)]:
+        assert lib.modse_linear_backward_workspace_bytes(*bad) == 0, bad
+
+    def back(T=4, k=64, n=32, act=2, ws=p, size=None, x=p, w=p, dy=p, z=p, dx=p, dw=p, dbias=p, none=False):
+        args = B._LinearGrads(x, w, dy, z, dx, dw, dbias)
+        return lib.modse_linear_backward(T, k, n, act, None if none else args, ws, need_b if size is None else size, None)
+
+    assert back(size=need_b - 1) == B.MODSE_ERR_WORKSPACE_TOO_SMALL
+    for bad in [dict(none=True), dict(act=4), dict(T=-1), dict(k=4), dict(n=4), dict(x=None), dict(w=None), dict(dy=None),
+                dict(z=None), dict(x=p + 8), dict(w=p + 8), dict(dy=p + 8), dict(z=p + 8), dict(dx=p + 8), dict(dw=p + 8),
+                dict(dbias=p + 2), dict(ws=None), dict(ws=p + 16), dict(dx=None, dw=None, dbias=None)]:
+        assert back(**bad) == inv, bad
+    assert lib.modse_check_workspace_status(None, None) == inv
