@@ -393,6 +393,44 @@ modse_status_t modse_linear_backward(int n_tokens, int d_in, int d_out, modse_ac
                                      const modse_linear_grads_t *args, void *workspace, size_t workspace_bytes,
                                      void *cuda_stream);
 
+/* Orthogonalised updates (the step of the Muon optimiser): for each matrix G of a
+ * set, by `steps` Newton-Schulz iterations on X0 = G / (|G|_F + eps),
+ *   A = X X^T,  X <- a X + (b A + c A^2) X,   update = scale X,
+ * where the shorter side of G plays the part of X's rows.  Muon's coefficients are
+ * a, b, c = 3.4445, -4.7750, 2.0315 and five steps.  A matrix of zeros gives zeros
+ * (with eps > 0).
+ * grad and update [rows, cols] with ld_grad, ld_update elements from row to row
+ * (>= cols), so a matrix may be a column block of a wider one; no alignment beyond the
+ * element's.  grad in `dtype` (MODSE_F32 or MODSE_BF16), update bf16, not
+ * overlapping any grad.  rows, cols in 1 .. 2^20, the shorter of them at most 2^17.
+ * The products read fp16 factors and accumulate in fp32, X is carried in 22 bits:
+ * the relative error of an update is of the order of its bf16 rounding.
+ * Coefficients that let a singular value of the iteration pass 7.5 are
+ * MODSE_ERR_UNSUPPORTED.  The workspace holds up to 16 matrices at a time; longer
+ * sets are worked off in order.
+ *
+ * modse_orthogonalize_wgrads does it for the expert matrices of a layer, straight
+ * from the gradients modse_backward wrote (dw_gate, dw_up, dw_down of `grads`; the
+ * router's is left out) into `updates` of the same layouts in bf16.  dtype says what
+ * the gradients are (MODSE_F32 for those of modse_set_output_f32 layers too).
+ * scales: NULL, or host floats [N][3], one a matrix: gate, up, down of expert 0, 1, ... */
+typedef struct {
+    const void *grad;
+    void *update;
+    long long ld_grad, ld_update;
+    int rows, cols;
+    float scale;
+} modse_matrix_t;
+size_t modse_orthogonalize_workspace_bytes(int n_matrices, const modse_matrix_t *matrices);
+modse_status_t modse_orthogonalize(modse_dtype_t dtype, int n_matrices, const modse_matrix_t *matrices, int steps,
+                                   const float *coefficients, float eps, void *workspace, size_t workspace_bytes,
+                                   void *cuda_stream);
+size_t modse_orthogonalize_wgrads_workspace_bytes(const modse_layer_t *layer);
+modse_status_t modse_orthogonalize_wgrads(const modse_layer_t *layer, modse_dtype_t dtype, const modse_wgrads_t *grads,
+                                          const modse_wgrads_t *updates, const float *scales, int steps,
+                                          const float *coefficients, float eps, void *workspace, size_t workspace_bytes,
+                                          void *cuda_stream);
+
 /* Synchronises the stream and reads the status word of the last call that used this
  * workspace (modse_linear, modse_linear_backward, modse_orthogonalize): MODSE_OK or
  * MODSE_ERR_DEVICE_TIMEOUT.                                                  */

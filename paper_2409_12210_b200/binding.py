@@ -57,6 +57,11 @@ class _LinearGrads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("x", "w", "dy", "z", "dx", "dw", "dbias")]
 
 
+class _Matrix(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("update", ctypes.c_void_p), ("ld_grad", ctypes.c_longlong),
+                ("ld_update", ctypes.c_longlong), ("rows", ctypes.c_int), ("cols", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
 _lib = None
 
 
@@ -159,6 +164,16 @@ def load():
     lib.modse_linear_backward_workspace_bytes.argtypes = [ci, ci, ci]
     lib.modse_linear_backward.restype = ci
     lib.modse_linear_backward.argtypes = [ci, ci, ci, ci, ctypes.POINTER(_LinearGrads), vp, sz, vp]
+    fp = ctypes.POINTER(ctypes.c_float)
+    lib.modse_orthogonalize_workspace_bytes.restype = sz
+    lib.modse_orthogonalize_workspace_bytes.argtypes = [ci, ctypes.POINTER(_Matrix)]
+    lib.modse_orthogonalize.restype = ci
+    lib.modse_orthogonalize.argtypes = [ci, ci, ctypes.POINTER(_Matrix), ci, fp, cf, vp, sz, vp]
+    lib.modse_orthogonalize_wgrads_workspace_bytes.restype = sz
+    lib.modse_orthogonalize_wgrads_workspace_bytes.argtypes = [vp]
+    lib.modse_orthogonalize_wgrads.restype = ci
+    lib.modse_orthogonalize_wgrads.argtypes = [vp, ci, ctypes.POINTER(_WGrads), ctypes.POINTER(_WGrads), fp, ci, fp, cf, vp,
+                                               sz, vp]
     lib.modse_check_workspace_status.restype = ci
     lib.modse_check_workspace_status.argtypes = [vp, vp]
     lib.modse_debug_use_fma_path.restype = None
@@ -366,6 +381,51 @@ def linear_backward(x, w, dy, z, activation: str, dx, dw, dbias, workspace) -> N
         raise ModseError(st, "modse_linear_backward")
 
 
+MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+def orthogonalize_workspace_bytes(shapes) -> int:
+    """Workspace bytes for matrices of these (rows, cols)."""
+    arr = (_Matrix * len(shapes))(*[_Matrix(None, None, c, c, r, c, 1.0) for r, c in shapes])
+    return int(load().modse_orthogonalize_workspace_bytes(len(shapes), arr))
+
+
+def _ld(name, t):
+    r, c = _rows(name, t)
+    ld = t.stride(0) if r > 1 else max(c, 1)
+    if (c > 1 and t.stride(1) != 1) or ld < c:
+        raise ValueError(f"{name}: expected rows of contiguous elements that do not overlap, got strides {t.stride()}")
+    return ld
+
+
+def orthogonalize(grads, updates, workspace, *, scales=None, steps: int = 5, coefficients=MUON_COEFFICIENTS,
+                  eps: float = 1e-7) -> None:
+    """modse_orthogonalize on the current stream: the Newton-Schulz iterate of each matrix of ``grads`` (all bf16 or all
+    fp32; rows may be strided, so column blocks of a wider matrix work) times its entry of ``scales`` into the bf16
+    matrix of the same place in ``updates``."""
+    import torch
+    n = len(grads)
+    if len(updates) != n or (scales is not None and len(scales) != n):
+        raise ValueError(f"{n} gradients, {len(updates)} updates, {n if scales is None else len(scales)} scales")
+    if n == 0:
+        return
+    dt, dev = grads[0].dtype, grads[0].device
+    code, stream = _dtype_code(grads[0]), _current_stream("grads", grads[0])
+    arr = (_Matrix * n)()
+    for i, (g, u, m) in enumerate(zip(grads, updates, arr)):
+        if g.dtype != dt or g.device != dev or u.dtype != torch.bfloat16 or u.device != dev or u.shape != g.shape:
+            raise ValueError(f"matrix {i}: expected a {dt} gradient and a bf16 update of one shape on {dev}, got "
+                             f"{g.dtype} {tuple(g.shape)} on {g.device} and {u.dtype} {tuple(u.shape)} on {u.device}")
+        m.ld_grad, m.ld_update = _ld(f"gradient {i}", g), _ld(f"update {i}", u)
+        m.grad, m.update = g.data_ptr(), u.data_ptr()
+        m.rows, m.cols = g.shape
+        m.scale = 1.0 if scales is None else scales[i]
+    st = load().modse_orthogonalize(code, n, arr, steps, (ctypes.c_float * 3)(*coefficients), eps,
+                                    *_workspace(workspace, dev), stream)
+    if st != MODSE_OK:
+        raise ModseError(st, "modse_orthogonalize")
+
+
 def check_workspace_status(workspace) -> int:
     """Status the last operator call on this workspace left (synchronises the current stream)."""
     import torch
@@ -549,6 +609,33 @@ class ModseLayer:
                                           dgamma.data_ptr() if dgamma is not None else None)
         if st != MODSE_OK:
             raise ModseError(st, "modse_set_noise_grads")
+
+    def orthogonalize_workspace_bytes(self) -> int:
+        return int(load().modse_orthogonalize_wgrads_workspace_bytes(self._h))
+
+    def orthogonalize_wgrads(self, dw_gate, dw_up, dw_down, up_gate, up_up, up_down, workspace, *, scales=None,
+                             steps: int = 5, coefficients=MUON_COEFFICIENTS, eps: float = 1e-7) -> None:
+        """Orthogonalised updates of every expert's three matrices from the gradients :meth:`backward` wrote (bf16, or
+        fp32 with :meth:`set_output_f32`) into bf16 tensors of the same layouts.  ``scales``: None or N x 3 numbers
+        (gate, up, down of each expert)."""
+        import torch
+        dt, dev = dw_gate.dtype, dw_gate.device
+        S, d, stream = sum(self.ffn_sizes), self.d_model, _current_stream("dw_gate", dw_gate)
+        wide, tall, bf = (d, S), (S, d), torch.bfloat16
+        g = _WGrads(None, _buffer("dw_gate", dw_gate, tall, dt, dev), _buffer("dw_up", dw_up, tall, dt, dev),
+                    _buffer("dw_down", dw_down, wide, dt, dev))
+        u = _WGrads(None, _buffer("up_gate", up_gate, tall, bf, dev), _buffer("up_up", up_up, tall, bf, dev),
+                    _buffer("up_down", up_down, wide, bf, dev))
+        flat = None
+        if scales is not None:
+            rows = [[float(v) for v in row] for row in scales]
+            if len(rows) != self.n_experts or any(len(row) != 3 for row in rows):
+                raise ValueError(f"scales: expected {self.n_experts} x 3 numbers")
+            flat = (ctypes.c_float * (3 * self.n_experts))(*[v for row in rows for v in row])
+        st = load().modse_orthogonalize_wgrads(self._h, _dtype_code(dw_gate), g, u, flat, steps,
+                                               (ctypes.c_float * 3)(*coefficients), eps, *_workspace(workspace, dev), stream)
+        if st != MODSE_OK:
+            raise ModseError(st, "modse_orthogonalize_wgrads")
 
     def set_output_f32(self, on: bool) -> None:
         st = load().modse_set_output_f32(self._h, int(bool(on)))

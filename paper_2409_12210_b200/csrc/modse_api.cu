@@ -159,6 +159,15 @@ static bool tc_supported(const modse_layer *L)
     return true;
 }
 
+int layer_experts(const modse_layer_t *layer) { return layer->meta.N; }
+void layer_expert(const modse_layer_t *layer, int e, int *d, int *S, int *offset, int *width)
+{
+    *d = layer->meta.d;
+    *S = layer->meta.S;
+    *offset = layer->meta.hoff[e];
+    *width = layer->h[e];
+}
+
 }  // namespace modse
 
 using namespace modse;

@@ -108,6 +108,10 @@ cudaError_t launch_canaries(void *ws, const WsLayout &L, bool check, int *status
 cudaError_t launch_aux_loss(const LayerMeta &m, int T, int nblk_bwd, const WsPtrs &p, float alpha, float *loss,
                             float *f, float *P, cudaStream_t s, int *launches);
 
+// Experts of a layer object, and where expert e lies: d_model, total width, width offset, width (modse_api.cu).
+int layer_experts(const modse_layer_t *layer);
+void layer_expert(const modse_layer_t *layer, int e, int *d, int *S, int *offset, int *width);
+
 // ---- shared by the operators around the layer (norm_kernels.cu) ----
 int device_sms();      // SMs of the current device (148 where the question fails)
 // out[c] = sum over r of part[r][c], in a fixed order

@@ -1,0 +1,237 @@
+"""Orthogonalised updates (modse_orthogonalize) against the iteration in 64 bits.
+
+Bound.  The documented roundings are: factors of the products in fp16 (2^-11 of a value), X carried in 22 bits, fp32
+accumulation, one rounding of the result to bf16 (2^-8).  What the first two do to the result depends on the spectrum, so
+the test runs the iteration in 64 bits with exactly these roundings put in by hand; its distance E from the iteration
+without them is the size of the error they cause.  A kernel that accumulates in another order meets other instances of
+the same roundings, so its own error before the last rounding is held to 2 E in norm, and an element to 10 times the
+root mean square of that, each plus the last rounding."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+A, B_, C = MUON = (3.4445, -4.7750, 2.0315)
+U32 = 2.0 ** -23
+
+
+def iterate(G, steps=5, k=MUON, eps=1e-7, rounded=False):
+    def fp16(t, s):
+        return (t * s).half().double() / s if rounded else t
+
+    X = G.double()
+    X = X / (X.norm() + eps)
+    tall = X.shape[0] > X.shape[1]
+    X = X.T if tall else X
+    if rounded:
+        hi = fp16(X, 4096.0)
+        X = hi + fp16(X - hi, 4096.0)
+    for i in range(steps):
+        Xh = fp16(X, 4096.0)
+        M = fp16(Xh @ Xh.T, 1024.0)
+        P = fp16(k[1] * M + k[2] * (M @ M), 1024.0)
+        X = k[0] * X + P @ Xh
+        if rounded and i + 1 < steps:
+            hi = fp16(X, 4096.0)
+            X = hi + fp16(X - hi, 4096.0)
+    return X.T if tall else X
+
+
+def check(out, G, scale=1.0, **kw):
+    ref, emu = iterate(G, **kw) * scale, iterate(G, rounded=True, **kw) * scale
+    long = max(G.shape)
+    # the fp32 sums: at most `long` additions a product, three products a step, amplified like the other errors (8 covers
+    # the worst slope of the last steps): far below E except where E happens to vanish (a 1 x 1 matrix, powers of two)
+    err = 2 * (emu - ref).norm() + 8 * 3 * 5 * min(long, 64) * U32 * ref.norm()
+    got = out.double()
+    assert float((got - ref).norm()) <= float(err + 2.0 ** -8 * ref.norm())
+    rms = err / max(1, ref.numel()) ** 0.5
+    bad = (got - ref).abs() > 10 * rms + 2.0 ** -8 * ref.abs() * 1.01
+    assert not bool(bad.any()), (int(bad.sum()), float((got - ref).abs().max()), float(rms))
+
+
+def gaussian(r, c, seed, dtype=torch.bfloat16):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(r, c, generator=g) * 0.02).to(dtype).cuda()
+
+
+def low_rank(r, c, rank, seed, dtype=torch.bfloat16):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(r, rank, generator=g) @ torch.randn(rank, c, generator=g) * 0.01).to(dtype).cuda()
+
+
+def run(grads, **kw):
+    from paper_2409_12210_b200 import binding as B
+    outs = [torch.full(g.shape, 7.0, dtype=torch.bfloat16, device="cuda") for g in grads]
+    n = B.orthogonalize_workspace_bytes([g.shape for g in grads])
+    ws = torch.full((n + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    B.orthogonalize(grads, outs, ws[:n], **kw)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    assert bool((ws[n:] == 0xA5).all())
+    return outs
+
+
+SHAPES = [(1, 1), (1, 77), (77, 1), (8, 8), (9, 200), (200, 9), (64, 96), (160, 64), (130, 130), (257, 300), (300, 257),
+          (512, 520), (1000, 264), (256, 4099), (640, 2048), (2816, 1024)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_one_matrix(shape, dtype):
+    G = gaussian(*shape, seed=3, dtype=dtype)
+    out, = run([G])
+    check(out, G)
+    again, = run([G])
+    assert torch.equal(out, again)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,rank", [((256, 700), 4), ((700, 256), 32), ((512, 512), 200), ((96, 64), 1)])
+def test_rank_deficient(shape, rank):
+    """What the rank leaves empty stays empty: noise there would be amplified by a^5."""
+    G = low_rank(*shape, rank, seed=4)
+    out, = run([G])
+    check(out, G)
+
+
+@pytest.mark.gpu
+def test_decaying_spectrum_and_singular_values():
+    g = torch.Generator().manual_seed(5)
+    u, _, v = torch.linalg.svd(torch.randn(300, 500, generator=g, dtype=torch.float64), full_matrices=False)
+    G = ((u * torch.logspace(0, -4, 300, dtype=torch.float64)) @ v).float().cuda()
+    out, = run([G])
+    check(out, G)
+    full = gaussian(200, 600, 6)
+    out, = run([full])
+    s = torch.linalg.svdvals(out.double())
+    assert 0.6 < float(s.min()) and float(s.max()) < 1.25          # where Muon's polynomial leaves them
+
+
+@pytest.mark.gpu
+def test_a_set_of_diverse_matrices_with_scales():
+    """More matrices than one launch holds, wide and tall ones mixed; every one as if it were alone in its group."""
+    shapes = [(96, 64), (64, 160), (257, 40), (1, 5), (128, 128), (300, 520), (33, 700)] * 3
+    grads = [gaussian(r, c, 10 + i, torch.float32) for i, (r, c) in enumerate(shapes)]
+    scales = [0.25 + 0.1 * i for i in range(len(shapes))]
+    for out, G, s in zip(run(grads, scales=scales), grads, scales):
+        check(out, G, scale=float(np.float32(s)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("offset", [0, 1, 8, 13])
+def test_column_blocks(dtype, offset):
+    """Gradients and updates as column blocks of wider matrices, aligned or not; the columns beside them stay."""
+    from paper_2409_12210_b200 import binding as B
+    wide = torch.randn(70, 401, device="cuda").to(dtype)
+    target = torch.full((70, 333), 7.0, dtype=torch.bfloat16, device="cuda")
+    g, u = wide[:, offset:offset + 200], target[:, offset:offset + 200]
+    ws = torch.empty(B.orthogonalize_workspace_bytes([(70, 200)]), dtype=torch.uint8, device="cuda")
+    B.orthogonalize([g], [u], ws)
+    check(u, g)
+    assert bool((target[:, :offset] == 7).all()) and bool((target[:, offset + 200:] == 7).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("steps,k", [(1, MUON), (8, MUON), (12, (1.5, -0.5, 0.0)), (3, (1.875, -1.25, 0.375))])
+def test_other_coefficients(steps, k):
+    G = gaussian(120, 200, 7, torch.float32)
+    out, = run([G], steps=steps, coefficients=k)
+    check(out, G, steps=steps, k=k)
+
+
+@pytest.mark.gpu
+def test_zero_tiny_huge_and_nan():
+    z = torch.zeros(40, 64, device="cuda")
+    tiny, huge = gaussian(40, 64, 8, torch.float32) * 1e-30, gaussian(40, 64, 8, torch.float32) * 1e25
+    bad = gaussian(40, 64, 9, torch.float32)
+    bad[3, 5] = float("nan")
+    outs = run([z, tiny, huge, bad])
+    assert bool((outs[0] == 0).all())
+    assert bool(torch.isnan(outs[3]).all())
+    check(outs[2], huge)
+    assert float(outs[1].abs().max()) < 1e-18                       # eps swamps a norm of 1e-30
+    out, = run([tiny], eps=0.0)
+    check(out, tiny, eps=0.0)
+
+
+@pytest.mark.gpu
+def test_replay_in_a_graph():
+    from paper_2409_12210_b200 import binding as B
+    G = gaussian(300, 500, 11)
+    ref, = run([G])
+    buf, out = torch.zeros_like(G), torch.empty_like(ref)
+    ws = torch.empty(B.orthogonalize_workspace_bytes([(300, 500)]), dtype=torch.uint8, device="cuda")
+    B.orthogonalize([G], [out], ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.orthogonalize([buf], [out], ws)
+    out.zero_()
+    buf.copy_(G)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, ref)
+
+
+@pytest.mark.gpu
+def test_binding_refusals():
+    from paper_2409_12210_b200 import binding as B
+    G, out = gaussian(16, 24, 0), torch.empty(16, 24, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(B.orthogonalize_workspace_bytes([(16, 24)]), dtype=torch.uint8, device="cuda")
+    for bad in [([G.t()], [out.t()]), ([G], [out.float()]), ([G], [out[:, :8]]), ([G, G.float()], [out, out]), ([G], []),
+                ([G.cpu()], [out.cpu()])]:
+        with pytest.raises(ValueError):
+            B.orthogonalize(*bad, ws)
+    with pytest.raises(B.ModseError):
+        B.orthogonalize([G], [out], ws[:256])
+    with pytest.raises(B.ModseError):
+        B.orthogonalize([G], [out], ws, coefficients=(9.0, 0.0, 0.0))
+    B.orthogonalize([], [], ws)
+
+
+def test_refusals_need_no_gpu():
+    import ctypes
+
+    from paper_2409_12210_b200 import binding as B
+    from paper_2409_12210_b200 import build
+    build.build()
+    lib = B.load()
+    p = 0x10000
+    inv = B.MODSE_ERR_INVALID_ARG
+    need = B.orthogonalize_workspace_bytes([(16, 24)])
+    assert need > 0 and need % 256 == 0
+    assert B.orthogonalize_workspace_bytes([]) > 0
+    for shape in [(0, 4), (4, 0), (-1, 4), (1 << 21, 4), (1 << 18, 1 << 18)]:
+        assert B.orthogonalize_workspace_bytes([shape]) == 0
+    # a set in groups: the workspace is the largest group's, not the sum
+    assert B.orthogonalize_workspace_bytes([(16, 24)] * 64) == B.orthogonalize_workspace_bytes([(16, 24)] * 16)
+
+    def call(dtype=B.MODSE_F32, n=1, steps=5, k=MUON, eps=1e-7, ws=p, size=None, grad=p, update=p, ldg=24, ldu=24, rows=16,
+             cols=24, scale=1.0, null=False):
+        arr = (B._Matrix * 1)(B._Matrix(grad, update, ldg, ldu, rows, cols, scale))
+        kk = None if k is None else (ctypes.c_float * 3)(*k)
+        return lib.modse_orthogonalize(dtype, n, None if null else arr, steps, kk, eps, ws, need if size is None else size, None)
+
+    assert call(n=0) == B.MODSE_OK
+    assert call(size=need - 1) == B.MODSE_ERR_WORKSPACE_TOO_SMALL
+    nan = float("nan")
+    for bad in [dict(dtype=2), dict(dtype=-1), dict(n=-1), dict(null=True), dict(steps=0), dict(steps=65), dict(k=None),
+                dict(k=(nan, 0, 0)), dict(eps=-1.0), dict(eps=nan), dict(ws=None), dict(ws=p + 128), dict(grad=None),
+                dict(update=None), dict(grad=p + 2), dict(update=p + 1), dict(ldg=23), dict(ldu=23), dict(rows=0),
+                dict(cols=0), dict(scale=nan)]:
+        assert call(**bad) == inv, bad
+    for k in [(8.0, 0.0, 0.0), (3.0, 3.0, 3.0), (1.0, 100.0, -100.0)]:
+        assert call(k=k) == B.MODSE_ERR_UNSUPPORTED, k
+    layer = B.ModseLayer(64, [96, 160, 112, 144], 2)
+    full = layer.orthogonalize_workspace_bytes()
+    assert full > 0 and lib.modse_orthogonalize_wgrads_workspace_bytes(None) == 0
+    k3 = (ctypes.c_float * 3)(*MUON)
+    g = B._WGrads(None, p, p, p)
+    f = lambda *a: lib.modse_orthogonalize_wgrads(*a, None)
+    assert f(None, B.MODSE_F32, g, g, None, 5, k3, 1e-7, p, full) == inv
+    assert f(layer._h, B.MODSE_F32, None, g, None, 5, k3, 1e-7, p, full) == inv
+    assert f(layer._h, B.MODSE_F32, B._WGrads(None, p, None, p), g, None, 5, k3, 1e-7, p, full) == inv
+    assert f(layer._h, B.MODSE_F32, g, g, None, 5, k3, 1e-7, p, full - 1) == B.MODSE_ERR_WORKSPACE_TOO_SMALL
+    layer.destroy()
