@@ -10,6 +10,8 @@ from __future__ import annotations
 import ctypes
 import os
 
+import torch
+
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libmodse.so")
 
@@ -256,7 +258,6 @@ def check_pairs(ffn_sizes):
 
 
 def _dtype_code(t):
-    import torch
     if t.dtype == torch.float32:
         return MODSE_F32
     if t.dtype == torch.bfloat16:
@@ -265,22 +266,24 @@ def _dtype_code(t):
 
 
 # ---- operators around the layer ---------------------------------------------
+# A call on a token or two takes a few microseconds on the GPU, so what these wrappers cost on the host is what such a
+# call costs: devices are compared by index and the stream is asked for by device, without the objects torch wraps them in.
 def _buffer(name, t, shape, dtype, device):
-    """Device address of a tensor that has to have this shape, type and device (None: a null pointer)."""
+    """Device address of a tensor that has to have this shape, type and device index (None: a null pointer)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, "
+    if t.dtype != dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on CUDA device {device}, "
                          f"got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
     return t.data_ptr()
 
 
 def _current_stream(name, t):
-    """Raw current stream of t's device, which has to be the current CUDA device."""
-    import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    """(raw current stream, device index) of t's device, which has to be the current CUDA device."""
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
         raise ValueError(f"{name}: expected a tensor on the current CUDA device, got one on {t.device}")
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device), device
 
 
 def _rows(name, t):
@@ -293,11 +296,9 @@ def add_rms_norm(x, residual, weight, eps: float, *, sum_out=None, y=None, y8=No
     """modse_add_rms_norm on the current stream: ``sum_out = x + residual`` and its root-mean-square norm times
     ``weight`` into ``y`` and, in 8 bits (torch.float8_e4m3fn) with one fp32 scale a row, into ``y8`` and ``y_scale``.
     ``residual`` and ``weight`` may be None, and so may any output the caller does not want."""
-    import torch
     T, d = shape = _rows("x", x)
-    dt, dev = x.dtype, x.device
-    code = _dtype_code(x)
-    stream = _current_stream("x", x)
+    dt, code = x.dtype, _dtype_code(x)
+    stream, dev = _current_stream("x", x)
     st = load().modse_add_rms_norm(
         code, T, d, _buffer("x", x, shape, dt, dev), _buffer("residual", residual, shape, dt, dev),
         _buffer("weight", weight, (d,), dt, dev), eps, _buffer("sum_out", sum_out, shape, dt, dev),
@@ -314,11 +315,9 @@ def add_rms_norm_backward_workspace_bytes(n_tokens: int, d_model: int) -> int:
 def add_rms_norm_backward(s, weight, eps: float, dy, dsum, dx, dweight=None, workspace=None) -> None:
     """modse_add_rms_norm_backward: ``s`` is the sum forward wrote, ``dsum`` (or None) the gradient that reaches it past
     the norm; ``dx`` receives the gradient of x and of the residual alike, ``dweight`` (fp32, or None) the weight's."""
-    import torch
     T, d = shape = _rows("s", s)
-    dt, dev = s.dtype, s.device
-    code = _dtype_code(s)
-    stream = _current_stream("s", s)
+    dt, code = s.dtype, _dtype_code(s)
+    stream, dev = _current_stream("s", s)
     st = load().modse_add_rms_norm_backward(
         code, T, d, _buffer("s", s, shape, dt, dev), _buffer("weight", weight, (d,), dt, dev), eps,
         _buffer("dy", dy, shape, dt, dev), _buffer("dsum", dsum, shape, dt, dev), _buffer("dx", dx, shape, dt, dev),
@@ -328,7 +327,6 @@ def add_rms_norm_backward(s, weight, eps: float, dy, dsum, dx, dweight=None, wor
 
 
 def _linear_code(dtype):
-    import torch
     if dtype == torch.bfloat16:
         return MODSE_BF16
     if dtype == torch.float8_e4m3fn:
@@ -345,11 +343,10 @@ def linear(x, w, y, workspace, *, bias=None, residual=None, activation: str = "n
     """modse_linear on the current stream: ``y = act(x w^T + bias) + residual``, the pre-activation into ``z`` if given.
     x [T, d_in] and w [d_out, d_in] are bf16, or torch.float8_e4m3fn with one fp32 scale a row (``x_scale``,
     ``w_scale``); everything else is bf16."""
-    import torch
     T, k = _rows("x", x)
     n = _rows("w", w)[0]
-    bf, dev, code = torch.bfloat16, x.device, _linear_code(x.dtype)
-    stream = _current_stream("x", x)
+    bf, code = torch.bfloat16, _linear_code(x.dtype)
+    stream, dev = _current_stream("x", x)
     f32, out = torch.float32, (T, n)
     args = _Linear(_buffer("x", x, (T, k), x.dtype, dev), _buffer("w", w, (n, k), x.dtype, dev),
                    _buffer("x_scale", x_scale, (T,), f32, dev), _buffer("w_scale", w_scale, (n,), f32, dev),
@@ -367,11 +364,10 @@ def linear_backward_workspace_bytes(n_tokens: int, d_in: int, d_out: int) -> int
 def linear_backward(x, w, dy, z, activation: str, dx, dw, dbias, workspace) -> None:
     """modse_linear_backward: the gradients of :func:`linear` on bf16 operands from ``dy`` and the saved ``z`` (None where
     there is no activation) into ``dx``, ``dw`` (bf16) and ``dbias`` (fp32); any of the three may be None."""
-    import torch
     T, k = _rows("x", x)
     n = _rows("w", w)[0]
-    bf, dev = torch.bfloat16, x.device
-    stream = _current_stream("x", x)
+    bf = torch.bfloat16
+    stream, dev = _current_stream("x", x)
     args = _LinearGrads(_buffer("x", x, (T, k), bf, dev), _buffer("w", w, (n, k), bf, dev),
                         _buffer("dy", dy, (T, n), bf, dev), _buffer("z", z, (T, n), bf, dev),
                         _buffer("dx", dx, (T, k), bf, dev), _buffer("dw", dw, (n, k), bf, dev),
@@ -403,18 +399,18 @@ def orthogonalize(grads, updates, workspace, *, scales=None, steps: int = 5, coe
     """modse_orthogonalize on the current stream: the Newton-Schulz iterate of each matrix of ``grads`` (all bf16 or all
     fp32; rows may be strided, so column blocks of a wider matrix work) times its entry of ``scales`` into the bf16
     matrix of the same place in ``updates``."""
-    import torch
     n = len(grads)
     if len(updates) != n or (scales is not None and len(scales) != n):
         raise ValueError(f"{n} gradients, {len(updates)} updates, {n if scales is None else len(scales)} scales")
     if n == 0:
         return
-    dt, dev = grads[0].dtype, grads[0].device
-    code, stream = _dtype_code(grads[0]), _current_stream("grads", grads[0])
+    dt, code = grads[0].dtype, _dtype_code(grads[0])
+    stream, dev = _current_stream("grads", grads[0])
     arr = (_Matrix * n)()
     for i, (g, u, m) in enumerate(zip(grads, updates, arr)):
-        if g.dtype != dt or g.device != dev or u.dtype != torch.bfloat16 or u.device != dev or u.shape != g.shape:
-            raise ValueError(f"matrix {i}: expected a {dt} gradient and a bf16 update of one shape on {dev}, got "
+        if (g.dtype != dt or g.get_device() != dev or u.dtype != torch.bfloat16 or u.get_device() != dev or
+                u.shape != g.shape):
+            raise ValueError(f"matrix {i}: expected a {dt} gradient and a bf16 update of one shape on CUDA device {dev}, got "
                              f"{g.dtype} {tuple(g.shape)} on {g.device} and {u.dtype} {tuple(u.shape)} on {u.device}")
         m.ld_grad, m.ld_update = _ld(f"gradient {i}", g), _ld(f"update {i}", u)
         m.grad, m.update = g.data_ptr(), u.data_ptr()
@@ -428,7 +424,6 @@ def orthogonalize(grads, updates, workspace, *, scales=None, steps: int = 5, coe
 
 def check_workspace_status(workspace) -> int:
     """Status the last operator call on this workspace left (synchronises the current stream)."""
-    import torch
     return int(load().modse_check_workspace_status(workspace.data_ptr(), torch.cuda.current_stream().cuda_stream))
 
 
@@ -436,8 +431,8 @@ def _workspace(t, device):
     """(address, bytes) of a workspace tensor."""
     if t is None:
         return None, 0
-    if t.device != device or not t.is_contiguous():
-        raise ValueError(f"workspace: expected a contiguous tensor on {device}, got one on {t.device}")
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on CUDA device {device}, got one on {t.device}")
     return t.data_ptr(), t.numel() * t.element_size()
 
 
@@ -619,8 +614,9 @@ class ModseLayer:
         fp32 with :meth:`set_output_f32`) into bf16 tensors of the same layouts.  ``scales``: None or N x 3 numbers
         (gate, up, down of each expert)."""
         import torch
-        dt, dev = dw_gate.dtype, dw_gate.device
-        S, d, stream = sum(self.ffn_sizes), self.d_model, _current_stream("dw_gate", dw_gate)
+        dt = dw_gate.dtype
+        stream, dev = _current_stream("dw_gate", dw_gate)
+        S, d = sum(self.ffn_sizes), self.d_model
         wide, tall, bf = (d, S), (S, d), torch.bfloat16
         g = _WGrads(None, _buffer("dw_gate", dw_gate, tall, dt, dev), _buffer("dw_up", dw_up, tall, dt, dev),
                     _buffer("dw_down", dw_down, wide, dt, dev))

@@ -17,6 +17,7 @@
 
 #include <algorithm>
 
+#include "activations.h"
 #include "dense_gemm.h"
 #include "tc_device.h"
 #include "tc_gemm.h"
@@ -50,6 +51,7 @@ template <int P> struct DenseParams {
     int *status, *counters;
     float *partial;
     unsigned long long wait_limit_ns;
+    int clear_status;
 };
 
 struct DenseTile {
@@ -175,25 +177,17 @@ __device__ __forceinline__ void pack_f16(const float (&v)[32], uint4 (&w)[4])
                           f16x2(v[8 * q + 4], v[8 * q + 5]), f16x2(v[8 * q + 6], v[8 * q + 7]));
 }
 
-template <int ACT>
-__device__ __forceinline__ float activate(float z)
-{
-    if constexpr (ACT == MODSE_ACT_RELU) return z < 0.f ? 0.f : z;       // a NaN stays
-    if constexpr (ACT == MODSE_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    if constexpr (ACT == MODSE_ACT_SILU) return __fdividef(z, 1.f + __expf(-z));
-    return z;
-}
 __device__ __forceinline__ void activate_all(float (&v)[32], int act)
 {
     if (act == MODSE_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = activate<MODSE_ACT_RELU>(v[i]);
+        for (int i = 0; i < 32; i += 2) activate2<MODSE_ACT_RELU>(v[i], v[i + 1]);
     } else if (act == MODSE_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = activate<MODSE_ACT_GELU>(v[i]);
+        for (int i = 0; i < 32; i += 2) activate2<MODSE_ACT_GELU>(v[i], v[i + 1]);
     } else if (act == MODSE_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = activate<MODSE_ACT_SILU>(v[i]);
+        for (int i = 0; i < 32; i += 2) activate2<MODSE_ACT_SILU>(v[i], v[i + 1]);
     }
 }
 
@@ -402,6 +396,8 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
             mbar_init(smem_u32(&st->tmem_empty[a]), 2 * kDenseEpiWarps);
         }
         st->abort_flag = 0;
+        // the first block to start clears the status word; a wait can expire a millisecond later at the earliest
+        if (prm.clear_status && blockIdx.x == 0) *prm.status = kDevOk;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -638,7 +634,7 @@ DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int
 }
 
 template <int MODE, int TYPE, int TN, int P>
-cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const LinearEpilogue *lin, void *ws, cudaStream_t s)
+cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const LinearEpilogue *lin, void *ws, int head, cudaStream_t s)
 {
     DenseParams<P> prm;
     int tiles = 0;
@@ -666,6 +662,7 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
     prm.counters = (int *)((unsigned char *)ws + kDenseCounterOffset);
     prm.partial = (float *)((unsigned char *)ws + kDenseHead);
     prm.wait_limit_ns = tc_wait_limit_ns();
+    prm.clear_status = head == kDenseHeadRaw;
 
     auto kern = dense_gemm_pair<MODE, TYPE, TN, P>;
     static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
@@ -677,20 +674,24 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
         if (e != cudaSuccess) return e;
         if (dev <= 63) attr_done |= 1ull << dev;
     }
+    if (head == kDenseHeadRaw && pl.splits > 1) {      // only cut tiles count arrivals
+        e = cudaMemsetAsync(ws, 0, kDenseZeroBytes, s);
+        if (e != cudaSuccess) return e;
+    }
     kern<<<2 * std::min(pairs, prm.items), kDenseThreads, kDenseSmem, s>>>(prm);
     return cudaGetLastError();
 }
 
 template <int MODE, int TYPE, int P>
-cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin, void *ws, size_t cap, cudaStream_t s)
+cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin, void *ws, size_t cap, int head, cudaStream_t s)
 {
     if (n > P) return cudaErrorInvalidValue;
     const DensePlan pl = dense_plan((DenseMode)MODE, (DenseType)TYPE, items, n, device_sms(), cap);
     if constexpr (MODE == DenseGram || MODE == DensePoly) {
-        return launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, ws, s);
+        return launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, ws, head, s);
     } else {
-        return pl.tn == 128 ? launch_tn<MODE, TYPE, 128, P>(pl, items, n, lin, ws, s)
-                            : launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, ws, s);
+        return pl.tn == 128 ? launch_tn<MODE, TYPE, 128, P>(pl, items, n, lin, ws, head, s)
+                            : launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, ws, head, s);
     }
 }
 
@@ -703,17 +704,17 @@ size_t dense_partial_bytes(DenseMode mode, DenseType type, const DenseItem *item
 }
 
 cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *items, int n, const LinearEpilogue *lin, void *ws,
-                         size_t partial_capacity, cudaStream_t s)
+                         size_t partial_capacity, int head, cudaStream_t s)
 {
     if (n < 1 || n > kDenseMaxProblems) return cudaErrorInvalidValue;
     switch (mode) {
     case DenseLinear:
-        return type == DenseE4m3 ? launch_mode<DenseLinear, DenseE4m3, 1>(items, n, lin, ws, partial_capacity, s)
-                                 : launch_mode<DenseLinear, DenseBf16, 1>(items, n, lin, ws, partial_capacity, s);
-    case DensePlain: return launch_mode<DensePlain, DenseBf16, 2>(items, n, lin, ws, partial_capacity, s);
-    case DenseGram: return launch_mode<DenseGram, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, s);
-    case DensePoly: return launch_mode<DensePoly, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, s);
-    case DenseStep: return launch_mode<DenseStep, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, s);
+        return type == DenseE4m3 ? launch_mode<DenseLinear, DenseE4m3, 1>(items, n, lin, ws, partial_capacity, head, s)
+                                 : launch_mode<DenseLinear, DenseBf16, 1>(items, n, lin, ws, partial_capacity, head, s);
+    case DensePlain: return launch_mode<DensePlain, DenseBf16, 2>(items, n, lin, ws, partial_capacity, head, s);
+    case DenseGram: return launch_mode<DenseGram, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, head, s);
+    case DensePoly: return launch_mode<DensePoly, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, head, s);
+    case DenseStep: return launch_mode<DenseStep, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, head, s);
     }
     return cudaErrorInvalidValue;
 }

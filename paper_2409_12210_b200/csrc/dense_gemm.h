@@ -56,8 +56,11 @@ struct DenseItem {
     long long k;             // length of the contraction in elements
 };
 
-// Workspace of a call that launches dense products: the status word, the arrival counters of cut tiles (both zeroed by
-// the call before its first launch; a launch leaves the counters zero), then the fp32 pieces of cut tiles.
+// Workspace of a call that launches dense products: the status word, the arrival counters of cut tiles, then the fp32
+// pieces of cut tiles.  A launch leaves the counters zero.  Before the first launch of a call the head is either zeroed
+// by another kernel of the call (kDenseHeadZero) or raw (kDenseHeadRaw): the launch then clears the status word itself
+// and zeroes the counters if it uses them.
+enum : int { kDenseHeadZero = 0, kDenseHeadRaw = 1 };
 constexpr int kDenseSms = 148;                         // workspace sizes are asked for without a device
 constexpr int kDenseMaxSplitItems = 128;               // pieces of one launch: at most one for each CTA pair
 constexpr size_t kDenseCounterOffset = 64;
@@ -69,6 +72,6 @@ size_t dense_partial_bytes(DenseMode mode, DenseType type, const DenseItem *item
 
 // Launches n products of one mode and type as one kernel on a workspace whose head is `ws`.
 cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *items, int n, const LinearEpilogue *lin, void *ws,
-                         size_t partial_capacity, cudaStream_t s);
+                         size_t partial_capacity, int head, cudaStream_t s);
 
 }  // namespace modse

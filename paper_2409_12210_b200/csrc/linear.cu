@@ -1,5 +1,7 @@
 // modse_linear and its gradient: host side and the elementwise part of the gradient.
+#include "activations.h"
 #include "dense_gemm.h"
+#include "linear_rows.h"
 
 namespace modse {
 namespace {
@@ -61,19 +63,6 @@ int backward_items(DenseItem *items, int T, int k, int n, const void *dz, const 
 constexpr int kDzRows = 64;          // rows of a block's strip
 constexpr int kDzCols = 256;         // columns of a block's strip: 32 lanes of 8, eight warps share its rows
 
-template <int ACT>
-__device__ __forceinline__ float act_slope(float z)
-{
-    if constexpr (ACT == MODSE_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-    if constexpr (ACT == MODSE_ACT_GELU)
-        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
-    if constexpr (ACT == MODSE_ACT_SILU) {
-        const float s = 1.f / (1.f + __expf(-z));
-        return s * (1.f + z * (1.f - s));
-    }
-    return 1.f;
-}
-
 __device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
 {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -87,36 +76,55 @@ __device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
 template <int ACT>
 __global__ void __launch_bounds__(256)
 linear_dz_kernel(const __nv_bfloat16 *__restrict__ dy, const __nv_bfloat16 *__restrict__ z, __nv_bfloat16 *__restrict__ dz,
-                 float *__restrict__ part, int T, int n)
+                 float *__restrict__ part, int *__restrict__ head, int T, int n)
 {
     __shared__ float sh[8][kDzCols];
+    if (blockIdx.x == 0 && blockIdx.y == 0)      // status word and counters of the products that follow
+        for (int i = threadIdx.x; i < (int)(kDenseZeroBytes / 4); i += 256) head[i] = 0;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int c = blockIdx.x * kDzCols + lane * 8, row0 = blockIdx.y * kDzRows;
     float sum[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] = 0.f;
     if (c < n) {
-#pragma unroll 4
-        for (int i = 0; i < kDzRows / 8; ++i) {
-            const int r = row0 + i * 8 + warp;
-            if (r >= T) break;
-            const size_t at = (size_t)r * n + c;
-            float g[8], f[8];
-            unpack8(*reinterpret_cast<const uint4 *>(dy + at), g);
-            if constexpr (ACT != MODSE_ACT_NONE) {
-                unpack8(*reinterpret_cast<const uint4 *>(z + at), f);
+        constexpr int kAt = 4;               // rows of a warp in flight
 #pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] *= act_slope<ACT>(f[j]);
-                uint32_t w[4];
+        for (int i0 = 0; i0 < kDzRows / 8; i0 += kAt) {
+            uint4 gv[kAt], fv[kAt];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    __nv_bfloat162 t = __floats2bfloat162_rn(g[2 * j], g[2 * j + 1]);
-                    w[j] = *reinterpret_cast<uint32_t *>(&t);
+            for (int i = 0; i < kAt; ++i) {
+                const int r = row0 + (i0 + i) * 8 + warp;
+                const size_t at = (size_t)r * n + c;
+                gv[i] = fv[i] = make_uint4(0, 0, 0, 0);
+                if (r < T) {
+                    gv[i] = *reinterpret_cast<const uint4 *>(dy + at);
+                    if constexpr (ACT != MODSE_ACT_NONE) fv[i] = *reinterpret_cast<const uint4 *>(z + at);
                 }
-                *reinterpret_cast<uint4 *>(dz + at) = make_uint4(w[0], w[1], w[2], w[3]);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += g[j];
+            for (int i = 0; i < kAt; ++i) {
+                const int r = row0 + (i0 + i) * 8 + warp;
+                float g[8], f[8];
+                unpack8(gv[i], g);
+                if constexpr (ACT != MODSE_ACT_NONE) {
+                    unpack8(fv[i], f);
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2) {
+                        act_slope2<ACT>(f[j], f[j + 1]);
+                        g[j] *= f[j];
+                        g[j + 1] *= f[j + 1];
+                    }
+                    uint32_t w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        __nv_bfloat162 t = __floats2bfloat162_rn(g[2 * j], g[2 * j + 1]);
+                        w[j] = *reinterpret_cast<uint32_t *>(&t);
+                    }
+                    if (r < T) *reinterpret_cast<uint4 *>(dz + (size_t)r * n + c) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += g[j];      // rows past the end hold zeros
+            }
         }
     }
     if (part == nullptr) return;
@@ -157,16 +165,16 @@ BackwardLayout backward_layout(int T, int k, int n)
     return L;
 }
 
-cudaError_t launch_dz(int act, const void *dy, const void *z, void *dz, float *part, int T, int n, cudaStream_t s)
+cudaError_t launch_dz(int act, const void *dy, const void *z, void *dz, float *part, int *head, int T, int n, cudaStream_t s)
 {
     const dim3 grid((n + kDzCols - 1) / kDzCols, dz_strips(T));
     const auto *g = (const __nv_bfloat16 *)dy, *f = (const __nv_bfloat16 *)z;
     auto *o = (__nv_bfloat16 *)dz;
     switch (act) {
-    case MODSE_ACT_RELU: linear_dz_kernel<MODSE_ACT_RELU><<<grid, 256, 0, s>>>(g, f, o, part, T, n); break;
-    case MODSE_ACT_GELU: linear_dz_kernel<MODSE_ACT_GELU><<<grid, 256, 0, s>>>(g, f, o, part, T, n); break;
-    case MODSE_ACT_SILU: linear_dz_kernel<MODSE_ACT_SILU><<<grid, 256, 0, s>>>(g, f, o, part, T, n); break;
-    default: linear_dz_kernel<MODSE_ACT_NONE><<<grid, 256, 0, s>>>(g, f, o, part, T, n); break;
+    case MODSE_ACT_RELU: linear_dz_kernel<MODSE_ACT_RELU><<<grid, 256, 0, s>>>(g, f, o, part, head, T, n); break;
+    case MODSE_ACT_GELU: linear_dz_kernel<MODSE_ACT_GELU><<<grid, 256, 0, s>>>(g, f, o, part, head, T, n); break;
+    case MODSE_ACT_SILU: linear_dz_kernel<MODSE_ACT_SILU><<<grid, 256, 0, s>>>(g, f, o, part, head, T, n); break;
+    default: linear_dz_kernel<MODSE_ACT_NONE><<<grid, 256, 0, s>>>(g, f, o, part, head, T, n); break;
     }
     return cudaGetLastError();
 }
@@ -189,6 +197,7 @@ size_t modse_linear_workspace_bytes(modse_dtype_t dtype, int n_tokens, int d_in,
         !countable(n_tokens, d_out))
         return 0;
     const DenseType type = dtype == MODSE_E4M3 ? DenseE4m3 : DenseBf16;
+    if (n_tokens <= kLinearRowsMax) return kDenseHead;
     const DenseItem it = forward_item(type, n_tokens, d_in, d_out, nullptr, nullptr);
     return kDenseHead + up256(dense_partial_bytes(DenseLinear, type, &it, 1));
 }
@@ -214,9 +223,12 @@ modse_status_t modse_linear(modse_dtype_t dtype, int n_tokens, int d_in, int d_o
     const DenseType type = f8 ? DenseE4m3 : DenseBf16;
     const LinearEpilogue lin{a.x_scale, a.w_scale, (const __nv_bfloat16 *)a.bias, (const __nv_bfloat16 *)a.residual,
                              (__nv_bfloat16 *)a.z, (__nv_bfloat16 *)a.y, (int)activation};
+    if (n_tokens <= kLinearRowsMax) {
+        MODSE_CUDA(launch_linear_rows(type, a.x, a.w, n_tokens, d_in, d_out, lin, (int *)workspace, s));
+        return MODSE_OK;
+    }
     const DenseItem it = forward_item(type, n_tokens, d_in, d_out, a.x, a.w);
-    MODSE_CUDA(cudaMemsetAsync(workspace, 0, kDenseZeroBytes, s));
-    MODSE_CUDA(dense_launch(DenseLinear, type, &it, 1, &lin, workspace, need - kDenseHead, s));
+    MODSE_CUDA(dense_launch(DenseLinear, type, &it, 1, &lin, workspace, need - kDenseHead, kDenseHeadRaw, s));
     return MODSE_OK;
 }
 
@@ -252,17 +264,18 @@ modse_status_t modse_linear_backward(int n_tokens, int d_in, int d_out, modse_ac
     if (workspace_bytes < need) return MODSE_ERR_WORKSPACE_TOO_SMALL;
     const BackwardLayout L = backward_layout(n_tokens, d_in, d_out);
     unsigned char *ws = (unsigned char *)workspace;
-    MODSE_CUDA(cudaMemsetAsync(workspace, 0, kDenseZeroBytes, s));
     const void *dz = a.dy;
     float *part = a.dbias ? (float *)(ws + L.part) : nullptr;
+    int head = kDenseHeadRaw;
     if (activation != MODSE_ACT_NONE || part) {
-        MODSE_CUDA(launch_dz((int)activation, a.dy, a.z, ws + L.dz, part, n_tokens, d_out, s));
+        MODSE_CUDA(launch_dz((int)activation, a.dy, a.z, ws + L.dz, part, (int *)ws, n_tokens, d_out, s));
+        head = kDenseHeadZero;
         if (activation != MODSE_ACT_NONE) dz = ws + L.dz;
         if (part) MODSE_CUDA(launch_column_sum(part, dz_strips(n_tokens), d_out, a.dbias, s));
     }
     DenseItem items[2];
     const int c = backward_items(items, n_tokens, d_in, d_out, dz, a.x, a.w, a.dx, a.dw);
-    if (c > 0) MODSE_CUDA(dense_launch(DensePlain, DenseBf16, items, c, nullptr, workspace, L.partial_bytes, s));
+    if (c > 0) MODSE_CUDA(dense_launch(DensePlain, DenseBf16, items, c, nullptr, workspace, L.partial_bytes, head, s));
     return MODSE_OK;
 }
 

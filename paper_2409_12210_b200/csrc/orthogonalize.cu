@@ -270,9 +270,9 @@ cudaError_t run_group(modse_dtype_t dtype, const modse_matrix_t *m, int n, int s
                 p.out1 = lo;           // a tile's lo is read and written by the warp that owns its rows
             }
         }
-        e = dense_launch(DenseGram, DenseF16, gram, n, nullptr, ws, L.partial_bytes, s);
-        if (e == cudaSuccess) e = dense_launch(DensePoly, DenseF16, poly, n, nullptr, ws, L.partial_bytes, s);
-        if (e == cudaSuccess) e = dense_launch(DenseStep, DenseF16, step, n, nullptr, ws, L.partial_bytes, s);
+        e = dense_launch(DenseGram, DenseF16, gram, n, nullptr, ws, L.partial_bytes, kDenseHeadZero, s);
+        if (e == cudaSuccess) e = dense_launch(DensePoly, DenseF16, poly, n, nullptr, ws, L.partial_bytes, kDenseHeadZero, s);
+        if (e == cudaSuccess) e = dense_launch(DenseStep, DenseF16, step, n, nullptr, ws, L.partial_bytes, kDenseHeadZero, s);
     }
     return e;
 }
