@@ -1,6 +1,7 @@
 // The activations of modse_linear and their slopes, shared by the epilogues and the gradient's elementwise pass.
 #pragma once
 
+#include "f32x2.h"
 #include "modse_internal.h"
 
 namespace modse {
@@ -17,29 +18,6 @@ __device__ __forceinline__ float rcp_approx(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-
-// Two fp32 numbers in a register pair: one instruction for both halves.
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pack2(float lo, float hi)
-{
-    f32x2 v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
-    return v;
-}
-__device__ __forceinline__ void unpack2(f32x2 v, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
-{
-    f32x2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
-{
-    f32x2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ f32x2 both(float v) { return pack2(v, v); }
 
 // Phi(z) - 1/2 of two numbers, Phi the normal distribution function, and e = exp(-z^2 / 2): the rational approximation
 // 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical Functions (erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2),

@@ -19,6 +19,7 @@
 
 #include "activations.h"
 #include "dense_gemm.h"
+#include "launch.h"
 #include "tc_device.h"
 #include "tc_gemm.h"
 
@@ -396,8 +397,10 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
             mbar_init(smem_u32(&st->tmem_empty[a]), 2 * kDenseEpiWarps);
         }
         st->abort_flag = 0;
-        // the first block to start clears the status word; a wait can expire a millisecond later at the earliest
-        if (prm.clear_status && blockIdx.x == 0) *prm.status = kDevOk;
+        for (int i = 0; i < min(prm.n_prob, 4); ++i) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&prm.a[i])) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&prm.b[i])) : "memory");
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -410,6 +413,10 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
     __syncthreads();
     cluster_sync_all();                 // both CTAs' barriers exist before any remote arrival or copy completion
     tc_fence_after();
+    wait_for_earlier_kernels();
+    allow_next_kernel();
+    // the first block clears the status word; a wait can expire a millisecond later at the earliest
+    if (prm.clear_status && blockIdx.x == 0 && tid == 0) *prm.status = kDevOk;
     const uint32_t tmem_base = st->tmem_base;
     const WaitCtx wc{&st->abort_flag, prm.status, prm.wait_limit_ns};
 
@@ -678,8 +685,7 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
         e = cudaMemsetAsync(ws, 0, kDenseZeroBytes, s);
         if (e != cudaSuccess) return e;
     }
-    kern<<<2 * std::min(pairs, prm.items), kDenseThreads, kDenseSmem, s>>>(prm);
-    return cudaGetLastError();
+    return launch_overlapped(kern, 2 * std::min(pairs, prm.items), kDenseThreads, kDenseSmem, s, prm);
 }
 
 template <int MODE, int TYPE, int P>

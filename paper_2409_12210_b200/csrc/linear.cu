@@ -1,6 +1,7 @@
 // modse_linear and its gradient: host side and the elementwise part of the gradient.
 #include "activations.h"
 #include "dense_gemm.h"
+#include "launch.h"
 #include "linear_rows.h"
 
 namespace modse {
@@ -75,10 +76,11 @@ __device__ __forceinline__ void unpack8(const uint4 &v, float (&f)[8])
 
 template <int ACT>
 __global__ void __launch_bounds__(256)
-linear_dz_kernel(const __nv_bfloat16 *__restrict__ dy, const __nv_bfloat16 *__restrict__ z, __nv_bfloat16 *__restrict__ dz,
-                 float *__restrict__ part, int *__restrict__ head, int T, int n)
+linear_dz_kernel(const __nv_bfloat16 *dy, const __nv_bfloat16 *z, __nv_bfloat16 *dz, float *part, int *head, int T, int n)
 {
     __shared__ float sh[8][kDzCols];
+    wait_for_earlier_kernels();
+    allow_next_kernel();
     if (blockIdx.x == 0 && blockIdx.y == 0)      // status word and counters of the products that follow
         for (int i = threadIdx.x; i < (int)(kDenseZeroBytes / 4); i += 256) head[i] = 0;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -171,12 +173,11 @@ cudaError_t launch_dz(int act, const void *dy, const void *z, void *dz, float *p
     const auto *g = (const __nv_bfloat16 *)dy, *f = (const __nv_bfloat16 *)z;
     auto *o = (__nv_bfloat16 *)dz;
     switch (act) {
-    case MODSE_ACT_RELU: linear_dz_kernel<MODSE_ACT_RELU><<<grid, 256, 0, s>>>(g, f, o, part, head, T, n); break;
-    case MODSE_ACT_GELU: linear_dz_kernel<MODSE_ACT_GELU><<<grid, 256, 0, s>>>(g, f, o, part, head, T, n); break;
-    case MODSE_ACT_SILU: linear_dz_kernel<MODSE_ACT_SILU><<<grid, 256, 0, s>>>(g, f, o, part, head, T, n); break;
-    default: linear_dz_kernel<MODSE_ACT_NONE><<<grid, 256, 0, s>>>(g, f, o, part, head, T, n); break;
+    case MODSE_ACT_RELU: return launch_overlapped(linear_dz_kernel<MODSE_ACT_RELU>, grid, 256, 0, s, g, f, o, part, head, T, n);
+    case MODSE_ACT_GELU: return launch_overlapped(linear_dz_kernel<MODSE_ACT_GELU>, grid, 256, 0, s, g, f, o, part, head, T, n);
+    case MODSE_ACT_SILU: return launch_overlapped(linear_dz_kernel<MODSE_ACT_SILU>, grid, 256, 0, s, g, f, o, part, head, T, n);
+    default: return launch_overlapped(linear_dz_kernel<MODSE_ACT_NONE>, grid, 256, 0, s, g, f, o, part, head, T, n);
     }
-    return cudaGetLastError();
 }
 
 }  // namespace

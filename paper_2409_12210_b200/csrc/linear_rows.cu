@@ -17,6 +17,7 @@
 
 #include "activations.h"
 #include "dense_gemm.h"
+#include "launch.h"
 #include "linear_rows.h"
 
 namespace modse {
@@ -106,6 +107,8 @@ linear_rows_kernel(const RowsArgs p)
     __shared__ float part[kWarps][NT * 8][MT * 16 + 1];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int n0 = blockIdx.x * (16 * MT);
+    wait_for_earlier_kernels();
+    allow_next_kernel();
     if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = kDevOk;
     // rows past the end read the last row; what they give is not stored
     const unsigned char *wr[2 * MT], *xr[NT];
@@ -185,8 +188,7 @@ linear_rows_kernel(const RowsArgs p)
 template <bool F8, int MT, int NT, int U>
 cudaError_t launch_one(const RowsArgs &p, cudaStream_t s)
 {
-    linear_rows_kernel<F8, MT, NT, U><<<(p.n + 16 * MT - 1) / (16 * MT), 32 * kWarps, 0, s>>>(p);
-    return cudaGetLastError();
+    return launch_overlapped(linear_rows_kernel<F8, MT, NT, U>, (p.n + 16 * MT - 1) / (16 * MT), 32 * kWarps, 0, s, p);
 }
 
 template <bool F8>

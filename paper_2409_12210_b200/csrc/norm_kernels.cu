@@ -8,6 +8,8 @@
 // block, VPT vectors each; the choice of (TPR, VPT) is in pick_shape.  All sums are fp32 of fp32 terms.
 #include <cuda_fp8.h>
 
+#include "f32x2.h"
+#include "launch.h"
 #include "modse_internal.h"
 
 namespace modse {
@@ -116,6 +118,8 @@ add_rms_norm_kernel(const NormArgs a)
     const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR;
     const int row = blockIdx.x * kRows + group;
     const bool live = row < a.T;                  // rows past the end take part in the barriers and touch no memory
+    wait_for_earlier_kernels();
+    allow_next_kernel();
     const int nv = a.d / 8;
     const size_t base = (size_t)(live ? row : 0) * a.d;
     Vec<T> xv[VPT], rv[VPT];
@@ -171,6 +175,13 @@ add_rms_norm_kernel(const NormArgs a)
     const bool tiny = scale < 1.17549435e-38f;
     const float inv = tiny ? 0.f : 1.f / scale;
     if (live && lane == 0) a.q_scale[row] = scale;
+    if (tiny) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[i][j] = scale > 0.f ? s[i][j] / scale : 0.f;
+    }
+    const float by = tiny ? 1.f : inv;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         const int v = lane + i * TPR;
@@ -180,7 +191,7 @@ add_rms_norm_kernel(const NormArgs a)
         for (int h = 0; h < 2; ++h) {
             float t[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) t[j] = tiny ? (scale > 0.f ? s[i][4 * h + j] / scale : 0.f) : s[i][4 * h + j] * inv;
+            for (int j = 0; j < 4; ++j) t[j] = s[i][4 * h + j] * by;
             const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(t[0], t[1]), __NV_SATFINITE, __NV_E4M3);
             const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(t[2], t[3]), __NV_SATFINITE, __NV_E4M3);
             w[h] = lo | (hi << 16);
@@ -197,148 +208,207 @@ struct NormBwdArgs {
     float eps;
 };
 
-// One block walks over its rows and keeps the columns' dweight sums in registers; kRowsAt rows are loaded together so
-// that enough bytes are in flight and the block meets once for all of them.
-template <typename T, int TPR, int VPT, int RA>
-__global__ void __launch_bounds__(TPR < kNormBlock ? kNormBlock : TPR)
+__device__ __forceinline__ void cp_async16(void *dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// The elements of a vector as four pairs, and back.
+__device__ __forceinline__ void pairs(const Vec<__nv_bfloat16> &v, f32x2 (&f)[4])
+{
+    const uint32_t w[4] = {v.a.x, v.a.y, v.a.z, v.a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+}
+__device__ __forceinline__ void pairs(const Vec<float> &v, f32x2 (&f)[4])
+{
+    f[0] = pack2(v.a.x, v.a.y);
+    f[1] = pack2(v.a.z, v.a.w);
+    f[2] = pack2(v.b.x, v.b.y);
+    f[3] = pack2(v.b.z, v.b.w);
+}
+template <typename T>
+__device__ __forceinline__ void store_pairs(T *p, const f32x2 (&f)[4])
+{
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack2(f[i], v[2 * i], v[2 * i + 1]);
+    store_vec(p, v);
+}
+
+// TPR threads of a 512-thread block share a row, VPT vectors each.  Every thread keeps a ring of two rows' pieces (s, dy,
+// dsum) in shared memory, filled by cp.async one row ahead, so that HBM is busy while a row's two sums and its dx are
+// formed; it reads back only the pieces it copied itself, so the only meeting is that of the row's warps over the sums (a
+// named barrier; none where the row is one warp's).  dweight sums stay in registers (VPT * 8 <= 32) and meet in shared
+// memory at the end, in the order of the row groups.
+// Rows too long for the ring (RING false: 1024 threads a row) are read from global memory twice instead, the second time
+// from L2.
+constexpr int kSlots = 2;
+template <typename T, int TPR, int VPT, bool RING>
+__global__ void __launch_bounds__(RING ? 512 : 1024, 1)
 add_rms_norm_bwd_kernel(const NormBwdArgs a)
 {
-    constexpr int kThreads = TPR < kNormBlock ? kNormBlock : TPR;
-    constexpr int kRows = kThreads / TPR, W = TPR / 32;
-    __shared__ float part[2][kThreads / 32][2 * RA];
-    __shared__ float dw_sh[kRows > 1 ? kThreads * VPT * 8 : 1];
-    const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR, wid = threadIdx.x >> 5;
-    const int nv = a.d / 8;
-    float dw[VPT][8];
+    extern __shared__ unsigned char ring[];
+    constexpr int kBwdThreads = RING ? 512 : 1024;
+    constexpr int kGroups = kBwdThreads / TPR, W = TPR / 32, kPieces = sizeof(T) / 2;      // 16-byte pieces of a vector
+    __shared__ float2 part[2][kBwdThreads / 32];
+    const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR, warp = threadIdx.x >> 5, nv = a.d / 8;
+    const bool with_sum = a.dsum != nullptr, with_weight = a.weight != nullptr;
+    // ring: [slot][tensor][vector][piece] of 16 bytes a thread, neighbouring threads side by side
+    unsigned char *mine = ring + threadIdx.x * 16;
+    auto piece = [&](int slot, int tensor, int i, int h) -> unsigned char * {
+        return mine + (size_t)(((slot * 3 + tensor) * VPT + i) * kPieces + h) * (kBwdThreads * 16);
+    };
+    int row = blockIdx.x * kGroups + group, slot = 0;
+    auto fetch = [&](int slot, int tensor, int i, Vec<T> &v) {
+        if constexpr (!RING) {
+            const T *src = (const T *)(tensor == 0 ? a.s : tensor == 1 ? a.dy : a.dsum);
+            load_vec(v, src + (size_t)row * a.d + 8 * (lane + TPR * i));
+        } else if constexpr (kPieces == 1) {
+            v.a = *reinterpret_cast<const uint4 *>(piece(slot, tensor, i, 0));
+        } else {
+            v.a = *reinterpret_cast<const float4 *>(piece(slot, tensor, i, 0));
+            v.b = *reinterpret_cast<const float4 *>(piece(slot, tensor, i, 1));
+        }
+    };
+    const int stride = gridDim.x * kGroups;
+    auto issue = [&](int row, int slot) {
+        if constexpr (!RING) return;
+        if (row < a.T) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int v = lane + TPR * i;
+                if (v < nv) {
+                    const size_t at = ((size_t)row * a.d + 8 * (size_t)v) * sizeof(T);
+#pragma unroll
+                    for (int h = 0; h < kPieces; ++h) {
+                        cp_async16(piece(slot, 0, i, h), (const unsigned char *)a.s + at + 16 * h);
+                        cp_async16(piece(slot, 1, i, h), (const unsigned char *)a.dy + at + 16 * h);
+                        if (with_sum) cp_async16(piece(slot, 2, i, h), (const unsigned char *)a.dsum + at + 16 * h);
+                    }
+                }
+            }
+        }
+        cp_async_commit();
+    };
+    f32x2 dw[VPT][4];
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dw[i][j] = 0.f;
-    int buf = 0;
-    for (int row0 = (blockIdx.x * kRows) * RA; row0 < a.T; row0 += gridDim.x * kRows * RA, buf ^= 1) {
-        Vec<T> sv[RA][VPT], yv[RA][VPT], av[RA][VPT];
+        for (int j = 0; j < 4; ++j) dw[i][j] = 0;
+    wait_for_earlier_kernels();
+    allow_next_kernel();
+    issue(row, 0);
+    const float inv_d = 1.f / (float)a.d;
+    for (; row < a.T; row += stride, slot ^= 1) {
+        issue(row + stride, slot ^ 1);
+        if constexpr (RING) cp_async_wait<1>();
+        Vec<T> sv[VPT], yv[VPT];
+        f32x2 ss2 = 0, us2 = 0;
 #pragma unroll
-        for (int r = 0; r < RA; ++r) {
-            const int row = row0 + group * RA + r;
+        for (int i = 0; i < VPT; ++i) {
+            const int v = lane + TPR * i;
+            if (v >= nv) continue;
+            fetch(slot, 0, i, sv[i]);
+            fetch(slot, 1, i, yv[i]);
+            f32x2 f[4], g[4], w[4];
+            pairs(sv[i], f);
+            pairs(yv[i], g);
+            if (with_weight) {
+                Vec<T> wv;
+                load_vec(wv, (const T *)a.weight + 8 * v);
+                pairs(wv, w);
+            }
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int v = lane + i * TPR;
-                const bool in = row < a.T && v < nv;
-                const size_t at = (size_t)row * a.d + 8 * (size_t)v;
-                if (in) {
-                    load_vec(sv[r][i], (const T *)a.s + at);
-                    load_vec(yv[r][i], (const T *)a.dy + at);
-                } else {
-                    zero_vec(sv[r][i]);
-                    zero_vec(yv[r][i]);
-                }
-                if (in && a.dsum) load_vec(av[r][i], (const T *)a.dsum + at);
-                else zero_vec(av[r][i]);
+            for (int j = 0; j < 4; ++j) {
+                ss2 = fma2(f[j], f[j], ss2);
+                us2 = fma2(with_weight ? mul2(g[j], w[j]) : g[j], f[j], us2);
             }
         }
-        float ss[RA], us[RA];
+        float ss, us, t0, t1;
+        unpack2(ss2, t0, t1);
+        ss = warp_sum(t0 + t1);
+        unpack2(us2, t0, t1);
+        us = warp_sum(t0 + t1);
+        if constexpr (W > 1) {
+            // the buffers alternate: nobody writes one again before the group's next barrier
+            if ((threadIdx.x & 31) == 0) part[slot][warp] = make_float2(ss, us);
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
+            ss = us = 0.f;
 #pragma unroll
-        for (int r = 0; r < RA; ++r) {
-            ss[r] = us[r] = 0.f;
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int v = lane + i * TPR;
-                float f[8], g[8], w[8];
-                unpack(sv[r][i], f);
-                unpack(yv[r][i], g);
-                if (a.weight && v < nv) {
-                    Vec<T> wv;
-                    load_vec(wv, (const T *)a.weight + 8 * v);
-                    unpack(wv, w);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float u = (a.weight && v < nv) ? g[j] * w[j] : g[j];
-                    ss[r] = fmaf(f[j], f[j], ss[r]);
-                    us[r] = fmaf(u, f[j], us[r]);
-                }
-            }
-            ss[r] = warp_sum(ss[r]);
-            us[r] = warp_sum(us[r]);
-        }
-        if constexpr (TPR > 32) {
-            if ((threadIdx.x & 31) == 0) {
-#pragma unroll
-                for (int r = 0; r < RA; ++r) {
-                    part[buf][wid][2 * r] = ss[r];
-                    part[buf][wid][2 * r + 1] = us[r];
-                }
-            }
-            __syncthreads();      // the two buffers alternate: one barrier per step separates reads from the next writes
-#pragma unroll
-            for (int r = 0; r < RA; ++r) {
-                ss[r] = us[r] = 0.f;
-#pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    ss[r] += part[buf][group * W + i][2 * r];
-                    us[r] += part[buf][group * W + i][2 * r + 1];
-                }
+            for (int i = 0; i < W; ++i) {
+                const float2 p = part[slot][group * W + i];
+                ss += p.x;
+                us += p.y;
             }
         }
+        const float rstd = 1.f / sqrtf(ss * inv_d + a.eps);
+        const f32x2 rstd2 = both(rstd), minus_c = both(-rstd * rstd * (us * inv_d));
 #pragma unroll
-        for (int r = 0; r < RA; ++r) {
-            const int row = row0 + group * RA + r;
-            if (row >= a.T) break;
-            const float rstd = 1.f / sqrtf(ss[r] / (float)a.d + a.eps);
-            const float c = rstd * rstd * (us[r] / (float)a.d);
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int v = lane + i * TPR;
-                if (v >= nv) continue;
-                float f[8], g[8], w[8], o[8], add[8];
-                unpack(sv[r][i], f);
-                unpack(yv[r][i], g);
-                unpack(av[r][i], add);
-                if (a.weight) {
-                    Vec<T> wv;
-                    load_vec(wv, (const T *)a.weight + 8 * v);
-                    unpack(wv, w);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float u = a.weight ? g[j] * w[j] : g[j];
-                    o[j] = rstd * (u - f[j] * c) + add[j];
-                    dw[i][j] = fmaf(g[j], f[j] * rstd, dw[i][j]);
-                }
-                store_vec((T *)a.dx + (size_t)row * a.d + 8 * (size_t)v, o);
+        for (int i = 0; i < VPT; ++i) {
+            const int v = lane + TPR * i;
+            if (v >= nv) continue;
+            f32x2 f[4], g[4], w[4], add[4], o[4];
+            if constexpr (!RING) {
+                fetch(slot, 0, i, sv[i]);
+                fetch(slot, 1, i, yv[i]);
             }
+            pairs(sv[i], f);
+            pairs(yv[i], g);
+            if (with_weight) {
+                Vec<T> wv;
+                load_vec(wv, (const T *)a.weight + 8 * v);
+                pairs(wv, w);
+            }
+            if (with_sum) {
+                Vec<T> av;
+                fetch(slot, 2, i, av);
+                pairs(av, add);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x2 t = fma2(f[j], minus_c, with_weight ? mul2(g[j], w[j]) : g[j]);
+                o[j] = with_sum ? fma2(rstd2, t, add[j]) : mul2(rstd2, t);
+                dw[i][j] = fma2(g[j], mul2(f[j], rstd2), dw[i][j]);
+            }
+            store_pairs((T *)a.dx + (size_t)row * a.d + 8 * (size_t)v, o);
         }
     }
     if (a.dw_part == nullptr) return;
-    float *out = a.dw_part + (size_t)blockIdx.x * a.d;
-    if constexpr (kRows == 1) {
+    if constexpr (RING) cp_async_wait<0>();
+    __syncthreads();
+    // the row groups' sums through the ring's memory, one group after the other
+    float *acc = reinterpret_cast<float *>(ring), *out = a.dw_part + (size_t)blockIdx.x * a.d;
+#pragma unroll 1
+    for (int g = 0; g < kGroups; ++g) {
+        if (group == g) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            const int v = lane + i * TPR;
-            if (v < nv) store_vec(out + 8 * v, dw[i]);
+            for (int i = 0; i < VPT; ++i) {
+                const int v = lane + TPR * i;
+                if (v >= nv) continue;
+                float t[8];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) unpack2(dw[i][j], t[2 * j], t[2 * j + 1]);
+                if (g > 0)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) t[j] += acc[8 * v + j];
+                store_vec(g + 1 < kGroups ? acc + 8 * v : out + 8 * v, t);
+            }
         }
-    } else {
-        // the row groups' sums meet in shared memory and are added in group order
-#pragma unroll
-        for (int i = 0; i < VPT; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) dw_sh[group * (TPR * VPT * 8) + 8 * (lane + i * TPR) + j] = dw[i][j];
         __syncthreads();
-        for (int c = threadIdx.x; c < a.d; c += kThreads) {
-            float t = 0.f;
-#pragma unroll
-            for (int g = 0; g < kRows; ++g) t += dw_sh[g * (TPR * VPT * 8) + c];
-            out[c] = t;
-        }
     }
 }
 
 // out[c] = sum over the blocks' partial rows, in block order within 32 interleaved runs that are added in order.
-__global__ void __launch_bounds__(1024) column_sum_kernel(const float *__restrict__ part, int n_rows, int d, float *__restrict__ out)
+__global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int n_rows, int d, float *__restrict__ out)
 {
     __shared__ float sh[32][33];
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), run = threadIdx.x >> 5;
     float acc = 0.f;
+    wait_for_earlier_kernels();
+    allow_next_kernel();
     if (c < d)
 #pragma unroll 8
         for (int r = run; r < n_rows; r += 32) acc += part[(size_t)r * d + c];
@@ -357,8 +427,7 @@ cudaError_t launch_norm(const NormArgs &a, cudaStream_t s)
 {
     constexpr int threads = TPR < kNormBlock ? kNormBlock : TPR;
     constexpr int rows = threads / TPR;
-    add_rms_norm_kernel<T, TPR, VPT><<<(a.T + rows - 1) / rows, threads, 0, s>>>(a);
-    return cudaGetLastError();
+    return launch_overlapped(add_rms_norm_kernel<T, TPR, VPT>, (a.T + rows - 1) / rows, threads, 0, s, a);
 }
 
 // Few rows: a row's latency counts, so it is spread over a block with one vector a thread where that holds it.
@@ -378,48 +447,74 @@ cudaError_t dispatch_norm(const NormArgs &a, int sms, cudaStream_t s)
     return launch_norm<T, 1024, 4>(a, s);
 }
 
-// Blocks of the backward kernel for a batch: the partial dweight rows they write are part of the workspace, whose size
-// is asked for without a device, so the count goes by the batch alone.
-constexpr int kBwdBlocks = 592;      // four for each of 148 SMs
-struct BwdShape { int tpr, vpt, rows_at; };
-BwdShape bwd_shape(int d)
+// Threads a row and vectors a thread of the backward kernel; its ring holds 2 x 3 x VPT vectors a thread.
+constexpr int kBwdThreads = 512;
+struct BwdShape { int tpr, vpt; };
+BwdShape bwd_shape(int d, int esz)
 {
-    const int nv = d / 8;
-    if (nv <= 32) return {32, 1, 2};
-    if (nv <= 64) return {32, 2, 2};
-    if (nv <= 128) return {128, 1, 4};
-    if (nv <= 256) return {256, 1, 4};
-    if (nv <= 512) return {256, 2, 2};
-    if (nv <= 1024) return {256, 4, 1};
-    if (nv <= 2048) return {256, 8, 1};
-    return {1024, 4, 1};
+    const int nv = d / 8, most = esz == 2 ? 4 : 2;      // vectors a thread that fit the ring
+    int tpr = 32;
+    while (tpr < kBwdThreads && tpr * most < nv) tpr *= 2;
+    if (tpr * most < nv) return {1024, 4};              // no ring
+    int vpt = 1;
+    while (vpt * tpr < nv) vpt *= 2;
+    return {tpr, vpt};
 }
+// Blocks for a batch: the partial dweight rows they write are part of the workspace, whose size is asked for without a
+// device or a type, so the count goes by the batch and the longer of the types' rows alone (148 SMs).
 int bwd_blocks(int T, int d)
 {
-    const BwdShape b = bwd_shape(d);
-    const int rows = (b.tpr < kNormBlock ? kNormBlock / b.tpr : 1) * b.rows_at;
-    const long long need = ((long long)T + rows - 1) / rows;
-    return (int)(need < kBwdBlocks ? need : kBwdBlocks);
+    const int tpr = bwd_shape(d, 4).tpr;
+    const long long groups = tpr < kBwdThreads ? kBwdThreads / tpr : 1, need = ((long long)T + groups - 1) / groups;
+    return (int)(need < 148 ? need : 148);
 }
 
-template <typename T, int TPR, int VPT, int RA>
+template <typename T, int TPR, int VPT>
 cudaError_t launch_bwd(const NormBwdArgs &a, int blocks, cudaStream_t s)
 {
-    add_rms_norm_bwd_kernel<T, TPR, VPT, RA><<<blocks, TPR < kNormBlock ? kNormBlock : TPR, 0, s>>>(a);
-    return cudaGetLastError();
+    if constexpr (TPR == 1024) {
+        return launch_overlapped(add_rms_norm_bwd_kernel<T, TPR, VPT, false>, blocks, 1024, 0, s, a);
+    }
+    auto kern = add_rms_norm_bwd_kernel<T, TPR, VPT, TPR != 1024>;
+    constexpr int smem = kBwdThreads * kSlots * 3 * VPT * 8 * (int)sizeof(T);
+    static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev > 63 || !((attr_done >> dev) & 1ull)) {
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        if (dev <= 63) attr_done |= 1ull << dev;
+    }
+    return launch_overlapped(kern, blocks, kBwdThreads, smem, s, a);
 }
 template <typename T>
 cudaError_t dispatch_bwd(const NormBwdArgs &a, int blocks, cudaStream_t s)
 {
-    const int nv = a.d / 8;
-    if (nv <= 32) return launch_bwd<T, 32, 1, 2>(a, blocks, s);
-    if (nv <= 64) return launch_bwd<T, 32, 2, 2>(a, blocks, s);
-    if (nv <= 128) return launch_bwd<T, 128, 1, 4>(a, blocks, s);
-    if (nv <= 256) return launch_bwd<T, 256, 1, 4>(a, blocks, s);
-    if (nv <= 512) return launch_bwd<T, 256, 2, 2>(a, blocks, s);
-    if (nv <= 1024) return launch_bwd<T, 256, 4, 1>(a, blocks, s);
-    if (nv <= 2048) return launch_bwd<T, 256, 8, 1>(a, blocks, s);
-    return launch_bwd<T, 1024, 4, 1>(a, blocks, s);
+    const BwdShape b = bwd_shape(a.d, (int)sizeof(T));
+    if constexpr (sizeof(T) == 2) {
+        switch (b.tpr * 8 + b.vpt) {
+        case 32 * 8 + 1: return launch_bwd<T, 32, 1>(a, blocks, s);
+        case 32 * 8 + 2: return launch_bwd<T, 32, 2>(a, blocks, s);
+        case 32 * 8 + 4: return launch_bwd<T, 32, 4>(a, blocks, s);
+        case 64 * 8 + 4: return launch_bwd<T, 64, 4>(a, blocks, s);
+        case 128 * 8 + 4: return launch_bwd<T, 128, 4>(a, blocks, s);
+        case 256 * 8 + 4: return launch_bwd<T, 256, 4>(a, blocks, s);
+        case 512 * 8 + 4: return launch_bwd<T, 512, 4>(a, blocks, s);
+        case 1024 * 8 + 4: return launch_bwd<T, 1024, 4>(a, blocks, s);
+        }
+    } else {
+        switch (b.tpr * 8 + b.vpt) {
+        case 32 * 8 + 1: return launch_bwd<T, 32, 1>(a, blocks, s);
+        case 32 * 8 + 2: return launch_bwd<T, 32, 2>(a, blocks, s);
+        case 64 * 8 + 2: return launch_bwd<T, 64, 2>(a, blocks, s);
+        case 128 * 8 + 2: return launch_bwd<T, 128, 2>(a, blocks, s);
+        case 256 * 8 + 2: return launch_bwd<T, 256, 2>(a, blocks, s);
+        case 512 * 8 + 2: return launch_bwd<T, 512, 2>(a, blocks, s);
+        case 1024 * 8 + 4: return launch_bwd<T, 1024, 4>(a, blocks, s);
+        }
+    }
+    return cudaErrorInvalidValue;
 }
 
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -441,8 +536,7 @@ int device_sms()
 
 cudaError_t launch_column_sum(const float *part, int n_rows, int d, float *out, cudaStream_t s)
 {
-    column_sum_kernel<<<(d + 31) / 32, 1024, 0, s>>>(part, n_rows, d, out);
-    return cudaGetLastError();
+    return launch_overlapped(column_sum_kernel, (d + 31) / 32, 1024, 0, s, part, n_rows, d, out);
 }
 
 }  // namespace modse

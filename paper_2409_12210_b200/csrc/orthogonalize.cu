@@ -18,6 +18,7 @@
 #include <cmath>
 
 #include "dense_gemm.h"
+#include "launch.h"
 
 namespace modse {
 namespace {
@@ -39,6 +40,7 @@ struct PrepMatrix {
 struct PrepArgs {
     PrepMatrix m[kGroup];
     double *parts;        // [group][kNormParts]
+    int *head;            // of the workspace, to be zeroed (null: zeroed already)
     float eps;
 };
 
@@ -80,6 +82,10 @@ __global__ void __launch_bounds__(256) square_sums_kernel(const __grid_constant_
     const int vecs = (m.cols + 7) / 8;
     const long long total = (long long)m.rows * vecs;
     const bool wide = wide_rows<T>(m);
+    wait_for_earlier_kernels();
+    allow_next_kernel();
+    if (a.head && blockIdx.x == 0 && blockIdx.y == 0)      // status word and counters of the products that follow
+        for (int i = threadIdx.x; i < (int)(kDenseZeroBytes / 4); i += 256) a.head[i] = 0;
     double acc = 0.0;       // squares of fp32 numbers overflow and underflow fp32 long before the numbers do
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)kNormParts * 256) {
         const int r = (int)(i / vecs), c = 8 * (int)(i - (long long)r * vecs);
@@ -105,6 +111,8 @@ __global__ void __launch_bounds__(256) normalise_kernel(const __grid_constant__ 
 {
     __shared__ float inv_sh;
     const PrepMatrix &m = a.m[blockIdx.y];
+    wait_for_earlier_kernels();
+    allow_next_kernel();
     if (threadIdx.x < 32) {
         const double *p = a.parts + blockIdx.y * kNormParts;
         double t = p[threadIdx.x] + p[threadIdx.x + 32];
@@ -222,12 +230,13 @@ bool coefficients_ok(float a, float b, float c, int steps)
 }
 
 cudaError_t run_group(modse_dtype_t dtype, const modse_matrix_t *m, int n, int steps, const float *k, float eps,
-                      unsigned char *ws, cudaStream_t s)
+                      unsigned char *ws, bool first, cudaStream_t s)
 {
     GroupLayout L;
     group_layout(m, n, L);
     PrepArgs prep{};
     prep.parts = (double *)(ws + L.parts);
+    prep.head = first ? (int *)ws : nullptr;
     prep.eps = eps;
     long long most = 0;
     for (int i = 0; i < n; ++i) {
@@ -237,14 +246,11 @@ cudaError_t run_group(modse_dtype_t dtype, const modse_matrix_t *m, int n, int s
     }
     const int blocks = (int)(most / 1024 < 1 ? 1 : most / 1024 > 1024 ? 1024 : most / 1024);
     const dim3 g1(kNormParts, n), g2(blocks, n);
-    if (dtype == MODSE_F32) {
-        square_sums_kernel<float><<<g1, 256, 0, s>>>(prep);
-        normalise_kernel<float><<<g2, 256, 0, s>>>(prep);
-    } else {
-        square_sums_kernel<__nv_bfloat16><<<g1, 256, 0, s>>>(prep);
-        normalise_kernel<__nv_bfloat16><<<g2, 256, 0, s>>>(prep);
-    }
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e = dtype == MODSE_F32 ? launch_overlapped(square_sums_kernel<float>, g1, 256, 0, s, prep)
+                                       : launch_overlapped(square_sums_kernel<__nv_bfloat16>, g1, 256, 0, s, prep);
+    if (e == cudaSuccess)
+        e = dtype == MODSE_F32 ? launch_overlapped(normalise_kernel<float>, g2, 256, 0, s, prep)
+                               : launch_overlapped(normalise_kernel<__nv_bfloat16>, g2, 256, 0, s, prep);
     DenseItem gram[kGroup], poly[kGroup], step[kGroup];
     for (int it = 0; e == cudaSuccess && it < steps; ++it) {
         const bool last = it + 1 == steps;
@@ -347,10 +353,9 @@ modse_status_t modse_orthogonalize(modse_dtype_t dtype, int n_matrices, const mo
     if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MODSE_ERR_INVALID_ARG;
     if (workspace_bytes < need) return MODSE_ERR_WORKSPACE_TOO_SMALL;
     const cudaStream_t s = (cudaStream_t)cuda_stream;
-    if (cudaMemsetAsync(workspace, 0, kDenseZeroBytes, s) != cudaSuccess) return MODSE_ERR_CUDA;
     for (int i = 0; i < n_matrices; i += kGroup)
         if (run_group(dtype, matrices + i, n_matrices - i < kGroup ? n_matrices - i : kGroup, steps, coefficients, eps,
-                      (unsigned char *)workspace, s) != cudaSuccess)
+                      (unsigned char *)workspace, i == 0, s) != cudaSuccess)
             return MODSE_ERR_CUDA;
     return MODSE_OK;
 }
