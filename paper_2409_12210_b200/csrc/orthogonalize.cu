@@ -19,13 +19,14 @@
 
 #include "dense_gemm.h"
 #include "launch.h"
+#include "orthogonalize_small.h"
 
 namespace modse {
 namespace {
 
 constexpr int kGroup = kDenseMaxProblems;     // matrices of one launch
 constexpr int kNormParts = 64;                // partial sums of squares of a matrix
-constexpr float kScaleX = 4096.f, kScaleA = 1024.f, kScaleB = 1024.f;
+constexpr float kScaleX = kOrthScaleX, kScaleA = kOrthScaleA, kScaleB = kOrthScaleB;
 constexpr double kMaxSigma = 7.5, kMaxB = 60.0;     // 7.5 * 2^12 and 60 * 2^10 are below fp16's 65504
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -312,6 +313,15 @@ modse_status_t check_call(modse_dtype_t dtype, int steps, const float *k, float 
     return coefficients_ok(k[0], k[1], k[2], steps) ? MODSE_OK : MODSE_ERR_UNSUPPORTED;
 }
 
+// The next matrices from index i on, up to a launch's worth, that take the grouped form (short sides above 128); i moves on.
+int next_group(const modse_matrix_t *m, int total, int &i, modse_matrix_t (&group)[kGroup])
+{
+    int n = 0;
+    for (; i < total && n < kGroup; ++i)
+        if (orthogonalize_small_cluster(m[i].rows, m[i].cols) == 0) group[n++] = m[i];
+    return n;
+}
+
 bool pointers_ok(modse_dtype_t dtype, const modse_matrix_t &m)
 {
     return m.grad != nullptr && m.update != nullptr && (reinterpret_cast<uintptr_t>(m.grad) & (dtype == MODSE_F32 ? 3 : 1)) == 0 &&
@@ -328,12 +338,15 @@ extern "C" {
 size_t modse_orthogonalize_workspace_bytes(int n_matrices, const modse_matrix_t *matrices)
 {
     if (n_matrices < 0 || (n_matrices > 0 && matrices == nullptr)) return 0;
-    size_t most = kDenseHead;
     for (int i = 0; i < n_matrices; ++i)
         if (!matrix_ok(matrices[i])) return 0;
-    for (int i = 0; i < n_matrices; i += kGroup) {
+    size_t most = kDenseHead;
+    modse_matrix_t group[kGroup];
+    for (int i = 0; i < n_matrices;) {
+        const int n = next_group(matrices, n_matrices, i, group);
+        if (n == 0) break;
         GroupLayout L;
-        group_layout(matrices + i, n_matrices - i < kGroup ? n_matrices - i : kGroup, L);
+        group_layout(group, n, L);
         most = L.total > most ? L.total : most;
     }
     return most;
@@ -353,10 +366,33 @@ modse_status_t modse_orthogonalize(modse_dtype_t dtype, int n_matrices, const mo
     if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MODSE_ERR_INVALID_ARG;
     if (workspace_bytes < need) return MODSE_ERR_WORKSPACE_TOO_SMALL;
     const cudaStream_t s = (cudaStream_t)cuda_stream;
-    for (int i = 0; i < n_matrices; i += kGroup)
-        if (run_group(dtype, matrices + i, n_matrices - i < kGroup ? n_matrices - i : kGroup, steps, coefficients, eps,
-                      (unsigned char *)workspace, i == 0, s) != cudaSuccess)
+    bool first = true;               // the call's first kernel zeroes the workspace head
+    SmallArgs small{};
+    for (int j = 0; j < 3; ++j) small.k[j] = coefficients[j];
+    small.eps = eps;
+    small.steps = steps;
+    int n = 0;
+    for (int i = 0; i <= n_matrices; ++i) {
+        if (i < n_matrices && orthogonalize_small_cluster(matrices[i].rows, matrices[i].cols) > 0) {
+            const modse_matrix_t &m = matrices[i];
+            small.m[n++] = {m.grad, (__nv_bfloat16 *)m.update, m.ld_grad, m.ld_update, m.rows, m.cols, m.scale};
+        }
+        if (n == kOrthSmallBatch || (i == n_matrices && n > 0)) {
+            small.head = first ? (int *)workspace : nullptr;
+            small.head_ints = (int)(kDenseZeroBytes / 4);
+            if (launch_orthogonalize_small(dtype == MODSE_F32, small, n, s) != cudaSuccess) return MODSE_ERR_CUDA;
+            first = false;
+            n = 0;
+        }
+    }
+    modse_matrix_t group[kGroup];
+    for (int i = 0; i < n_matrices;) {
+        const int c = next_group(matrices, n_matrices, i, group);
+        if (c == 0) break;
+        if (run_group(dtype, group, c, steps, coefficients, eps, (unsigned char *)workspace, first, s) != cudaSuccess)
             return MODSE_ERR_CUDA;
+        first = false;
+    }
     return MODSE_OK;
 }
 

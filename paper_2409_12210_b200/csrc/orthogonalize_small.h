@@ -1,0 +1,33 @@
+// The one-kernel form of modse_orthogonalize for matrices with a short side.
+#pragma once
+
+#include "modse_internal.h"
+
+namespace modse {
+
+// powers of two the fp16 factors of the iteration are stored with (see orthogonalize.cu)
+constexpr float kOrthScaleX = 4096.f, kOrthScaleA = 1024.f, kOrthScaleB = 1024.f;
+constexpr int kOrthSmallMax = 128;     // longest shorter side of this form
+constexpr int kOrthSmallBatch = 32;    // matrices of a launch
+
+struct SmallMatrix {
+    const void *g;
+    __nv_bfloat16 *out;
+    long long ld_g, ld_out;
+    int rows, cols;
+    float scale;
+};
+struct SmallArgs {
+    SmallMatrix m[kOrthSmallBatch];
+    float k[3];
+    float eps;
+    int steps;
+    int head_ints;       // words of the workspace head to zero (none: head is null)
+    int *head;
+};
+
+// Blocks a matrix of this shape takes (1, 2, 4 or 8), 0: not for this form.
+int orthogonalize_small_cluster(int rows, int cols);
+cudaError_t launch_orthogonalize_small(bool f32, const SmallArgs &a, int n, cudaStream_t s);
+
+}  // namespace modse
