@@ -11,7 +11,7 @@ namespace modse {
 // What happens to an accumulator on its way out.
 enum DenseMode : int {
     DenseLinear = 0,   // y = act(acc * sx * sw + bias) + residual, z beside it
-    DensePlain = 1,    // out = acc (bf16 or fp32)
+    DensePlain = 1,    // out = acc (bf16)
     DenseGram = 2,     // out = alpha acc (fp16), symmetric
     DensePoly = 3,     // out = alpha acc + beta in0 (fp16), symmetric
     DenseStep = 4      // x = alpha acc + beta (hi + lo): hi, lo (fp16), or the final bf16 result
@@ -22,7 +22,7 @@ enum : int {
     kDenseBMn = 2,     // same for the column operand ([K, N], not [N, K])
     kDenseSym = 4,     // out is symmetric: tiles below the diagonal are not computed but mirrored
     kDenseLast = 8,    // DenseStep: write the final result
-    kDenseF32 = 16     // DensePlain: out is fp32
+    kDenseTmaOut = 16  // set by the launch: the final result's rows are aligned for TMA
 };
 
 // One product out[M, N] = sum_k A[m, k] B[n, k] of a launch.
