@@ -281,7 +281,7 @@ def _buffer(name, t, shape, dtype, device):
 def _current_stream(name, t):
     """(raw current stream, device index) of t's device, which has to be the current CUDA device."""
     device = t.get_device()
-    if device < 0 or device != torch.cuda.current_device():
+    if device < 0 or device != torch._C._cuda_getDevice():
         raise ValueError(f"{name}: expected a tensor on the current CUDA device, got one on {t.device}")
     return torch._C._cuda_getCurrentRawStream(device), device
 

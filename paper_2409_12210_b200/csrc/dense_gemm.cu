@@ -54,6 +54,7 @@ template <int P> struct DenseParams {
     float *partial;
     unsigned long long wait_limit_ns;
     int clear_status;
+    DenseColumnSum sum;
 };
 
 struct DenseTile {
@@ -62,6 +63,16 @@ struct DenseTile {
     int split;
     bool mirror;     // symmetric output: also write the transposed tile
 };
+
+// The round-th item of a pair, -1: none.  The items of several products are sorted by decreasing length; every other round
+// is dealt in the other direction, so that who got the longest item of one round gets the shortest of the next (1001
+// tokens' dx and dw, 24 tiles of 44 k-blocks and 66 of 16: 34 -> 26 us).
+template <int P>
+__device__ __forceinline__ int dense_item(int round, int who, int n, int items)
+{
+    const int item = round * n + ((P > 1 && (round & 1)) ? n - 1 - who : who);
+    return item < items ? item : -1;
+}
 
 template <int TN, int P>
 __device__ __forceinline__ DenseTile dense_decode(const DenseParams<P> &prm, int item, int &cursor)
@@ -207,38 +218,46 @@ __device__ __forceinline__ void activate_all(float (&v)[32], int act)
     }
 }
 
-// What a chunk of 32 rows (from r0) x 32 columns (from c0) reads from memory; the first chunk's is requested before the
-// accumulator is waited for, the others' while the accumulator's columns are on their way.
+// What a chunk of 32 rows (from r0) x 32 columns (from c0) reads from memory.  The first chunk's is requested before the
+// accumulator is waited for, the next one's as soon as the registers of the present one are free.
 template <int MODE, bool F8> struct ChunkInputs {
     uint4 raw[MODE == DensePlain || MODE == DenseGram ? 1 : 4];      // residual, or the first input
     uint4 raw2[MODE == DenseStep ? 4 : 1];
     uint4 bias[MODE == DenseLinear ? 4 : 1];
     float sx;
 };
-template <int MODE, bool F8>
+enum : int { kLoadFirst = 1, kLoadSecond = 2, kLoadBias = 4, kLoadAll = 7 };
+template <int WHAT, int MODE, bool F8>
 __device__ __forceinline__ void chunk_load(ChunkInputs<MODE, F8> &in, const DenseProblem &q, const LinearEpilogue &lin, int r0,
                                            int c0, int lane)
 {
-    const int rows = min(32, q.M - r0), pieces = (min(32, q.N - c0) + 7) >> 3;
+    const int rows = min(32, q.M - r0), pieces = (min(32, q.N - c0) + 7) >> 3;      // none where c0 lies outside
     if constexpr (MODE == DenseLinear) {
-        if (lin.residual) rows_load(lane, (const unsigned char *)(lin.residual + (long long)r0 * q.N + c0), 2ll * q.N, rows, pieces, in.raw);
-        if (lin.bias)
+        if constexpr ((WHAT & kLoadFirst) != 0)
+            if (lin.residual) rows_load(lane, (const unsigned char *)(lin.residual + (long long)r0 * q.N + c0), 2ll * q.N, rows, pieces, in.raw);
+        if constexpr ((WHAT & kLoadBias) != 0) {
+            if (lin.bias)
 #pragma unroll
-            for (int p = 0; p < 4; ++p) in.bias[p] = p < pieces ? __ldg(reinterpret_cast<const uint4 *>(lin.bias + c0) + p) : make_uint4(0, 0, 0, 0);
-        if constexpr (F8) in.sx = lane < rows ? __ldg(lin.sx + r0 + lane) : 0.f;
+                for (int p = 0; p < 4; ++p) in.bias[p] = p < pieces ? __ldg(reinterpret_cast<const uint4 *>(lin.bias + c0) + p) : make_uint4(0, 0, 0, 0);
+            if constexpr (F8) in.sx = lane < rows ? __ldg(lin.sx + r0 + lane) : 0.f;
+        }
     } else if constexpr (MODE == DensePoly) {
-        rows_load(lane, (const unsigned char *)((const __half *)q.in0 + (long long)r0 * q.ld_out + c0), 2 * q.ld_out, rows, pieces, in.raw);
+        if constexpr ((WHAT & kLoadFirst) != 0)
+            rows_load(lane, (const unsigned char *)((const __half *)q.in0 + (long long)r0 * q.ld_out + c0), 2 * q.ld_out, rows, pieces, in.raw);
     } else if constexpr (MODE == DenseStep) {
         const long long at = (long long)r0 * q.ld_in + c0;
-        rows_load(lane, (const unsigned char *)((const __half *)q.in0 + at), 2 * q.ld_in, rows, pieces, in.raw);
-        rows_load(lane, (const unsigned char *)((const __half *)q.in1 + at), 2 * q.ld_in, rows, pieces, in.raw2);
+        if constexpr ((WHAT & kLoadFirst) != 0)
+            rows_load(lane, (const unsigned char *)((const __half *)q.in0 + at), 2 * q.ld_in, rows, pieces, in.raw);
+        if constexpr ((WHAT & kLoadSecond) != 0)
+            rows_load(lane, (const unsigned char *)((const __half *)q.in1 + at), 2 * q.ld_in, rows, pieces, in.raw2);
     }
 }
 
-// Finishes the chunk; v: this lane's row.
+// Finishes the chunk and requests the inputs of the one that starts at column `next` (an outside column: of none); v: this
+// lane's row.
 template <int MODE, bool F8>
-__device__ __forceinline__ void chunk_finish(const ChunkInputs<MODE, F8> &in, const DenseProblem &q, const LinearEpilogue &lin,
-                                             const CUtensorMap *o0, const CUtensorMap *o1, bool mirror, int r0, int c0, int lane,
+__device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const DenseProblem &q, const LinearEpilogue &lin,
+                                             const CUtensorMap *o0, const CUtensorMap *o1, bool mirror, int r0, int c0, int next, int lane,
                                              Staging &stg, float (&v)[32])
 {
     const int rows = min(32, q.M - r0), cols = min(32, q.N - c0);
@@ -262,6 +281,7 @@ __device__ __forceinline__ void chunk_finish(const ChunkInputs<MODE, F8> &in, co
                     v[8 * p + 2 * i + 1] += f.y;
                 }
         }
+        chunk_load<kLoadBias>(in, q, lin, r0, next, lane);
         if (lin.z) {
             pack_bf16(v, w);
             tile_out(stg, stg.take(lane), lane, o1, c0, r0, w);
@@ -271,6 +291,7 @@ __device__ __forceinline__ void chunk_finish(const ChunkInputs<MODE, F8> &in, co
         if (lin.residual) {
             uint4 own[4];
             rows_hand(buf, lane, in.raw, own);
+            chunk_load<kLoadFirst>(in, q, lin, r0, next, lane);
 #pragma unroll
             for (int p = 0; p < 4; ++p)
 #pragma unroll
@@ -290,6 +311,7 @@ __device__ __forceinline__ void chunk_finish(const ChunkInputs<MODE, F8> &in, co
         if constexpr (MODE == DensePoly) {
             uint4 own[4];
             rows_hand(buf, lane, in.raw, own);
+            chunk_load<kLoadFirst>(in, q, lin, r0, next, lane);
 #pragma unroll
             for (int p = 0; p < 4; ++p)
 #pragma unroll
@@ -315,11 +337,15 @@ __device__ __forceinline__ void chunk_finish(const ChunkInputs<MODE, F8> &in, co
         unsigned char *buf = stg.take(lane);
         uint4 own[4];
         rows_hand(buf, lane, in.raw, own);
+        chunk_load<kLoadFirst>(in, q, lin, r0, next, lane);
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= q.alpha;
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            if (k == 1) rows_hand(buf, lane, in.raw2, own);
+            if (k == 1) {
+                rows_hand(buf, lane, in.raw2, own);
+                chunk_load<kLoadSecond>(in, q, lin, r0, next, lane);
+            }
 #pragma unroll
             for (int p = 0; p < 4; ++p)
 #pragma unroll
@@ -442,7 +468,9 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
             uint32_t phase = 0;
             long long issued = 0;
             bool ok = true;
-            for (int item = cluster_id; ok && item < prm.items; item += n_clusters) {
+            for (int it = 0; ok; ++it) {
+                const int item = dense_item<P>(it, cluster_id, n_clusters, prm.items);
+                if (item < 0) break;
                 const DenseTile t = dense_decode<TN, P>(prm, item, cursor);
                 const int flags = prm.prob[t.p].flags;
                 const CUtensorMap *am = &prm.a[t.p], *bm = &prm.b[t.p];
@@ -484,10 +512,12 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
     } else if (warp == 1) {
         // ===================== MMA issuer (leader only) =====================
         if (lane == 0 && rank == 0) {
-            int stage = 0, cursor = 0, it = 0;
+            int stage = 0, cursor = 0;
             uint32_t phase = 0;
             bool ok = true;
-            for (int item = cluster_id; ok && item < prm.items; item += n_clusters, ++it) {
+            for (int it = 0; ok; ++it) {
+                const int item = dense_item<P>(it, cluster_id, n_clusters, prm.items);
+                if (item < 0) break;
                 const DenseTile t = dense_decode<TN, P>(prm, item, cursor);
                 const int flags = prm.prob[t.p].flags;
                 const bool a_mn = (flags & kDenseAMn) != 0, b_mn = (flags & kDenseBMn) != 0;
@@ -517,7 +547,18 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
                 umma_commit_pair(smem_u32(&st->tmem_full[acc]));
             }
         }
-    } else if (warp >= kDenseFirstEpi) {
+    } else if (warp < kDenseFirstEpi) {
+        // ===================== column sums of a [rows, cols] fp32 matrix beside the products =====================
+        if constexpr (MODE == DensePlain) {
+            const int step = 2 * (int)gridDim.x * 32;
+            for (int c = (2 * (int)blockIdx.x + warp - 2) * 32 + lane; c < prm.sum.cols; c += step) {
+                float t = 0.f;
+#pragma unroll 8
+                for (int r = 0; r < prm.sum.rows; ++r) t += __ldcg(prm.sum.part + (size_t)r * prm.sum.cols + c);
+                prm.sum.out[c] = t;
+            }
+        }
+    } else {
         // ===================== epilogue (both CTAs) =====================
         const int quad = warp & 3;                          // tensor-memory lanes this warp may read
         const int cq = (warp - kDenseFirstEpi) >> 2;        // which half of the tile's columns
@@ -526,8 +567,10 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
         const uint32_t leader_empty1 = map_to_cta(smem_u32(&st->tmem_empty[1]), 0);
         constexpr int kChunks = TN / 64;                    // 32-column chunks a warp owns
         constexpr bool kF8 = TYPE == DenseE4m3;
-        int cursor = 0, it = 0;
-        for (int item = cluster_id; item < prm.items; item += n_clusters, ++it) {
+        int cursor = 0;
+        for (int it = 0;; ++it) {
+            const int item = dense_item<P>(it, cluster_id, n_clusters, prm.items);
+            if (item < 0) break;
             const DenseTile t = dense_decode<TN, P>(prm, item, cursor);
             const DenseProblem &q = prm.prob[t.p];
             const CUtensorMap *o0 = &prm.o0[t.p], *o1 = &prm.o1[t.p];
@@ -535,7 +578,7 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
             const int r0 = t.m0 + rank * 128 + quad * 32, c0 = t.n0 + cq * kHalf;
             const bool any = r0 < q.M && c0 < q.N;
             ChunkInputs<MODE, kF8> in;
-            if (any && t.tail < 0) chunk_load(in, q, prm.lin, r0, c0, lane);
+            if (any && t.tail < 0) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
             if (!mbar_wait(smem_u32(&st->tmem_full[acc]), (uint32_t)(it >> 1) & 1u, wc)) break;
             tc_fence_after();
             const uint32_t tacc = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * kDenseAccCols + cq * kHalf);
@@ -551,13 +594,13 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
                     if (c0 + 32 * c >= q.N) break;
                     uint32_t w[32];
                     tmem_ld32(tacc + 32 * c, w);
-                    if (c > 0 && t.tail < 0) chunk_load(in, q, prm.lin, r0, c0 + 32 * c, lane);
                     tmem_ld_wait();
                     float v[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
                     if (t.tail < 0) {
-                        chunk_finish(in, q, prm.lin, o0, o1, t.mirror, r0, c0 + 32 * c, lane, stg, v);
+                        chunk_finish(in, q, prm.lin, o0, o1, t.mirror, r0, c0 + 32 * c,
+                                     c + 1 < kChunks ? c0 + 32 * c + 32 : q.N, lane, stg, v);
                     } else {
                         float4 *dst = strip + (size_t)t.split * kPieceStride + (size_t)c * 256;
 #pragma unroll
@@ -580,7 +623,7 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
 #pragma unroll 1
                     for (int c = 0; c < kChunks; ++c) {
                         if (c0 + 32 * c >= q.N) break;
-                        chunk_load(in, q, prm.lin, r0, c0 + 32 * c, lane);
+                        if (c == 0) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
                         float v[32];
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = 0.f;
@@ -593,7 +636,8 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
                                 v[4 * j] += f.x; v[4 * j + 1] += f.y; v[4 * j + 2] += f.z; v[4 * j + 3] += f.w;
                             }
                         }
-                        chunk_finish(in, q, prm.lin, o0, o1, t.mirror, r0, c0 + 32 * c, lane, stg, v);
+                        chunk_finish(in, q, prm.lin, o0, o1, t.mirror, r0, c0 + 32 * c,
+                                     c + 1 < kChunks ? c0 + 32 * c + 32 : q.N, lane, stg, v);
                     }
                 }
             }
@@ -678,7 +722,7 @@ DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int
 }
 
 template <int MODE, int TYPE, int TN, int P>
-cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const LinearEpilogue *lin, void *ws, int head, cudaStream_t s)
+cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const LinearEpilogue *lin, const DenseColumnSum *sum, void *ws, int head, cudaStream_t s)
 {
     DenseParams<P> prm;
     int tiles = 0;
@@ -723,6 +767,7 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
     prm.partial = (float *)((unsigned char *)ws + kDenseHead);
     prm.wait_limit_ns = tc_wait_limit_ns();
     prm.clear_status = head == kDenseHeadRaw;
+    prm.sum = sum ? *sum : DenseColumnSum{};
 
     auto kern = dense_gemm_pair<MODE, TYPE, TN, P>;
     static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
@@ -742,15 +787,15 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
 }
 
 template <int MODE, int TYPE, int P>
-cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin, void *ws, size_t cap, int head, cudaStream_t s)
+cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin, const DenseColumnSum *sum, void *ws, size_t cap, int head, cudaStream_t s)
 {
     if (n > P) return cudaErrorInvalidValue;
     const DensePlan pl = dense_plan((DenseMode)MODE, (DenseType)TYPE, items, n, device_sms(), cap);
     if constexpr (MODE == DenseGram || MODE == DensePoly) {
-        return launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, ws, head, s);
+        return launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, sum, ws, head, s);
     } else {
-        return pl.tn == 128 ? launch_tn<MODE, TYPE, 128, P>(pl, items, n, lin, ws, head, s)
-                            : launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, ws, head, s);
+        return pl.tn == 128 ? launch_tn<MODE, TYPE, 128, P>(pl, items, n, lin, sum, ws, head, s)
+                            : launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, sum, ws, head, s);
     }
 }
 
@@ -762,18 +807,22 @@ size_t dense_partial_bytes(DenseMode mode, DenseType type, const DenseItem *item
     return pl.splits > 1 ? (size_t)(pl.items - pl.full) * 256 * pl.tn * 4 : 0;
 }
 
-cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *items, int n, const LinearEpilogue *lin, void *ws,
-                         size_t partial_capacity, int head, cudaStream_t s)
+cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *list, int n, const LinearEpilogue *lin,
+                         const DenseColumnSum *sum, void *ws, size_t partial_capacity, int head, cudaStream_t s)
 {
     if (n < 1 || n > kDenseMaxProblems) return cudaErrorInvalidValue;
+    // longest contraction first (see dense_item)
+    DenseItem items[kDenseMaxProblems];
+    std::copy(list, list + n, items);
+    std::stable_sort(items, items + n, [](const DenseItem &a, const DenseItem &b) { return a.k > b.k; });
     switch (mode) {
     case DenseLinear:
-        return type == DenseE4m3 ? launch_mode<DenseLinear, DenseE4m3, 1>(items, n, lin, ws, partial_capacity, head, s)
-                                 : launch_mode<DenseLinear, DenseBf16, 1>(items, n, lin, ws, partial_capacity, head, s);
-    case DensePlain: return launch_mode<DensePlain, DenseBf16, 2>(items, n, lin, ws, partial_capacity, head, s);
-    case DenseGram: return launch_mode<DenseGram, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, head, s);
-    case DensePoly: return launch_mode<DensePoly, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, head, s);
-    case DenseStep: return launch_mode<DenseStep, DenseF16, kDenseMaxProblems>(items, n, lin, ws, partial_capacity, head, s);
+        return type == DenseE4m3 ? launch_mode<DenseLinear, DenseE4m3, 1>(items, n, lin, sum, ws, partial_capacity, head, s)
+                                 : launch_mode<DenseLinear, DenseBf16, 1>(items, n, lin, sum, ws, partial_capacity, head, s);
+    case DensePlain: return launch_mode<DensePlain, DenseBf16, 2>(items, n, lin, sum, ws, partial_capacity, head, s);
+    case DenseGram: return launch_mode<DenseGram, DenseF16, kDenseMaxProblems>(items, n, lin, sum, ws, partial_capacity, head, s);
+    case DensePoly: return launch_mode<DensePoly, DenseF16, kDenseMaxProblems>(items, n, lin, sum, ws, partial_capacity, head, s);
+    case DenseStep: return launch_mode<DenseStep, DenseF16, kDenseMaxProblems>(items, n, lin, sum, ws, partial_capacity, head, s);
     }
     return cudaErrorInvalidValue;
 }

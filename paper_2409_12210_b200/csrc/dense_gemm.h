@@ -44,6 +44,13 @@ struct LinearEpilogue {
     int act;
 };
 
+// out[c] = sum over r of part[r][c], in order, done beside the products of a DensePlain launch (cols 0: none).
+struct DenseColumnSum {
+    const float *part;
+    float *out;
+    int rows, cols;
+};
+
 constexpr int kDenseMaxProblems = 16;
 // An operand as it lies in memory: rows x cols elements, ld elements from row to row (a multiple of 16 bytes).
 struct DenseOperand {
@@ -71,7 +78,7 @@ constexpr size_t kDenseHead = (kDenseZeroBytes + 255) / 256 * 256;
 size_t dense_partial_bytes(DenseMode mode, DenseType type, const DenseItem *items, int n);
 
 // Launches n products of one mode and type as one kernel on a workspace whose head is `ws`.
-cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *items, int n, const LinearEpilogue *lin, void *ws,
-                         size_t partial_capacity, int head, cudaStream_t s);
+cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *list, int n, const LinearEpilogue *lin,
+                         const DenseColumnSum *sum, void *ws, size_t partial_capacity, int head, cudaStream_t s);
 
 }  // namespace modse

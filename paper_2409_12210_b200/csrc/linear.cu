@@ -229,7 +229,7 @@ modse_status_t modse_linear(modse_dtype_t dtype, int n_tokens, int d_in, int d_o
         return MODSE_OK;
     }
     const DenseItem it = forward_item(type, n_tokens, d_in, d_out, a.x, a.w);
-    MODSE_CUDA(dense_launch(DenseLinear, type, &it, 1, &lin, workspace, need - kDenseHead, kDenseHeadRaw, s));
+    MODSE_CUDA(dense_launch(DenseLinear, type, &it, 1, &lin, nullptr, workspace, need - kDenseHead, kDenseHeadRaw, s));
     return MODSE_OK;
 }
 
@@ -272,11 +272,14 @@ modse_status_t modse_linear_backward(int n_tokens, int d_in, int d_out, modse_ac
         MODSE_CUDA(launch_dz((int)activation, a.dy, a.z, ws + L.dz, part, (int *)ws, n_tokens, d_out, s));
         head = kDenseHeadZero;
         if (activation != MODSE_ACT_NONE) dz = ws + L.dz;
-        if (part) MODSE_CUDA(launch_column_sum(part, dz_strips(n_tokens), d_out, a.dbias, s));
     }
     DenseItem items[2];
     const int c = backward_items(items, n_tokens, d_in, d_out, dz, a.x, a.w, a.dx, a.dw);
-    if (c > 0) MODSE_CUDA(dense_launch(DensePlain, DenseBf16, items, c, nullptr, workspace, L.partial_bytes, head, s));
+    const DenseColumnSum sum{part, a.dbias, dz_strips(n_tokens), d_out};
+    if (c > 0)
+        MODSE_CUDA(dense_launch(DensePlain, DenseBf16, items, c, nullptr, part ? &sum : nullptr, workspace, L.partial_bytes, head, s));
+    else if (part)
+        MODSE_CUDA(launch_column_sum(part, dz_strips(n_tokens), d_out, a.dbias, s));
     return MODSE_OK;
 }
 

@@ -15,7 +15,6 @@
 // checks on the host that the coefficients keep every singular value inside the range this leaves.
 #include <cuda_fp16.h>
 
-#include <algorithm>
 #include <cmath>
 
 #include "dense_gemm.h"
@@ -278,9 +277,9 @@ cudaError_t run_group(modse_dtype_t dtype, const modse_matrix_t *m, int n, int s
                 p.out1 = lo;           // a tile's lo is read and written by the warp that owns its rows
             }
         }
-        e = dense_launch(DenseGram, DenseF16, gram, n, nullptr, ws, L.partial_bytes, kDenseHeadZero, s);
-        if (e == cudaSuccess) e = dense_launch(DensePoly, DenseF16, poly, n, nullptr, ws, L.partial_bytes, kDenseHeadZero, s);
-        if (e == cudaSuccess) e = dense_launch(DenseStep, DenseF16, step, n, nullptr, ws, L.partial_bytes, kDenseHeadZero, s);
+        e = dense_launch(DenseGram, DenseF16, gram, n, nullptr, nullptr, ws, L.partial_bytes, kDenseHeadZero, s);
+        if (e == cudaSuccess) e = dense_launch(DensePoly, DenseF16, poly, n, nullptr, nullptr, ws, L.partial_bytes, kDenseHeadZero, s);
+        if (e == cudaSuccess) e = dense_launch(DenseStep, DenseF16, step, n, nullptr, nullptr, ws, L.partial_bytes, kDenseHeadZero, s);
     }
     return e;
 }
@@ -315,17 +314,12 @@ modse_status_t check_call(modse_dtype_t dtype, int steps, const float *k, float 
 }
 
 // The next matrices from index i on, up to a launch's worth, that take the grouped form (short sides above 128); i moves
-// on.  Longest first: a launch deals its tiles to the CTA pairs in rounds, and a tile of X X^T takes as long as the
-// matrix's longer side, so that matrices of one length should share a round (the 2816..8448-wide experts' matrices in
-// their own order left the pairs idle for a third of that product: 217 us against 160).
+// on.
 int next_group(const modse_matrix_t *m, int total, int &i, modse_matrix_t (&group)[kGroup])
 {
     int n = 0;
     for (; i < total && n < kGroup; ++i)
         if (orthogonalize_small_cluster(m[i].rows, m[i].cols) == 0) group[n++] = m[i];
-    std::stable_sort(group, group + n, [](const modse_matrix_t &a, const modse_matrix_t &b) {
-        return std::max(a.rows, a.cols) > std::max(b.rows, b.cols);
-    });
     return n;
 }
 
