@@ -68,6 +68,19 @@ __device__ __forceinline__ float warp_sum(float v)
     return v;
 }
 
+// Sums of two numbers over a warp with six exchanges instead of ten: the half-warps trade one number each, then every half
+// sums its own.
+__device__ __forceinline__ void warp_sum2(float &a, float &b)
+{
+    const bool upper = (threadIdx.x & 16) != 0;
+    float v = (upper ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, upper ? a : b, 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    const float other = __shfl_xor_sync(0xFFFFFFFFu, v, 16);
+    a = upper ? other : v;
+    b = upper ? v : other;
+}
+
 // Sum over the TPR threads of a row (every one of them gets it; fixed order).  `slot`: this row's TPR / 32 words.
 template <int TPR>
 __device__ __forceinline__ float row_sum(float v, float *slot)
@@ -243,19 +256,19 @@ __device__ __forceinline__ void store_pairs(T *p, const f32x2 (&f)[4])
 // formed; it reads back only the pieces it copied itself, so the only meeting is that of the row's warps over the sums (a
 // named barrier; none where the row is one warp's).  dweight sums stay in registers (VPT * 8 <= 32) and meet in shared
 // memory at the end, in the order of the row groups.
-// Rows too long for the ring (RING false: 1024 threads a row) are read from global memory twice instead, the second time
+// Rows too long for the ring (1024 threads a row) are read from global memory twice instead, the second time
 // from L2.
 constexpr int kSlots = 2;
-template <typename T, int TPR, int VPT, bool RING>
-__global__ void __launch_bounds__(RING ? 512 : 1024, 1)
+template <typename T, int TPR, int VPT, bool WEIGHT, bool SUM>
+__global__ void __launch_bounds__(TPR == 1024 ? 1024 : 512, 1)
 add_rms_norm_bwd_kernel(const NormBwdArgs a)
 {
+    constexpr bool RING = TPR != 1024;
     extern __shared__ unsigned char ring[];
     constexpr int kBwdThreads = RING ? 512 : 1024;
     constexpr int kGroups = kBwdThreads / TPR, W = TPR / 32, kPieces = sizeof(T) / 2;      // 16-byte pieces of a vector
     __shared__ float2 part[2][kBwdThreads / 32];
     const int group = threadIdx.x / TPR, lane = threadIdx.x % TPR, warp = threadIdx.x >> 5, nv = a.d / 8;
-    const bool with_sum = a.dsum != nullptr, with_weight = a.weight != nullptr;
     // ring: [slot][tensor][vector][piece] of 16 bytes a thread, neighbouring threads side by side
     unsigned char *mine = ring + threadIdx.x * 16;
     auto piece = [&](int slot, int tensor, int i, int h) -> unsigned char * {
@@ -286,7 +299,7 @@ add_rms_norm_bwd_kernel(const NormBwdArgs a)
                     for (int h = 0; h < kPieces; ++h) {
                         cp_async16(piece(slot, 0, i, h), (const unsigned char *)a.s + at + 16 * h);
                         cp_async16(piece(slot, 1, i, h), (const unsigned char *)a.dy + at + 16 * h);
-                        if (with_sum) cp_async16(piece(slot, 2, i, h), (const unsigned char *)a.dsum + at + 16 * h);
+                        if constexpr (SUM) cp_async16(piece(slot, 2, i, h), (const unsigned char *)a.dsum + at + 16 * h);
                     }
                 }
             }
@@ -316,7 +329,7 @@ add_rms_norm_bwd_kernel(const NormBwdArgs a)
             f32x2 f[4], g[4], w[4];
             pairs(sv[i], f);
             pairs(yv[i], g);
-            if (with_weight) {
+            if constexpr (WEIGHT) {
                 Vec<T> wv;
                 load_vec(wv, (const T *)a.weight + 8 * v);
                 pairs(wv, w);
@@ -324,14 +337,15 @@ add_rms_norm_bwd_kernel(const NormBwdArgs a)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 ss2 = fma2(f[j], f[j], ss2);
-                us2 = fma2(with_weight ? mul2(g[j], w[j]) : g[j], f[j], us2);
+                us2 = fma2(WEIGHT ? mul2(g[j], w[j]) : g[j], f[j], us2);
             }
         }
         float ss, us, t0, t1;
         unpack2(ss2, t0, t1);
-        ss = warp_sum(t0 + t1);
+        ss = t0 + t1;
         unpack2(us2, t0, t1);
-        us = warp_sum(t0 + t1);
+        us = t0 + t1;
+        warp_sum2(ss, us);
         if constexpr (W > 1) {
             // the buffers alternate: nobody writes one again before the group's next barrier
             if ((threadIdx.x & 31) == 0) part[slot][warp] = make_float2(ss, us);
@@ -344,7 +358,7 @@ add_rms_norm_bwd_kernel(const NormBwdArgs a)
                 us += p.y;
             }
         }
-        const float rstd = 1.f / sqrtf(ss * inv_d + a.eps);
+        const float rstd = rsqrtf(ss * inv_d + a.eps);       // within two units of the last place
         const f32x2 rstd2 = both(rstd), minus_c = both(-rstd * rstd * (us * inv_d));
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
@@ -357,20 +371,20 @@ add_rms_norm_bwd_kernel(const NormBwdArgs a)
             }
             pairs(sv[i], f);
             pairs(yv[i], g);
-            if (with_weight) {
+            if constexpr (WEIGHT) {
                 Vec<T> wv;
                 load_vec(wv, (const T *)a.weight + 8 * v);
                 pairs(wv, w);
             }
-            if (with_sum) {
+            if constexpr (SUM) {
                 Vec<T> av;
                 fetch(slot, 2, i, av);
                 pairs(av, add);
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const f32x2 t = fma2(f[j], minus_c, with_weight ? mul2(g[j], w[j]) : g[j]);
-                o[j] = with_sum ? fma2(rstd2, t, add[j]) : mul2(rstd2, t);
+                const f32x2 t = fma2(f[j], minus_c, WEIGHT ? mul2(g[j], w[j]) : g[j]);
+                o[j] = SUM ? fma2(rstd2, t, add[j]) : mul2(rstd2, t);
                 dw[i][j] = fma2(g[j], mul2(f[j], rstd2), dw[i][j]);
             }
             store_pairs((T *)a.dx + (size_t)row * a.d + 8 * (size_t)v, o);
@@ -379,25 +393,27 @@ add_rms_norm_bwd_kernel(const NormBwdArgs a)
     if (a.dw_part == nullptr) return;
     if constexpr (RING) cp_async_wait<0>();
     __syncthreads();
-    // the row groups' sums through the ring's memory, one group after the other
-    float *acc = reinterpret_cast<float *>(ring), *out = a.dw_part + (size_t)blockIdx.x * a.d;
-#pragma unroll 1
-    for (int g = 0; g < kGroups; ++g) {
-        if (group == g) {
+    float *out = a.dw_part + (size_t)blockIdx.x * a.d;
+    if constexpr (kGroups == 1) {
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int v = lane + TPR * i;
-                if (v >= nv) continue;
-                float t[8];
+        for (int i = 0; i < VPT; ++i)
+            if (lane + TPR * i < nv) store_pairs(out + 8 * (lane + TPR * i), dw[i]);
+    } else {
+        // the row groups' sums meet in the ring's memory and are added in group order
+        float *acc = reinterpret_cast<float *>(ring);
+        constexpr int kRow = TPR * VPT * 8;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) unpack2(dw[i][j], t[2 * j], t[2 * j + 1]);
-                if (g > 0)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) t[j] += acc[8 * v + j];
-                store_vec(g + 1 < kGroups ? acc + 8 * v : out + 8 * v, t);
-            }
-        }
+        for (int i = 0; i < VPT; ++i) store_pairs(acc + group * kRow + 8 * (lane + TPR * i), dw[i]);
         __syncthreads();
+        for (int c = 4 * threadIdx.x; c < a.d; c += 4 * kBwdThreads) {
+            float4 t = *reinterpret_cast<const float4 *>(acc + c);
+#pragma unroll
+            for (int g = 1; g < kGroups; ++g) {
+                const float4 f = *reinterpret_cast<const float4 *>(acc + g * kRow + c);
+                t.x += f.x; t.y += f.y; t.z += f.z; t.w += f.w;
+            }
+            *reinterpret_cast<float4 *>(out + c) = t;
+        }
     }
 }
 
@@ -469,24 +485,28 @@ int bwd_blocks(int T, int d)
     return (int)(need < 148 ? need : 148);
 }
 
-template <typename T, int TPR, int VPT>
-cudaError_t launch_bwd(const NormBwdArgs &a, int blocks, cudaStream_t s)
+template <typename T, int TPR, int VPT, bool WEIGHT, bool SUM>
+cudaError_t launch_bwd_form(const NormBwdArgs &a, int blocks, cudaStream_t s)
 {
-    if constexpr (TPR == 1024) {
-        return launch_overlapped(add_rms_norm_bwd_kernel<T, TPR, VPT, false>, blocks, 1024, 0, s, a);
-    }
-    auto kern = add_rms_norm_bwd_kernel<T, TPR, VPT, TPR != 1024>;
-    constexpr int smem = kBwdThreads * kSlots * 3 * VPT * 8 * (int)sizeof(T);
+    auto kern = add_rms_norm_bwd_kernel<T, TPR, VPT, WEIGHT, SUM>;
+    constexpr int threads = TPR == 1024 ? 1024 : kBwdThreads;
+    constexpr int smem = TPR == 1024 ? 0 : kBwdThreads * kSlots * 3 * VPT * 8 * (int)sizeof(T);
     static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev > 63 || !((attr_done >> dev) & 1ull)) {
+    if (smem > 0 && (dev > 63 || !((attr_done >> dev) & 1ull))) {
         e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
         if (dev <= 63) attr_done |= 1ull << dev;
     }
-    return launch_overlapped(kern, blocks, kBwdThreads, smem, s, a);
+    return launch_overlapped(kern, blocks, threads, smem, s, a);
+}
+template <typename T, int TPR, int VPT>
+cudaError_t launch_bwd(const NormBwdArgs &a, int blocks, cudaStream_t s)
+{
+    if (a.weight) return a.dsum ? launch_bwd_form<T, TPR, VPT, true, true>(a, blocks, s) : launch_bwd_form<T, TPR, VPT, true, false>(a, blocks, s);
+    return a.dsum ? launch_bwd_form<T, TPR, VPT, false, true>(a, blocks, s) : launch_bwd_form<T, TPR, VPT, false, false>(a, blocks, s);
 }
 template <typename T>
 cudaError_t dispatch_bwd(const NormBwdArgs &a, int blocks, cudaStream_t s)
