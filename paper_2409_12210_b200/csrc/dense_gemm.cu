@@ -133,11 +133,8 @@ struct Staging {
         return base + which * kEpiBufBytes;
     }
 };
-__device__ __forceinline__ void tile_out(Staging &st, unsigned char *buf, int lane, const CUtensorMap *map, int x, int y,
-                                         const uint4 (&w)[4])
+__device__ __forceinline__ void tile_send(unsigned char *buf, int lane, const CUtensorMap *map, int x, int y)
 {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4 *>(buf + epi_piece(lane, q)) = w[q];
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if (lane == 0) {
@@ -145,6 +142,12 @@ __device__ __forceinline__ void tile_out(Staging &st, unsigned char *buf, int la
                      ::"l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(buf)), "r"(x), "r"(y) : "memory");
         asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
+}
+__device__ __forceinline__ void tile_out(unsigned char *buf, int lane, const CUtensorMap *map, int x, int y, const uint4 (&w)[4])
+{
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4 *>(buf + epi_piece(lane, q)) = w[q];
+    tile_send(buf, lane, map, x, y);
 }
 
 // 32 rows x 64 bytes from global memory, four neighbouring lanes the 64 bytes of a row; `at` points at (first row of the
@@ -284,7 +287,7 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
         chunk_load<kLoadBias>(in, q, lin, r0, next, lane);
         if (lin.z) {
             pack_bf16(v, w);
-            tile_out(stg, stg.take(lane), lane, o1, c0, r0, w);
+            tile_out(stg.take(lane), lane, o1, c0, r0, w);
         }
         activate_all(v, lin.act);
         unsigned char *buf = stg.take(lane);
@@ -302,10 +305,10 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
                 }
         }
         pack_bf16(v, w);
-        tile_out(stg, buf, lane, o0, c0, r0, w);
+        tile_out(buf, lane, o0, c0, r0, w);
     } else if constexpr (MODE == DensePlain) {
         pack_bf16(v, w);
-        tile_out(stg, stg.take(lane), lane, o0, c0, r0, w);
+        tile_out(stg.take(lane), lane, o0, c0, r0, w);
     } else if constexpr (MODE == DenseGram || MODE == DensePoly) {
         unsigned char *buf = stg.take(lane);
         if constexpr (MODE == DensePoly) {
@@ -325,13 +328,14 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
             for (int i = 0; i < 32; ++i) v[i] *= q.alpha;
         }
         pack_f16(v, w);
-        tile_out(stg, buf, lane, o0, c0, r0, w);
-        if (mirror && lane < rows) {
-            // the transposed block: a lane's values lie one output row apart, a warp's lanes side by side
-            __half *t = (__half *)q.out0 + (long long)c0 * q.ld_out + r0 + lane;
+        tile_out(buf, lane, o0, c0, r0, w);
+        if (mirror) {
+            // the transposed block goes out the same way: a lane's values go down a column of the staging buffer
+            buf = stg.take(lane);
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-                if (i < cols) t[(long long)i * q.ld_out] = __float2half_rn(v[i]);
+                *reinterpret_cast<__half *>(buf + epi_piece(i, lane >> 3) + (lane & 7) * 2) = __float2half_rn(v[i]);
+            tile_send(buf, lane, o0, r0, c0);
         }
     } else {
         unsigned char *buf = stg.take(lane);
@@ -360,7 +364,7 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
             for (int i = 0; i < 32; ++i) v[i] *= q.scale;
             pack_bf16(v, w);
             if (q.flags & kDenseTmaOut) {
-                tile_out(stg, buf, lane, o0, c0, r0, w);
+                tile_out(buf, lane, o0, c0, r0, w);
             } else {
                 // rows that TMA cannot write (any alignment): a warp writes one row after the other, a column a lane
 #pragma unroll
@@ -375,7 +379,7 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
             }
         } else {
             pack_f16(v, w);
-            tile_out(stg, buf, lane, o0, c0, r0, w);
+            tile_out(buf, lane, o0, c0, r0, w);
 #pragma unroll
             for (int p = 0; p < 4; ++p)
 #pragma unroll
@@ -385,7 +389,7 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
                     v[8 * p + 2 * i + 1] -= f.y;
                 }
             pack_f16(v, w);
-            tile_out(stg, stg.take(lane), lane, o1, c0, r0, w);
+            tile_out(stg.take(lane), lane, o1, c0, r0, w);
         }
     }
 }

@@ -25,7 +25,7 @@ namespace modse {
 namespace {
 
 constexpr int kGroup = kDenseMaxProblems;     // matrices of one launch
-constexpr int kNormParts = 64;                // partial sums of squares of a matrix
+constexpr int kNormParts = 128;               // partial sums of squares of a matrix
 constexpr float kScaleX = kOrthScaleX, kScaleA = kOrthScaleA, kScaleB = kOrthScaleB;
 constexpr double kMaxSigma = 7.5, kMaxB = 60.0;     // 7.5 * 2^12 and 60 * 2^10 are below fp16's 65504
 
@@ -87,13 +87,36 @@ __global__ void __launch_bounds__(256) square_sums_kernel(const __grid_constant_
     allow_next_kernel();
     if (a.head && blockIdx.x == 0 && blockIdx.y == 0)      // status word and counters of the products that follow
         for (int i = threadIdx.x; i < (int)(kDenseZeroBytes / 4); i += 256) a.head[i] = 0;
-    double acc = 0.0;       // squares of fp32 numbers overflow and underflow fp32 long before the numbers do
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)kNormParts * 256) {
-        const int r = (int)(i / vecs), c = 8 * (int)(i - (long long)r * vecs);
-        float f[8];
-        load8((const T *)m.g + r * m.ld + c, wide && c + 8 <= m.cols, m.cols - c, f);
+    // Squares of fp32 numbers leave fp32's range long before the numbers do: eight are summed in fp32 where the sum is well
+    // inside it (what underflows beside it does not count), in fp64 otherwise, and all sums are fp64.
+    double acc = 0.0;
+    constexpr int kAt = 4;                    // vectors in flight
+    const long long step = (long long)gridDim.x * 256;
+    for (long long i0 = (long long)blockIdx.x * 256 + threadIdx.x; i0 < total; i0 += kAt * step) {
+        float f[kAt][8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc = fma((double)f[j], (double)f[j], acc);
+        for (int k = 0; k < kAt; ++k) {
+            const long long i = i0 + k * step;
+            if (i < total) {
+                const int r = (int)(i / vecs), c = 8 * (int)(i - (long long)r * vecs);
+                load8((const T *)m.g + r * m.ld + c, wide && c + 8 <= m.cols, m.cols - c, f[k]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[k][j] = 0.f;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAt; ++k) {
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s = fmaf(f[k][j], f[k][j], s);
+            if (s >= 1e-30f && s <= 1e30f) {
+                acc += (double)s;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc = fma((double)f[k][j], (double)f[k][j], acc);
+            }
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, o);
@@ -116,7 +139,9 @@ __global__ void __launch_bounds__(256) normalise_kernel(const __grid_constant__ 
     allow_next_kernel();
     if (threadIdx.x < 32) {
         const double *p = a.parts + blockIdx.y * kNormParts;
-        double t = p[threadIdx.x] + p[threadIdx.x + 32];
+        double t = 0.0;
+#pragma unroll
+        for (int i = 0; i < kNormParts / 32; ++i) t += p[threadIdx.x + 32 * i];
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
         if (threadIdx.x == 0) inv_sh = (float)((double)kScaleX / (sqrt(t) + (double)a.eps));
