@@ -1,16 +1,21 @@
 // Dense products on Blackwell tensor cores: a persistent kernel in which a pair of CTAs on neighbouring SMs computes
-// 256 x 256 (or 256 x 128) output tiles with tcgen05.mma.cta_group::2.
+// output tiles with tcgen05.mma.cta_group::2 (M = 256, up to 256 columns); operands are read K-major or MN-major straight
+// from where they lie.  Each CTA of a pair stages its own rows of the row operand and half of the column operand by TMA.
 //
-// Each CTA of a pair stages its own 128 rows of the row operand and half of the column operand by TMA (six stages of
-// 32 KB) and holds the accumulator rows of its half in tensor memory; two accumulators fit, so the epilogue of one
-// tile overlaps the main loop of the next.  Operands are read K-major or MN-major straight from where they lie.
-// What bounds the main loop is the rate at which shared memory fills from L2 (32 KB a k-block of 128 bytes against 512
-// clocks of MMA), as for the layer's grouped products; a 128-column tile is for outputs with too few tiles to fill the GPU.
+// Two tile shapes, chosen by dense_plan:
+//   512 x 256  each CTA holds two 128-row halves that share the column operand: 48 KB of shared memory to fill a k-block
+//              of 1024 MMA clocks.  What bounds the smaller tile is that fill rate (32 KB in 512 clocks against about 56
+//              bytes a clock and SM from L2), so this one runs the tensor cores faster; but both accumulators (all of
+//              tensor memory) belong to one tile.  Its epilogue is hidden in part: the halves are drained one after
+//              the other, and the next tile's first k-blocks are multiplied into the half that is free already.
+//   256 x 256 / 256 x 128  one 128-row half a CTA; two accumulators in flight, the epilogue of one tile overlaps the
+//              main loop of the next.  For outputs with too few tiles to fill the GPU.
 //
-// Tail: the tiles left over after the last full round over the CTA pairs would leave most pairs idle for a whole
-// tile.  They are cut along the contraction instead, into as many pieces as there are pairs for them; every piece
-// writes its fp32 accumulator to the workspace, and the epilogue warp that arrives last at a 32-row strip adds the
-// pieces of that strip in order (so the sum does not depend on who was last) and runs the epilogue on it.
+// Tail.  The tiles left over after the last full round over the CTA pairs would leave most pairs idle for a whole tile.
+// Of the tall shape they are handed out as their 256-row halves where those still fit one round.  Of the other they are
+// cut along the contraction; every piece writes its fp32 accumulator to the workspace, and the epilogue warp that
+// arrives last at a 32-row strip adds the pieces of that strip in order (so the sum does not depend on who was last)
+// and runs the epilogue on it.
 //
 // Every wait is bounded; one that expires records kDevTimeout in the status word and the CTAs drain and leave.
 #include <cuda_fp16.h>
@@ -26,9 +31,13 @@
 namespace modse {
 namespace {
 
-constexpr int kDenseStages = 6;
-constexpr int kDenseStageBytes = 32768;          // 16 KB of rows, up to 16 KB of columns
-constexpr uint32_t kDenseRows = 16384;           // a CTA's 128 rows of 128 bytes
+constexpr uint32_t kDenseRows = 16384;           // 128 rows of 128 bytes
+constexpr int kDenseMaxStages = 6;
+template <bool TALL> struct DenseShape {
+    static constexpr int kStages = TALL ? 4 : 6;
+    static constexpr int kStageBytes = TALL ? 49152 : 32768;      // one or two times 16 KB of rows, up to 16 KB of columns
+    static constexpr int kTileRows = TALL ? 512 : 256;
+};
 constexpr int kDenseEpiWarps = 8;
 constexpr int kDenseFirstEpi = 4;                // warps 0-1: TMA, MMA; 2-3 idle so that the epilogue starts on a warpgroup
 constexpr int kDenseThreads = 32 * (kDenseFirstEpi + kDenseEpiWarps);
@@ -37,19 +46,19 @@ constexpr int kDenseTmemCols = 512;
 constexpr int kDenseGroupRows = 8;               // row tiles whose column tiles are walked before the next group's
 
 struct DenseTail {
-    unsigned long long full[kDenseStages], empty[kDenseStages], tmem_full[2], tmem_empty[2];
+    unsigned long long full[kDenseMaxStages], empty[kDenseMaxStages], tmem_full[2], tmem_empty[2];
     unsigned int tmem_base;
     int abort_flag;
 };
 constexpr int kDenseEpiBytes = 2 * kEpiBufBytes;    // two staging buffers an epilogue warp
-constexpr size_t kDenseSmem = 1024 + (size_t)kDenseStages * kDenseStageBytes + kDenseEpiWarps * kDenseEpiBytes + sizeof(DenseTail);
+constexpr size_t kDenseSmem = 1024 + (size_t)196608 + kDenseEpiWarps * kDenseEpiBytes + sizeof(DenseTail);
 static_assert(kDenseSmem <= 232448, "shared memory per CTA");
 
 template <int P> struct DenseParams {
     CUtensorMap a[P], b[P], o0[P], o1[P];     // operands; outputs as boxes of 32 rows x 64 bytes
     DenseProblem prob[P];
     LinearEpilogue lin;
-    int n_prob, tiles, full_tiles, splits, items;   // tiles [0, full_tiles) are whole, the others cut into `splits` pieces
+    int n_prob, full_tiles, splits, items;   // tiles [0, full_tiles) are whole, the others cut into `splits` pieces
     int *status, *counters;
     float *partial;
     unsigned long long wait_limit_ns;
@@ -59,9 +68,10 @@ template <int P> struct DenseParams {
 
 struct DenseTile {
     int p, m0, n0, kb0, kb1;
-    int tail;        // index among the cut tiles, -1: a whole tile
+    int tail;        // index among the tiles cut along the contraction, -1: a whole tile
     int split;
-    bool mirror;     // symmetric output: also write the transposed tile
+    bool two;        // the second 256-row half is computed too (tall tiles)
+    bool skip;       // a half that lies outside the output
 };
 
 // The round-th item of a pair, -1: none.  The items of several products are sorted by decreasing length; every other round
@@ -74,39 +84,50 @@ __device__ __forceinline__ int dense_item(int round, int who, int n, int items)
     return item < items ? item : -1;
 }
 
-template <int TN, int P>
+template <int TN, bool TALL, int P>
 __device__ __forceinline__ DenseTile dense_decode(const DenseParams<P> &prm, int item, int &cursor)
 {
     DenseTile t;
-    int tile = item;
+    int tile = item, half = -1;
     t.tail = -1;
     t.split = 0;
-    if (item >= prm.full_tiles) {
-        const int r = item - prm.full_tiles;
-        t.tail = r / prm.splits;
-        t.split = r - t.tail * prm.splits;
-        tile = prm.full_tiles + t.tail;
-        if (prm.splits == 1) t.tail = -1;
+    if (item >= prm.full_tiles && prm.splits > 1) {
+        const int r = item - prm.full_tiles, c = r / prm.splits;
+        tile = prm.full_tiles + c;
+        if constexpr (TALL) {
+            half = r - c * prm.splits;
+        } else {
+            t.tail = c;
+            t.split = r - c * prm.splits;
+        }
     }
     if constexpr (P > 1)
         while (cursor + 1 < prm.n_prob && tile >= prm.prob[cursor + 1].tile0) ++cursor;
     t.p = cursor;
     const DenseProblem &q = prm.prob[cursor];
+    constexpr int kUnits = TALL ? 2 : 1;         // 256-row units of a tile
     int local = tile - q.tile0, mb, nb;
-    t.mirror = false;
+    bool below = false;                          // symmetric: the second half lies below the diagonal
     if (q.flags & kDenseSym) {
-        mb = 0;                              // row by row of the upper triangle (square tiles)
-        while (local >= q.nt - mb) { local -= q.nt - mb; ++mb; }
-        nb = mb + local;
-        t.mirror = nb > mb;
+        mb = 0;                                  // row by row of the upper triangle, in units of 256
+        while (local >= q.nt - kUnits * mb) { local -= q.nt - kUnits * mb; ++mb; }
+        nb = kUnits * mb + local;
+        below = nb < kUnits * mb + kUnits - 1;
     } else {
         const int per = kDenseGroupRows * q.nt, g = local / per, rem = local - g * per;
         const int rows = min(kDenseGroupRows, q.mt - g * kDenseGroupRows);
         nb = rem / rows;
         mb = g * kDenseGroupRows + rem - nb * rows;
     }
-    t.m0 = mb * 256;
+    t.m0 = mb * DenseShape<TALL>::kTileRows;
     t.n0 = nb * TN;
+    t.two = TALL && !below && t.m0 + 256 < q.M;
+    t.skip = false;
+    if (half >= 0) {
+        t.skip = half == 1 && !t.two;
+        t.two = false;
+        t.m0 += 256 * half;
+    }
     t.kb0 = 0;
     t.kb1 = q.nk;
     if (t.tail >= 0) {
@@ -225,11 +246,10 @@ __device__ __forceinline__ void activate_all(float (&v)[32], int act)
 // accumulator is waited for, the next one's as soon as the registers of the present one are free.
 template <int MODE, bool F8> struct ChunkInputs {
     uint4 raw[MODE == DensePlain || MODE == DenseGram ? 1 : 4];      // residual, or the first input
-    uint4 raw2[MODE == DenseStep ? 4 : 1];
     uint4 bias[MODE == DenseLinear ? 4 : 1];
     float sx;
 };
-enum : int { kLoadFirst = 1, kLoadSecond = 2, kLoadBias = 4, kLoadAll = 7 };
+enum : int { kLoadFirst = 1, kLoadBias = 2, kLoadAll = 3 };
 template <int WHAT, int MODE, bool F8>
 __device__ __forceinline__ void chunk_load(ChunkInputs<MODE, F8> &in, const DenseProblem &q, const LinearEpilogue &lin, int r0,
                                            int c0, int lane)
@@ -251,8 +271,6 @@ __device__ __forceinline__ void chunk_load(ChunkInputs<MODE, F8> &in, const Dens
         const long long at = (long long)r0 * q.ld_in + c0;
         if constexpr ((WHAT & kLoadFirst) != 0)
             rows_load(lane, (const unsigned char *)((const __half *)q.in0 + at), 2 * q.ld_in, rows, pieces, in.raw);
-        if constexpr ((WHAT & kLoadSecond) != 0)
-            rows_load(lane, (const unsigned char *)((const __half *)q.in1 + at), 2 * q.ld_in, rows, pieces, in.raw2);
     }
 }
 
@@ -260,7 +278,7 @@ __device__ __forceinline__ void chunk_load(ChunkInputs<MODE, F8> &in, const Dens
 // lane's row.
 template <int MODE, bool F8>
 __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const DenseProblem &q, const LinearEpilogue &lin,
-                                             const CUtensorMap *o0, const CUtensorMap *o1, bool mirror, int r0, int c0, int next, int lane,
+                                             const CUtensorMap *o0, const CUtensorMap *o1, int r0, int c0, int next, int lane,
                                              Staging &stg, float (&v)[32])
 {
     const int rows = min(32, q.M - r0), cols = min(32, q.N - c0);
@@ -323,14 +341,18 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
                     v[8 * p + 2 * i] = fmaf(q.beta, f.x, q.alpha * v[8 * p + 2 * i]);
                     v[8 * p + 2 * i + 1] = fmaf(q.beta, f.y, q.alpha * v[8 * p + 2 * i + 1]);
                 }
+            if (c0 == r0) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] += i == lane ? q.scale : 0.f;
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] *= q.alpha;
         }
         pack_f16(v, w);
         tile_out(buf, lane, o0, c0, r0, w);
-        if (mirror) {
-            // the transposed block goes out the same way: a lane's values go down a column of the staging buffer
+        if ((c0 >> 8) > (r0 >> 8)) {
+            // off the diagonal (in units of 256) the transposed block goes out the same way: a lane's values go down a column of the staging buffer
             buf = stg.take(lane);
 #pragma unroll
             for (int i = 0; i < 32; ++i)
@@ -343,22 +365,13 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
         rows_hand(buf, lane, in.raw, own);
         chunk_load<kLoadFirst>(in, q, lin, r0, next, lane);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= q.alpha;
+        for (int p = 0; p < 4; ++p)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            if (k == 1) {
-                rows_hand(buf, lane, in.raw2, own);
-                chunk_load<kLoadSecond>(in, q, lin, r0, next, lane);
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = from_f16x2(word_of(own[p], i));
+                v[8 * p + 2 * i] = fmaf(q.beta, f.x, q.alpha * v[8 * p + 2 * i]);
+                v[8 * p + 2 * i + 1] = fmaf(q.beta, f.y, q.alpha * v[8 * p + 2 * i + 1]);
             }
-#pragma unroll
-            for (int p = 0; p < 4; ++p)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 f = from_f16x2(word_of(own[p], i));
-                    v[8 * p + 2 * i] = fmaf(q.beta, f.x, v[8 * p + 2 * i]);
-                    v[8 * p + 2 * i + 1] = fmaf(q.beta, f.y, v[8 * p + 2 * i + 1]);
-                }
-        }
         if (q.flags & kDenseLast) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] *= q.scale;
@@ -413,16 +426,18 @@ __device__ __forceinline__ uint32_t dense_idesc(bool a_mn, bool b_mn, int n)
            ((uint32_t)(n >> 3) << 17) | (16u << 24);
 }
 
-template <int MODE, int TYPE, int TN, int P>
+template <int MODE, int TYPE, int TN, bool TALL, int P>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kDenseThreads, 1)
 dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
 {
+    using Sh = DenseShape<TALL>;
+    constexpr int kStages = Sh::kStages;
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t pad = ((raw + 1023u) & ~1023u) - raw;
     unsigned char *smem = smem_raw + pad;
     const uint32_t stage_base = raw + pad;
-    unsigned char *epi_bufs = smem + (size_t)kDenseStages * kDenseStageBytes;
+    unsigned char *epi_bufs = smem + (size_t)kStages * Sh::kStageBytes;
     DenseTail *st = reinterpret_cast<DenseTail *>(epi_bufs + kDenseEpiWarps * kDenseEpiBytes);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -430,10 +445,14 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
     const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
     constexpr int kElems = TYPE == DenseE4m3 ? 128 : 64;       // elements in 128 bytes
     constexpr int kHalf = TN / 2;                              // column-operand rows staged by each CTA
-    constexpr uint32_t kTx = 2u * (kDenseRows + kHalf * 128u); // bytes of both CTAs a stage
+    constexpr uint32_t kColsAt = TALL ? 2 * kDenseRows : kDenseRows;      // column operand inside a stage
 
     if (tid == 0) {
-        for (int s = 0; s < kDenseStages; ++s) {
+        for (int i = 0; i < min(prm.n_prob, 4); ++i) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&prm.a[i])) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&prm.b[i])) : "memory");
+        }
+        for (int s = 0; s < kStages; ++s) {
             mbar_init(smem_u32(&st->full[s]), 1);
             mbar_init(smem_u32(&st->empty[s]), 1);
         }
@@ -442,10 +461,6 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
             mbar_init(smem_u32(&st->tmem_empty[a]), 2 * kDenseEpiWarps);
         }
         st->abort_flag = 0;
-        for (int i = 0; i < min(prm.n_prob, 4); ++i) {
-            asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&prm.a[i])) : "memory");
-            asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&prm.b[i])) : "memory");
-        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -472,42 +487,48 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
             uint32_t phase = 0;
             long long issued = 0;
             bool ok = true;
-            for (int it = 0; ok; ++it) {
-                const int item = dense_item<P>(it, cluster_id, n_clusters, prm.items);
+            for (int round = 0; ok; ++round) {
+                const int item = dense_item<P>(round, cluster_id, n_clusters, prm.items);
                 if (item < 0) break;
-                const DenseTile t = dense_decode<TN, P>(prm, item, cursor);
+                const DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
+                if (t.skip) continue;
                 const int flags = prm.prob[t.p].flags;
                 const CUtensorMap *am = &prm.a[t.p], *bm = &prm.b[t.p];
-                const int ar = t.m0 + rank * 128, br = t.n0 + rank * kHalf;
+                const int ar = t.m0 + rank * 128, br = t.n0 + rank * kHalf, halves = t.two ? 2 : 1;
+                const uint32_t bytes = 2u * (halves * kDenseRows + kHalf * 128u);      // of both CTAs
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if (!mbar_wait(smem_u32(&st->empty[stage]), phase ^ 1u, wc)) { ok = false; break; }
                     const uint32_t bar = map_to_cta(smem_u32(&st->full[stage]), 0);
-                    if (rank == 0) mbar_arrive_expect_tx(smem_u32(&st->full[stage]), kTx);
-                    const uint32_t dst = stage_base + stage * kDenseStageBytes;
-                    if (flags & kDenseAMn) {
-                        tma_load_2d_pair(dst, am, bar, ar, kb * 64);
-                        tma_load_2d_pair(dst + kBoxBytes, am, bar, ar + 64, kb * 64);
-                    } else {
-                        tma_load_2d_pair(dst, am, bar, kb * kElems, ar);
+                    if (rank == 0) mbar_arrive_expect_tx(smem_u32(&st->full[stage]), bytes);
+                    const uint32_t dst = stage_base + stage * Sh::kStageBytes;
+                    for (int h = 0; h < halves; ++h) {
+                        const uint32_t to = dst + h * kDenseRows;
+                        const int row = ar + 256 * h;
+                        if (flags & kDenseAMn) {
+                            tma_load_2d_pair(to, am, bar, row, kb * 64);
+                            tma_load_2d_pair(to + kBoxBytes, am, bar, row + 64, kb * 64);
+                        } else {
+                            tma_load_2d_pair(to, am, bar, kb * kElems, row);
+                        }
                     }
                     if (flags & kDenseBMn) {
 #pragma unroll
                         for (int i = 0; i < kHalf / 64; ++i)
-                            tma_load_2d_pair(dst + kDenseRows + i * kBoxBytes, bm, bar, br + 64 * i, kb * 64);
+                            tma_load_2d_pair(dst + kColsAt + i * kBoxBytes, bm, bar, br + 64 * i, kb * 64);
                     } else {
-                        tma_load_2d_pair(dst + kDenseRows, bm, bar, kb * kElems, br);
+                        tma_load_2d_pair(dst + kColsAt, bm, bar, kb * kElems, br);
                     }
                     ++issued;
-                    if (++stage == kDenseStages) { stage = 0; phase ^= 1u; }
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
                 }
             }
             if (!ok && rank == 0) {
                 // the copies of both CTAs complete on the leader's barriers: it lets those in flight land
-                const int n = issued < kDenseStages ? (int)issued : kDenseStages;
+                const int n = issued < kStages ? (int)issued : kStages;
                 for (int i = 1; i <= n; ++i) {
                     int s2 = stage - i;
                     uint32_t ph = phase;
-                    if (s2 < 0) { s2 += kDenseStages; ph ^= 1u; }
+                    if (s2 < 0) { s2 += kStages; ph ^= 1u; }
                     const unsigned long long tb = global_ns();
                     while (!mbar_try_wait(smem_u32(&st->full[s2]), ph) && global_ns() - tb < prm.wait_limit_ns) {}
                 }
@@ -516,39 +537,87 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
     } else if (warp == 1) {
         // ===================== MMA issuer (leader only) =====================
         if (lane == 0 && rank == 0) {
-            int stage = 0, cursor = 0;
-            uint32_t phase = 0;
+            int stage = 0, cursor = 0, it = 0;
+            uint32_t phase = 0, used0 = 0, used1 = 0;      // how often each accumulator has been handed to the epilogue
             bool ok = true;
-            for (int it = 0; ok; ++it) {
-                const int item = dense_item<P>(it, cluster_id, n_clusters, prm.items);
+            for (int round = 0; ok; ++round) {
+                const int item = dense_item<P>(round, cluster_id, n_clusters, prm.items);
                 if (item < 0) break;
-                const DenseTile t = dense_decode<TN, P>(prm, item, cursor);
+                const DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
+                if (t.skip) continue;
                 const int flags = prm.prob[t.p].flags;
                 const bool a_mn = (flags & kDenseAMn) != 0, b_mn = (flags & kDenseBMn) != 0;
                 const uint32_t a_step = a_mn ? (2048u >> 4) : (32u >> 4), b_step = b_mn ? (2048u >> 4) : (32u >> 4);
                 const uint32_t idesc = dense_idesc<TYPE>(a_mn, b_mn, TN);
-                const int acc = it & 1;
-                if (!mbar_wait(smem_u32(&st->tmem_empty[acc]), ((uint32_t)(it >> 1) & 1u) ^ 1u, wc)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t tacc = tmem_base + (uint32_t)(acc * kDenseAccCols);
-                for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                    if (!mbar_wait(smem_u32(&st->full[stage]), phase, wc)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t addr = stage_base + stage * kDenseStageBytes;
-                    const uint64_t adesc = make_desc(addr, a_mn), bdesc = make_desc(addr + kDenseRows, b_mn);
+                // the four products of half h and the stage at `s` into accumulator columns `to`
+                auto multiply = [&](int s, int h, uint32_t to, bool fresh) {
+                    const uint32_t addr = stage_base + s * Sh::kStageBytes;
+                    const uint64_t adesc = make_desc(addr + h * kDenseRows, a_mn), bdesc = make_desc(addr + kColsAt, b_mn);
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks) {
-                        const uint32_t more = (kb > t.kb0 || ks > 0) ? 1u : 0u;
+                        const uint32_t more = (!fresh || ks > 0) ? 1u : 0u;
                         if constexpr (TYPE == DenseE4m3)
-                            umma_f8_pair(tacc, adesc + (uint64_t)(ks * a_step), bdesc + (uint64_t)(ks * b_step), idesc, more);
+                            umma_f8_pair(to, adesc + (uint64_t)(ks * a_step), bdesc + (uint64_t)(ks * b_step), idesc, more);
                         else
-                            umma_bf16_pair(tacc, adesc + (uint64_t)(ks * a_step), bdesc + (uint64_t)(ks * b_step), idesc, more);
+                            umma_bf16_pair(to, adesc + (uint64_t)(ks * a_step), bdesc + (uint64_t)(ks * b_step), idesc, more);
                     }
-                    umma_commit_pair(smem_u32(&st->empty[stage]));
-                    if (++stage == kDenseStages) { stage = 0; phase ^= 1u; }
+                };
+                if constexpr (!TALL) {
+                    const int acc = it++ & 1;
+                    uint32_t &used = acc ? used1 : used0;
+                    if (!mbar_wait(smem_u32(&st->tmem_empty[acc]), (used & 1u) ^ 1u, wc)) { ok = false; break; }
+                    ++used;
+                    tc_fence_after();
+                    for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                        if (!mbar_wait(smem_u32(&st->full[stage]), phase, wc)) { ok = false; break; }
+                        tc_fence_after();
+                        multiply(stage, 0, tmem_base + (uint32_t)(acc * kDenseAccCols), kb == t.kb0);
+                        umma_commit_pair(smem_u32(&st->empty[stage]));
+                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                    }
+                    if (!ok) break;
+                    umma_commit_pair(smem_u32(&st->tmem_full[acc]));
+                } else {
+                    if (!mbar_wait(smem_u32(&st->tmem_empty[0]), (used0 & 1u) ^ 1u, wc)) { ok = false; break; }
+                    ++used0;
+                    tc_fence_after();
+                    int kb = t.kb0;
+                    if (t.two) {
+                        // the first k-blocks into the first half while the second half's accumulator is still being
+                        // drained, then the same stages into the second half
+                        const int ahead = min(kStages, t.kb1 - t.kb0);
+                        int s = stage;
+                        uint32_t ph = phase;
+                        for (int i = 0; i < ahead; ++i) {
+                            if (!mbar_wait(smem_u32(&st->full[s]), ph, wc)) { ok = false; break; }
+                            tc_fence_after();
+                            multiply(s, 0, tmem_base, i == 0);
+                            if (++s == kStages) { s = 0; ph ^= 1u; }
+                        }
+                        if (!ok) break;
+                        if (t.kb0 + ahead == t.kb1) umma_commit_pair(smem_u32(&st->tmem_full[0]));
+                        if (!mbar_wait(smem_u32(&st->tmem_empty[1]), (used1 & 1u) ^ 1u, wc)) { ok = false; break; }
+                        ++used1;
+                        tc_fence_after();
+                        for (int i = 0; i < ahead; ++i) {
+                            multiply(stage, 1, tmem_base + kDenseAccCols, i == 0);
+                            umma_commit_pair(smem_u32(&st->empty[stage]));
+                            if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                        }
+                        kb += ahead;
+                    }
+                    for (; kb < t.kb1; ++kb) {
+                        if (!mbar_wait(smem_u32(&st->full[stage]), phase, wc)) { ok = false; break; }
+                        tc_fence_after();
+                        multiply(stage, 0, tmem_base, kb == t.kb0);
+                        if (kb + 1 == t.kb1) umma_commit_pair(smem_u32(&st->tmem_full[0]));
+                        if (t.two) multiply(stage, 1, tmem_base + kDenseAccCols, false);
+                        umma_commit_pair(smem_u32(&st->empty[stage]));
+                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                    }
+                    if (!ok) break;
+                    if (t.two) umma_commit_pair(smem_u32(&st->tmem_full[1]));
                 }
-                if (!ok) break;
-                umma_commit_pair(smem_u32(&st->tmem_full[acc]));
             }
         }
     } else if (warp < kDenseFirstEpi) {
@@ -571,77 +640,83 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
         const uint32_t leader_empty1 = map_to_cta(smem_u32(&st->tmem_empty[1]), 0);
         constexpr int kChunks = TN / 64;                    // 32-column chunks a warp owns
         constexpr bool kF8 = TYPE == DenseE4m3;
-        int cursor = 0;
-        for (int it = 0;; ++it) {
-            const int item = dense_item<P>(it, cluster_id, n_clusters, prm.items);
+        int cursor = 0, it = 0;
+        uint32_t used0 = 0, used1 = 0;                      // how often each accumulator has been drained
+        bool ok = true;
+        for (int round = 0; ok; ++round) {
+            const int item = dense_item<P>(round, cluster_id, n_clusters, prm.items);
             if (item < 0) break;
-            const DenseTile t = dense_decode<TN, P>(prm, item, cursor);
+            const DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
+            if (t.skip) continue;
             const DenseProblem &q = prm.prob[t.p];
             const CUtensorMap *o0 = &prm.o0[t.p], *o1 = &prm.o1[t.p];
-            const int acc = it & 1;
-            const int r0 = t.m0 + rank * 128 + quad * 32, c0 = t.n0 + cq * kHalf;
-            const bool any = r0 < q.M && c0 < q.N;
-            ChunkInputs<MODE, kF8> in;
-            if (any && t.tail < 0) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
-            if (!mbar_wait(smem_u32(&st->tmem_full[acc]), (uint32_t)(it >> 1) & 1u, wc)) break;
-            tc_fence_after();
-            const uint32_t tacc = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * kDenseAccCols + cq * kHalf);
-            // a cut tile's strip: 32 rows x kHalf columns, float4 j of all lanes side by side
-            float4 *strip = nullptr;
-            if (t.tail >= 0)
-                strip = reinterpret_cast<float4 *>(prm.partial) +
-                        ((size_t)(t.tail * prm.splits) * 16 + rank * 8 + cq * 4 + quad) * (32 * kHalf / 4) + lane;
-            constexpr size_t kPieceStride = (size_t)16 * (32 * kHalf / 4);
-            if (any) {
+            const int c0 = t.n0 + cq * kHalf, halves = t.two ? 2 : 1, first = TALL ? 0 : (it++ & 1);
 #pragma unroll 1
-                for (int c = 0; c < kChunks; ++c) {
-                    if (c0 + 32 * c >= q.N) break;
-                    uint32_t w[32];
-                    tmem_ld32(tacc + 32 * c, w);
-                    tmem_ld_wait();
-                    float v[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
-                    if (t.tail < 0) {
-                        chunk_finish(in, q, prm.lin, o0, o1, t.mirror, r0, c0 + 32 * c,
-                                     c + 1 < kChunks ? c0 + 32 * c + 32 : q.N, lane, stg, v);
-                    } else {
-                        float4 *dst = strip + (size_t)t.split * kPieceStride + (size_t)c * 256;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) __stcg(dst + 32 * j, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-                    }
-                }
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_remote(acc ? leader_empty1 : leader_empty0);
-            if (t.tail >= 0 && any) {
-                __threadfence();
-                __syncwarp();
-                int seen = 0;
-                if (lane == 0) seen = atomicAdd(prm.counters + t.tail * 16 + rank * 8 + cq * 4 + quad, 1);
-                seen = __shfl_sync(0xFFFFFFFFu, seen, 0);
-                if (seen == prm.splits - 1) {
-                    __threadfence();
-                    if (lane == 0) prm.counters[t.tail * 16 + rank * 8 + cq * 4 + quad] = 0;   // for the next launch
+            for (int h = 0; h < halves; ++h) {
+                const int acc = TALL ? h : first, r0 = t.m0 + 256 * h + rank * 128 + quad * 32;
+                const bool any = r0 < q.M && c0 < q.N;
+                ChunkInputs<MODE, kF8> in;
+                if (any && t.tail < 0) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
+                if (!mbar_wait(smem_u32(&st->tmem_full[acc]), (acc ? used1 : used0) & 1u, wc)) { ok = false; break; }
+                if (acc) ++used1; else ++used0;
+                tc_fence_after();
+                const uint32_t tacc = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * kDenseAccCols + cq * kHalf);
+                // a cut tile's strip: 32 rows x kHalf columns, float4 j of all lanes side by side
+                constexpr size_t kStrip = 32 * kHalf / 4, kPiece = 2 * kDenseEpiWarps * kStrip;
+                const int strip_id = rank * kDenseEpiWarps + cq * 4 + quad;
+                float4 *strip = nullptr;
+                if (t.tail >= 0)
+                    strip = reinterpret_cast<float4 *>(prm.partial) + (size_t)(t.tail * prm.splits) * kPiece + strip_id * kStrip + lane;
+                if (any) {
 #pragma unroll 1
                     for (int c = 0; c < kChunks; ++c) {
                         if (c0 + 32 * c >= q.N) break;
-                        if (c == 0) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
+                        uint32_t w[32];
+                        tmem_ld32(tacc + 32 * c, w);
+                        tmem_ld_wait();
                         float v[32];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = 0.f;
-#pragma unroll 1
-                        for (int s = 0; s < prm.splits; ++s) {
-                            const float4 *src = strip + (size_t)s * kPieceStride + (size_t)c * 256;
+                        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
+                        if (t.tail < 0) {
+                            chunk_finish(in, q, prm.lin, o0, o1, r0, c0 + 32 * c, c + 1 < kChunks ? c0 + 32 * c + 32 : q.N, lane, stg, v);
+                        } else {
+                            float4 *dst = strip + (size_t)t.split * kPiece + (size_t)c * 256;
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const float4 f = __ldcg(src + 32 * j);
-                                v[4 * j] += f.x; v[4 * j + 1] += f.y; v[4 * j + 2] += f.z; v[4 * j + 3] += f.w;
-                            }
+                            for (int j = 0; j < 8; ++j) __stcg(dst + 32 * j, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
                         }
-                        chunk_finish(in, q, prm.lin, o0, o1, t.mirror, r0, c0 + 32 * c,
-                                     c + 1 < kChunks ? c0 + 32 * c + 32 : q.N, lane, stg, v);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote(acc ? leader_empty1 : leader_empty0);
+                if (t.tail >= 0 && any) {
+                    __threadfence();
+                    __syncwarp();
+                    int seen = 0;
+                    int *counter = prm.counters + t.tail * 2 * kDenseEpiWarps + strip_id;
+                    if (lane == 0) seen = atomicAdd(counter, 1);
+                    seen = __shfl_sync(0xFFFFFFFFu, seen, 0);
+                    if (seen == prm.splits - 1) {
+                        __threadfence();
+                        if (lane == 0) *counter = 0;               // for the next launch
+                        chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
+#pragma unroll 1
+                        for (int c = 0; c < kChunks; ++c) {
+                            if (c0 + 32 * c >= q.N) break;
+                            float v[32];
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] = 0.f;
+#pragma unroll 1
+                            for (int s = 0; s < prm.splits; ++s) {
+                                const float4 *src = strip + (size_t)s * kPiece + (size_t)c * 256;
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    const float4 f = __ldcg(src + 32 * j);
+                                    v[4 * j] += f.x; v[4 * j + 1] += f.y; v[4 * j + 2] += f.z; v[4 * j + 3] += f.w;
+                                }
+                            }
+                            chunk_finish(in, q, prm.lin, o0, o1, r0, c0 + 32 * c, c + 1 < kChunks ? c0 + 32 * c + 32 : q.N, lane, stg, v);
+                        }
                     }
                 }
             }
@@ -688,44 +763,71 @@ bool encode_output(CUtensorMap *map, const void *base, long long rows, long long
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How a launch is cut: tile width, whole tiles, pieces of the rest.
-struct DensePlan { int tn, tiles, full, splits, items; };
+// How a launch is cut: tile shape, whole tiles, pieces of the rest.
+struct DensePlan {
+    bool tall;
+    int tn, tiles, full, splits, items;
+};
 
 int dense_nk(DenseType type, long long k) { return (int)((k + (type == DenseE4m3 ? 127 : 63)) / (type == DenseE4m3 ? 128 : 64)); }
 
-DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int n, int sms, size_t partial_capacity)
+long long dense_tiles(const DenseProblem &p, bool tall, int tn)
+{
+    const long long mt = (p.M + (tall ? 511 : 255)) / (tall ? 512 : 256), nt = (p.N + tn - 1) / tn;
+    if (!(p.flags & kDenseSym)) return mt * nt;
+    long long c = 0;
+    for (long long m = 0; m < mt; ++m) c += nt - (tall ? 2 : 1) * m;
+    return c;
+}
+
+DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int n, bool light, int sms, size_t partial_capacity)
 {
     const int pairs = std::max(1, sms / 2);
-    auto count = [&](int tn) {
+    auto count = [&](bool tall, int tn) {
         long long tiles = 0;
-        for (int i = 0; i < n; ++i) {
-            const long long mt = (items[i].p.M + 255) / 256, nt = (items[i].p.N + tn - 1) / tn;
-            tiles += (items[i].p.flags & kDenseSym) ? nt * (nt + 1) / 2 : mt * nt;
-        }
+        for (int i = 0; i < n; ++i) tiles += dense_tiles(items[i].p, tall, tn);
         return tiles;
     };
     DensePlan pl;
+    // Tall tiles where they fill the GPU at least once and the epilogue that shows is a light one (a conversion and a store;
+    // `light`) behind a long main loop.  A round of them takes about 1024 x 1.05 clocks a k-block and the epilogue, a round
+    // of 256-row tiles 585 a k-block.  Measured, tall against not: dx and dw of 16384 x 2048 -> 5632 504 against 580 us,
+    // the product alone 250 against 262, with K 5632 273 against 283; but 350 against 303 with bias, gelu and z, 293
+    // against 282 with a residual, 205 against 148 from 8-bit rows, 56 against 58 with 16 k-blocks.
+    const long long talls = count(true, 256), squares = count(false, 256);
+    const long long whole = talls / pairs, rest = talls % pairs;
+    const double tall_rounds = (double)whole + (rest == 0 ? 0.0 : 2 * rest <= pairs ? 0.57 : 1.0);
+    const double square_rounds = (double)((squares + pairs - 1) / pairs);
+    int least_nk = 1 << 30;
+    for (int i = 0; i < n; ++i) least_nk = std::min(least_nk, dense_nk(type, items[i].k));
+    pl.tall = light && least_nk >= 24 && talls >= pairs && tall_rounds * 1.13 <= square_rounds * 0.585;
+    if (pl.tall) {
+        pl.tn = 256;
+        pl.tiles = (int)talls;
+        pl.full = (int)(whole * pairs);
+        pl.splits = (rest > 0 && 2 * rest <= pairs) ? 2 : 1;
+        pl.items = pl.full + (int)rest * pl.splits;
+        return pl;
+    }
     // 256-column tiles unless the whole output has less than half a tile for each CTA pair: then 128-column tiles
     // (symmetric outputs have square tiles)
-    pl.tn = (mode != DenseGram && mode != DensePoly && count(256) * 2 <= pairs) ? 128 : 256;
-    pl.tiles = (int)count(pl.tn);
+    pl.tn = (mode != DenseGram && mode != DensePoly && squares * 2 <= pairs) ? 128 : 256;
+    pl.tiles = (int)count(false, pl.tn);
     pl.full = pl.tiles / pairs * pairs;
     const int left = pl.tiles - pl.full;
     pl.splits = 1;
     if (left > 0) {
-        int min_nk = 1 << 30;
-        for (int i = 0; i < n; ++i) min_nk = std::min(min_nk, dense_nk(type, items[i].k));
         // One round over the pairs, as many pieces as the workspace holds, at least 16 k-blocks each: joining them costs
         // about 4.5 us, twelve k-blocks' time (704 x 704, 300 tokens: 11.7 us in three pieces, 7.2 whole).
         const long long held = (long long)(partial_capacity / ((size_t)256 * pl.tn * 4));
-        const long long sp = std::min<long long>({std::min(pairs, kDenseMaxSplitItems) / left, min_nk / 16, 16, held / left});
+        const long long sp = std::min<long long>({std::min(pairs, kDenseMaxSplitItems) / left, least_nk / 16, 16, held / left});
         pl.splits = (int)std::max<long long>(1, sp);
     }
     pl.items = pl.full + left * pl.splits;
     return pl;
 }
 
-template <int MODE, int TYPE, int TN, int P>
+template <int MODE, int TYPE, int TN, bool TALL, int P>
 cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const LinearEpilogue *lin, const DenseColumnSum *sum, void *ws, int head, cudaStream_t s)
 {
     DenseParams<P> prm;
@@ -735,10 +837,10 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
         DenseProblem &q = prm.prob[i];
         q = it.p;
         q.nk = dense_nk((DenseType)TYPE, it.k);
-        q.mt = (q.M + 255) / 256;
+        q.mt = (q.M + DenseShape<TALL>::kTileRows - 1) / DenseShape<TALL>::kTileRows;
         q.nt = (q.N + TN - 1) / TN;
         q.tile0 = tiles;
-        tiles += (q.flags & kDenseSym) ? q.nt * (q.nt + 1) / 2 : q.mt * q.nt;
+        tiles += (int)dense_tiles(q, TALL, TN);
         if (!encode_operand(&prm.a[i], it.a, TYPE, (q.flags & kDenseAMn) ? 64 : 128) ||
             !encode_operand(&prm.b[i], it.b, TYPE, (q.flags & kDenseBMn) ? 64 : TN / 2))
             return cudaErrorInvalidValue;
@@ -762,7 +864,6 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
     const int pairs = std::max(1, device_sms() / 2);
     prm.lin = lin ? *lin : LinearEpilogue{};
     prm.n_prob = n;
-    prm.tiles = tiles;
     prm.full_tiles = pl.full;
     prm.splits = pl.splits;
     prm.items = pl.items;
@@ -773,7 +874,7 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
     prm.clear_status = head == kDenseHeadRaw;
     prm.sum = sum ? *sum : DenseColumnSum{};
 
-    auto kern = dense_gemm_pair<MODE, TYPE, TN, P>;
+    auto kern = dense_gemm_pair<MODE, TYPE, TN, TALL, P>;
     static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -783,7 +884,7 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
         if (e != cudaSuccess) return e;
         if (dev <= 63) attr_done |= 1ull << dev;
     }
-    if (head == kDenseHeadRaw && pl.splits > 1) {      // only cut tiles count arrivals
+    if (head == kDenseHeadRaw && !TALL && pl.splits > 1) {      // only cut tiles count arrivals
         e = cudaMemsetAsync(ws, 0, kDenseZeroBytes, s);
         if (e != cudaSuccess) return e;
     }
@@ -794,21 +895,21 @@ template <int MODE, int TYPE, int P>
 cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin, const DenseColumnSum *sum, void *ws, size_t cap, int head, cudaStream_t s)
 {
     if (n > P) return cudaErrorInvalidValue;
-    const DensePlan pl = dense_plan((DenseMode)MODE, (DenseType)TYPE, items, n, device_sms(), cap);
-    if constexpr (MODE == DenseGram || MODE == DensePoly) {
-        return launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, sum, ws, head, s);
-    } else {
-        return pl.tn == 128 ? launch_tn<MODE, TYPE, 128, P>(pl, items, n, lin, sum, ws, head, s)
-                            : launch_tn<MODE, TYPE, 256, P>(pl, items, n, lin, sum, ws, head, s);
-    }
+    const bool light = MODE == DensePlain || (MODE == DenseLinear && TYPE == DenseBf16 && !lin->residual && !lin->z && lin->act <= MODSE_ACT_RELU);
+    const DensePlan pl = dense_plan((DenseMode)MODE, (DenseType)TYPE, items, n, light, device_sms(), cap);
+    if constexpr (MODE == DensePlain || (MODE == DenseLinear && TYPE == DenseBf16))
+        if (pl.tall) return launch_tn<MODE, TYPE, 256, true, P>(pl, items, n, lin, sum, ws, head, s);
+    if constexpr (MODE != DenseGram && MODE != DensePoly)
+        if (pl.tn == 128) return launch_tn<MODE, TYPE, 128, false, P>(pl, items, n, lin, sum, ws, head, s);
+    return launch_tn<MODE, TYPE, 256, false, P>(pl, items, n, lin, sum, ws, head, s);
 }
 
 }  // namespace
 
 size_t dense_partial_bytes(DenseMode mode, DenseType type, const DenseItem *items, int n)
 {
-    const DensePlan pl = dense_plan(mode, type, items, n, kDenseSms, ~(size_t)0 >> 1);
-    return pl.splits > 1 ? (size_t)(pl.items - pl.full) * 256 * pl.tn * 4 : 0;
+    const DensePlan pl = dense_plan(mode, type, items, n, false, kDenseSms, ~(size_t)0 >> 1);
+    return !pl.tall && pl.splits > 1 ? (size_t)(pl.items - pl.full) * 256 * pl.tn * 4 : 0;
 }
 
 cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *list, int n, const LinearEpilogue *lin,

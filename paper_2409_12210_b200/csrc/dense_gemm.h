@@ -13,8 +13,8 @@ enum DenseMode : int {
     DenseLinear = 0,   // y = act(acc * sx * sw + bias) + residual, z beside it
     DensePlain = 1,    // out = acc (bf16)
     DenseGram = 2,     // out = alpha acc (fp16), symmetric
-    DensePoly = 3,     // out = alpha acc + beta in0 (fp16), symmetric
-    DenseStep = 4      // x = alpha acc + beta (hi + lo): hi, lo (fp16), or the final bf16 result
+    DensePoly = 3,     // out = alpha acc + beta in0 + scale I (fp16), symmetric
+    DenseStep = 4      // x = alpha acc + beta in0: its two fp16 halves, or the final bf16 result times scale
 };
 enum DenseType : int { DenseBf16 = 0, DenseF16 = 1, DenseE4m3 = 2 };
 enum : int {
@@ -32,7 +32,7 @@ struct DenseProblem {
     int tile0;               // this problem's first tile in the launch's list
     int flags;
     float alpha, beta, scale;
-    const void *in0, *in1;
+    const void *in0;
     void *out0, *out1;
     long long ld_in, ld_out; // elements
 };

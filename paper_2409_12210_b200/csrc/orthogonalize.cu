@@ -1,16 +1,17 @@
 // modse_orthogonalize: Newton-Schulz iteration on a set of matrices of diverse sizes.
 //
-//   X0 = G / (|G|_F + eps);  repeat: A = X X^T (the shorter side),  B = b A + c A^2,  X <- a X + B X;  update = scale X
+//   X0 = G / (|G|_F + eps);  repeat: A = X X^T (the shorter side),  B = a I + b A + c A^2,  X <- B X;  update = scale X
 //
 // Three grouped products an iteration over all matrices of a call (dense_gemm.cu): A and B are symmetric, so only tiles
 // on and above the diagonal are computed; a tall matrix is not transposed, its products read X along the other axis.
 //
 // Numbers.  The products read fp16 factors (11 bits, against 8 of bf16: the error of the result is an eighth) and
-// accumulate in fp32.  X itself is carried as the sum of two fp16 numbers (22 bits): the iteration multiplies small
-// singular values by a at every step while the product's part of them is tiny, so a rounding of the X that is carried on
-// is amplified by a^steps (485 for Muon's five steps) and swamps them, and a rounding of the X that enters the product is
-// not.  On 64-bit models of the iteration (Gaussian, low-rank and decaying spectra, shorter side 256-1024) the relative
-// error of the result is 0.02-0.17 % this way, against 0.1-6.6 % with X carried in fp16 and 1-50 % in bf16.
+// accumulate in fp32.  X itself is carried as the sum hi + lo of two fp16 numbers (22 bits) and the step is
+// B hi + a lo: the iteration multiplies small singular values by a at every step, so a rounding of the X that is carried
+// on is amplified by a^steps (485 for Muon's five steps) and swamps them; a rounding of B only scales what is there, and
+// lo's share of (b A + c A^2) X is below the roundings of the product.  On 64-bit models of the iteration (Gaussian,
+// low-rank and decaying spectra, shorter side 256-1024) the relative error of the result is 0.10-0.17 % this way (a
+// bf16 rounding alone is 0.17 %), against 0.1-6.6 % with X carried in fp16 and 1-50 % in bf16.
 // Factors are stored scaled by powers of two (X by 2^12, A and B by 2^10) to stay clear of fp16's subnormals; the call
 // checks on the host that the coefficients keep every singular value inside the range this leaves.
 #include <cuda_fp16.h>
@@ -68,6 +69,13 @@ __device__ __forceinline__ void load8(const T *p, bool wide, int valid, float (&
     }
 }
 
+// Row of the i-th vector of a matrix of `vecs` vectors a row; 32-bit division where the count allows it (a 64-bit one costs
+// more than the eight elements it leads to).
+__device__ __forceinline__ int row_of(long long i, int vecs, long long total)
+{
+    return total <= 0x7FFFFFFF ? (int)((unsigned)i / (unsigned)vecs) : (int)(i / vecs);
+}
+
 // 8 elements of a row a thread: 16-byte loads where the matrix allows them for all of its rows.
 template <typename T>
 __device__ __forceinline__ bool wide_rows(const PrepMatrix &m)
@@ -98,7 +106,7 @@ __global__ void __launch_bounds__(256) square_sums_kernel(const __grid_constant_
         for (int k = 0; k < kAt; ++k) {
             const long long i = i0 + k * step;
             if (i < total) {
-                const int r = (int)(i / vecs), c = 8 * (int)(i - (long long)r * vecs);
+                const int r = row_of(i, vecs, total), c = 8 * (int)(i - (long long)r * vecs);
                 load8((const T *)m.g + r * m.ld + c, wide && c + 8 <= m.cols, m.cols - c, f[k]);
             } else {
 #pragma unroll
@@ -152,7 +160,7 @@ __global__ void __launch_bounds__(256) normalise_kernel(const __grid_constant__ 
     const long long total = (long long)m.rows * vecs, ldx = 8ll * vecs;
     const bool wide = wide_rows<T>(m);
     for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long long)gridDim.x * 256) {
-        const int r = (int)(i / vecs), c = 8 * (int)(i - (long long)r * vecs);
+        const int r = row_of(i, vecs, total), c = 8 * (int)(i - (long long)r * vecs);
         float f[8];
         load8((const T *)m.g + r * m.ld + c, wide && c + 8 <= m.cols, m.cols - c, f);
         uint32_t h[4], l[4];
@@ -244,9 +252,9 @@ bool coefficients_ok(float a, float b, float c, int steps)
     for (int s = 0; s < steps; ++s) {
         double next = 0.0;
         for (int i = 0; i <= 1024; ++i) {
-            const double x = top * i / 1024.0, x2 = x * x, q = (double)b * x2 + (double)c * x2 * x2;
+            const double x = top * i / 1024.0, x2 = x * x, q = (double)a + (double)b * x2 + (double)c * x2 * x2;
             if (!(std::fabs(q) <= kMaxB)) return false;
-            const double y = std::fabs(x * ((double)a + q));
+            const double y = std::fabs(x * q);
             next = y > next ? y : next;
         }
         if (!(next <= kMaxSigma)) return false;
@@ -287,9 +295,9 @@ cudaError_t run_group(modse_dtype_t dtype, const modse_matrix_t *m, int n, int s
             step_items(m[i], cur, (__half *)(ws + sp.a), (__half *)(ws + sp.b), gram[i], poly[i], step[i]);
             poly[i].p.alpha = k[2] * kScaleB / (kScaleA * kScaleA);
             poly[i].p.beta = k[1] * kScaleB / kScaleA;
+            poly[i].p.scale = k[0] * kScaleB;
             DenseProblem &p = step[i].p;
-            p.in0 = cur;
-            p.in1 = lo;
+            p.in0 = lo;
             p.alpha = 1.f / kScaleB;
             p.beta = k[0];
             if (last) {

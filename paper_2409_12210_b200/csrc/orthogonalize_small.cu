@@ -5,8 +5,8 @@
 // memory for all iterations and multiplies with mma.sync.  Per iteration:
 //   A = X X^T    every block over its own columns; blocks of a cluster leave fp32 partial sums in their shared memory and
 //                each adds up (in block order) and hands out its share of A through distributed shared memory;
-//   B = bA + cA^2  computed by every block for itself (a 128 x 128 product is cheaper than another meeting);
-//   X <- aX + BX   every block on its own columns.
+//   B = aI + bA + cA^2  computed by every block for itself (a 128 x 128 product is cheaper than another meeting);
+//   X <- B hi + a lo   every block on its own columns.
 // The roundings are those of the grouped form (orthogonalize.cu): fp16 factors scaled by powers of two, X in 22 bits.
 // A tall matrix is transposed on its way in and out.
 #include <cuda_fp16.h>
@@ -190,6 +190,7 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
     const int nt = np / 16, pt = per / 16;
     const int fr = lane >> 2, fc = 2 * (lane & 3);          // a fragment's row (and row + 8) and columns (two of eight)
     const float beta = args.k[1] * kOrthScaleB / kOrthScaleA, alpha = args.k[2] * kOrthScaleB / (kOrthScaleA * kOrthScaleA);
+    const float diagonal = args.k[0] * kOrthScaleB;
     constexpr float kGram = kOrthScaleA / (kOrthScaleX * kOrthScaleX);
     for (int it = 0; it < args.steps; ++it) {
         const size_t cur_off = (it & 1) ? L.hi1 : L.hi0, next_off = (it & 1) ? L.hi0 : L.hi1;
@@ -238,13 +239,14 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
                 for (int r = 0; r < 2; ++r) {
                     const int at = (i0 + fr + 8 * r) * L.as + j0 + 8 * h + fc;
                     const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(A + at));
+                    const int off = (j0 + 8 * h + fc) - (i0 + fr + 8 * r);      // a I: this element's, or its neighbour's
                     *reinterpret_cast<uint32_t *>(B + at) =
-                        half2_bits(fmaf(beta, f.x, alpha * acc[h][2 * r]), fmaf(beta, f.y, alpha * acc[h][2 * r + 1]));
+                        half2_bits(fmaf(beta, f.x, alpha * acc[h][2 * r]) + (off == 0 ? diagonal : 0.f),
+                                   fmaf(beta, f.y, alpha * acc[h][2 * r + 1]) + (off == -1 ? diagonal : 0.f));
                 }
         }
         __syncthreads();
         const bool last = it + 1 == args.steps;
-        const __half *hi = reinterpret_cast<const __half *>(smem + cur_off);
         __half *next = reinterpret_cast<__half *>(smem + next_off);
         for (int t = warp; t < nt * pt; t += kWarps) {
             const int i0 = t / pt * 16, j0 = t % pt * 16;
@@ -255,10 +257,9 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const int at = (i0 + fr + 8 * r) * L.xs + j0 + 8 * h + fc;
-                    const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(hi + at));
                     const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(lo + at));
-                    const float v0 = fmaf(args.k[0], x.x + y.x, acc[h][2 * r] * (1.f / kOrthScaleB));
-                    const float v1 = fmaf(args.k[0], x.y + y.y, acc[h][2 * r + 1] * (1.f / kOrthScaleB));
+                    const float v0 = fmaf(args.k[0], y.x, acc[h][2 * r] * (1.f / kOrthScaleB));
+                    const float v1 = fmaf(args.k[0], y.y, acc[h][2 * r + 1] * (1.f / kOrthScaleB));
                     if (last) {
                         const float s = m.scale / kOrthScaleX;
                         *reinterpret_cast<__nv_bfloat162 *>(next + at) = __floats2bfloat162_rn(v0 * s, v1 * s);

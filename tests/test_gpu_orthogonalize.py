@@ -1,6 +1,6 @@
 """Orthogonalised updates (modse_orthogonalize) against the iteration in 64 bits.
 
-Bound.  The documented roundings are: factors of the products in fp16 (2^-11 of a value), X carried in 22 bits, fp32
+Bound.  The documented roundings are: factors of the products in fp16 (2^-11 of a value; X's as its leading half), X carried in 22 bits, fp32
 accumulation, one rounding of the result to bf16 (2^-8).  What the first two do to the result depends on the spectrum, so
 the test runs the iteration in 64 bits with exactly these roundings put in by hand; its distance E from the iteration
 without them is the size of the error they cause.  A kernel that accumulates in another order meets other instances of
@@ -29,8 +29,9 @@ def iterate(G, steps=5, k=MUON, eps=1e-7, rounded=False):
     for i in range(steps):
         Xh = fp16(X, 4096.0)
         M = fp16(Xh @ Xh.T, 1024.0)
-        P = fp16(k[1] * M + k[2] * (M @ M), 1024.0)
-        X = k[0] * X + P @ Xh
+        # the step as it is computed: (a I + b A + c A^2) in fp16 times the leading half of X, plus a times the rest
+        P = fp16(k[0] * torch.eye(len(M), dtype=M.dtype, device=M.device) + k[1] * M + k[2] * (M @ M), 1024.0)
+        X = P @ Xh + k[0] * (X - Xh)
         if rounded and i + 1 < steps:
             hi = fp16(X, 4096.0)
             X = hi + fp16(X - hi, 4096.0)
