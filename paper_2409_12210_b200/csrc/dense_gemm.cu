@@ -105,14 +105,14 @@ __device__ __forceinline__ DenseTile dense_decode(const DenseParams<P> &prm, int
         while (cursor + 1 < prm.n_prob && tile >= prm.prob[cursor + 1].tile0) ++cursor;
     t.p = cursor;
     const DenseProblem &q = prm.prob[cursor];
-    constexpr int kUnits = TALL ? 2 : 1;         // 256-row units of a tile
+    constexpr int kUnits = DenseShape<TALL>::kTileRows / TN;      // column tiles as wide as a row tile is high
     int local = tile - q.tile0, mb, nb;
     bool below = false;                          // symmetric: the second half lies below the diagonal
     if (q.flags & kDenseSym) {
-        mb = 0;                                  // row by row of the upper triangle, in units of 256
+        mb = 0;                                  // row by row of the upper triangle; squares on the diagonal are whole
         while (local >= q.nt - kUnits * mb) { local -= q.nt - kUnits * mb; ++mb; }
         nb = kUnits * mb + local;
-        below = nb < kUnits * mb + kUnits - 1;
+        below = TALL && local == 0;
     } else {
         const int per = kDenseGroupRows * q.nt, g = local / per, rem = local - g * per;
         const int rows = min(kDenseGroupRows, q.mt - g * kDenseGroupRows);
@@ -776,7 +776,7 @@ long long dense_tiles(const DenseProblem &p, bool tall, int tn)
     const long long mt = (p.M + (tall ? 511 : 255)) / (tall ? 512 : 256), nt = (p.N + tn - 1) / tn;
     if (!(p.flags & kDenseSym)) return mt * nt;
     long long c = 0;
-    for (long long m = 0; m < mt; ++m) c += nt - (tall ? 2 : 1) * m;
+    for (long long m = 0; m < mt; ++m) c += nt - (tall ? 512 : 256) / tn * m;
     return c;
 }
 
@@ -809,9 +809,9 @@ DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int
         pl.items = pl.full + (int)rest * pl.splits;
         return pl;
     }
-    // 256-column tiles unless the whole output has less than half a tile for each CTA pair: then 128-column tiles
-    // (symmetric outputs have square tiles)
-    pl.tn = (mode != DenseGram && mode != DensePoly && squares * 2 <= pairs) ? 128 : 256;
+    // 256-column tiles unless the whole output has less than half a tile for each CTA pair: then 128-column tiles, whose
+    // epilogue, which shows in a launch of one round, is half as long
+    pl.tn = squares * 2 <= pairs ? 128 : 256;
     pl.tiles = (int)count(false, pl.tn);
     pl.full = pl.tiles / pairs * pairs;
     const int left = pl.tiles - pl.full;
@@ -899,8 +899,7 @@ cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin
     const DensePlan pl = dense_plan((DenseMode)MODE, (DenseType)TYPE, items, n, light, device_sms(), cap);
     if constexpr (MODE == DensePlain || (MODE == DenseLinear && TYPE == DenseBf16))
         if (pl.tall) return launch_tn<MODE, TYPE, 256, true, P>(pl, items, n, lin, sum, ws, head, s);
-    if constexpr (MODE != DenseGram && MODE != DensePoly)
-        if (pl.tn == 128) return launch_tn<MODE, TYPE, 128, false, P>(pl, items, n, lin, sum, ws, head, s);
+    if (pl.tn == 128) return launch_tn<MODE, TYPE, 128, false, P>(pl, items, n, lin, sum, ws, head, s);
     return launch_tn<MODE, TYPE, 256, false, P>(pl, items, n, lin, sum, ws, head, s);
 }
 

@@ -346,13 +346,26 @@ modse_status_t check_call(modse_dtype_t dtype, int steps, const float *k, float 
     return coefficients_ok(k[0], k[1], k[2], steps) ? MODSE_OK : MODSE_ERR_UNSUPPORTED;
 }
 
-// The next matrices from index i on, up to a launch's worth, that take the grouped form (short sides above 128); i moves
-// on.
-int next_group(const modse_matrix_t *m, int total, int &i, modse_matrix_t (&group)[kGroup])
+// Which form a matrix of a set takes.  Short sides above 128 take the grouped one.  The others take the one-kernel form,
+// unless the set needs grouped launches anyway and they all fit beside its matrices there: those launches wait more than
+// they compute when matrices are small, and the two forms would run one after the other (86 x 717 with 1508 x 717: 257 us
+// in both forms, 190 in one).
+struct SetPlan { bool small_form; };      // whether the one-kernel form is used
+SetPlan plan_set(const modse_matrix_t *m, int total)
+{
+    int grouped = 0, small = 0;
+    for (int i = 0; i < total; ++i) (orthogonalize_small_cluster(m[i].rows, m[i].cols) > 0 ? small : grouped) += 1;
+    const int room = (kGroup - grouped % kGroup) % kGroup;
+    return {grouped == 0 || small > room};
+}
+bool takes_small(const SetPlan &p, const modse_matrix_t &m) { return p.small_form && orthogonalize_small_cluster(m.rows, m.cols) > 0; }
+
+// The next matrices from index i on, up to a launch's worth, that take the grouped form; i moves on.
+int next_group(const SetPlan &p, const modse_matrix_t *m, int total, int &i, modse_matrix_t (&group)[kGroup])
 {
     int n = 0;
     for (; i < total && n < kGroup; ++i)
-        if (orthogonalize_small_cluster(m[i].rows, m[i].cols) == 0) group[n++] = m[i];
+        if (!takes_small(p, m[i])) group[n++] = m[i];
     return n;
 }
 
@@ -374,10 +387,11 @@ size_t modse_orthogonalize_workspace_bytes(int n_matrices, const modse_matrix_t 
     if (n_matrices < 0 || (n_matrices > 0 && matrices == nullptr)) return 0;
     for (int i = 0; i < n_matrices; ++i)
         if (!matrix_ok(matrices[i])) return 0;
+    const SetPlan plan = plan_set(matrices, n_matrices);
     size_t most = kDenseHead;
     modse_matrix_t group[kGroup];
     for (int i = 0; i < n_matrices;) {
-        const int n = next_group(matrices, n_matrices, i, group);
+        const int n = next_group(plan, matrices, n_matrices, i, group);
         if (n == 0) break;
         GroupLayout L;
         group_layout(group, n, L);
@@ -400,6 +414,7 @@ modse_status_t modse_orthogonalize(modse_dtype_t dtype, int n_matrices, const mo
     if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MODSE_ERR_INVALID_ARG;
     if (workspace_bytes < need) return MODSE_ERR_WORKSPACE_TOO_SMALL;
     const cudaStream_t s = (cudaStream_t)cuda_stream;
+    const SetPlan plan = plan_set(matrices, n_matrices);
     bool first = true;               // the call's first kernel zeroes the workspace head
     SmallArgs small{};
     for (int j = 0; j < 3; ++j) small.k[j] = coefficients[j];
@@ -407,7 +422,7 @@ modse_status_t modse_orthogonalize(modse_dtype_t dtype, int n_matrices, const mo
     small.steps = steps;
     int n = 0;
     for (int i = 0; i <= n_matrices; ++i) {
-        if (i < n_matrices && orthogonalize_small_cluster(matrices[i].rows, matrices[i].cols) > 0) {
+        if (i < n_matrices && takes_small(plan, matrices[i])) {
             const modse_matrix_t &m = matrices[i];
             small.m[n++] = {m.grad, (__nv_bfloat16 *)m.update, m.ld_grad, m.ld_update, m.rows, m.cols, m.scale};
         }
@@ -421,7 +436,7 @@ modse_status_t modse_orthogonalize(modse_dtype_t dtype, int n_matrices, const mo
     }
     modse_matrix_t group[kGroup];
     for (int i = 0; i < n_matrices;) {
-        const int c = next_group(matrices, n_matrices, i, group);
+        const int c = next_group(plan, matrices, n_matrices, i, group);
         if (c == 0) break;
         if (run_group(dtype, group, c, steps, coefficients, eps, (unsigned char *)workspace, first, s) != cudaSuccess)
             return MODSE_ERR_CUDA;

@@ -62,36 +62,70 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// 16 x 16 block (i0, j0) of P Q^T, P and Q row-major with row lengths ps, qs (halves), k a multiple of 16.
-// acc[0]: columns j0 .. j0+7, acc[1]: the next eight.
-__device__ __forceinline__ void block_nt(float (&acc)[2][4], uint32_t p, int ps, uint32_t q, int qs, int i0, int j0, int k, int lane)
+// A warp's block of 16 MI x 16 NJ numbers of P Q^T (TRANS false: Q [columns][k]) or P Q (TRANS: Q [k][columns]) from (i0, j0)
+// on, all row-major in shared memory with row lengths ps, qs (halves), k a multiple of 16; 16 x 16 pieces at or past row
+// `rows` or column `cols` are left out.  What bounds these products is reading the fragments (a 16 x 16 block reads as
+// much as it multiplies), so a warp takes as large a block as leaves work for the others.
+template <bool TRANS, int MI, int NJ>
+__device__ __forceinline__ void warp_block(float (&acc)[MI][NJ][2][4], uint32_t p, int ps, uint32_t q, int qs, int i0, int j0,
+                                           int rows, int cols, int k, int lane)
 {
-    // matrices of a load: rows 0-7 / 8-15 at k 0-7, then the same rows at k 8-15
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[i][j][e >> 2][e & 3] = 0.f;
+    // matrices of a load of P: rows 0-7 / 8-15 at k 0-7, then the same rows at k 8-15
     const uint32_t pa = p + (uint32_t)((i0 + (lane & 15)) * ps + (lane >> 4) * 8) * 2;
-    // for Q: rows 0-7 at k 0-7, rows 0-7 at k 8-15, rows 8-15 at k 0-7, rows 8-15 at k 8-15
-    const uint32_t qa = q + (uint32_t)((j0 + (lane & 7) + ((lane >> 4) << 3)) * qs + ((lane >> 3) & 1) * 8) * 2;
+    // of Q^T: rows 0-7 at k 0-7, rows 0-7 at k 8-15, rows 8-15 at k 0-7, rows 8-15 at k 8-15;
+    // of Q, transposed on the way: k rows 0-7 / 8-15 at columns 0-7, then at columns 8-15
+    const uint32_t qa = TRANS ? q + (uint32_t)((lane & 15) * qs + j0 + (lane >> 4) * 8) * 2
+                              : q + (uint32_t)((j0 + (lane & 7) + ((lane >> 4) << 3)) * qs + ((lane >> 3) & 1) * 8) * 2;
 #pragma unroll 4
     for (int kk = 0; kk < k; kk += 16) {
-        uint32_t a[4], b[4];
-        ldsm4(a, pa + kk * 2);
-        ldsm4(b, qa + kk * 2);
-        mma_f16(acc[0], a, b[0], b[1]);
-        mma_f16(acc[1], a, b[2], b[3]);
+        uint32_t a[MI][4], b[NJ][4];
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+            if (i == 0 || i0 + 16 * i < rows) ldsm4(a[i], pa + (uint32_t)(16 * i * ps + kk) * 2);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            if (j == 0 || j0 + 16 * j < cols) {
+                if constexpr (TRANS) ldsm4_t(b[j], qa + (uint32_t)(kk * qs + 16 * j) * 2);
+                else ldsm4(b[j], qa + (uint32_t)(16 * j * qs + kk) * 2);
+            }
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                if ((i == 0 || i0 + 16 * i < rows) && (j == 0 || j0 + 16 * j < cols)) {
+                    mma_f16(acc[i][j][0], a[i], b[j][0], b[j][1]);
+                    mma_f16(acc[i][j][1], a[i], b[j][2], b[j][3]);
+                }
     }
 }
-// 16 x 16 block (i0, j0) of P Q, Q [k][columns] row-major.
-__device__ __forceinline__ void block_nn(float (&acc)[2][4], uint32_t p, int ps, uint32_t q, int qs, int i0, int j0, int k, int lane)
+// All blocks of a rows x cols product shared out over the warps; put(row, column, v0, v1) gets every two neighbouring
+// numbers of a row.
+template <bool TRANS, int MI, int NJ, typename F>
+__device__ __forceinline__ void warp_product(uint32_t p, int ps, uint32_t q, int qs, int rows, int cols, int k, int warp,
+                                             int lane, F &&put)
 {
-    const uint32_t pa = p + (uint32_t)((i0 + (lane & 15)) * ps + (lane >> 4) * 8) * 2;
-    // transposed loads: k rows 0-7 / 8-15 at columns 0-7, then at columns 8-15
-    const uint32_t qa = q + (uint32_t)((lane & 15) * qs + j0 + (lane >> 4) * 8) * 2;
-#pragma unroll 4
-    for (int kk = 0; kk < k; kk += 16) {
-        uint32_t a[4], b[4];
-        ldsm4(a, pa + kk * 2);
-        ldsm4_t(b, qa + (uint32_t)(kk * qs) * 2);
-        mma_f16(acc[0], a, b[0], b[1]);
-        mma_f16(acc[1], a, b[2], b[3]);
+    const int tj = (cols + 16 * NJ - 1) / (16 * NJ), tiles = (rows + 16 * MI - 1) / (16 * MI) * tj;
+    const int fr = lane >> 2, fc = 2 * (lane & 3);          // a fragment's row (and row + 8) and columns (two of eight)
+    for (int t = warp; t < tiles; t += kWarps) {
+        const int i0 = t / tj * 16 * MI, j0 = t % tj * 16 * NJ;
+        float acc[MI][NJ][2][4];
+        warp_block<TRANS, MI, NJ>(acc, p, ps, q, qs, i0, j0, rows, cols, k, lane);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+                if ((i == 0 || i0 + 16 * i < rows) && (j == 0 || j0 + 16 * j < cols))
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+                            put(i0 + 16 * i + fr + 8 * r, j0 + 16 * j + 8 * h + fc, acc[i][j][h][2 * r], acc[i][j][h][2 * r + 1]);
     }
 }
 
@@ -139,35 +173,42 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
     if (args.head && blockIdx.x == 0)
         for (int i = tid; i < args.head_ints; i += kThreads) args.head[i] = 0;
 
-    // the elements (i, j) of this block's columns, threads along the contiguous axis of the matrix, eight loads in flight
+    // this block's elements, threads along the contiguous axis of the matrix: element e of `count` (a row of it padded to 32)
+    // lies at (r, c) of the matrix; up to kAt a thread stay in registers from the norm to the conversion
     const T *g = (const T *)m.g + (tall ? (long long)c0 * m.ld_g : (long long)c0);
-    auto each = [&](auto &&f) {
-        constexpr int kAt = 8;
-        const int outer = tall ? mine : n, inner = tall ? n : mine;
-        for (int r0 = warp; r0 < outer; r0 += kAt * kWarps)
-            for (int c = lane; c < inner; c += 32) {
-                float v[kAt];
+    const unsigned outer = tall ? mine : n, inner = tall ? n : mine, width = (inner + 31) / 32 * 32, count = outer * width;
+    constexpr unsigned kAt = 24;
+    float v[kAt];
+    auto load = [&](unsigned from) {
 #pragma unroll
-                for (int k = 0; k < kAt; ++k)
-                    v[k] = r0 + k * kWarps < outer ? (float)g[(long long)(r0 + k * kWarps) * m.ld_g + c] : 0.f;
-#pragma unroll
-                for (int k = 0; k < kAt; ++k)
-                    if (r0 + k * kWarps < outer) f(tall ? c : r0 + k * kWarps, tall ? r0 + k * kWarps : c, v[k]);
-            }
+        for (unsigned k = 0; k < kAt; ++k) {
+            const unsigned e = from + k * kThreads + tid, r = width ? e / width : 0, c = e - r * width;
+            v[k] = e < count && c < inner ? (float)g[(long long)r * m.ld_g + c] : 0.f;
+        }
     };
     double sq = 0.0;
-    each([&](int, int, float v) { sq = fma((double)v, (double)v, sq); });
+    for (unsigned from = 0; from < count; from += kAt * kThreads) {
+        load(from);
+#pragma unroll
+        for (unsigned k = 0; k < kAt; ++k) sq = fma((double)v[k], (double)v[k], sq);
+    }
     // padding: zero rows and columns take part in the products
-    for (int i = tid; i < (int)((3 * (size_t)np * L.xs) / 2); i += kThreads) reinterpret_cast<uint32_t *>(smem)[i] = 0;
+    for (int i = warp; i < np; i += kWarps)
+        for (int j = (i < n ? mine : 0) + lane; j < L.xs; j += 32) {
+            reinterpret_cast<__half *>(smem + L.hi0)[i * L.xs + j] = __ushort_as_half(0);
+            reinterpret_cast<__half *>(smem + L.hi1)[i * L.xs + j] = __ushort_as_half(0);
+            lo[i * L.xs + j] = __ushort_as_half(0);
+        }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sq += __shfl_xor_sync(0xFFFFFFFFu, sq, o);
     if (lane == 0) warp_sums[warp] = sq;
     __syncthreads();
-    if (tid == 0) {
-        double t = 0.0;
-        for (int w = 0; w < kWarps; ++w) t += warp_sums[w];
-        for (int r = 0; r < C; ++r) {
-            const uint32_t to = C > 1 ? map_to_cta(smem_u32(&block_sums[rank]), r) : smem_u32(&block_sums[0]);
+    if (warp == 0) {
+        double t = lane < kWarps ? warp_sums[lane] : 0.0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+        if (lane < C) {
+            const uint32_t to = C > 1 ? map_to_cta(smem_u32(&block_sums[rank]), lane) : smem_u32(&block_sums[0]);
             asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(t) : "memory");
         }
     }
@@ -176,19 +217,24 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
     double total = 0.0;
     for (int r = 0; r < C; ++r) total += block_sums[r];
     const float inv = (float)((double)kOrthScaleX / (sqrt(total) + (double)args.eps));
-    {
+    for (unsigned from = 0; from < count; from += kAt * kThreads) {
         __half *hi = reinterpret_cast<__half *>(smem + L.hi0);
-        each([&](int i, int j, float v) {
-            const float x = v * inv;
-            const __half h = __float2half_rn(x);
-            hi[i * L.xs + j] = h;
-            lo[i * L.xs + j] = __float2half_rn(x - __half2float(h));
-        });
+        if (count > kAt * kThreads) load(from);
+#pragma unroll
+        for (unsigned k = 0; k < kAt; ++k) {
+            const unsigned e = from + k * kThreads + tid, r = e / width, c = e - r * width;
+            if (e < count && c < inner) {
+                const int at = tall ? c * L.xs + r : r * L.xs + c;
+                const float x = v[k] * inv;
+                const __half h = __float2half_rn(x);
+                hi[at] = h;
+                lo[at] = __float2half_rn(x - __half2float(h));
+            }
+        }
     }
     __syncthreads();
 
-    const int nt = np / 16, pt = per / 16;
-    const int fr = lane >> 2, fc = 2 * (lane & 3);          // a fragment's row (and row + 8) and columns (two of eight)
+    const bool large = np == kOrthSmallMax;      // 32 x 32 a warp leaves none of the sixteen idle
     const float beta = args.k[1] * kOrthScaleB / kOrthScaleA, alpha = args.k[2] * kOrthScaleB / (kOrthScaleA * kOrthScaleA);
     const float diagonal = args.k[0] * kOrthScaleB;
     constexpr float kGram = kOrthScaleA / (kOrthScaleX * kOrthScaleX);
@@ -197,21 +243,12 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
         const uint32_t cur = base + (uint32_t)cur_off;
         __half *A = reinterpret_cast<__half *>(smem + L.a), *B = reinterpret_cast<__half *>(smem + L.b);
         float *part = reinterpret_cast<float *>(smem + L.part);
-        for (int t = warp; t < nt * nt; t += kWarps) {
-            const int i0 = t / nt * 16, j0 = t % nt * 16;
-            float acc[2][4] = {};
-            block_nt(acc, cur, L.xs, cur, L.xs, i0, j0, per, lane);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int i = i0 + fr + 8 * r, j = j0 + 8 * h + fc;
-                    if (C == 1)
-                        *reinterpret_cast<uint32_t *>(A + i * L.as + j) = half2_bits(acc[h][2 * r] * kGram, acc[h][2 * r + 1] * kGram);
-                    else
-                        *reinterpret_cast<float2 *>(part + i * np + j) = make_float2(acc[h][2 * r], acc[h][2 * r + 1]);
-                }
-        }
+        auto put_gram = [&](int i, int j, float v0, float v1) {
+            if (C == 1) *reinterpret_cast<uint32_t *>(A + i * L.as + j) = half2_bits(v0 * kGram, v1 * kGram);
+            else *reinterpret_cast<float2 *>(part + i * np + j) = make_float2(v0, v1);
+        };
+        if (large) warp_product<false, 2, 2>(cur, L.xs, cur, L.xs, np, np, per, warp, lane, put_gram);
+        else warp_product<false, 1, 2>(cur, L.xs, cur, L.xs, np, np, per, warp, lane, put_gram);
         if (C > 1) {
             cluster_sync_all();
             // four neighbouring elements a thread, shares of the blocks interleaved
@@ -229,48 +266,35 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
         } else {
             __syncthreads();
         }
-        for (int t = warp; t < nt * nt; t += kWarps) {
-            const int i0 = t / nt * 16, j0 = t % nt * 16;
-            float acc[2][4] = {};
-            block_nt(acc, base + (uint32_t)L.a, L.as, base + (uint32_t)L.a, L.as, i0, j0, np, lane);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int at = (i0 + fr + 8 * r) * L.as + j0 + 8 * h + fc;
-                    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(A + at));
-                    const int off = (j0 + 8 * h + fc) - (i0 + fr + 8 * r);      // a I: this element's, or its neighbour's
-                    *reinterpret_cast<uint32_t *>(B + at) =
-                        half2_bits(fmaf(beta, f.x, alpha * acc[h][2 * r]) + (off == 0 ? diagonal : 0.f),
-                                   fmaf(beta, f.y, alpha * acc[h][2 * r + 1]) + (off == -1 ? diagonal : 0.f));
-                }
-        }
+        const uint32_t a_at = base + (uint32_t)L.a, b_at = base + (uint32_t)L.b;
+        auto put_poly = [&](int i, int j, float v0, float v1) {
+            const int at = i * L.as + j;
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(A + at));
+            *reinterpret_cast<uint32_t *>(B + at) = half2_bits(fmaf(beta, f.x, alpha * v0) + (i == j ? diagonal : 0.f),
+                                                               fmaf(beta, f.y, alpha * v1) + (i == j + 1 ? diagonal : 0.f));
+        };
+        if (large) warp_product<false, 2, 2>(a_at, L.as, a_at, L.as, np, np, np, warp, lane, put_poly);
+        else warp_product<false, 1, 2>(a_at, L.as, a_at, L.as, np, np, np, warp, lane, put_poly);
         __syncthreads();
         const bool last = it + 1 == args.steps;
+        const float by = last ? m.scale / kOrthScaleX : 1.f;
         __half *next = reinterpret_cast<__half *>(smem + next_off);
-        for (int t = warp; t < nt * pt; t += kWarps) {
-            const int i0 = t / pt * 16, j0 = t % pt * 16;
-            float acc[2][4] = {};
-            block_nn(acc, base + (uint32_t)L.b, L.as, cur, L.xs, i0, j0, np, lane);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int at = (i0 + fr + 8 * r) * L.xs + j0 + 8 * h + fc;
-                    const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(lo + at));
-                    const float v0 = fmaf(args.k[0], y.x, acc[h][2 * r] * (1.f / kOrthScaleB));
-                    const float v1 = fmaf(args.k[0], y.y, acc[h][2 * r + 1] * (1.f / kOrthScaleB));
-                    if (last) {
-                        const float s = m.scale / kOrthScaleX;
-                        *reinterpret_cast<__nv_bfloat162 *>(next + at) = __floats2bfloat162_rn(v0 * s, v1 * s);
-                    } else {
-                        const __half2 hh = __floats2half2_rn(v0, v1);
-                        const float2 back = __half22float2(hh);
-                        *reinterpret_cast<__half2 *>(next + at) = hh;
-                        *reinterpret_cast<uint32_t *>(lo + at) = half2_bits(v0 - back.x, v1 - back.y);
-                    }
-                }
-        }
+        auto put_step = [&](int i, int j, float v0, float v1) {
+            const int at = i * L.xs + j;
+            const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(lo + at));
+            v0 = fmaf(args.k[0], y.x, v0 * (1.f / kOrthScaleB));
+            v1 = fmaf(args.k[0], y.y, v1 * (1.f / kOrthScaleB));
+            if (last) {
+                *reinterpret_cast<__nv_bfloat162 *>(next + at) = __floats2bfloat162_rn(v0 * by, v1 * by);
+            } else {
+                const __half2 hh = __floats2half2_rn(v0, v1);
+                const float2 back = __half22float2(hh);
+                *reinterpret_cast<__half2 *>(next + at) = hh;
+                *reinterpret_cast<uint32_t *>(lo + at) = half2_bits(v0 - back.x, v1 - back.y);
+            }
+        };
+        if (large) warp_product<true, 2, 2>(b_at, L.as, cur, L.xs, np, per, np, warp, lane, put_step);
+        else warp_product<true, 1, 2>(b_at, L.as, cur, L.xs, np, per, np, warp, lane, put_step);
         __syncthreads();
     }
     // the result lies as bf16 in the buffer the last iteration wrote
