@@ -63,12 +63,10 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
 }
 
 // A warp's block of 16 MI x 16 NJ numbers of P Q^T (TRANS false: Q [columns][k]) or P Q (TRANS: Q [k][columns]) from (i0, j0)
-// on, all row-major in shared memory with row lengths ps, qs (halves), k a multiple of 16; 16 x 16 pieces at or past row
-// `rows` or column `cols` are left out.  What bounds these products is reading the fragments (a 16 x 16 block reads as
-// much as it multiplies), so a warp takes as large a block as leaves work for the others.
+// on, all row-major in shared memory with row lengths ps, qs (halves), k a multiple of 16.
 template <bool TRANS, int MI, int NJ>
 __device__ __forceinline__ void warp_block(float (&acc)[MI][NJ][2][4], uint32_t p, int ps, uint32_t q, int qs, int i0, int j0,
-                                           int rows, int cols, int k, int lane)
+                                           int k, int lane)
 {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -82,50 +80,68 @@ __device__ __forceinline__ void warp_block(float (&acc)[MI][NJ][2][4], uint32_t 
     // of Q, transposed on the way: k rows 0-7 / 8-15 at columns 0-7, then at columns 8-15
     const uint32_t qa = TRANS ? q + (uint32_t)((lane & 15) * qs + j0 + (lane >> 4) * 8) * 2
                               : q + (uint32_t)((j0 + (lane & 7) + ((lane >> 4) << 3)) * qs + ((lane >> 3) & 1) * 8) * 2;
-#pragma unroll 4
+#pragma unroll 2
     for (int kk = 0; kk < k; kk += 16) {
         uint32_t a[MI][4], b[NJ][4];
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
-            if (i == 0 || i0 + 16 * i < rows) ldsm4(a[i], pa + (uint32_t)(16 * i * ps + kk) * 2);
+        for (int i = 0; i < MI; ++i) ldsm4(a[i], pa + (uint32_t)(16 * i * ps + kk) * 2);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-            if (j == 0 || j0 + 16 * j < cols) {
-                if constexpr (TRANS) ldsm4_t(b[j], qa + (uint32_t)(kk * qs + 16 * j) * 2);
-                else ldsm4(b[j], qa + (uint32_t)(16 * j * qs + kk) * 2);
+        for (int j = 0; j < NJ; ++j) {
+            if constexpr (TRANS) ldsm4_t(b[j], qa + (uint32_t)(kk * qs + 16 * j) * 2);
+            else ldsm4(b[j], qa + (uint32_t)(16 * j * qs + kk) * 2);
+        }
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                mma_f16(acc[i][j][0], a[i], b[j][0], b[j][1]);
+                mma_f16(acc[i][j][1], a[i], b[j][2], b[j][3]);
             }
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                if ((i == 0 || i0 + 16 * i < rows) && (j == 0 || j0 + 16 * j < cols)) {
-                    mma_f16(acc[i][j][0], a[i], b[j][0], b[j][1]);
-                    mma_f16(acc[i][j][1], a[i], b[j][2], b[j][3]);
-                }
     }
 }
-// All blocks of a rows x cols product shared out over the warps; put(row, column, v0, v1) gets every two neighbouring
-// numbers of a row.
-template <bool TRANS, int MI, int NJ, typename F>
+template <bool TRANS, int MI, int NJ, typename G, typename F>
+__device__ __forceinline__ void warp_tile(uint32_t p, int ps, uint32_t q, int qs, int i0, int j0, int k, int lane, G &get, F &put)
+{
+    const int fr = lane >> 2, fc = 2 * (lane & 3);          // a fragment's row (and row + 8) and columns (two of eight)
+    float acc[MI][NJ][2][4];
+    uint32_t in[MI][NJ][2][2];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) in[i][j][h][r] = get(i0 + 16 * i + fr + 8 * r, j0 + 16 * j + 8 * h + fc);
+    warp_block<TRANS, MI, NJ>(acc, p, ps, q, qs, i0, j0, k, lane);
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    put(i0 + 16 * i + fr + 8 * r, j0 + 16 * j + 8 * h + fc, acc[i][j][h][2 * r], acc[i][j][h][2 * r + 1], in[i][j][h][r]);
+}
+// All 16 MI x 16 NJ blocks of a rows x cols product (multiples of 16) shared out over the warps.  For every two
+// neighbouring numbers of a row, get(row, column) reads what their epilogue needs before the products begin (after them
+// every read would wait for the writes before it) and put(row, column, v0, v1, what get read) writes.  Reading the
+// fragments costs as much as multiplying them in a 16 x 16 block, so a warp takes as large a block as leaves work for
+// the others.
+template <bool TRANS, int MI, int NJ, typename G, typename F>
 __device__ __forceinline__ void warp_product(uint32_t p, int ps, uint32_t q, int qs, int rows, int cols, int k, int warp,
-                                             int lane, F &&put)
+                                             int lane, G &&get, F &&put)
 {
     const int tj = (cols + 16 * NJ - 1) / (16 * NJ), tiles = (rows + 16 * MI - 1) / (16 * MI) * tj;
-    const int fr = lane >> 2, fc = 2 * (lane & 3);          // a fragment's row (and row + 8) and columns (two of eight)
     for (int t = warp; t < tiles; t += kWarps) {
         const int i0 = t / tj * 16 * MI, j0 = t % tj * 16 * NJ;
-        float acc[MI][NJ][2][4];
-        warp_block<TRANS, MI, NJ>(acc, p, ps, q, qs, i0, j0, rows, cols, k, lane);
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                if ((i == 0 || i0 + 16 * i < rows) && (j == 0 || j0 + 16 * j < cols))
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int r = 0; r < 2; ++r)
-                            put(i0 + 16 * i + fr + 8 * r, j0 + 16 * j + 8 * h + fc, acc[i][j][h][2 * r], acc[i][j][h][2 * r + 1]);
+        if (i0 + 16 * MI <= rows && j0 + 16 * NJ <= cols) {
+            warp_tile<TRANS, MI, NJ>(p, ps, q, qs, i0, j0, k, lane, get, put);
+        } else {
+            for (int i = i0; i < min(i0 + 16 * MI, rows); i += 16)
+                for (int j = j0; j < min(j0 + 16 * NJ, cols); j += 16) warp_tile<TRANS, 1, 1>(p, ps, q, qs, i, j, k, lane, get, put);
+        }
     }
 }
 
@@ -173,25 +189,33 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
     if (args.head && blockIdx.x == 0)
         for (int i = tid; i < args.head_ints; i += kThreads) args.head[i] = 0;
 
-    // this block's elements, threads along the contiguous axis of the matrix: element e of `count` (a row of it padded to 32)
-    // lies at (r, c) of the matrix; up to kAt a thread stay in registers from the norm to the conversion
+    // the elements (i, j) of this block's columns, threads along the contiguous axis of the matrix, eight loads in flight,
+    // eight rows of it at a time (zeros past the end)
     const T *g = (const T *)m.g + (tall ? (long long)c0 * m.ld_g : (long long)c0);
-    const unsigned outer = tall ? mine : n, inner = tall ? n : mine, width = (inner + 31) / 32 * 32, count = outer * width;
-    constexpr unsigned kAt = 24;
-    float v[kAt];
-    auto load = [&](unsigned from) {
+    constexpr int kAt = 8;
+    const int outer = tall ? mine : n, inner = tall ? n : mine;
+    auto each = [&](auto &&f) {
+        for (int r0 = warp; r0 < outer; r0 += kAt * kWarps)
+            for (int c = lane; c < inner; c += 32) {
+                float v[kAt];
 #pragma unroll
-        for (unsigned k = 0; k < kAt; ++k) {
-            const unsigned e = from + k * kThreads + tid, r = width ? e / width : 0, c = e - r * width;
-            v[k] = e < count && c < inner ? (float)g[(long long)r * m.ld_g + c] : 0.f;
-        }
+                for (int k = 0; k < kAt; ++k)
+                    v[k] = r0 + k * kWarps < outer ? (float)g[(long long)(r0 + k * kWarps) * m.ld_g + c] : 0.f;
+                f(r0, c, v);
+            }
     };
-    double sq = 0.0;
-    for (unsigned from = 0; from < count; from += kAt * kThreads) {
-        load(from);
+    double sq = 0.0;      // eight squares in fp32 where their sum is well inside its range, in fp64 otherwise
+    each([&](int, int, const float (&v)[kAt]) {
+        float t = 0.f;
 #pragma unroll
-        for (unsigned k = 0; k < kAt; ++k) sq = fma((double)v[k], (double)v[k], sq);
-    }
+        for (int k = 0; k < kAt; ++k) t = fmaf(v[k], v[k], t);
+        if (t >= 1e-30f && t <= 1e30f) {
+            sq += (double)t;
+        } else {
+#pragma unroll
+            for (int k = 0; k < kAt; ++k) sq = fma((double)v[k], (double)v[k], sq);
+        }
+    });
     // padding: zero rows and columns take part in the products
     for (int i = warp; i < np; i += kWarps)
         for (int j = (i < n ? mine : 0) + lane; j < L.xs; j += 32) {
@@ -217,20 +241,20 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
     double total = 0.0;
     for (int r = 0; r < C; ++r) total += block_sums[r];
     const float inv = (float)((double)kOrthScaleX / (sqrt(total) + (double)args.eps));
-    for (unsigned from = 0; from < count; from += kAt * kThreads) {
+    {
         __half *hi = reinterpret_cast<__half *>(smem + L.hi0);
-        if (count > kAt * kThreads) load(from);
+        const int step = kWarps * (tall ? 1 : L.xs);
+        each([&](int r0, int c, const float (&v)[kAt]) {
+            int at = tall ? c * L.xs + r0 : r0 * L.xs + c;
 #pragma unroll
-        for (unsigned k = 0; k < kAt; ++k) {
-            const unsigned e = from + k * kThreads + tid, r = e / width, c = e - r * width;
-            if (e < count && c < inner) {
-                const int at = tall ? c * L.xs + r : r * L.xs + c;
-                const float x = v[k] * inv;
-                const __half h = __float2half_rn(x);
-                hi[at] = h;
-                lo[at] = __float2half_rn(x - __half2float(h));
-            }
-        }
+            for (int k = 0; k < kAt; ++k, at += step)
+                if (r0 + k * kWarps < outer) {
+                    const float x = v[k] * inv;
+                    const __half h = __float2half_rn(x);
+                    hi[at] = h;
+                    lo[at] = __float2half_rn(x - __half2float(h));
+                }
+        });
     }
     __syncthreads();
 
@@ -243,12 +267,13 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
         const uint32_t cur = base + (uint32_t)cur_off;
         __half *A = reinterpret_cast<__half *>(smem + L.a), *B = reinterpret_cast<__half *>(smem + L.b);
         float *part = reinterpret_cast<float *>(smem + L.part);
-        auto put_gram = [&](int i, int j, float v0, float v1) {
+        auto get_none = [](int, int) { return 0u; };
+        auto put_gram = [&](int i, int j, float v0, float v1, uint32_t) {
             if (C == 1) *reinterpret_cast<uint32_t *>(A + i * L.as + j) = half2_bits(v0 * kGram, v1 * kGram);
             else *reinterpret_cast<float2 *>(part + i * np + j) = make_float2(v0, v1);
         };
-        if (large) warp_product<false, 2, 2>(cur, L.xs, cur, L.xs, np, np, per, warp, lane, put_gram);
-        else warp_product<false, 1, 2>(cur, L.xs, cur, L.xs, np, np, per, warp, lane, put_gram);
+        if (large) warp_product<false, 2, 2>(cur, L.xs, cur, L.xs, np, np, per, warp, lane, get_none, put_gram);
+        else warp_product<false, 1, 2>(cur, L.xs, cur, L.xs, np, np, per, warp, lane, get_none, put_gram);
         if (C > 1) {
             cluster_sync_all();
             // four neighbouring elements a thread, shares of the blocks interleaved
@@ -267,21 +292,22 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
             __syncthreads();
         }
         const uint32_t a_at = base + (uint32_t)L.a, b_at = base + (uint32_t)L.b;
-        auto put_poly = [&](int i, int j, float v0, float v1) {
-            const int at = i * L.as + j;
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(A + at));
-            *reinterpret_cast<uint32_t *>(B + at) = half2_bits(fmaf(beta, f.x, alpha * v0) + (i == j ? diagonal : 0.f),
+        auto get_poly = [&](int i, int j) { return *reinterpret_cast<const uint32_t *>(A + i * L.as + j); };
+        auto put_poly = [&](int i, int j, float v0, float v1, uint32_t in) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&in));
+            *reinterpret_cast<uint32_t *>(B + i * L.as + j) = half2_bits(fmaf(beta, f.x, alpha * v0) + (i == j ? diagonal : 0.f),
                                                                fmaf(beta, f.y, alpha * v1) + (i == j + 1 ? diagonal : 0.f));
         };
-        if (large) warp_product<false, 2, 2>(a_at, L.as, a_at, L.as, np, np, np, warp, lane, put_poly);
-        else warp_product<false, 1, 2>(a_at, L.as, a_at, L.as, np, np, np, warp, lane, put_poly);
+        if (large) warp_product<false, 2, 2>(a_at, L.as, a_at, L.as, np, np, np, warp, lane, get_poly, put_poly);
+        else warp_product<false, 1, 2>(a_at, L.as, a_at, L.as, np, np, np, warp, lane, get_poly, put_poly);
         __syncthreads();
         const bool last = it + 1 == args.steps;
         const float by = last ? m.scale / kOrthScaleX : 1.f;
         __half *next = reinterpret_cast<__half *>(smem + next_off);
-        auto put_step = [&](int i, int j, float v0, float v1) {
+        auto get_step = [&](int i, int j) { return *reinterpret_cast<const uint32_t *>(lo + i * L.xs + j); };
+        auto put_step = [&](int i, int j, float v0, float v1, uint32_t in) {
             const int at = i * L.xs + j;
-            const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(lo + at));
+            const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&in));
             v0 = fmaf(args.k[0], y.x, v0 * (1.f / kOrthScaleB));
             v1 = fmaf(args.k[0], y.y, v1 * (1.f / kOrthScaleB));
             if (last) {
@@ -293,8 +319,8 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
                 *reinterpret_cast<uint32_t *>(lo + at) = half2_bits(v0 - back.x, v1 - back.y);
             }
         };
-        if (large) warp_product<true, 2, 2>(b_at, L.as, cur, L.xs, np, per, np, warp, lane, put_step);
-        else warp_product<true, 1, 2>(b_at, L.as, cur, L.xs, np, per, np, warp, lane, put_step);
+        if (large) warp_product<true, 2, 2>(b_at, L.as, cur, L.xs, np, per, np, warp, lane, get_step, put_step);
+        else warp_product<true, 1, 2>(b_at, L.as, cur, L.xs, np, per, np, warp, lane, get_step, put_step);
         __syncthreads();
     }
     // the result lies as bf16 in the buffer the last iteration wrote
