@@ -463,8 +463,9 @@ void modse_debug_set_epilogue_warps(int mask_128, int mask_256, int mask_pair);
  * records MODSE_ERR_DEVICE_TIMEOUT in the status word, lets its copies in flight land, frees its tensor
  * memory and returns; modse_debug_set_wait_limit_ms changes the limit (1..60000).
  * modse_debug_skip_tile_loads(product, tile) makes the CTA that is handed tile `tile` of grouped product
- * `product` (0..5) issue no loads for it and stop producing, so that its consumers run into that limit with
- * nothing in flight; (-1, -1) switches it off.  For tests of the time-out path on tiny inputs.          */
+ * `product` (0..5; 6: the products of modse_linear, its gradient and modse_orthogonalize, whose `tile` counts
+ * a launch's work items) issue no loads for it and stop producing, so that its consumers run into that limit
+ * with nothing in flight; (-1, -1) switches it off.  For tests of the time-out path on tiny inputs.          */
 void modse_debug_set_wait_limit_ms(int ms);
 void modse_debug_skip_tile_loads(int product, int tile);
 

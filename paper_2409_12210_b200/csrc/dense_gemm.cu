@@ -63,6 +63,7 @@ template <int P> struct DenseParams {
     float *partial;
     unsigned long long wait_limit_ns;
     int clear_status;
+    int skip_item;       // debugging: the producers that get this item stop without loading it (-1: none)
     DenseColumnSum sum;
 };
 
@@ -489,7 +490,7 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
             bool ok = true;
             for (int round = 0; ok; ++round) {
                 const int item = dense_item<P>(round, cluster_id, n_clusters, prm.items);
-                if (item < 0) break;
+                if (item < 0 || item == prm.skip_item) break;
                 const DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
                 if (t.skip) continue;
                 const int flags = prm.prob[t.p].flags;
@@ -873,6 +874,7 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
     prm.wait_limit_ns = tc_wait_limit_ns();
     prm.clear_status = head == kDenseHeadRaw;
     prm.sum = sum ? *sum : DenseColumnSum{};
+    prm.skip_item = tc_skip_tile(kTcDenseProducts);
 
     auto kern = dense_gemm_pair<MODE, TYPE, TN, TALL, P>;
     static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)

@@ -87,6 +87,7 @@ void tc_set_dynamic_tiles(int on) { g_dynamic_tiles = on ? 1 : 0; }
 void tc_set_wait_limit_ms(int ms) { g_wait_limit_ms = ms < 1 ? 1 : (ms > 60000 ? 60000 : ms); }
 unsigned long long tc_wait_limit_ns() { return (unsigned long long)g_wait_limit_ms * 1000000ull; }
 void tc_set_skip_tile(int kind, int tile) { g_skip_kind = kind; g_skip_tile = tile; }
+int tc_skip_tile(int kind) { return g_skip_kind == kind ? g_skip_tile : -1; }
 void tc_set_epilogue_warps16(int narrow_mask, int wide_mask, int pair_mask)
 {
     g_epi16_narrow = narrow_mask & 63;

@@ -156,6 +156,30 @@ def test_backward(shape, act):
 
 
 @pytest.mark.gpu
+def test_512_row_tiles():
+    """Shapes whose products run on 512-row tiles: a ragged last tile with one 256-row half, column edges, a tail dealt out
+    as halves (forward) and two products in one launch with more than one round (backward)."""
+    from paper_2409_12210_b200 import binding as B
+    rng = np.random.default_rng(11)
+    T, k, n = 19300, 1544, 1000
+    x, w, b = rand(rng, T, k).bfloat16(), rand(rng, n, k, std=k ** -0.5).bfloat16(), rand(rng, n).bfloat16()
+    y, margin = guarded((T, n))
+    ws, ws_margin = workspace(B.linear_workspace_bytes(x.dtype, T, k, n))
+    B.linear(x, w, y, ws, bias=b, activation="relu")
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    ref = (x.double() @ w.double().T + b.double()).clamp_min(0)
+    mag = x.double().abs() @ w.double().abs().T + b.double().abs()
+    assert bool(((y.double() - ref).abs() <= BF * ref + (k + 64) * U * mag * (1 + BF)).all())
+    assert bool((margin == 3).all()) and bool((ws_margin == 0xA5).all())
+    T, k, n = 9300, 2056, 1544
+    x, w, dy, _, dx, dw, db = run_backward(T, k, n, "none")
+    X, W, G = x.double(), w.double(), dy.double()
+    for got, ref, mag, terms in ((dx, G @ W, G.abs() @ W.abs(), n), (dw, G.T @ X, G.abs().T @ X.abs(), T)):
+        assert bool(((got.double() - ref).abs() <= BF * ref.abs() + (terms + 64) * U * mag * (1 + BF)).all())
+    assert bool(((db.double() - G.sum(0)).abs() <= (T / 8 + 200) * U * G.abs().sum(0)).all())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("want", [("dx",), ("dw",), ("db",), ("dx", "db")])
 def test_backward_outputs_that_are_not_wanted_are_left_alone(want):
     full = run_backward(257, 648, 1032, "silu")
@@ -302,3 +326,29 @@ def test_refusals_need_no_gpu():
                 dict(dbias=p + 2), dict(ws=None), dict(ws=p + 16), dict(dx=None, dw=None, dbias=None)]:
         assert back(**bad) == inv, bad
     assert lib.modse_check_workspace_status(None, None) == inv
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,k", [(300, 256), (20000, 256), (18944, 1544)])
+def test_a_wait_that_runs_out_is_reported_and_the_gpu_stays_usable(T, k):
+    """The producers of one CTA pair are told to load nothing for one item: nothing of theirs is in flight, their consumers
+    give up after the (shortened) limit, the kernel returns and the host reads the time-out; the next call is correct."""
+    from paper_2409_12210_b200 import binding as B
+    rng = np.random.default_rng(9)
+    n = 1024 if k > 1000 else 512
+    x, w = rand(rng, T, k).bfloat16(), rand(rng, n, k, std=0.06).bfloat16()
+    y, ref = torch.empty(T, n, device="cuda").bfloat16(), torch.empty(T, n, device="cuda").bfloat16()
+    ws = torch.empty(B.linear_workspace_bytes(x.dtype, T, k, n), dtype=torch.uint8, device="cuda")
+    B.linear(x, w, ref, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    B.debug_set_wait_limit_ms(50)
+    B.debug_skip_tile_loads(6, 0)
+    try:
+        B.linear(x, w, y, ws)
+        assert B.check_workspace_status(ws) == B.MODSE_ERR_DEVICE_TIMEOUT
+    finally:
+        B.debug_set_wait_limit_ms(2000)
+        B.debug_skip_tile_loads(-1, -1)
+    B.linear(x, w, y, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    assert torch.equal(y, ref)
