@@ -99,18 +99,31 @@ __global__ void __launch_bounds__(256) square_sums_kernel(const __grid_constant_
     // inside it (what underflows beside it does not count), in fp64 otherwise, and all sums are fp64.
     double acc = 0.0;
     constexpr int kAt = 4;                    // vectors in flight
+    const bool whole = wide && m.cols % 8 == 0 && total <= 0x7FFFFFFF;
     const long long step = (long long)gridDim.x * 256;
     for (long long i0 = (long long)blockIdx.x * 256 + threadIdx.x; i0 < total; i0 += kAt * step) {
         float f[kAt][8];
+        if (whole && i0 + (kAt - 1) * step < total) {
+            // no branch between the loads: it would make each wait for the one before (88 us against 39 for 185 MB)
+            const T *at[kAt];
 #pragma unroll
-        for (int k = 0; k < kAt; ++k) {
-            const long long i = i0 + k * step;
-            if (i < total) {
-                const int r = row_of(i, vecs, total), c = 8 * (int)(i - (long long)r * vecs);
-                load8((const T *)m.g + r * m.ld + c, wide && c + 8 <= m.cols, m.cols - c, f[k]);
-            } else {
+            for (int k = 0; k < kAt; ++k) {
+                const unsigned i = (unsigned)(i0 + k * step);
+                at[k] = (const T *)m.g + (m.ld == m.cols ? 8ll * i : (long long)(i / (unsigned)vecs) * m.ld + 8 * (i % (unsigned)vecs));
+            }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[k][j] = 0.f;
+            for (int k = 0; k < kAt; ++k) load8(at[k], true, 8, f[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kAt; ++k) {
+                const long long i = i0 + k * step;
+                if (i < total) {
+                    const int r = (int)(i / vecs), c = 8 * (int)(i - (long long)r * vecs);
+                    load8((const T *)m.g + r * m.ld + c, wide && c + 8 <= m.cols, m.cols - c, f[k]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[k][j] = 0.f;
+                }
             }
         }
 #pragma unroll
