@@ -40,9 +40,10 @@ BURST_REGION_S = 1.0                   # timed regions shorter than this run on 
 # dram__bytes_read.sum + dram__bytes_write.sum per launch from the ncu captures summarised in
 # profiles/tc_grouped_gemm_pair_train_16k_ncu.md (one kernel and one launch per ncu run, --clock-control none);
 # valid only for that workload, for the library's default tile plan and for the kernel source they were taken
-# from (first 16 hex digits of the SHA-256 of csrc/tc_gemm.cu), otherwise "traffic" is reported as null.
+# from (first 16 hex digits of the SHA-256 of csrc/tc_gemm.cu followed by csrc/tc_device.h, into which the kernels'
+# building blocks moved unchanged since the capture), otherwise "traffic" is reported as null.
 NCU_TRAFFIC = {
-    "workload": "train_16k", "tc_gemm_sha256_16": "4025bd8c15f9c71a",
+    "workload": "train_16k", "tc_gemm_sha256_16": "cf8bb7ef1b49b5ba",
     "bytes_per_launch": {"upgate_gemm_swiglu": 1.592e9, "down_gemm": 1.022e9, "down_dgrad_swiglu_bwd": 1.849e9,
                          "down_wgrad": 0.688e9, "upgate_dgrad": 1.976e9, "upgate_wgrad": 1.244e9},
 }
@@ -53,8 +54,9 @@ def ncu_traffic(stage: str, workload: str):
     (the caller also drops it when a tile plan other than the captured default is in use)."""
     import hashlib
     try:
-        src = os.path.join(ROOT, "paper_2409_12210_b200", "csrc", "tc_gemm.cu")
-        digest = hashlib.sha256(open(src, "rb").read()).hexdigest()[:16]
+        src = os.path.join(ROOT, "paper_2409_12210_b200", "csrc")
+        digest = hashlib.sha256(b"".join(open(os.path.join(src, f), "rb").read()
+                                         for f in ("tc_gemm.cu", "tc_device.h"))).hexdigest()[:16]
     except OSError:
         return None
     if workload != NCU_TRAFFIC["workload"] or digest != NCU_TRAFFIC["tc_gemm_sha256_16"]:
