@@ -326,8 +326,9 @@ const char *modse_stage_name(int stage);
  * Outputs, each of them optional, at least one: sum (may be x or residual
  * itself), y, and y_e4m3 [T, d] bytes together with y_scale [T].  The norm is
  * taken from the fp32 sum, not from its rounding into `sum`; each output is
- * rounded once.  A row of zeros has scale 0 and zero bytes; a row that holds a NaN
- * has scale NaN.                                                             */
+ * rounded once.  A row of zeros has scale 0 and zero bytes (with eps > 0); a row
+ * that holds a NaN or an infinity has scale NaN.  Squares are summed in fp32:
+ * magnitudes above 1e19 overflow the mean.                                   */
 modse_status_t modse_add_rms_norm(modse_dtype_t dtype, int n_tokens, int d_model, const void *x, const void *residual,
                                   const void *weight, float eps, void *sum, void *y, void *y_e4m3, float *y_scale,
                                   void *cuda_stream);

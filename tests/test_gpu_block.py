@@ -134,3 +134,94 @@ def test_eight_bit_rows_from_the_norm_into_the_product():
         plain = (a / np.sqrt((a * a).mean(1, keepdims=True) + 1e-5) * f64(gamma)) @ f64(w).T
         typical = np.sqrt((plain * plain).mean() / 512)
         assert np.abs(f64(y) - plain).max() <= 5 * np.sqrt(512) * 2 ** -3 / np.sqrt(3) * typical
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 elements in a tensor: the last rows come out as they do on their own."""
+    from paper_2409_12210_b200 import binding as B
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    T, d = 1_050_003, 2056                                          # 2.16e9 elements
+    x = torch.empty(T, d, **bf)
+    x[-5:].normal_(generator=g)
+    x[:-5] = 1
+    w = torch.ones(d, **bf)
+    y, tail = torch.zeros(T, d, **bf), torch.empty(5, d, **bf)
+    B.add_rms_norm(x, None, w, 1e-5, y=y)
+    B.add_rms_norm(x[-5:].contiguous(), None, w, 1e-5, y=tail)
+    # another number of rows may take another shape of block, so sums may differ in their last bits: one bf16 step at most
+    assert torch.allclose(y[-5:].float(), tail.float(), rtol=2.0 ** -7, atol=0)
+    dw = torch.empty(d, device="cuda")
+    ws = torch.empty(B.add_rms_norm_backward_workspace_bytes(T, d), dtype=torch.uint8, device="cuda")
+    dx = y                                                          # the gradient over the norm's output
+    dy_tail, x_tail = y[-5:].clone(), x[-5:].clone()
+    B.add_rms_norm_backward(x, w, 1e-5, y, None, dx, dw, ws)
+    ref = torch.empty(5, d, **bf)
+    B.add_rms_norm_backward(x_tail, w, 1e-5, dy_tail, None, ref, None)      # no weight gradient: no workspace
+    scale = float(ref.float().abs().max())
+    assert float((dx[-5:].float() - ref.float()).abs().max()) <= 2.0 ** -7 * scale
+    del x, y, dx
+    T, k, n = 262_147, 64, 8200                                     # 2.15e9 outputs
+    x, w, b = torch.randn(T, k, generator=g, device="cuda").bfloat16(), torch.randn(n, k, generator=g, device="cuda").bfloat16(), torch.zeros(n, **bf)
+    y = torch.zeros(T, n, **bf)
+    ws = torch.empty(B.linear_workspace_bytes(x.dtype, T, k, n), dtype=torch.uint8, device="cuda")
+    r = torch.zeros(T, n, **bf)
+    r[-3:] = 1
+    B.linear(x, w, y, ws, bias=b, residual=r)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    ref = x[-3:].double() @ w.double().T + 1
+    assert bool(((y[-3:].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + 1e-3).all())
+    del r
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(n, device="cuda")
+    ws = torch.empty(B.linear_backward_workspace_bytes(T, k, n), dtype=torch.uint8, device="cuda")
+    B.linear_backward(x, w, y, y, "relu", dx, dw, db, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    dz = (y[-3:] * (y[-3:] > 0)).double()
+    ref, mag = dz @ w.double(), dz.abs() @ w.double().abs()
+    assert bool(((dx[-3:].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + (n + 64) * 2.0 ** -23 * mag).all())
+
+
+FIRST_CALLS = """
+import torch
+from paper_2409_12210_b200 import binding as B
+bf = dict(dtype=torch.bfloat16, device="cuda")
+x, w, g = torch.randn(300, 256, **bf), torch.randn(512, 256, **bf), torch.randn(256, **bf)
+s, y, dx, dg = torch.empty_like(x), torch.empty(300, 512, **bf), torch.empty_like(x), torch.empty(256, device="cuda")
+dw, db, u, t = torch.empty_like(w), torch.empty(512, device="cuda"), torch.empty_like(w), torch.empty(64, 96, **bf)
+u8 = lambda n: torch.empty(n, dtype=torch.uint8, device="cuda")
+w1, w2, w3 = u8(B.add_rms_norm_backward_workspace_bytes(300, 256)), u8(B.linear_workspace_bytes(x.dtype, 300, 256, 512)), u8(B.linear_backward_workspace_bytes(300, 256, 512))
+w4, w5 = u8(B.orthogonalize_workspace_bytes([(512, 256)])), u8(B.orthogonalize_workspace_bytes([(64, 96)]))
+m = torch.randn(64, 96, **bf)
+def block():
+    B.add_rms_norm(x, x, g, 1e-5, y=s)
+    B.linear(s, w, y, w2)
+    B.linear(s[:3], w, y[:3], w2)
+    B.linear_backward(s, w, y, y, "silu", dx, dw, db, w3)
+    B.add_rms_norm_backward(x, g, 1e-5, dx, None, dx, dg, w1)
+    B.orthogonalize([dw], [u], w4)
+    B.orthogonalize([m], [t], w5)
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    block()
+graph.replay()
+torch.cuda.synchronize()
+first = [v.clone() for v in (s, y, dx, dw, db, dg, u, t)]
+for v in (s, y, dx, dw, db, dg, u, t):
+    v.zero_()
+block()
+torch.cuda.synchronize()
+for a, b in zip(first, (s, y, dx, dw, db, dg, u, t)):
+    assert torch.equal(a, b) and bool(torch.isfinite(a.float()).all()) and bool((a != 0).any())
+print("same")
+"""
+
+
+def test_first_calls_of_a_process_inside_a_capture():
+    """Nothing has to be called once before it is captured, and a replay gives what the calls give."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and "same" in out.stdout, out.stderr[-2000:]
