@@ -17,6 +17,10 @@
 // arrives last at a 32-row strip adds the pieces of that strip in order (so the sum does not depend on who was last)
 // and runs the epilogue on it.
 //
+// Few tiles (at most 32).  Two or four pairs form a cluster that shares one tile: each multiplies its part of the
+// contraction, hands the column chunks of its accumulator that another pair finishes to that pair through distributed
+// shared memory (the stages are free by then), and adds up, in the pairs' order, and finishes its own.
+//
 // Every wait is bounded; one that expires records kDevTimeout in the status word and the CTAs drain and leave.
 #include <cuda_fp16.h>
 
@@ -59,6 +63,7 @@ template <int P> struct DenseParams {
     DenseProblem prob[P];
     LinearEpilogue lin;
     int n_prob, full_tiles, splits, items;   // tiles [0, full_tiles) are whole, the others cut into `splits` pieces
+    int share;                               // CTA pairs of a cluster that share a tile (1: none)
     int *status, *counters;
     float *partial;
     unsigned long long wait_limit_ns;
@@ -136,6 +141,14 @@ __device__ __forceinline__ DenseTile dense_decode(const DenseParams<P> &prm, int
         t.kb1 = (int)((long long)q.nk * (t.split + 1) / prm.splits);
     }
     return t;
+}
+
+// A pair's part of the contraction of a tile that a cluster shares.
+__device__ __forceinline__ void take_share(DenseTile &t, int sharer, int share)
+{
+    const int n = t.kb1;
+    t.kb0 = n * sharer / share;
+    t.kb1 = n * (sharer + 1) / share;
 }
 
 // ---- epilogue pieces: a warp holds 32 rows x 32 columns, one row a lane ----
@@ -427,9 +440,20 @@ __device__ __forceinline__ uint32_t dense_idesc(bool a_mn, bool b_mn, int n)
            ((uint32_t)(n >> 3) << 17) | (16u << 24);
 }
 
-template <int MODE, int TYPE, int TN, bool TALL, int P>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kDenseThreads, 1)
-dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
+// Arrives on the barrier at the same offset in both CTAs of a pair (mask: their ranks in the cluster) once the MMAs issued
+// so far are done.
+__device__ __forceinline__ void commit_to(uint32_t bar, uint32_t mask)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((unsigned short)mask) : "memory");
+}
+__device__ __forceinline__ void st_cluster_f4(uint32_t addr, const float4 &v)
+{
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+
+template <int MODE, int TYPE, int TN, bool TALL, bool SHARED, int P>
+__device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
 {
     using Sh = DenseShape<TALL>;
     constexpr int kStages = Sh::kStages;
@@ -442,8 +466,10 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
     DenseTail *st = reinterpret_cast<DenseTail *>(epi_bufs + kDenseEpiWarps * kDenseEpiBytes);
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int rank = (int)cluster_ctarank();
-    const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+    const int in_cluster = (int)cluster_ctarank(), rank = in_cluster & 1, leader = SHARED ? in_cluster & ~1 : 0, sharer = in_cluster >> 1;
+    const int share = SHARED ? prm.share : 1;
+    const int cluster_id = SHARED ? blockIdx.x / (2 * share) : blockIdx.x >> 1, n_clusters = SHARED ? gridDim.x / (2 * share) : gridDim.x >> 1;
+    const uint32_t pair_mask = 3u << leader;
     constexpr int kElems = TYPE == DenseE4m3 ? 128 : 64;       // elements in 128 bytes
     constexpr int kHalf = TN / 2;                              // column-operand rows staged by each CTA
     constexpr uint32_t kColsAt = TALL ? 2 * kDenseRows : kDenseRows;      // column operand inside a stage
@@ -491,7 +517,8 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
             for (int round = 0; ok; ++round) {
                 const int item = dense_item<P>(round, cluster_id, n_clusters, prm.items);
                 if (item < 0 || item == prm.skip_item) break;
-                const DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
+                DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
+                if constexpr (SHARED) take_share(t, sharer, share);
                 if (t.skip) continue;
                 const int flags = prm.prob[t.p].flags;
                 const CUtensorMap *am = &prm.a[t.p], *bm = &prm.b[t.p];
@@ -499,7 +526,7 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
                 const uint32_t bytes = 2u * (halves * kDenseRows + kHalf * 128u);      // of both CTAs
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if (!mbar_wait(smem_u32(&st->empty[stage]), phase ^ 1u, wc)) { ok = false; break; }
-                    const uint32_t bar = map_to_cta(smem_u32(&st->full[stage]), 0);
+                    const uint32_t bar = map_to_cta(smem_u32(&st->full[stage]), leader);
                     if (rank == 0) mbar_arrive_expect_tx(smem_u32(&st->full[stage]), bytes);
                     const uint32_t dst = stage_base + stage * Sh::kStageBytes;
                     for (int h = 0; h < halves; ++h) {
@@ -544,7 +571,8 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
             for (int round = 0; ok; ++round) {
                 const int item = dense_item<P>(round, cluster_id, n_clusters, prm.items);
                 if (item < 0) break;
-                const DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
+                DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
+                if constexpr (SHARED) take_share(t, sharer, share);
                 if (t.skip) continue;
                 const int flags = prm.prob[t.p].flags;
                 const bool a_mn = (flags & kDenseAMn) != 0, b_mn = (flags & kDenseBMn) != 0;
@@ -573,11 +601,11 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
                         if (!mbar_wait(smem_u32(&st->full[stage]), phase, wc)) { ok = false; break; }
                         tc_fence_after();
                         multiply(stage, 0, tmem_base + (uint32_t)(acc * kDenseAccCols), kb == t.kb0);
-                        umma_commit_pair(smem_u32(&st->empty[stage]));
+                        commit_to(smem_u32(&st->empty[stage]), pair_mask);
                         if (++stage == kStages) { stage = 0; phase ^= 1u; }
                     }
                     if (!ok) break;
-                    umma_commit_pair(smem_u32(&st->tmem_full[acc]));
+                    commit_to(smem_u32(&st->tmem_full[acc]), pair_mask);
                 } else {
                     if (!mbar_wait(smem_u32(&st->tmem_empty[0]), (used0 & 1u) ^ 1u, wc)) { ok = false; break; }
                     ++used0;
@@ -596,13 +624,13 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
                             if (++s == kStages) { s = 0; ph ^= 1u; }
                         }
                         if (!ok) break;
-                        if (t.kb0 + ahead == t.kb1) umma_commit_pair(smem_u32(&st->tmem_full[0]));
+                        if (t.kb0 + ahead == t.kb1) commit_to(smem_u32(&st->tmem_full[0]), pair_mask);
                         if (!mbar_wait(smem_u32(&st->tmem_empty[1]), (used1 & 1u) ^ 1u, wc)) { ok = false; break; }
                         ++used1;
                         tc_fence_after();
                         for (int i = 0; i < ahead; ++i) {
                             multiply(stage, 1, tmem_base + kDenseAccCols, i == 0);
-                            umma_commit_pair(smem_u32(&st->empty[stage]));
+                            commit_to(smem_u32(&st->empty[stage]), pair_mask);
                             if (++stage == kStages) { stage = 0; phase ^= 1u; }
                         }
                         kb += ahead;
@@ -611,13 +639,13 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
                         if (!mbar_wait(smem_u32(&st->full[stage]), phase, wc)) { ok = false; break; }
                         tc_fence_after();
                         multiply(stage, 0, tmem_base, kb == t.kb0);
-                        if (kb + 1 == t.kb1) umma_commit_pair(smem_u32(&st->tmem_full[0]));
+                        if (kb + 1 == t.kb1) commit_to(smem_u32(&st->tmem_full[0]), pair_mask);
                         if (t.two) multiply(stage, 1, tmem_base + kDenseAccCols, false);
-                        umma_commit_pair(smem_u32(&st->empty[stage]));
+                        commit_to(smem_u32(&st->empty[stage]), pair_mask);
                         if (++stage == kStages) { stage = 0; phase ^= 1u; }
                     }
                     if (!ok) break;
-                    if (t.two) umma_commit_pair(smem_u32(&st->tmem_full[1]));
+                    if (t.two) commit_to(smem_u32(&st->tmem_full[1]), pair_mask);
                 }
             }
         }
@@ -637,8 +665,8 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
         const int quad = warp & 3;                          // tensor-memory lanes this warp may read
         const int cq = (warp - kDenseFirstEpi) >> 2;        // which half of the tile's columns
         Staging stg{epi_bufs + (warp - kDenseFirstEpi) * kDenseEpiBytes, 0};
-        const uint32_t leader_empty0 = map_to_cta(smem_u32(&st->tmem_empty[0]), 0);
-        const uint32_t leader_empty1 = map_to_cta(smem_u32(&st->tmem_empty[1]), 0);
+        const uint32_t leader_empty0 = map_to_cta(smem_u32(&st->tmem_empty[0]), leader);
+        const uint32_t leader_empty1 = map_to_cta(smem_u32(&st->tmem_empty[1]), leader);
         constexpr int kChunks = TN / 64;                    // 32-column chunks a warp owns
         constexpr bool kF8 = TYPE == DenseE4m3;
         int cursor = 0, it = 0;
@@ -647,7 +675,8 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
         for (int round = 0; ok; ++round) {
             const int item = dense_item<P>(round, cluster_id, n_clusters, prm.items);
             if (item < 0) break;
-            const DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
+            DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
+                if constexpr (SHARED) take_share(t, sharer, share);
             if (t.skip) continue;
             const DenseProblem &q = prm.prob[t.p];
             const CUtensorMap *o0 = &prm.o0[t.p], *o1 = &prm.o1[t.p];
@@ -657,10 +686,11 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
                 const int acc = TALL ? h : first, r0 = t.m0 + 256 * h + rank * 128 + quad * 32;
                 const bool any = r0 < q.M && c0 < q.N;
                 ChunkInputs<MODE, kF8> in;
-                if (any && t.tail < 0) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
+                if (any && t.tail < 0 && !SHARED) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
                 if (!mbar_wait(smem_u32(&st->tmem_full[acc]), (acc ? used1 : used0) & 1u, wc)) { ok = false; break; }
                 if (acc) ++used1; else ++used0;
                 tc_fence_after();
+                if constexpr (SHARED) continue;              // finished below, together with the other pairs
                 const uint32_t tacc = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * kDenseAccCols + cq * kHalf);
                 // a cut tile's strip: 32 rows x kHalf columns, float4 j of all lanes side by side
                 constexpr size_t kStrip = 32 * kHalf / 4, kPiece = 2 * kDenseEpiWarps * kStrip;
@@ -722,7 +752,77 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
                 }
             }
         }
-        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // the outputs have left shared memory
+        if (!SHARED && lane == 0)
+            asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // the outputs have left shared memory
+    }
+
+    // ---- a tile shared by the pairs of a cluster (one item a cluster; every thread meets twice) ----
+    if constexpr (SHARED) {
+        constexpr int kChunks = TN / 64;                // 32-column chunks a warp reads
+        constexpr uint32_t kChunkBytes = 32 * 32 * 4;
+        int cursor = 0;
+        const DenseTile t = dense_decode<TN, TALL, P>(prm, cluster_id, cursor);
+        const DenseProblem &q = prm.prob[t.p];
+        const int quad = warp & 3, cq = (warp - kDenseFirstEpi) >> 2;
+        const int r0 = t.m0 + rank * 128 + quad * 32, c0 = t.n0 + cq * kHalf;
+        const bool works = warp >= kDenseFirstEpi && r0 < q.M;
+        const uint32_t tacc = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(cq * kHalf);
+        // chunk ch of the tile's TN / 32 belongs to pair ch % share; a pair's chunks lie in its stages by sender and place
+        auto slot = [&](int sender, int ch) {
+            return stage_base + (uint32_t)(((sender * (TN / 32 / share) + ch / share) * 4 + quad) * kChunkBytes) + lane * 16;
+        };
+        __syncwarp();
+        tc_fence_before();
+        cluster_sync_all();                             // every pair's products are done: the stages are free
+        tc_fence_after();
+        if (works)
+#pragma unroll 1
+            for (int c = 0; c < kChunks; ++c) {
+                const int ch = cq * kChunks + c, owner = ch % share;
+                if (c0 + 32 * c >= q.N || owner == sharer) continue;
+                uint32_t w[32];
+                tmem_ld32(tacc + 32 * c, w);
+                tmem_ld_wait();
+                const uint32_t to = map_to_cta(slot(sharer, ch), 2 * owner + rank);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    st_cluster_f4(to + 512 * j, make_float4(__uint_as_float(w[4 * j]), __uint_as_float(w[4 * j + 1]),
+                                                            __uint_as_float(w[4 * j + 2]), __uint_as_float(w[4 * j + 3])));
+            }
+        __syncwarp();
+        cluster_sync_all();                             // what the others sent has arrived
+        if (works) {
+            Staging stg{epi_bufs + (warp - kDenseFirstEpi) * kDenseEpiBytes, 0};
+#pragma unroll 1
+            for (int c = 0; c < kChunks; ++c) {
+                const int ch = cq * kChunks + c;
+                if (c0 + 32 * c >= q.N || ch % share != sharer) continue;
+                ChunkInputs<MODE, TYPE == DenseE4m3> in;
+                chunk_load<kLoadAll>(in, q, prm.lin, r0, c0 + 32 * c, lane);
+                uint32_t w[32];
+                tmem_ld32(tacc + 32 * c, w);
+                tmem_ld_wait();
+                float v[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = 0.f;
+#pragma unroll 1
+                for (int s = 0; s < share; ++s) {
+                    if (s == sharer) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(w[i]);
+                    } else {
+                        const float4 *src = reinterpret_cast<const float4 *>(smem + (slot(s, ch) - stage_base));
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const float4 f = src[32 * j];
+                            v[4 * j] += f.x; v[4 * j + 1] += f.y; v[4 * j + 2] += f.z; v[4 * j + 3] += f.w;
+                        }
+                    }
+                }
+                chunk_finish(in, q, prm.lin, &prm.o0[t.p], &prm.o1[t.p], r0, c0 + 32 * c, q.N, lane, stg, v);
+            }
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        }
     }
 
     // ---- teardown: neither CTA leaves while its partner may still touch its shared or tensor memory ----
@@ -733,6 +833,19 @@ dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kDenseTmemCols) : "memory");
     }
+}
+
+template <int MODE, int TYPE, int TN, bool TALL, int P>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kDenseThreads, 1)
+dense_gemm_pair(const __grid_constant__ DenseParams<P> prm)
+{
+    dense_gemm_body<MODE, TYPE, TN, TALL, false, P>(prm);
+}
+// clusters of prm.share pairs, one tile each
+template <int MODE, int TYPE, int TN, int P>
+__global__ void __launch_bounds__(kDenseThreads, 1) dense_gemm_shared(const __grid_constant__ DenseParams<P> prm)
+{
+    dense_gemm_body<MODE, TYPE, TN, false, true, P>(prm);
 }
 
 // A 2-D tensor map: `cols` contiguous elements a row, boxes of 128 bytes x box_rows rows, 128-byte swizzle.
@@ -764,10 +877,14 @@ bool encode_output(CUtensorMap *map, const void *base, long long rows, long long
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Tiles up to which clusters of two and of four pairs all find room at once (with 16 clusters of four the last ones waited
+// for a place: 2048 x 2048, 64 tokens 19 us against 14).
+constexpr int kDenseShare2 = 32, kDenseShare4 = 12;
+
 // How a launch is cut: tile shape, whole tiles, pieces of the rest.
 struct DensePlan {
     bool tall;
-    int tn, tiles, full, splits, items;
+    int tn, tiles, full, splits, items, share;
 };
 
 int dense_nk(DenseType type, long long k) { return (int)((k + (type == DenseE4m3 ? 127 : 63)) / (type == DenseE4m3 ? 128 : 64)); }
@@ -790,6 +907,7 @@ DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int
         return tiles;
     };
     DensePlan pl;
+    pl.share = 1;
     // Tall tiles where they fill the GPU at least once and the epilogue that shows is a light one (a conversion and a store;
     // `light`) behind a long main loop.  A round of them takes about 1024 x 1.05 clocks a k-block and the epilogue, a round
     // of 256-row tiles 585 a k-block.  Measured, tall against not: dx and dw of 16384 x 2048 -> 5632 504 against 580 us,
@@ -824,11 +942,25 @@ DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int
         const long long sp = std::min<long long>({std::min(pairs, kDenseMaxSplitItems) / left, least_nk / 16, 16, held / left});
         pl.splits = (int)std::max<long long>(1, sp);
     }
+    // Few tiles: two or four pairs of a cluster on each, where that beats cutting the tiles (in us: 0.33 a k-block, 2 for
+    // the cluster's two meetings, 4.5 for joining pieces through memory).  Measured, shared against cut or whole: 2048 x
+    // 2048 11.3 against 14.7 us with 64 tokens and 12.9 against 16.1 with 512; 8448 x 1024 from 8-bit rows 12.9 against 17.5.
+    if (pl.full == 0 && pl.tn == 128) {
+        double best = pl.splits > 1 ? 0.33 * least_nk / pl.splits + 4.5 : 0.33 * least_nk;
+        for (int share = 2; share <= 4; share *= 2) {
+            const double cost = 0.33 * least_nk / share + 2.0;
+            if (pl.tiles <= (share == 2 ? kDenseShare2 : kDenseShare4) * pairs / 74 && least_nk >= 2 * share && cost < best) {
+                best = cost;
+                pl.share = share;
+                pl.splits = 1;
+            }
+        }
+    }
     pl.items = pl.full + left * pl.splits;
     return pl;
 }
 
-template <int MODE, int TYPE, int TN, bool TALL, int P>
+template <int MODE, int TYPE, int TN, bool TALL, bool SHARED, int P>
 cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const LinearEpilogue *lin, const DenseColumnSum *sum, void *ws, int head, cudaStream_t s)
 {
     DenseParams<P> prm;
@@ -868,6 +1000,7 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
     prm.full_tiles = pl.full;
     prm.splits = pl.splits;
     prm.items = pl.items;
+    prm.share = pl.share;
     prm.status = (int *)ws;
     prm.counters = (int *)((unsigned char *)ws + kDenseCounterOffset);
     prm.partial = (float *)((unsigned char *)ws + kDenseHead);
@@ -876,7 +1009,9 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
     prm.sum = sum ? *sum : DenseColumnSum{};
     prm.skip_item = tc_skip_tile(kTcDenseProducts);
 
-    auto kern = dense_gemm_pair<MODE, TYPE, TN, TALL, P>;
+    void (*kern)(DenseParams<P>);
+    if constexpr (SHARED) kern = dense_gemm_shared<MODE, TYPE, TN, P>;
+    else kern = dense_gemm_pair<MODE, TYPE, TN, TALL, P>;
     static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -890,6 +1025,7 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
         e = cudaMemsetAsync(ws, 0, kDenseZeroBytes, s);
         if (e != cudaSuccess) return e;
     }
+    if constexpr (SHARED) return launch_clusters(kern, 2 * pl.share, 2 * pl.share * prm.items, kDenseThreads, kDenseSmem, s, prm);
     return launch_overlapped(kern, 2 * std::min(pairs, prm.items), kDenseThreads, kDenseSmem, s, prm);
 }
 
@@ -900,9 +1036,11 @@ cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin
     const bool light = MODE == DensePlain || (MODE == DenseLinear && TYPE == DenseBf16 && !lin->residual && !lin->z && lin->act <= MODSE_ACT_RELU);
     const DensePlan pl = dense_plan((DenseMode)MODE, (DenseType)TYPE, items, n, light, device_sms(), cap);
     if constexpr (MODE == DensePlain || (MODE == DenseLinear && TYPE == DenseBf16))
-        if (pl.tall) return launch_tn<MODE, TYPE, 256, true, P>(pl, items, n, lin, sum, ws, head, s);
-    if (pl.tn == 128) return launch_tn<MODE, TYPE, 128, false, P>(pl, items, n, lin, sum, ws, head, s);
-    return launch_tn<MODE, TYPE, 256, false, P>(pl, items, n, lin, sum, ws, head, s);
+        if (pl.tall) return launch_tn<MODE, TYPE, 256, true, false, P>(pl, items, n, lin, sum, ws, head, s);
+    if (pl.share > 1)       // so few tiles are 128 columns wide
+        return launch_tn<MODE, TYPE, 128, false, true, P>(pl, items, n, lin, sum, ws, head, s);
+    if (pl.tn == 128) return launch_tn<MODE, TYPE, 128, false, false, P>(pl, items, n, lin, sum, ws, head, s);
+    return launch_tn<MODE, TYPE, 256, false, false, P>(pl, items, n, lin, sum, ws, head, s);
 }
 
 }  // namespace

@@ -348,20 +348,7 @@ cudaError_t launch(const SmallArgs &a, int n, int cluster, size_t smem, cudaStre
         if (e != cudaSuccess) return e;
         if (dev <= 63) attr_done |= 1ull << dev;
     }
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(n * cluster);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = s;
-    cudaLaunchAttribute at[2]{};
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = cluster;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kern, a);
+    return launch_clusters(kern, cluster, n * cluster, kThreads, smem, s, a);
 }
 
 size_t smem_of(int rows, int cols, int cluster)

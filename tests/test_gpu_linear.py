@@ -329,7 +329,7 @@ def test_refusals_need_no_gpu():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T,k", [(300, 256), (20000, 256), (18944, 1544)])
+@pytest.mark.parametrize("T,k", [(300, 256), (300, 2048), (20000, 256), (18944, 1544)])
 def test_a_wait_that_runs_out_is_reported_and_the_gpu_stays_usable(T, k):
     """The producers of one CTA pair are told to load nothing for one item: nothing of theirs is in flight, their consumers
     give up after the (shortened) limit, the kernel returns and the host reads the time-out; the next call is correct."""
