@@ -18,7 +18,8 @@ ACTS = ["none", "relu", "gelu", "silu"]
 BF, U = 2.0 ** -8, 2.0 ** -23
 # (T, d_in, d_out): one token, few, ragged tiles, one tile over, several tiles with a tail, many tiles
 SHAPES = [(1, 8, 8), (1, 2048, 2048), (3, 136, 264), (17, 4096, 24), (32, 512, 1000), (33, 64, 136), (64, 1024, 4096),
-          (127, 200, 72), (129, 80, 520), (257, 648, 1032), (300, 2816, 2048), (1000, 256, 384), (2500, 512, 2048)]
+          (127, 200, 72), (129, 80, 520), (257, 648, 1032), (300, 2816, 2048), (1000, 256, 384), (2500, 512, 2048),
+          (200, 2048, 264), (1100, 72, 1032), (1100, 136, 1032)]      # tiles shared by two and by four pairs of CTAs
 
 
 def f64(t):
