@@ -676,7 +676,7 @@ __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
             const int item = dense_item<P>(round, cluster_id, n_clusters, prm.items);
             if (item < 0) break;
             DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
-                if constexpr (SHARED) take_share(t, sharer, share);
+            if constexpr (SHARED) take_share(t, sharer, share);
             if (t.skip) continue;
             const DenseProblem &q = prm.prob[t.p];
             const CUtensorMap *o0 = &prm.o0[t.p], *o1 = &prm.o1[t.p];

@@ -5,14 +5,14 @@
 
 namespace modse {
 
-// A kernel launched by launch_overlapped sets itself up (barriers, tensor memory, address arithmetic) while the kernel
-// ahead of it drains, and calls wait_for_earlier_kernels before it touches global memory: from there on everything the
-// stream held before it has completed and is visible.  A kernel that calls allow_next_kernel lets one launched this way
-// start its set-up as soon as SMs have room; without the call it may start when the blocks have left.
+// A kernel launched by launch_overlapped or launch_clusters sets itself up (barriers, tensor memory, address arithmetic)
+// while the kernel ahead of it drains, and calls wait_for_earlier_kernels before it touches global memory: from there on
+// everything the stream held before it has completed and is visible.  A kernel that calls allow_next_kernel lets one
+// launched this way start its set-up as soon as SMs have room; without the call it may start when the blocks have left.
 __device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
-// The same with blocks in clusters of `cluster`.
+// Such a launch, with blocks in clusters of `cluster`.
 template <typename... P, typename... A>
 cudaError_t launch_clusters(void (*kern)(P...), int cluster, dim3 grid, dim3 block, size_t smem, cudaStream_t s, A &&...args)
 {
