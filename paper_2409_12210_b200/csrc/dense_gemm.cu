@@ -19,7 +19,8 @@
 //
 // Few tiles (at most 32).  Two or four pairs form a cluster that shares one tile: each multiplies its part of the
 // contraction, hands the column chunks of its accumulator that another pair finishes to that pair through distributed
-// shared memory (the stages are free by then), and adds up, in the pairs' order, and finishes its own.
+// shared memory (into what the 128-column tile leaves free of each stage), and adds up, in the pairs' order, and finishes
+// its own.
 //
 // Every wait is bounded; one that expires records kDevTimeout in the status word and the CTAs drain and leave.
 #include <cuda_fp16.h>
@@ -452,6 +453,79 @@ __device__ __forceinline__ void st_cluster_f4(uint32_t addr, const float4 &v)
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
+// The epilogue warps of a tile that the pairs of a cluster share (one item a cluster): chunk ch of its TN / 32 column chunks
+// is finished by pair ch % share.  What the other pairs send lies in the 8 KB that a stage of a 128-column tile leaves
+// free, where no copy of the main loop writes, so that a warp sends as soon as its pair's products are done.
+template <int MODE, int TYPE, int TN, int P>
+__device__ __forceinline__ void finish_shared(const DenseParams<P> &prm, unsigned char *smem, uint32_t stage_base, DenseTail *st,
+                                              const WaitCtx &wc, uint32_t tmem_base, int item, int sharer, int rank, int warp, int lane)
+{
+    using Sh = DenseShape<false>;
+    constexpr int kChunks = TN / 64;                // 32-column chunks a warp reads; of them it finishes one at most
+    constexpr uint32_t kChunkBytes = 32 * 32 * 4, kFreeAt = kDenseRows + TN / 2 * 128;
+    static_assert(kFreeAt + 2 * kChunkBytes == Sh::kStageBytes && Sh::kStages * 2 >= 3 * 4 && kChunks == 2, "slots");
+    const int share = prm.share;
+    int cursor = 0;
+    const DenseTile t = dense_decode<TN, false, P>(prm, item, cursor);
+    const DenseProblem &q = prm.prob[t.p];
+    const int quad = warp & 3, cq = (warp - kDenseFirstEpi) >> 2;
+    const int r0 = t.m0 + rank * 128 + quad * 32, c0 = t.n0 + cq * (TN / 2);
+    const uint32_t tacc = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(cq * (TN / 2));
+    // what pair `sender` has of chunk ch, in the shared memory of the pair that finishes it
+    auto slot = [&](int sender, int ch) {
+        const int k = ((sender - (sender > ch % share)) * (TN / 32 / share) + ch / share) * 4 + quad;
+        return (uint32_t)((k >> 1) * Sh::kStageBytes + kFreeAt + (k & 1) * kChunkBytes + lane * 16);
+    };
+    int own = -1;
+    for (int c = 0; c < kChunks; ++c)
+        if ((cq * kChunks + c) % share == sharer && c0 + 32 * c < q.N && r0 < q.M) own = c;
+    ChunkInputs<MODE, TYPE == DenseE4m3> in;
+    if (own >= 0) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0 + 32 * own, lane);
+    const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&st->tmem_full[0]), 0, wc));
+    tc_fence_after();
+    if (ok && r0 < q.M)
+#pragma unroll 1
+        for (int c = 0; c < kChunks; ++c) {
+            const int ch = cq * kChunks + c, owner = ch % share;
+            if (c0 + 32 * c >= q.N || owner == sharer) continue;
+            uint32_t w[32];
+            tmem_ld32(tacc + 32 * c, w);
+            tmem_ld_wait();
+            const uint32_t to = map_to_cta(stage_base + slot(sharer, ch), 2 * owner + rank);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                st_cluster_f4(to + 512 * j, make_float4(__uint_as_float(w[4 * j]), __uint_as_float(w[4 * j + 1]),
+                                                        __uint_as_float(w[4 * j + 2]), __uint_as_float(w[4 * j + 3])));
+        }
+    __syncwarp();
+    cluster_sync_all();                             // what the others sent has arrived
+    if (!ok || own < 0) return;
+    Staging stg{smem + (size_t)Sh::kStages * Sh::kStageBytes + (warp - kDenseFirstEpi) * kDenseEpiBytes, 0};
+    const int ch = cq * kChunks + own;
+    uint32_t w[32];
+    tmem_ld32(tacc + 32 * own, w);
+    tmem_ld_wait();
+    float v[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = 0.f;
+#pragma unroll 1
+    for (int s = 0; s < share; ++s) {
+        if (s == sharer) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(w[i]);
+        } else {
+            const float4 *src = reinterpret_cast<const float4 *>(smem + slot(s, ch));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float4 f = src[32 * j];
+                v[4 * j] += f.x; v[4 * j + 1] += f.y; v[4 * j + 2] += f.z; v[4 * j + 3] += f.w;
+            }
+        }
+    }
+    chunk_finish(in, q, prm.lin, &prm.o0[t.p], &prm.o1[t.p], r0, c0 + 32 * own, q.N, lane, stg, v);
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
 template <int MODE, int TYPE, int TN, bool TALL, bool SHARED, int P>
 __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
 {
@@ -660,6 +734,8 @@ __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
                 prm.sum.out[c] = t;
             }
         }
+    } else if constexpr (SHARED) {
+        finish_shared<MODE, TYPE, TN>(prm, smem, stage_base, st, wc, tmem_base, cluster_id, sharer, rank, warp, lane);
     } else {
         // ===================== epilogue (both CTAs) =====================
         const int quad = warp & 3;                          // tensor-memory lanes this warp may read
@@ -675,8 +751,7 @@ __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
         for (int round = 0; ok; ++round) {
             const int item = dense_item<P>(round, cluster_id, n_clusters, prm.items);
             if (item < 0) break;
-            DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
-            if constexpr (SHARED) take_share(t, sharer, share);
+            const DenseTile t = dense_decode<TN, TALL, P>(prm, item, cursor);
             if (t.skip) continue;
             const DenseProblem &q = prm.prob[t.p];
             const CUtensorMap *o0 = &prm.o0[t.p], *o1 = &prm.o1[t.p];
@@ -686,11 +761,10 @@ __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
                 const int acc = TALL ? h : first, r0 = t.m0 + 256 * h + rank * 128 + quad * 32;
                 const bool any = r0 < q.M && c0 < q.N;
                 ChunkInputs<MODE, kF8> in;
-                if (any && t.tail < 0 && !SHARED) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
-                if (!mbar_wait(smem_u32(&st->tmem_full[acc]), (acc ? used1 : used0) & 1u, wc)) { ok = false; break; }
+                if (any && t.tail < 0) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&st->tmem_full[acc]), (acc ? used1 : used0) & 1u, wc))) { ok = false; break; }
                 if (acc) ++used1; else ++used0;
                 tc_fence_after();
-                if constexpr (SHARED) continue;              // finished below, together with the other pairs
                 const uint32_t tacc = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(acc * kDenseAccCols + cq * kHalf);
                 // a cut tile's strip: 32 rows x kHalf columns, float4 j of all lanes side by side
                 constexpr size_t kStrip = 32 * kHalf / 4, kPiece = 2 * kDenseEpiWarps * kStrip;
@@ -752,77 +826,14 @@ __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
                 }
             }
         }
-        if (!SHARED && lane == 0)
+        if (lane == 0)
             asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");     // the outputs have left shared memory
     }
 
-    // ---- a tile shared by the pairs of a cluster (one item a cluster; every thread meets twice) ----
-    if constexpr (SHARED) {
-        constexpr int kChunks = TN / 64;                // 32-column chunks a warp reads
-        constexpr uint32_t kChunkBytes = 32 * 32 * 4;
-        int cursor = 0;
-        const DenseTile t = dense_decode<TN, TALL, P>(prm, cluster_id, cursor);
-        const DenseProblem &q = prm.prob[t.p];
-        const int quad = warp & 3, cq = (warp - kDenseFirstEpi) >> 2;
-        const int r0 = t.m0 + rank * 128 + quad * 32, c0 = t.n0 + cq * kHalf;
-        const bool works = warp >= kDenseFirstEpi && r0 < q.M;
-        const uint32_t tacc = tmem_base + ((uint32_t)(quad * 32) << 16) + (uint32_t)(cq * kHalf);
-        // chunk ch of the tile's TN / 32 belongs to pair ch % share; a pair's chunks lie in its stages by sender and place
-        auto slot = [&](int sender, int ch) {
-            return stage_base + (uint32_t)(((sender * (TN / 32 / share) + ch / share) * 4 + quad) * kChunkBytes) + lane * 16;
-        };
+    // the warps that finish a shared tile meet the other pairs' in the middle of it; the rest of the warps join them there
+    if (SHARED && warp < kDenseFirstEpi) {
         __syncwarp();
-        tc_fence_before();
-        cluster_sync_all();                             // every pair's products are done: the stages are free
-        tc_fence_after();
-        if (works)
-#pragma unroll 1
-            for (int c = 0; c < kChunks; ++c) {
-                const int ch = cq * kChunks + c, owner = ch % share;
-                if (c0 + 32 * c >= q.N || owner == sharer) continue;
-                uint32_t w[32];
-                tmem_ld32(tacc + 32 * c, w);
-                tmem_ld_wait();
-                const uint32_t to = map_to_cta(slot(sharer, ch), 2 * owner + rank);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    st_cluster_f4(to + 512 * j, make_float4(__uint_as_float(w[4 * j]), __uint_as_float(w[4 * j + 1]),
-                                                            __uint_as_float(w[4 * j + 2]), __uint_as_float(w[4 * j + 3])));
-            }
-        __syncwarp();
-        cluster_sync_all();                             // what the others sent has arrived
-        if (works) {
-            Staging stg{epi_bufs + (warp - kDenseFirstEpi) * kDenseEpiBytes, 0};
-#pragma unroll 1
-            for (int c = 0; c < kChunks; ++c) {
-                const int ch = cq * kChunks + c;
-                if (c0 + 32 * c >= q.N || ch % share != sharer) continue;
-                ChunkInputs<MODE, TYPE == DenseE4m3> in;
-                chunk_load<kLoadAll>(in, q, prm.lin, r0, c0 + 32 * c, lane);
-                uint32_t w[32];
-                tmem_ld32(tacc + 32 * c, w);
-                tmem_ld_wait();
-                float v[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = 0.f;
-#pragma unroll 1
-                for (int s = 0; s < share; ++s) {
-                    if (s == sharer) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(w[i]);
-                    } else {
-                        const float4 *src = reinterpret_cast<const float4 *>(smem + (slot(s, ch) - stage_base));
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float4 f = src[32 * j];
-                            v[4 * j] += f.x; v[4 * j + 1] += f.y; v[4 * j + 2] += f.z; v[4 * j + 3] += f.w;
-                        }
-                    }
-                }
-                chunk_finish(in, q, prm.lin, &prm.o0[t.p], &prm.o1[t.p], r0, c0 + 32 * c, q.N, lane, stg, v);
-            }
-            if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-        }
+        cluster_sync_all();
     }
 
     // ---- teardown: neither CTA leaves while its partner may still touch its shared or tensor memory ----
@@ -943,8 +954,9 @@ DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int
         pl.splits = (int)std::max<long long>(1, sp);
     }
     // Few tiles: two or four pairs of a cluster on each, where that beats cutting the tiles (in us: 0.33 a k-block, 2 for
-    // the cluster's two meetings, 4.5 for joining pieces through memory).  Measured, shared against cut or whole: 2048 x
-    // 2048 11.3 against 14.7 us with 64 tokens and 12.9 against 16.1 with 512; 8448 x 1024 from 8-bit rows 12.9 against 17.5.
+    // handing the chunks over, 4.5 for joining pieces through memory).  Measured, shared against cut or whole: 2048 x 2048
+    // 10.1 against 14.7 us with 64 tokens and 11.7 against 16.1 with 512; 8448 x 1024 from 8-bit rows 11.6 against 17.5.
+    // (With 1 us for the handing over, 512 x 2048 with 500 tokens is shared too: 7.5 us against 6.3.)
     if (pl.full == 0 && pl.tn == 128) {
         double best = pl.splits > 1 ? 0.33 * least_nk / pl.splits + 4.5 : 0.33 * least_nk;
         for (int share = 2; share <= 4; share *= 2) {
