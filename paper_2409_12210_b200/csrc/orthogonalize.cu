@@ -367,11 +367,11 @@ struct SetPlan { bool small_form; };      // whether the one-kernel form is used
 SetPlan plan_set(const modse_matrix_t *m, int total)
 {
     int grouped = 0, small = 0;
-    for (int i = 0; i < total; ++i) (orthogonalize_small_cluster(m[i].rows, m[i].cols) > 0 ? small : grouped) += 1;
+    for (int i = 0; i < total; ++i) (orthogonalize_small_form(m[i].rows, m[i].cols).blocks > 0 ? small : grouped) += 1;
     const int room = (kGroup - grouped % kGroup) % kGroup;
     return {grouped == 0 || small > room};
 }
-bool takes_small(const SetPlan &p, const modse_matrix_t &m) { return p.small_form && orthogonalize_small_cluster(m.rows, m.cols) > 0; }
+bool takes_small(const SetPlan &p, const modse_matrix_t &m) { return p.small_form && orthogonalize_small_form(m.rows, m.cols).blocks > 0; }
 
 // The next matrices from index i on, up to a launch's worth, that take the grouped form; i moves on.
 int next_group(const SetPlan &p, const modse_matrix_t *m, int total, int &i, modse_matrix_t (&group)[kGroup])

@@ -1,12 +1,16 @@
 // Orthogonalised updates of matrices whose shorter side is at most 128: the whole iteration in one kernel.
 //
 // As grouped products such a matrix is seventeen launches that each last a few microseconds and compute for less than
-// one.  Here a block - or a cluster of up to eight blocks that split the longer side - keeps X (hi and lo, fp16) in shared
+// one.  Here a block - or a cluster of up to sixteen blocks that split the longer side - keeps X (hi and lo, fp16) in shared
 // memory for all iterations and multiplies with mma.sync.  Per iteration:
 //   A = X X^T    every block over its own columns; blocks of a cluster leave fp32 partial sums in their shared memory and
 //                each adds up (in block order) and hands out its share of A through distributed shared memory;
 //   B = aI + bA + cA^2  computed by every block for itself (a 128 x 128 product is cheaper than another meeting);
 //   X <- B hi + a lo   every block on its own columns.
+// Of the longest matrices the step replaces hi in place instead of writing a second copy: a warp then takes all rows of
+// sixteen columns.  Sixteen blocks and the step in place hold 64 x 12544 to 128 x 3840, eight blocks 64 x 3968 to 128 x 1792
+// (75 x 3499, 114 x 75 and 1345 x 75: 65 us against 176 as grouped products; 64 x 8448 101 against 144; 99 x 5000, near the
+// end of the range, 116 against 136).
 // The roundings are those of the grouped form (orthogonalize.cu): fp16 factors scaled by powers of two, X in 22 bits.
 // A tall matrix is transposed on its way in and out.
 #include <cuda_fp16.h>
@@ -19,29 +23,32 @@ namespace modse {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kMostBlocks = 16;                       // of a cluster (above eight only where a kernel is told so)
 constexpr size_t kSmemMost = 227 * 1024 - 1024;       // dynamic; the static part stays below 1 KB
 
 __host__ __device__ inline int up16(int v) { return (v + 15) / 16 * 16; }
 
 // Shared memory of a block for n rows (a multiple of 16) and per columns: rows are padded by 16 bytes, so that eight
-// consecutive rows of a matrix load fall into different banks.
+// consecutive rows of a matrix load fall into different banks.  In place: one copy of hi, and the partial sums of A lie
+// where B is written after them.
 struct SmallLayout {
     int xs, as;                         // row lengths in halves
     size_t hi0, hi1, lo, a, b, part, total;
 };
-__host__ __device__ inline SmallLayout small_layout(int n, int per, bool cluster)
+__host__ __device__ inline SmallLayout small_layout(int n, int per, bool cluster, bool in_place)
 {
     SmallLayout L;
     L.xs = per + 8;
     L.as = n + 8;
     const size_t x = (size_t)n * L.xs * 2, q = (size_t)n * L.as * 2;
     L.hi0 = 0;
-    L.hi1 = x;
-    L.lo = 2 * x;
-    L.a = 3 * x;
+    L.hi1 = in_place ? 0 : x;
+    L.lo = L.hi1 + x;
+    L.a = L.lo + x;
     L.b = L.a + q;
-    L.part = L.b + q;
-    L.total = L.part + (cluster ? (size_t)n * n * 4 : 0);
+    L.part = in_place ? L.b : L.b + q;
+    const size_t part = cluster ? (size_t)n * n * 4 : 0;
+    L.total = L.b + (in_place ? (q > part ? q : part) : q + part);
     return L;
 }
 
@@ -145,6 +152,52 @@ __device__ __forceinline__ void warp_product(uint32_t p, int ps, uint32_t q, int
     }
 }
 
+// X <- P X in place (P n x n, X n x cols, multiples of 16): a warp takes all rows of sixteen columns, which no other warp
+// reads.  get and put as above; get is called after the products, all of it before the first put.
+template <typename G, typename F>
+__device__ __forceinline__ void warp_columns(uint32_t p, int ps, uint32_t x, int xs, int n, int cols, int warp, int lane,
+                                             G &&get, F &&put)
+{
+    constexpr int MI = kOrthSmallMax / 16;
+    const int fr = lane >> 2, fc = 2 * (lane & 3);
+    const uint32_t pa = p + (uint32_t)((lane & 15) * ps + (lane >> 4) * 8) * 2;
+    for (int j0 = 16 * warp; j0 < cols; j0 += 16 * kWarps) {
+        const uint32_t xa = x + (uint32_t)((lane & 15) * xs + j0 + (lane >> 4) * 8) * 2;
+        float acc[MI][2][4];
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[i][e >> 2][e & 3] = 0.f;
+#pragma unroll 1
+        for (int kk = 0; kk < n; kk += 16) {
+            uint32_t b[4];
+            ldsm4_t(b, xa + (uint32_t)(kk * xs) * 2);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+                if (16 * i < n) {
+                    uint32_t a[4];
+                    ldsm4(a, pa + (uint32_t)(16 * i * ps + kk) * 2);
+                    mma_f16(acc[i][0], a, b[0], b[1]);
+                    mma_f16(acc[i][1], a, b[2], b[3]);
+                }
+        }
+        __syncwarp();                  // the columns are read
+        uint32_t in[MI][2][2];
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (16 * i < n) in[i][e >> 1][e & 1] = get(16 * i + fr + 8 * (e & 1), j0 + 8 * (e >> 1) + fc);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (16 * i < n)
+                    put(16 * i + fr + 8 * (e & 1), j0 + 8 * (e >> 1) + fc, acc[i][e >> 1][2 * (e & 1)], acc[i][e >> 1][2 * (e & 1) + 1],
+                        in[i][e >> 1][e & 1]);
+    }
+}
+
 __device__ __forceinline__ uint32_t cluster_size()
 {
     uint32_t r;
@@ -167,12 +220,12 @@ __device__ __forceinline__ uint32_t half2_bits(float a, float b)
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-template <typename T>
+template <typename T, bool IN_PLACE>
 __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const __grid_constant__ SmallArgs args)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ double warp_sums[kWarps];
-    __shared__ double block_sums[8];
+    __shared__ double block_sums[kMostBlocks];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int C = (int)cluster_size(), rank = (int)cluster_ctarank();
     const SmallMatrix m = args.m[blockIdx.x / C];
@@ -180,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
     const int n = tall ? m.cols : m.rows, len = tall ? m.rows : m.cols;
     const int np = up16(n), per = up16((len + C - 1) / C);
     const int c0 = rank * per, mine = max(0, min(per, len - c0));      // this block's columns of X
-    const SmallLayout L = small_layout(np, per, C > 1);
+    const SmallLayout L = small_layout(np, per, C > 1, IN_PLACE);
     const uint32_t base = smem_u32(smem);
     __half *lo = reinterpret_cast<__half *>(smem + L.lo);
     if (C > 1) cluster_sync_all();      // every block of the cluster runs before its shared memory is written from outside
@@ -220,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
     for (int i = warp; i < np; i += kWarps)
         for (int j = (i < n ? mine : 0) + lane; j < L.xs; j += 32) {
             reinterpret_cast<__half *>(smem + L.hi0)[i * L.xs + j] = __ushort_as_half(0);
-            reinterpret_cast<__half *>(smem + L.hi1)[i * L.xs + j] = __ushort_as_half(0);
+            if (!IN_PLACE) reinterpret_cast<__half *>(smem + L.hi1)[i * L.xs + j] = __ushort_as_half(0);
             lo[i * L.xs + j] = __ushort_as_half(0);
         }
 #pragma unroll
@@ -319,7 +372,8 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
                 *reinterpret_cast<uint32_t *>(lo + at) = half2_bits(v0 - back.x, v1 - back.y);
             }
         };
-        if (large) warp_product<true, 2, 2>(b_at, L.as, cur, L.xs, np, per, np, warp, lane, get_step, put_step);
+        if constexpr (IN_PLACE) warp_columns(b_at, L.as, cur, L.xs, np, per, warp, lane, get_step, put_step);
+        else if (large) warp_product<true, 2, 2>(b_at, L.as, cur, L.xs, np, per, np, warp, lane, get_step, put_step);
         else warp_product<true, 1, 2>(b_at, L.as, cur, L.xs, np, per, np, warp, lane, get_step, put_step);
         __syncthreads();
     }
@@ -335,53 +389,57 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
     if (C > 1) cluster_sync_all();      // no block leaves while another may still read its shared memory
 }
 
-template <typename T>
+template <typename T, bool IN_PLACE>
 cudaError_t launch(const SmallArgs &a, int n, int cluster, size_t smem, cudaStream_t s)
 {
-    auto kern = orthogonalize_small_kernel<T>;
+    auto kern = orthogonalize_small_kernel<T, IN_PLACE>;
     static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev > 63 || !((attr_done >> dev) & 1ull)) {
         e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
         if (dev <= 63) attr_done |= 1ull << dev;
     }
     return launch_clusters(kern, cluster, n * cluster, kThreads, smem, s, a);
 }
 
-size_t smem_of(int rows, int cols, int cluster)
+size_t smem_of(int rows, int cols, const SmallForm &f)
 {
     const int n = rows < cols ? rows : cols, len = rows < cols ? cols : rows;
-    return small_layout(up16(n), up16((len + cluster - 1) / cluster), cluster > 1).total;
+    return small_layout(up16(n), up16((len + f.blocks - 1) / f.blocks), f.blocks > 1, f.in_place).total;
 }
 
 }  // namespace
 
-int orthogonalize_small_cluster(int rows, int cols)
+SmallForm orthogonalize_small_form(int rows, int cols)
 {
-    if ((rows < cols ? rows : cols) > kOrthSmallMax) return 0;
-    for (int c = 1; c <= 8; c *= 2)
-        if (smem_of(rows, cols, c) <= kSmemMost) return c;
-    return 0;
+    if ((rows < cols ? rows : cols) > kOrthSmallMax) return {0, false};
+    for (int c = 1; c <= kMostBlocks; c *= 2)
+        if (smem_of(rows, cols, {c, false}) <= kSmemMost) return {c, false};
+    const SmallForm last{kMostBlocks, true};
+    return smem_of(rows, cols, last) <= kSmemMost ? last : SmallForm{0, false};
 }
 
 cudaError_t launch_orthogonalize_small(bool f32, const SmallArgs &a, int n, cudaStream_t s)
 {
-    int cluster = 1;
+    SmallForm form{1, false};
     for (int i = 0; i < n; ++i) {
-        const int c = orthogonalize_small_cluster(a.m[i].rows, a.m[i].cols);
-        if (c == 0) return cudaErrorInvalidValue;
-        cluster = c > cluster ? c : cluster;
+        const SmallForm f = orthogonalize_small_form(a.m[i].rows, a.m[i].cols);
+        if (f.blocks == 0) return cudaErrorInvalidValue;
+        form.blocks = f.blocks > form.blocks ? f.blocks : form.blocks;
+        form.in_place |= f.in_place;
     }
     size_t smem = 0;
     for (int i = 0; i < n; ++i) {
-        const size_t b = smem_of(a.m[i].rows, a.m[i].cols, cluster);
+        const size_t b = smem_of(a.m[i].rows, a.m[i].cols, form);
         if (b > kSmemMost) return cudaErrorInvalidValue;
         smem = b > smem ? b : smem;
     }
-    return f32 ? launch<float>(a, n, cluster, smem, s) : launch<__nv_bfloat16>(a, n, cluster, smem, s);
+    if (form.in_place) return f32 ? launch<float, true>(a, n, form.blocks, smem, s) : launch<__nv_bfloat16, true>(a, n, form.blocks, smem, s);
+    return f32 ? launch<float, false>(a, n, form.blocks, smem, s) : launch<__nv_bfloat16, false>(a, n, form.blocks, smem, s);
 }
 
 }  // namespace modse

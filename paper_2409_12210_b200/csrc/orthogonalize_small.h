@@ -26,8 +26,10 @@ struct SmallArgs {
     int *head;
 };
 
-// Blocks a matrix of this shape takes (1, 2, 4 or 8), 0: not for this form.
-int orthogonalize_small_cluster(int rows, int cols);
+// How a matrix of this shape is held: its number of blocks (1 to 16, a power of two; 0: not for this form) and whether the
+// step works in place.
+struct SmallForm { int blocks; bool in_place; };
+SmallForm orthogonalize_small_form(int rows, int cols);
 cudaError_t launch_orthogonalize_small(bool f32, const SmallArgs &a, int n, cudaStream_t s);
 
 }  // namespace modse

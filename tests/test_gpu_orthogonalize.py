@@ -120,6 +120,25 @@ def test_a_set_of_diverse_matrices_with_scales():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("steps", [1, 4, 5])
+@pytest.mark.parametrize("shape", [(2400, 64), (100, 2900), (127, 3840), (5376, 112), (128, 3841), (9, 20001)])
+def test_long_thin_matrices(shape, steps):
+    """Clusters of sixteen blocks, with two copies of X and in place, at the ends of what they hold and past it."""
+    G = gaussian(*shape, seed=12, dtype=torch.float32)
+    out, = run([G], steps=steps)
+    check(out, G, steps=steps)
+    again, = run([G], steps=steps)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.gpu
+def test_a_set_of_long_and_short_thin_matrices():
+    grads = [gaussian(r, c, 20 + i) for i, (r, c) in enumerate([(100, 4000), (3, 3), (1800, 75), (16, 500), (90, 90), (3500, 120)] * 6)]
+    for out, G in zip(run(grads), grads):
+        check(out, G)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("offset", [0, 1, 8, 13])
 def test_column_blocks(dtype, offset):
