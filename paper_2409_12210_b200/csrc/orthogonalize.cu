@@ -363,15 +363,23 @@ modse_status_t check_call(modse_dtype_t dtype, int steps, const float *k, float 
 // unless the set needs grouped launches anyway and they all fit beside its matrices there: those launches wait more than
 // they compute when matrices are small, and the two forms would run one after the other (86 x 717 with 1508 x 717: 257 us
 // in both forms, 190 in one).
-struct SetPlan { bool small_form; };      // whether the one-kernel form is used
+// Clusters of sixteen blocks are for sets of at most seven matrices, as many as run at the same time (3500 x 128: seven of
+// them 102 us against 168 in the grouped form, eight 200 against 170); all matrices of a launch take the same cluster.
+constexpr int kWideSet = 7;
+struct SetPlan {
+    bool small_form;      // whether the one-kernel form is used
+    int most;             // blocks of a cluster there
+};
+bool fits_small(const modse_matrix_t &m, int most) { return orthogonalize_small_form(m.rows, m.cols, most).blocks > 0; }
 SetPlan plan_set(const modse_matrix_t *m, int total)
 {
+    const int most = total <= kWideSet ? 16 : 8;
     int grouped = 0, small = 0;
-    for (int i = 0; i < total; ++i) (orthogonalize_small_form(m[i].rows, m[i].cols).blocks > 0 ? small : grouped) += 1;
+    for (int i = 0; i < total; ++i) (fits_small(m[i], most) ? small : grouped) += 1;
     const int room = (kGroup - grouped % kGroup) % kGroup;
-    return {grouped == 0 || small > room};
+    return {grouped == 0 || small > room, most};
 }
-bool takes_small(const SetPlan &p, const modse_matrix_t &m) { return p.small_form && orthogonalize_small_form(m.rows, m.cols).blocks > 0; }
+bool takes_small(const SetPlan &p, const modse_matrix_t &m) { return p.small_form && fits_small(m, p.most); }
 
 // The next matrices from index i on, up to a launch's worth, that take the grouped form; i moves on.
 int next_group(const SetPlan &p, const modse_matrix_t *m, int total, int &i, modse_matrix_t (&group)[kGroup])
@@ -442,7 +450,7 @@ modse_status_t modse_orthogonalize(modse_dtype_t dtype, int n_matrices, const mo
         if (n == kOrthSmallBatch || (i == n_matrices && n > 0)) {
             small.head = first ? (int *)workspace : nullptr;
             small.head_ints = (int)(kDenseZeroBytes / 4);
-            if (launch_orthogonalize_small(dtype == MODSE_F32, small, n, s) != cudaSuccess) return MODSE_ERR_CUDA;
+            if (launch_orthogonalize_small(dtype == MODSE_F32, small, n, plan.most, s) != cudaSuccess) return MODSE_ERR_CUDA;
             first = false;
             n = 0;
         }

@@ -9,8 +9,8 @@
 //   X <- B hi + a lo   every block on its own columns.
 // Of the longest matrices the step replaces hi in place instead of writing a second copy: a warp then takes all rows of
 // sixteen columns.  Sixteen blocks and the step in place hold 64 x 12544 to 128 x 3840, eight blocks 64 x 3968 to 128 x 1792
-// (75 x 3499, 114 x 75 and 1345 x 75: 65 us against 176 as grouped products; 64 x 8448 101 against 144; 99 x 5000, near the
-// end of the range, 116 against 136).
+// (75 x 3499, 114 x 75 and 1345 x 75: 63 us against 175 as grouped products; 64 x 8448 97 against 141; 99 x 5000, near the
+// end of the range, 115 against 133).
 // The roundings are those of the grouped form (orthogonalize.cu): fp16 factors scaled by powers of two, X in 22 bits.
 // A tall matrix is transposed on its way in and out.
 #include <cuda_fp16.h>
@@ -242,19 +242,22 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
     if (args.head && blockIdx.x == 0)
         for (int i = tid; i < args.head_ints; i += kThreads) args.head[i] = 0;
 
-    // the elements (i, j) of this block's columns, threads along the contiguous axis of the matrix, eight loads in flight,
-    // eight rows of it at a time (zeros past the end)
+    // the elements (i, j) of this block's columns, threads along the contiguous axis of the matrix, two pieces of eight rows
+    // in flight (zeros past the end)
     const T *g = (const T *)m.g + (tall ? (long long)c0 * m.ld_g : (long long)c0);
     constexpr int kAt = 8;
     const int outer = tall ? mine : n, inner = tall ? n : mine;
     auto each = [&](auto &&f) {
         for (int r0 = warp; r0 < outer; r0 += kAt * kWarps)
-            for (int c = lane; c < inner; c += 32) {
-                float v[kAt];
+            for (int c = lane; c < inner; c += 64) {
+                float v[2][kAt];
 #pragma unroll
                 for (int k = 0; k < kAt; ++k)
-                    v[k] = r0 + k * kWarps < outer ? (float)g[(long long)(r0 + k * kWarps) * m.ld_g + c] : 0.f;
-                f(r0, c, v);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        v[h][k] = r0 + k * kWarps < outer && c + 32 * h < inner ? (float)g[(long long)(r0 + k * kWarps) * m.ld_g + c + 32 * h] : 0.f;
+                f(r0, c, v[0]);
+                if (c + 32 < inner) f(r0, c + 32, v[1]);
             }
     };
     double sq = 0.0;      // eight squares in fp32 where their sum is well inside its range, in fp64 otherwise
@@ -414,20 +417,20 @@ size_t smem_of(int rows, int cols, const SmallForm &f)
 
 }  // namespace
 
-SmallForm orthogonalize_small_form(int rows, int cols)
+SmallForm orthogonalize_small_form(int rows, int cols, int most)
 {
     if ((rows < cols ? rows : cols) > kOrthSmallMax) return {0, false};
-    for (int c = 1; c <= kMostBlocks; c *= 2)
+    for (int c = 1; c <= most; c *= 2)
         if (smem_of(rows, cols, {c, false}) <= kSmemMost) return {c, false};
     const SmallForm last{kMostBlocks, true};
-    return smem_of(rows, cols, last) <= kSmemMost ? last : SmallForm{0, false};
+    return most == kMostBlocks && smem_of(rows, cols, last) <= kSmemMost ? last : SmallForm{0, false};
 }
 
-cudaError_t launch_orthogonalize_small(bool f32, const SmallArgs &a, int n, cudaStream_t s)
+cudaError_t launch_orthogonalize_small(bool f32, const SmallArgs &a, int n, int most, cudaStream_t s)
 {
     SmallForm form{1, false};
     for (int i = 0; i < n; ++i) {
-        const SmallForm f = orthogonalize_small_form(a.m[i].rows, a.m[i].cols);
+        const SmallForm f = orthogonalize_small_form(a.m[i].rows, a.m[i].cols, most);
         if (f.blocks == 0) return cudaErrorInvalidValue;
         form.blocks = f.blocks > form.blocks ? f.blocks : form.blocks;
         form.in_place |= f.in_place;

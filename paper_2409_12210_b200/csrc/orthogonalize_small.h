@@ -26,10 +26,10 @@ struct SmallArgs {
     int *head;
 };
 
-// How a matrix of this shape is held: its number of blocks (1 to 16, a power of two; 0: not for this form) and whether the
-// step works in place.
+// How a matrix of this shape is held: its number of blocks (a power of two up to `most`, 8 or 16; 0: not for this form) and
+// whether the step works in place (of sixteen blocks only).
 struct SmallForm { int blocks; bool in_place; };
-SmallForm orthogonalize_small_form(int rows, int cols);
-cudaError_t launch_orthogonalize_small(bool f32, const SmallArgs &a, int n, cudaStream_t s);
+SmallForm orthogonalize_small_form(int rows, int cols, int most);
+cudaError_t launch_orthogonalize_small(bool f32, const SmallArgs &a, int n, int most, cudaStream_t s);
 
 }  // namespace modse

@@ -132,8 +132,9 @@ def test_long_thin_matrices(shape, steps):
 
 
 @pytest.mark.gpu
-def test_a_set_of_long_and_short_thin_matrices():
-    grads = [gaussian(r, c, 20 + i) for i, (r, c) in enumerate([(100, 4000), (3, 3), (1800, 75), (16, 500), (90, 90), (3500, 120)] * 6)]
+@pytest.mark.parametrize("sets", [1, 6])
+def test_a_set_of_long_and_short_thin_matrices(sets):
+    grads = [gaussian(r, c, 20 + i) for i, (r, c) in enumerate([(100, 4000), (3, 3), (1800, 75), (16, 500), (90, 90), (3500, 120)] * sets)]
     for out, G in zip(run(grads), grads):
         check(out, G)
 
