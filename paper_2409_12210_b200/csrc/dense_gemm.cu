@@ -994,7 +994,9 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
             ok = encode_output(&prm.o0[i], lin->y, q.M, q.N, q.N) && (lin->z == nullptr || encode_output(&prm.o1[i], lin->z, q.M, q.N, q.N));
         } else if constexpr (MODE == DenseStep) {
             if (q.flags & kDenseLast) {
-                if (((q.ld_out & 7) | (reinterpret_cast<uintptr_t>(q.out0) & 15)) == 0) {
+                // A copy of a box that the last column cuts ends at a multiple of 16 bytes, past that column (600 x 1100 in rows
+                // of 1128: four columns beside the block were zeroed), so the width has to be a multiple of 8 as well.
+                if ((((q.ld_out | q.N) & 7) | (reinterpret_cast<uintptr_t>(q.out0) & 15)) == 0) {
                     q.flags |= kDenseTmaOut;
                     ok = encode_output(&prm.o0[i], q.out0, q.M, q.N, q.ld_out);
                 }

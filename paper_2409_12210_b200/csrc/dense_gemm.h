@@ -22,7 +22,7 @@ enum : int {
     kDenseBMn = 2,     // same for the column operand ([K, N], not [N, K])
     kDenseSym = 4,     // out is symmetric: tiles below the diagonal are not computed but mirrored
     kDenseLast = 8,    // DenseStep: write the final result
-    kDenseTmaOut = 16  // set by the launch: the final result's rows are aligned for TMA
+    kDenseTmaOut = 16  // set by the launch: the final result's rows are aligned for TMA and whole 16-byte pieces long
 };
 
 // One product out[M, N] = sum_k A[m, k] B[n, k] of a launch.

@@ -155,6 +155,32 @@ def test_column_blocks(dtype, offset):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [1100])
+def test_column_blocks_of_every_alignment_in_one_launch(cols, dtype):
+    """Grouped products with updates as column blocks of wider matrices: 1100 columns end inside a 16-byte piece, and the
+    columns beside a block stay whatever the alignment of its rows.  Gradients as blocks of wider matrices too, aligned
+    and not; 240 tiles, so that every CTA pair has several."""
+    from paper_2409_12210_b200 import binding as B
+    g = torch.Generator(device="cuda").manual_seed(17)
+    places = [0, 1, 8, 13, 0, 3, 16, 8, 2, 0, 24, 5, 0, 7, 8, 11]
+    wide = [torch.randn(600, 1136, generator=g, device="cuda").to(dtype) * 0.02 for _ in places]
+    targets = [torch.full((600, 1128 + (i % 3)), 7.0, dtype=torch.bfloat16, device="cuda") for i in range(len(places))]
+    grads = [w[:, (5 * o) % 32:(5 * o) % 32 + cols] for w, o in zip(wide, places)]
+    ups = [t[:, o:o + cols] for t, o in zip(targets, places)]
+    assert {t.data_ptr() % 16 == 0 and t.stride(0) % 8 == 0 for t in ups} == {True, False}
+    ws = torch.empty(B.orthogonalize_workspace_bytes([(600, cols)] * 16), dtype=torch.uint8, device="cuda")
+    B.orthogonalize(grads, ups, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    for u, m, t, o in zip(ups, grads, targets, places):
+        check(u, m)
+        assert bool((t[:, :o] == 7).all()) and bool((t[:, o + cols:] == 7).all())
+    first = [u.clone() for u in ups]
+    B.orthogonalize(grads, ups, ws)
+    assert all(torch.equal(a, b) for a, b in zip(first, ups))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("steps,k", [(1, MUON), (8, MUON), (12, (1.5, -0.5, 0.0)), (3, (1.875, -1.25, 0.375))])
 def test_other_coefficients(steps, k):
     G = gaussian(120, 200, 7, torch.float32)
