@@ -160,7 +160,8 @@ __device__ __forceinline__ void take_share(DenseTile &t, int sharer, int share)
 struct Staging {
     unsigned char *base;
     int which;
-    // the next buffer, free to be written
+    // The next buffer, free to be written: all groups but the latest have been read, and that one, committed for the other
+    // buffer, is all that may be left.  So whoever takes a buffer commits one group for it, an empty one if nothing is copied.
     __device__ __forceinline__ unsigned char *take(int lane)
     {
         which ^= 1;
@@ -404,6 +405,9 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
                     for (int r = 0; r < rows; ++r)
                         out[r * q.ld_out + lane] = *reinterpret_cast<const __nv_bfloat16 *>(buf + epi_piece(r, lane >> 3) + (lane & 7) * 2);
                 __syncwarp();
+                // an empty group in the place of this buffer's copy: Staging::take counts one for every buffer, and without
+                // it the next one would be written while a copy of an earlier matrix's rows may still be reading it
+                if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             }
         } else {
             pack_f16(v, w);

@@ -156,11 +156,12 @@ def test_column_blocks(dtype, offset):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("cols", [1100])
+@pytest.mark.parametrize("cols", [1100, 1104])
 def test_column_blocks_of_every_alignment_in_one_launch(cols, dtype):
     """Grouped products with updates as column blocks of wider matrices: 1100 columns end inside a 16-byte piece, and the
-    columns beside a block stay whatever the alignment of its rows.  Gradients as blocks of wider matrices too, aligned
-    and not; 240 tiles, so that every CTA pair has several."""
+    columns beside a block stay whatever the alignment of its rows; of 1104 columns the aligned blocks leave by TMA and the
+    others by plain stores, so that a warp's two staging buffers pass from one kind to the other.  Gradients as blocks of
+    wider matrices too, aligned and not; 240 tiles, so that every CTA pair has several."""
     from paper_2409_12210_b200 import binding as B
     g = torch.Generator(device="cuda").manual_seed(17)
     places = [0, 1, 8, 13, 0, 3, 16, 8, 2, 0, 24, 5, 0, 7, 8, 11]
