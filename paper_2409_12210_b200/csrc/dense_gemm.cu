@@ -259,7 +259,8 @@ __device__ __forceinline__ void activate_all(float (&v)[32], int act)
 }
 
 // What a chunk of 32 rows (from r0) x 32 columns (from c0) reads from memory.  The first chunk's is requested before the
-// accumulator is waited for, the next one's as soon as the registers of the present one are free.
+// accumulator is waited for, the next one's as soon as the registers of the present one are free.  Plain loads all: scales
+// and bias may come from the kernel ahead, which may still be writing them when this one starts.
 template <int MODE, bool F8> struct ChunkInputs {
     uint4 raw[MODE == DensePlain || MODE == DenseGram ? 1 : 4];      // residual, or the first input
     uint4 bias[MODE == DenseLinear ? 4 : 1];
@@ -277,8 +278,8 @@ __device__ __forceinline__ void chunk_load(ChunkInputs<MODE, F8> &in, const Dens
         if constexpr ((WHAT & kLoadBias) != 0) {
             if (lin.bias)
 #pragma unroll
-                for (int p = 0; p < 4; ++p) in.bias[p] = p < pieces ? __ldg(reinterpret_cast<const uint4 *>(lin.bias + c0) + p) : make_uint4(0, 0, 0, 0);
-            if constexpr (F8) in.sx = lane < rows ? __ldg(lin.sx + r0 + lane) : 0.f;
+                for (int p = 0; p < 4; ++p) in.bias[p] = p < pieces ? *(reinterpret_cast<const uint4 *>(lin.bias + c0) + p) : make_uint4(0, 0, 0, 0);
+            if constexpr (F8) in.sx = lane < rows ? lin.sx[r0 + lane] : 0.f;
         }
     } else if constexpr (MODE == DensePoly) {
         if constexpr ((WHAT & kLoadFirst) != 0)
@@ -304,7 +305,7 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
 #pragma unroll
             for (int p = 0; p < 8; ++p)
                 if (4 * p < cols) {
-                    const float4 f = __ldg(reinterpret_cast<const float4 *>(lin.sw + c0) + p);
+                    const float4 f = *(reinterpret_cast<const float4 *>(lin.sw + c0) + p);
                     v[4 * p] *= in.sx * f.x; v[4 * p + 1] *= in.sx * f.y; v[4 * p + 2] *= in.sx * f.z; v[4 * p + 3] *= in.sx * f.w;
                 }
         }

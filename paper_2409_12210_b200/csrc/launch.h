@@ -9,6 +9,8 @@ namespace modse {
 // while the kernel ahead of it drains, and calls wait_for_earlier_kernels before it touches global memory: from there on
 // everything the stream held before it has completed and is visible.  A kernel that calls allow_next_kernel lets one
 // launched this way start its set-up as soon as SMs have room; without the call it may start when the blocks have left.
+// What an earlier kernel writes is not read-only for the lifetime of a kernel that starts this early: it is read with plain
+// loads, not through ld.global.nc (__ldg).
 __device__ __forceinline__ void wait_for_earlier_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void allow_next_kernel() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -44,12 +44,14 @@ __device__ __forceinline__ void widen(uint32_t v, uint32_t &lo, uint32_t &hi)
         : "=r"(lo), "=r"(hi) : "r"(v));
 }
 
-// 16 bytes, or zeros where there are none.  volatile: the loads of a step stay ahead of its products
+// 16 bytes, or zeros where there are none.  volatile: the loads of a step stay ahead of its products.  Not the read-only
+// path: the kernel ahead may still be writing x when this one starts, and that path promises nothing for such data, even
+// where it is read after wait_for_earlier_kernels.
 __device__ __forceinline__ uint4 load_stream(const unsigned char *p, bool in)
 {
     uint4 v;
     asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\t"
-                 "mov.b32 %3, 0;\n\t@q ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+                 "mov.b32 %3, 0;\n\t@q ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
                  : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((int)in));
     return v;
 }
@@ -57,7 +59,7 @@ __device__ __forceinline__ uint4 load_shared_rows(const unsigned char *p, bool i
 {
     uint4 v;
     asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\t"
-                 "mov.b32 %3, 0;\n\t@q ld.global.nc.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+                 "mov.b32 %3, 0;\n\t@q ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
                  : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((int)in));
     return v;
 }

@@ -418,7 +418,7 @@ add_rms_norm_bwd_kernel(const NormBwdArgs a)
 }
 
 // out[c] = sum over the blocks' partial rows, in block order within 32 interleaved runs that are added in order.
-__global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int n_rows, int d, float *__restrict__ out)
+__global__ void __launch_bounds__(1024) column_sum_kernel(const float *part, int n_rows, int d, float *out)
 {
     __shared__ float sh[32][33];
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), run = threadIdx.x >> 5;

@@ -259,6 +259,34 @@ def test_in_place_residual_replay_and_two_streams():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 24, 300, 2500])
+def test_a_chain_of_overlapped_calls_reads_what_the_call_before_it_wrote(T):
+    """Norm and 8-bit product in turn on the same buffers, inputs changing from call to call and nothing waited for: rows
+    and scales are those of the norm just ahead, whose kernel is still running when the product's starts."""
+    from paper_2409_12210_b200 import binding as B
+    rng = np.random.default_rng(T)
+    k, n, calls = 512, 1032, 24
+    xs = [rand(rng, T, k).bfloat16() * (1 + i) for i in range(calls)]
+    w, sw = rand(rng, n, k).to(torch.float8_e4m3fn), rand(rng, n).abs() + 0.1
+    q, sc = torch.empty(T, k, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(T, device="cuda")
+    ws = torch.empty(B.linear_workspace_bytes(q.dtype, T, k, n), dtype=torch.uint8, device="cuda")
+    outs = [torch.empty(T, n, device="cuda").bfloat16() for _ in range(2 * calls)]
+
+    def step(x, y):
+        B.add_rms_norm(x, None, None, 1.0, y8=q, y_scale=sc)       # eps 1: the rows' size stays in the result
+        B.linear(q, w, y, ws, x_scale=sc, w_scale=sw)
+
+    for x, y in zip(xs, outs):
+        step(x, y)
+        torch.cuda.synchronize()
+    for x, y in zip(xs, outs[calls:]):
+        step(x, y)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, outs[calls:]))
+    assert not torch.equal(outs[0], outs[1])
+
+
+@pytest.mark.gpu
 def test_empty_batch_and_binding_refusals():
     from paper_2409_12210_b200 import binding as B
     bf = dict(dtype=torch.bfloat16, device="cuda")
