@@ -227,6 +227,67 @@ def test_far_activations_and_special_values():
         assert bool((y[3:] == 0).all())
 
 
+def tail64(z, name):
+    """gelu, silu and their slopes without cancellation, for z < 0."""
+    if name == "silu":
+        s = np.exp(z) / (1 + np.exp(z))
+        return z * s, s * (1 + z * (1 - s))
+    q = 0.5 * np.vectorize(math.erfc)(-z / math.sqrt(2))
+    return z * q, q + z * np.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [8, 40])
+@pytest.mark.parametrize("act,low", [("gelu", -12.75), ("silu", -86.0)])
+def test_left_tails_of_the_activations(act, low, T):
+    """Far left the functions go to zero and keep their leading digits.  Bound relative to the value: one rounding to bf16
+    (none for dbias), 6.1e-5 for the approximation of the tail, and the exponential's argument, off by two roundings of at
+    most 2^-24 |q|, |q| <= 128 log2(e) 2^-1 .. 125: 2 * 125 * 2^-24 ln 2 = 1.1e-5, with a few units of the approximate
+    functions 2^-22 each: 1e-4 in all.  The slope adds terms of opposite sign: q and z phi, both relative to |z| phi."""
+    from paper_2409_12210_b200 import binding as B
+    z = torch.linspace(low, -0.5, 8 * T).bfloat16().cuda().view(T, 8)
+    x, w = torch.zeros(T, 8, device="cuda").bfloat16(), torch.eye(8, device="cuda").bfloat16()
+    x.copy_(z)                                     # z = x I, exactly
+    y, saved = torch.empty_like(z), torch.empty_like(z)
+    ws = torch.empty(B.linear_workspace_bytes(x.dtype, T, 8, 8), dtype=torch.uint8, device="cuda")
+    B.linear(x, w, y, ws, activation=act, z=saved)
+    assert torch.equal(saved, z)
+    Z = f64(z)
+    ref, slope = tail64(Z, act)
+    assert np.all(np.abs(f64(y) - ref) <= (BF + 1e-4) * np.abs(ref))
+    n = 8 * T
+    flat, dy, db = z.view(1, n), torch.ones(1, n, device="cuda").bfloat16(), torch.empty(n, device="cuda")
+    ws = torch.empty(B.linear_backward_workspace_bytes(1, 8, n), dtype=torch.uint8, device="cuda")
+    x, w = torch.zeros(1, 8, device="cuda").bfloat16(), torch.zeros(n, 8, device="cuda").bfloat16()
+    B.linear_backward(x, w, dy, flat, act, None, None, db, ws)
+    size = np.abs(Z) * np.exp(-Z * Z / 2) if act == "gelu" else (1 - Z) * np.exp(Z)
+    assert np.all(np.abs(f64(db) - slope.ravel()) <= 1e-4 * size.ravel())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [5, 40])
+def test_infinities_go_where_the_limits_are(T):
+    from paper_2409_12210_b200 import binding as B
+    inf = float("inf")
+    x = torch.zeros(T, 8, device="cuda").bfloat16()
+    x[0, 0], x[1, 0], x[2, 0] = inf, -inf, float("nan")
+    w = torch.zeros(16, 8, device="cuda").bfloat16()
+    w[:, 0] = 1
+    y, z = torch.empty(T, 16, device="cuda").bfloat16(), torch.empty(T, 16, device="cuda").bfloat16()
+    ws = torch.empty(B.linear_workspace_bytes(x.dtype, T, 8, 16), dtype=torch.uint8, device="cuda")
+    back = torch.empty(B.linear_backward_workspace_bytes(1, 8, 16), dtype=torch.uint8, device="cuda")
+    db, one = torch.empty(16, device="cuda"), torch.ones(1, 16, device="cuda").bfloat16()
+    for act in ACTS:
+        B.linear(x, w, y, ws, activation=act, z=z)
+        assert bool((z[0] == inf).all()) and bool((z[1] == -inf).all()) and bool(torch.isnan(z[2]).all())
+        assert bool((y[0] == inf).all()) and bool((y[1] == (-inf if act == "none" else 0)).all())
+        assert bool(torch.isnan(y[2]).all()) and bool((y[3:] == 0).all())
+        if act != "none":
+            for row, slope in ((0, 1.0), (1, 0.0)):
+                B.linear_backward(x[:1], w, one, z[row:row + 1], act, None, None, db, back)
+                assert bool((db == slope).all())
+
+
 @pytest.mark.gpu
 def test_in_place_residual_replay_and_two_streams():
     from paper_2409_12210_b200 import binding as B
