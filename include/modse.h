@@ -379,7 +379,8 @@ modse_status_t modse_linear(modse_dtype_t dtype, int n_tokens, int d_in, int d_o
 /* Gradient of the bf16 product, from dy [T, d_out] and the z that forward saved (may
  * be NULL for MODSE_ACT_NONE):
  *   dz = dy act'(z),  dx = dz w,  dw = dz^T x,  dbias = sum_t dz
- * (the residual's gradient is dy itself; relu'(0) = 0).  dx [T, d_in] and
+ * (the residual's gradient is dy itself; relu'(0) = 0, and where relu's slope is 0
+ * dz is 0 whatever dy holds).  dx [T, d_in] and
  * dw [d_out, d_in] bf16, dbias [d_out] fp32; each may be NULL, all overwritten, none
  * overlaps an input.  At most 4194240 tokens.
  * dz enters the products rounded to bf16 once (they read 16-bit operands) and

@@ -80,14 +80,11 @@ __device__ __forceinline__ void activate2(float &a, float &b)
     }
 }
 
-// Slopes of two numbers; NaN and infinities as above.
+// Slopes of two numbers; NaN and infinities as above.  relu's is in times_slope2.
 template <int ACT>
 __device__ __forceinline__ void act_slope2(float &a, float &b)
 {
-    if constexpr (ACT == MODSE_ACT_RELU) {
-        a = a > 0.f ? 1.f : 0.f;
-        b = b > 0.f ? 1.f : 0.f;
-    } else if constexpr (ACT == MODSE_ACT_GELU) {
+    if constexpr (ACT == MODSE_ACT_GELU) {
         // Phi(z) + z phi(z), Phi from the tail on its own side
         f32x2 e;
         const float m0 = min_nan(fabsf(a), 16.f), m1 = min_nan(fabsf(b), 16.f);
@@ -103,8 +100,20 @@ __device__ __forceinline__ void act_slope2(float &a, float &b)
         const float s0 = rcp_approx(1.f + ex2_approx(q0)), s1 = rcp_approx(1.f + ex2_approx(q1));
         a = s0 * fmaf(a, 1.f - s0, 1.f);
         b = s1 * fmaf(b, 1.f - s1, 1.f);
+    }
+}
+
+// g times the slope at z, for two numbers.  relu selects: what it masks is 0 even where g is infinite or NaN.
+template <int ACT>
+__device__ __forceinline__ void times_slope2(float &g0, float &g1, float z0, float z1)
+{
+    if constexpr (ACT == MODSE_ACT_RELU) {
+        g0 = z0 > 0.f ? g0 : 0.f;
+        g1 = z1 > 0.f ? g1 : 0.f;
     } else {
-        a = b = 1.f;
+        act_slope2<ACT>(z0, z1);
+        g0 *= z0;
+        g1 *= z1;
     }
 }
 

@@ -111,11 +111,7 @@ linear_dz_kernel(const __nv_bfloat16 *dy, const __nv_bfloat16 *z, __nv_bfloat16 
                 if constexpr (ACT != MODSE_ACT_NONE) {
                     unpack8(fv[i], f);
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) {
-                        act_slope2<ACT>(f[j], f[j + 1]);
-                        g[j] *= f[j];
-                        g[j + 1] *= f[j + 1];
-                    }
+                    for (int j = 0; j < 8; j += 2) times_slope2<ACT>(g[j], g[j + 1], f[j], f[j + 1]);
                     uint32_t w[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {

@@ -265,6 +265,26 @@ def test_left_tails_of_the_activations(act, low, T):
 
 
 @pytest.mark.gpu
+def test_relu_masks_infinities_and_nan_in_the_incoming_gradient():
+    from paper_2409_12210_b200 import binding as B
+    rng = np.random.default_rng(7)
+    T, k, n = 70, 72, 136
+    x, w, z, dy = (rand(rng, *s).bfloat16() for s in ((T, k), (n, k), (T, n), (T, n)))
+    z[:, ::5] = 0
+    z[0, 1], z[1, 2] = -float("inf"), -1.0
+    clean, dirty = torch.where(z > 0, dy, 0), dy.clone()
+    for i, v in enumerate((float("inf"), -float("inf"), float("nan"))):
+        dirty.view(-1)[i::3] = torch.where(z.view(-1)[i::3] > 0, dirty.view(-1)[i::3], v)
+    outs = []
+    for g in (clean, dirty):
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(n, device="cuda")
+        ws = torch.empty(B.linear_backward_workspace_bytes(T, k, n), dtype=torch.uint8, device="cuda")
+        B.linear_backward(x, w, g, z, "relu", dx, dw, db, ws)
+        outs.append((dx, dw, db))
+    assert all(torch.equal(a, b) and bool(torch.isfinite(a).all()) for a, b in zip(*outs))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("T", [5, 40])
 def test_infinities_go_where_the_limits_are(T):
     from paper_2409_12210_b200 import binding as B
