@@ -359,7 +359,9 @@ modse_status_t modse_add_rms_norm_backward(modse_dtype_t dtype, int n_tokens, in
  * the unrounded z, once.  Products are accumulated in fp32.
  * relu, gelu (z Phi(z), Phi the normal distribution function), silu (z / (1 + e^-z)).
  * The workspace's first bytes hold a status word that modse_check_workspace_status
- * reads (a bounded wait inside a kernel may expire, as in modse_forward).     */
+ * reads (a bounded wait inside a kernel may expire, as in modse_forward).  Its size,
+ * and that of the gradient's, never falls with n_tokens: one that serves a batch
+ * serves every smaller one.                                                  */
 typedef enum {
     MODSE_ACT_NONE = 0,
     MODSE_ACT_RELU = 1,
@@ -409,7 +411,8 @@ modse_status_t modse_linear_backward(int n_tokens, int d_in, int d_out, modse_ac
  * the relative error of an update is of the order of its bf16 rounding.
  * Coefficients that let a singular value of the iteration pass 7.5 are
  * MODSE_ERR_UNSUPPORTED.  The workspace holds up to 16 matrices at a time; longer
- * sets are worked off in order.
+ * sets are worked off in order.  Its size is that of the very set it was asked for: a
+ * part of the set may need more (the whole may take another form).
  *
  * modse_orthogonalize_wgrads does it for the expert matrices of a layer, straight
  * from the gradients modse_backward wrote (dw_gate, dw_up, dw_down of `grads`; the

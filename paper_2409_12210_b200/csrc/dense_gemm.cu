@@ -1070,6 +1070,22 @@ size_t dense_partial_bytes(DenseMode mode, DenseType type, const DenseItem *item
     return !pl.tall && pl.splits > 1 ? (size_t)(pl.items - pl.full) * 256 * pl.tn * 4 : 0;
 }
 
+size_t dense_partial_bound(DenseType type, const DenseItem *items, int n)
+{
+    // dense_plan cuts into at most one piece a pair, at least 16 k-blocks and at most 16 pieces a tile
+    const long long pairs = kDenseSms / 2;
+    long long squares = 0, narrow = 0;
+    int least_nk = 1 << 30;
+    for (int i = 0; i < n; ++i) {
+        squares += dense_tiles(items[i].p, false, 256);
+        narrow += dense_tiles(items[i].p, false, 128);
+        least_nk = std::min(least_nk, dense_nk(type, items[i].k));
+    }
+    const long long each = std::min(least_nk / 16, 16);
+    if (each < 2) return 0;
+    return squares * 2 <= pairs ? (size_t)std::min(pairs, narrow * each) * 256 * 128 * 4 : (size_t)pairs * 256 * 256 * 4;
+}
+
 cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *list, int n, const LinearEpilogue *lin,
                          const DenseColumnSum *sum, void *ws, size_t partial_capacity, int head, cudaStream_t s)
 {

@@ -152,7 +152,7 @@ BackwardLayout backward_layout(int T, int k, int n)
     for (int which = 1; which <= 3; ++which) {        // dx alone, dw alone, both: the largest of the three
         const int c = backward_items(items, T, k, n, nullptr, nullptr, nullptr, (which & 1) ? (void *)1 : nullptr,
                                      (which & 2) ? (void *)1 : nullptr);
-        const size_t b = dense_partial_bytes(DensePlain, DenseBf16, items, c);
+        const size_t b = dense_partial_bound(DenseBf16, items, c);
         need = b > need ? b : need;
     }
     L.partials = kDenseHead;
@@ -196,7 +196,7 @@ size_t modse_linear_workspace_bytes(modse_dtype_t dtype, int n_tokens, int d_in,
     const DenseType type = dtype == MODSE_E4M3 ? DenseE4m3 : DenseBf16;
     if (n_tokens <= kLinearRowsMax) return kDenseHead;
     const DenseItem it = forward_item(type, n_tokens, d_in, d_out, nullptr, nullptr);
-    return kDenseHead + up256(dense_partial_bytes(DenseLinear, type, &it, 1));
+    return kDenseHead + up256(dense_partial_bound(type, &it, 1));
 }
 
 modse_status_t modse_linear(modse_dtype_t dtype, int n_tokens, int d_in, int d_out, modse_activation_t activation,

@@ -392,6 +392,42 @@ def test_empty_batch_and_binding_refusals():
         B.linear(x.float(), w.float(), y, ws)
 
 
+@pytest.mark.gpu
+def test_a_workspace_for_the_largest_batch_serves_the_smaller_ones():
+    from paper_2409_12210_b200 import binding as B
+    rng = np.random.default_rng(13)
+    k, n, most = 2048, 1408, 8192
+    w = rand(rng, n, k, std=k ** -0.5).bfloat16()
+    ws, margin = workspace(B.linear_workspace_bytes(w.dtype, most, k, n))
+    back, back_margin = workspace(B.linear_backward_workspace_bytes(most, k, n))
+    for T in (1, 33, 500, 2048, 3300, 8192):
+        x, dy = rand(rng, T, k).bfloat16(), rand(rng, T, n).bfloat16()
+        outs = []
+        for a, b in ((ws, back), (None, None)):
+            a = workspace(B.linear_workspace_bytes(w.dtype, T, k, n))[0] if a is None else a
+            b = workspace(B.linear_backward_workspace_bytes(T, k, n))[0] if b is None else b
+            y, dx, dw = torch.empty_like(dy), torch.empty_like(x), torch.empty_like(w)
+            B.linear(x, w, y, a)
+            B.linear_backward(x, w, dy, None, "none", dx, dw, None, b)
+            assert B.check_workspace_status(a) == B.MODSE_OK and B.check_workspace_status(b) == B.MODSE_OK
+            outs.append((y, dx, dw))
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+    assert bool((margin == 0xA5).all()) and bool((back_margin == 0xA5).all())
+
+
+def test_workspace_sizes_never_fall_with_the_batch():
+    from paper_2409_12210_b200 import binding as B
+    from paper_2409_12210_b200 import build
+    build.build()
+    batches = list(range(1, 2000, 37)) + [2048, 2304, 4096, 6144, 8192, 8193, 12000, 16384, 20000, 65536, 1 << 20]
+    for k, n in [(2048, 5632), (5632, 2048), (2048, 2048), (8448, 1024), (64, 64), (512, 8448), (1536, 2816), (8192, 136)]:
+        for size in (lambda T: B.linear_workspace_bytes(torch.bfloat16, T, k, n),
+                     lambda T: B.linear_workspace_bytes(torch.float8_e4m3fn, T, k, n),
+                     lambda T: B.linear_backward_workspace_bytes(T, k, n)):
+            sizes = [size(T) for T in batches]
+            assert sizes == sorted(sizes) and sizes[0] > 0
+
+
 def test_refusals_need_no_gpu():
     from paper_2409_12210_b200 import binding as B
     from paper_2409_12210_b200 import build
