@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(256) square_sums_kernel(const __grid_constant_
 template <typename T>
 __global__ void __launch_bounds__(256) normalise_kernel(const __grid_constant__ PrepArgs a)
 {
-    __shared__ float inv_sh;
+    __shared__ StartScale start_sh;
     const PrepMatrix &m = a.m[blockIdx.y];
     wait_for_earlier_kernels();
     allow_next_kernel();
@@ -165,10 +165,10 @@ __global__ void __launch_bounds__(256) normalise_kernel(const __grid_constant__ 
         for (int i = 0; i < kNormParts / 32; ++i) t += p[threadIdx.x + 32 * i];
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
-        if (threadIdx.x == 0) inv_sh = (float)((double)kScaleX / (sqrt(t) + (double)a.eps));
+        if (threadIdx.x == 0) start_sh = start_scale(sqrt(t), a.eps);
     }
     __syncthreads();
-    const float inv = inv_sh;
+    const StartScale start = start_sh;
     const int vecs = (m.cols + 7) / 8;
     const long long total = (long long)m.rows * vecs, ldx = 8ll * vecs;
     const bool wide = wide_rows<T>(m);
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(256) normalise_kernel(const __grid_constant__ 
         uint32_t h[4], l[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float x = f[2 * j] * inv, y = f[2 * j + 1] * inv;
+            const float x = f[2 * j] * start.pre * start.inv, y = f[2 * j + 1] * start.pre * start.inv;
             const __half2 hh = __floats2half2_rn(x, y);
             const float2 back = __half22float2(hh);
             const __half2 ll = __floats2half2_rn(x - back.x, y - back.y);

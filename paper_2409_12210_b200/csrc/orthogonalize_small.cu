@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
     else __syncthreads();
     double total = 0.0;
     for (int r = 0; r < C; ++r) total += block_sums[r];
-    const float inv = (float)((double)kOrthScaleX / (sqrt(total) + (double)args.eps));
+    const StartScale start = start_scale(sqrt(total), args.eps);
     {
         __half *hi = reinterpret_cast<__half *>(smem + L.hi0);
         const int step = kWarps * (tall ? 1 : L.xs);
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1) orthogonalize_small_kernel(const 
 #pragma unroll
             for (int k = 0; k < kAt; ++k, at += step)
                 if (r0 + k * kWarps < outer) {
-                    const float x = v[k] * inv;
+                    const float x = v[k] * start.pre * start.inv;
                     const __half h = __float2half_rn(x);
                     hi[at] = h;
                     lo[at] = __float2half_rn(x - __half2float(h));

@@ -10,6 +10,16 @@ constexpr float kOrthScaleX = 4096.f, kOrthScaleA = 1024.f, kOrthScaleB = 1024.f
 constexpr int kOrthSmallMax = 128;     // longest shorter side of this form
 constexpr int kOrthSmallBatch = 32;    // matrices of a launch
 
+// X0 = G pre inv holds kOrthScaleX G / (|G| + eps).  One fp32 factor would overflow where |G| + eps is below 1e-35 (a matrix of
+// zeros would give NaN for a tiny eps) and lose digits above 1e41, so a power of two goes ahead of it there.
+struct StartScale { float pre, inv; };
+__device__ __forceinline__ StartScale start_scale(double norm, float eps)
+{
+    const double by = (double)kOrthScaleX / (norm + (double)eps);
+    const float pre = by > 1e30 ? 0x1p80f : by < 1e-30 ? 0x1p-80f : 1.f;
+    return {pre, (float)(by / (double)pre)};
+}
+
 struct SmallMatrix {
     const void *g;
     __nv_bfloat16 *out;

@@ -205,6 +205,23 @@ def test_zero_tiny_huge_and_nan():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(40, 64), (200, 300)])
+def test_norms_and_eps_at_the_ends_of_fp32(shape):
+    """One kernel and grouped products: zeros with an eps below the normal range, matrices of subnormal numbers, and sums of
+    squares far past fp32."""
+    zeros = torch.zeros(*shape, device="cuda")
+    for eps in (1e-36, 1e-38, 1e-44):
+        out, = run([zeros], eps=eps)
+        assert bool((out == 0).all())
+    tiny = gaussian(*shape, 8, torch.float32) * 1e-37
+    assert 0 < float(tiny.abs().max()) < 2.0 ** -126 * 1.5
+    huge = gaussian(*shape, 9, torch.float32).sign() * 3e38
+    for G in (tiny, huge):
+        out, = run([G], eps=0.0)
+        check(out, G, eps=0.0)
+
+
+@pytest.mark.gpu
 def test_replay_in_a_graph():
     from paper_2409_12210_b200 import binding as B
     G = gaussian(300, 500, 11)
