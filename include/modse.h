@@ -438,7 +438,7 @@ modse_status_t modse_orthogonalize_wgrads(const modse_layer_t *layer, modse_dtyp
 
 /* Synchronises the stream and reads the status word of the last call that used this
  * workspace (modse_linear, modse_linear_backward, modse_orthogonalize): MODSE_OK or
- * MODSE_ERR_DEVICE_TIMEOUT.                                                  */
+ * MODSE_ERR_DEVICE_TIMEOUT.  A call without tokens or matrices leaves MODSE_OK there. */
 modse_status_t modse_check_workspace_status(const void *workspace, void *cuda_stream);
 
 /* Debugging aid, process-wide: when on, bf16 layers run their grouped GEMMs on

@@ -402,10 +402,10 @@ def orthogonalize(grads, updates, workspace, *, scales=None, steps: int = 5, coe
     n = len(grads)
     if len(updates) != n or (scales is not None and len(scales) != n):
         raise ValueError(f"{n} gradients, {len(updates)} updates, {n if scales is None else len(scales)} scales")
-    if n == 0:
+    if n == 0 and workspace is None:
         return
-    dt, code = grads[0].dtype, _dtype_code(grads[0])
-    stream, dev = _current_stream("grads", grads[0])
+    dt, code = (grads[0].dtype, _dtype_code(grads[0])) if n else (None, MODSE_BF16)
+    stream, dev = _current_stream("grads", grads[0]) if n else _current_stream("workspace", workspace)
     arr = (_Matrix * n)()
     for i, (g, u, m) in enumerate(zip(grads, updates, arr)):
         if (g.dtype != dt or g.get_device() != dev or u.dtype != torch.bfloat16 or u.get_device() != dev or

@@ -177,6 +177,13 @@ cudaError_t launch_dz(int act, const void *dy, const void *z, void *dz, float *p
 }
 
 }  // namespace
+
+void clear_workspace_status(void *workspace, size_t workspace_bytes, cudaStream_t s)
+{
+    if (workspace == nullptr || !aligned(workspace, 256) || workspace_bytes < sizeof(int)) return;
+    if (cudaMemsetAsync(workspace, 0, sizeof(int), s) != cudaSuccess) (void)cudaGetLastError();
+}
+
 }  // namespace modse
 
 using namespace modse;
@@ -206,7 +213,10 @@ modse_status_t modse_linear(modse_dtype_t dtype, int n_tokens, int d_in, int d_o
     if (args == nullptr || activation < MODSE_ACT_NONE || activation > MODSE_ACT_SILU) return MODSE_ERR_INVALID_ARG;
     const size_t need = modse_linear_workspace_bytes(dtype, n_tokens, d_in, d_out);
     if (need == 0) return MODSE_ERR_INVALID_ARG;
-    if (n_tokens == 0) return MODSE_OK;
+    if (n_tokens == 0) {
+        clear_workspace_status(workspace, workspace_bytes, (cudaStream_t)cuda_stream);
+        return MODSE_OK;
+    }
     const modse_linear_t &a = *args;
     if (a.x == nullptr || a.w == nullptr || a.y == nullptr || !aligned(a.x, 16) || !aligned(a.w, 16) || !aligned(a.bias, 16) ||
         !aligned(a.residual, 16) || !aligned(a.z, 16) || !aligned(a.y, 16))
@@ -248,6 +258,7 @@ modse_status_t modse_linear_backward(int n_tokens, int d_in, int d_out, modse_ac
     if (!aligned(a.dw, 16) || !aligned(a.dbias, 4)) return MODSE_ERR_INVALID_ARG;
     const cudaStream_t s = (cudaStream_t)cuda_stream;
     if (n_tokens == 0) {
+        clear_workspace_status(workspace, workspace_bytes, s);
         if (a.dw) MODSE_CUDA(cudaMemsetAsync(a.dw, 0, (size_t)d_out * d_in * 2, s));
         if (a.dbias) MODSE_CUDA(cudaMemsetAsync(a.dbias, 0, (size_t)d_out * 4, s));
         return MODSE_OK;

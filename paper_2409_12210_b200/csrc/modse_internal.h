@@ -116,6 +116,9 @@ void layer_expert(const modse_layer_t *layer, int e, int *d, int *S, int *offset
 int device_sms();      // SMs of the current device (148 where the question fails)
 // out[c] = sum over r of part[r][c], in a fixed order
 cudaError_t launch_column_sum(const float *part, int n_rows, int d, float *out, cudaStream_t s);
+// For calls that have nothing to do: the status word their caller may read afterwards.  Such a call succeeds without a
+// workspace, and without a device too, so what cannot be cleared is not an error (linear.cu).
+void clear_workspace_status(void *workspace, size_t workspace_bytes, cudaStream_t s);
 
 // ---- fp32-FMA grouped GEMMs and SwiGLU elementwise (simt_gemm.cu) ----
 enum GemmKind : int {

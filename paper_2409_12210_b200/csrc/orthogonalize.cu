@@ -429,7 +429,10 @@ modse_status_t modse_orthogonalize(modse_dtype_t dtype, int n_matrices, const mo
     if (st != MODSE_OK) return st;
     const size_t need = modse_orthogonalize_workspace_bytes(n_matrices, matrices);
     if (need == 0) return MODSE_ERR_INVALID_ARG;
-    if (n_matrices == 0) return MODSE_OK;
+    if (n_matrices == 0) {
+        clear_workspace_status(workspace, workspace_bytes, (cudaStream_t)cuda_stream);
+        return MODSE_OK;
+    }
     for (int i = 0; i < n_matrices; ++i)
         if (!pointers_ok(dtype, matrices[i])) return MODSE_ERR_INVALID_ARG;
     if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return MODSE_ERR_INVALID_ARG;

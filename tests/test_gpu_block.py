@@ -181,6 +181,20 @@ def test_offsets_past_32_bits():
     assert bool(((dx[-3:].double() - ref).abs() <= 2.0 ** -8 * ref.abs() + (n + 64) * 2.0 ** -23 * mag).all())
 
 
+def test_calls_with_nothing_to_do_leave_a_clean_status_word():
+    from paper_2409_12210_b200 import binding as B
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    x, w, y = torch.empty(0, 64, **bf), torch.zeros(32, 64, **bf), torch.empty(0, 32, **bf)
+    dw, db = torch.ones(32, 64, **bf), torch.ones(32, device="cuda")
+    calls = [lambda ws: B.linear(x, w, y, ws), lambda ws: B.linear_backward(x, w, y, y, "gelu", x, dw, db, ws),
+             lambda ws: B.orthogonalize([], [], ws)]
+    for call in calls:
+        ws = torch.full((1 << 20,), 0xA5, dtype=torch.uint8, device="cuda")
+        call(ws)
+        assert B.check_workspace_status(ws) == B.MODSE_OK
+        assert bool((ws[4:] == 0xA5).all())
+
+
 FIRST_CALLS = """
 import torch
 from paper_2409_12210_b200 import binding as B
