@@ -10,8 +10,6 @@ from __future__ import annotations
 import ctypes
 import os
 
-import torch
-
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "libmodse.so")
 
@@ -65,6 +63,13 @@ class _Matrix(ctypes.Structure):
 
 
 _lib = None
+torch = None      # bound by the first call that is handed tensors: loading and the host-side calls do without it
+
+
+def _bind_torch():
+    global torch
+    import torch as module
+    torch = module
 
 
 def lib_path() -> str:
@@ -258,6 +263,8 @@ def check_pairs(ffn_sizes):
 
 
 def _dtype_code(t):
+    if torch is None:
+        _bind_torch()
     if t.dtype == torch.float32:
         return MODSE_F32
     if t.dtype == torch.bfloat16:
@@ -280,6 +287,8 @@ def _buffer(name, t, shape, dtype, device):
 
 def _current_stream(name, t):
     """(raw current stream, device index) of t's device, which has to be the current CUDA device."""
+    if torch is None:
+        _bind_torch()
     device = t.get_device()
     if device < 0 or device != torch._C._cuda_getDevice():
         raise ValueError(f"{name}: expected a tensor on the current CUDA device, got one on {t.device}")
@@ -327,6 +336,8 @@ def add_rms_norm_backward(s, weight, eps: float, dy, dsum, dx, dweight=None, wor
 
 
 def _linear_code(dtype):
+    if torch is None:
+        _bind_torch()
     if dtype == torch.bfloat16:
         return MODSE_BF16
     if dtype == torch.float8_e4m3fn:
@@ -345,9 +356,9 @@ def linear(x, w, y, workspace, *, bias=None, residual=None, activation: str = "n
     ``w_scale``); everything else is bf16."""
     T, k = _rows("x", x)
     n = _rows("w", w)[0]
-    bf, code = torch.bfloat16, _linear_code(x.dtype)
+    code = _linear_code(x.dtype)
     stream, dev = _current_stream("x", x)
-    f32, out = torch.float32, (T, n)
+    bf, f32, out = torch.bfloat16, torch.float32, (T, n)
     args = _Linear(_buffer("x", x, (T, k), x.dtype, dev), _buffer("w", w, (n, k), x.dtype, dev),
                    _buffer("x_scale", x_scale, (T,), f32, dev), _buffer("w_scale", w_scale, (n,), f32, dev),
                    _buffer("bias", bias, (n,), bf, dev), _buffer("residual", residual, out, bf, dev),
@@ -366,8 +377,8 @@ def linear_backward(x, w, dy, z, activation: str, dx, dw, dbias, workspace) -> N
     there is no activation) into ``dx``, ``dw`` (bf16) and ``dbias`` (fp32); any of the three may be None."""
     T, k = _rows("x", x)
     n = _rows("w", w)[0]
-    bf = torch.bfloat16
     stream, dev = _current_stream("x", x)
+    bf = torch.bfloat16
     args = _LinearGrads(_buffer("x", x, (T, k), bf, dev), _buffer("w", w, (n, k), bf, dev),
                         _buffer("dy", dy, (T, n), bf, dev), _buffer("z", z, (T, n), bf, dev),
                         _buffer("dx", dx, (T, k), bf, dev), _buffer("dw", dw, (n, k), bf, dev),
@@ -424,6 +435,7 @@ def orthogonalize(grads, updates, workspace, *, scales=None, steps: int = 5, coe
 
 def check_workspace_status(workspace) -> int:
     """Status the last operator call on this workspace left (synchronises the current stream)."""
+    import torch
     return int(load().modse_check_workspace_status(workspace.data_ptr(), torch.cuda.current_stream().cuda_stream))
 
 

@@ -140,3 +140,24 @@ def test_fusion_flags_and_debug_switches_need_no_gpu():
     B.debug_skip_tile_loads(-1, -1)
     B.debug_set_dynamic_tiles(True)
     B.debug_set_default_tile_plan(B.DEFAULT_TILE_PLAN)
+
+
+WITHOUT_TORCH = """
+import sys
+sys.modules["torch"] = None                    # any import of it raises
+from paper_2409_12210_b200 import binding as B
+assert B.status_string(0) and B.check_pairs([96, 160, 112, 144])[0]
+layer = B.ModseLayer(64, [96, 160, 112, 144], 2)
+assert layer.workspace_bytes(B.MODSE_F32, 100, True) > 0 and layer.orthogonalize_workspace_bytes() > 0
+assert B.add_rms_norm_backward_workspace_bytes(4, 64) > 0 and B.linear_backward_workspace_bytes(4, 64, 32) > 0
+assert B.orthogonalize_workspace_bytes([(16, 24)]) > 0
+layer.destroy()
+print("done")
+"""
+
+
+def test_host_side_calls_do_without_torch():
+    import subprocess
+    import sys
+    out = subprocess.run([sys.executable, "-c", WITHOUT_TORCH], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and "done" in out.stdout, out.stderr[-2000:]
