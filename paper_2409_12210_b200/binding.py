@@ -434,9 +434,10 @@ def orthogonalize(grads, updates, workspace, *, scales=None, steps: int = 5, coe
 
 
 def check_workspace_status(workspace) -> int:
-    """Status the last operator call on this workspace left (synchronises the current stream)."""
-    import torch
-    return int(load().modse_check_workspace_status(workspace.data_ptr(), torch.cuda.current_stream().cuda_stream))
+    """Status the last operator call on this workspace left (synchronises the current stream, which has to be the call's).
+    Like the calls it wants the workspace on the current device: another device's stream would not have been waited for."""
+    stream, dev = _current_stream("workspace", workspace)
+    return int(load().modse_check_workspace_status(_workspace(workspace, dev)[0], stream))
 
 
 def _workspace(t, device):

@@ -161,3 +161,9 @@ def test_host_side_calls_do_without_torch():
     import sys
     out = subprocess.run([sys.executable, "-c", WITHOUT_TORCH], cwd=ROOT, capture_output=True, text=True, timeout=300)
     assert out.returncode == 0 and "done" in out.stdout, out.stderr[-2000:]
+
+
+def test_status_of_a_workspace_that_is_not_on_the_current_device_is_refused():
+    torch = pytest.importorskip("torch")
+    with pytest.raises(ValueError):
+        B.check_workspace_status(torch.zeros(256, dtype=torch.uint8))
