@@ -1001,7 +1001,8 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
             if (q.flags & kDenseLast) {
                 // A copy of a box that the last column cuts ends at a multiple of 16 bytes, past that column (600 x 1100 in rows
                 // of 1128: four columns beside the block were zeroed), so the width has to be a multiple of 8 as well.
-                if ((((q.ld_out | q.N) & 7) | (reinterpret_cast<uintptr_t>(q.out0) & 15)) == 0) {
+                // (A tensor map's rows are less than 2^40 bytes apart; a matrix of one row may say more.)
+                if ((((q.ld_out | q.N) & 7) | (reinterpret_cast<uintptr_t>(q.out0) & 15)) == 0 && q.ld_out < 1ll << 39) {
                     q.flags |= kDenseTmaOut;
                     ok = encode_output(&prm.o0[i], q.out0, q.M, q.N, q.ld_out);
                 }

@@ -222,6 +222,23 @@ def test_norms_and_eps_at_the_ends_of_fp32(shape):
 
 
 @pytest.mark.gpu
+def test_one_row_with_the_longest_row_distance():
+    """A single row's distance to the next is never used; grouped products (65536 columns do not fit the one-kernel form)."""
+    import ctypes
+
+    from paper_2409_12210_b200 import binding as B
+    G, out = gaussian(1, 65536, 14), torch.full((1, 65536), 7.0, dtype=torch.bfloat16, device="cuda")
+    far = (1 << 40) - 8
+    arr = (B._Matrix * 1)(B._Matrix(G.data_ptr(), out.data_ptr(), far, far, 1, 65536, 1.0))
+    n = B.load().modse_orthogonalize_workspace_bytes(1, arr)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    st = B.load().modse_orthogonalize(B.MODSE_BF16, 1, arr, 5, (ctypes.c_float * 3)(*MUON), 1e-7, ws.data_ptr(), n,
+                                      torch.cuda.current_stream().cuda_stream)
+    assert st == B.MODSE_OK and B.check_workspace_status(ws) == B.MODSE_OK
+    check(out, G)
+
+
+@pytest.mark.gpu
 def test_replay_in_a_graph():
     from paper_2409_12210_b200 import binding as B
     G = gaussian(300, 500, 11)
