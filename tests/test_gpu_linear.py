@@ -156,6 +156,76 @@ def test_backward(shape, act):
     assert np.all(np.abs(f64(db) - dz.sum(0)) <= tol)
 
 
+# Shapes some of whose tiles are cut along the contraction on 74 CTA pairs (at least 32 k-blocks, and a last round that leaves
+# room): the last 6, 7 or 16 of more tiles than pairs in two pieces, ragged edges among them; few tiles in two to eight pieces.
+CUT = [(2500, 2304, 2048), (2100, 2056, 2056), (1000, 2048, 1032), (64, 5632, 2048), (40, 8448, 1032), (33, 8448, 136)]
+CUT8 = [(2500, 4112, 2056), (1000, 4096, 1032), (40, 16400, 136)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", CUT)
+@pytest.mark.parametrize("act,bias,residual,save", [("silu", True, True, True), ("relu", True, False, False)])
+def test_cut_tiles_bf16(shape, act, bias, residual, save):
+    check_forward(*shape, False, act, bias, residual, save)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", CUT8)
+@pytest.mark.parametrize("act,bias,residual,save", [("none", False, True, False), ("silu", True, False, True)])
+def test_cut_tiles_e4m3(shape, act, bias, residual, save):
+    check_forward(*shape, True, act, bias, residual, save)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(2100, 2056, 2056), (300, 2304, 2304)])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_cut_tiles_backward(shape, act):
+    """dx and dw in one launch whose last tiles are cut; dx alone of the second shape, in 128-column tiles."""
+    test_backward(shape, act)
+    full, part = run_backward(*shape, act), run_backward(*shape, act, ("dx",))
+    assert torch.allclose(full[4].float(), part[4].float(), rtol=2.0 ** -7, atol=1e-5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(2500, 2304, 2048), (40, 8448, 1032)])
+def test_cut_tiles_in_graphs(shape):
+    """The counters that find a strip's last piece are zero again after every launch: replays, two graphs with a workspace
+    each running at once, and eager calls between them."""
+    from paper_2409_12210_b200 import binding as B
+    T, k, n = shape
+    rng = np.random.default_rng(15)
+    xs = [rand(rng, T, k).bfloat16() for _ in range(3)]
+    w, r = rand(rng, n, k, std=k ** -0.5).bfloat16(), rand(rng, T, n).bfloat16()
+    size = B.linear_workspace_bytes(w.dtype, T, k, n)
+    wss = [workspace(size) for _ in range(3)]
+    refs = []
+    for x in xs:
+        y = torch.empty_like(r)
+        B.linear(x, w, y, wss[2][0], residual=r, activation="silu")
+        refs.append(y)
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    ins, outs, graphs = [torch.zeros_like(xs[0]) for _ in sides], [torch.empty_like(r) for _ in sides], []
+    torch.cuda.synchronize()
+    for side, x, y, ws in zip(sides, ins, outs, wss):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            B.linear(x, w, y, ws[0], residual=r, activation="silu")
+        graphs.append(graph)
+    for i in range(3):
+        for j, (side, graph) in enumerate(zip(sides, graphs)):
+            with torch.cuda.stream(side):
+                ins[j].copy_(xs[(i + j) % 3])
+                for _ in range(4):
+                    graph.replay()
+        torch.cuda.synchronize()
+        for j in range(2):
+            assert torch.equal(outs[j], refs[(i + j) % 3])
+        B.linear(xs[i], w, outs[0], wss[0][0], residual=r, activation="silu")
+        assert B.check_workspace_status(wss[0][0]) == B.MODSE_OK and torch.equal(outs[0], refs[i])
+        torch.cuda.synchronize()
+    assert all(bool((margin == 0xA5).all()) for _, margin in wss)
+
+
 @pytest.mark.gpu
 def test_512_row_tiles():
     """Shapes whose products run on 512-row tiles: a ragged last tile with one 256-row half, column edges, a tail dealt out

@@ -182,6 +182,51 @@ def test_column_blocks_of_every_alignment_in_one_launch(cols, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(1300, 2100), (2203, 2100), (2100, 2203), (2900, 2904)])
+def test_tiles_cut_along_the_contraction(shape):
+    """On 74 CTA pairs: 36 narrow tiles of X X^T in two pieces each; the last 7 tiles of the step, wide and tall, written by
+    plain stores into a column block; the last 4 of 78 symmetric tiles of X X^T and of the polynomial."""
+    from paper_2409_12210_b200 import binding as B
+    G = gaussian(*shape, seed=18)
+    target = torch.full((shape[0], shape[1] + 9), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = target[:, 3:3 + shape[1]]
+    n = B.orthogonalize_workspace_bytes([shape])
+    ws = torch.full((n + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    B.orthogonalize([G], [out], ws[:n])
+    assert B.check_workspace_status(ws) == B.MODSE_OK and bool((ws[n:] == 0xA5).all())
+    check(out, G)
+    assert bool((target[:, :3] == 7).all()) and bool((target[:, 3 + shape[1]:] == 7).all())
+    first = out.clone()
+    B.orthogonalize([G], [out], ws[:n])
+    assert torch.equal(first, out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d,sizes", [(256, (128, 384, 192, 320)), (64, (96, 160, 112, 144)), (520, (272, 304, 144, 432))])
+def test_updates_of_a_layer(d, sizes, dtype):
+    """The expert matrices of a layer against the iteration in 64 bits: rows of the gate and up gradients, column blocks of
+    the down gradients, a scale a matrix; grouped products, the one-kernel form, and widths above and below the d_model."""
+    from paper_2409_12210_b200 import binding as B
+    layer = B.ModseLayer(d, list(sizes), 2)
+    S = sum(sizes)
+    grads = [gaussian(S, d, 21, dtype), gaussian(S, d, 22, dtype), gaussian(d, S, 23, dtype)]
+    ups = [torch.full(g.shape, 7.0, dtype=torch.bfloat16, device="cuda") for g in grads]
+    n = layer.orthogonalize_workspace_bytes()
+    ws = torch.full((n + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+    scales = [[0.5 + 0.25 * e, 1.0, 2.0 - 0.25 * e] for e in range(len(sizes))]
+    layer.orthogonalize_wgrads(*grads, *ups, ws[:n], scales=scales)
+    assert B.check_workspace_status(ws) == B.MODSE_OK and bool((ws[n:] == 0xA5).all())
+    off = 0
+    for e, h in enumerate(sizes):
+        rows, cols = slice(off, off + h), (slice(None), slice(off, off + h))
+        for j, at in enumerate((rows, rows, cols)):
+            check(ups[j][at], grads[j][at], scale=scales[e][j])
+        off += h
+    layer.destroy()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("steps,k", [(1, MUON), (8, MUON), (12, (1.5, -0.5, 0.0)), (3, (1.875, -1.25, 0.375))])
 def test_other_coefficients(steps, k):
     G = gaussian(120, 200, 7, torch.float32)
