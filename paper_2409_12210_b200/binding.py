@@ -295,10 +295,14 @@ def _current_stream(name, t):
     return torch._C._cuda_getCurrentRawStream(device), device
 
 
+_INT_MAX = 2 ** 31 - 1
+
+
 def _rows(name, t):
-    if t.dim() != 2:
-        raise ValueError(f"{name}: expected two dimensions, got shape {tuple(t.shape)}")
-    return t.shape
+    shape = t.shape
+    if len(shape) != 2 or shape[0] > _INT_MAX or shape[1] > _INT_MAX:      # ctypes would cut longer extents down silently
+        raise ValueError(f"{name}: expected two dimensions of less than 2^31, got shape {tuple(shape)}")
+    return shape
 
 
 def add_rms_norm(x, residual, weight, eps: float, *, sum_out=None, y=None, y8=None, y_scale=None) -> None:

@@ -167,3 +167,17 @@ def test_status_of_a_workspace_that_is_not_on_the_current_device_is_refused():
     torch = pytest.importorskip("torch")
     with pytest.raises(ValueError):
         B.check_workspace_status(torch.zeros(256, dtype=torch.uint8))
+
+
+def test_extents_past_31_bits_are_refused_not_truncated():
+    torch = pytest.importorskip("torch")
+    for shape in [(2 ** 32 + 8, 64), (64, 2 ** 32 + 64)]:
+        t = torch.empty(shape, dtype=torch.bfloat16, device="meta")
+        small = torch.empty((64, 64), dtype=torch.bfloat16, device="meta")
+        for call in (lambda: B.add_rms_norm(t, None, None, 1e-5, y=t),
+                     lambda: B.add_rms_norm_backward(t, None, 1e-5, t, None, t),
+                     lambda: B.linear(t, small, t, None), lambda: B.linear(small, t, t, None),
+                     lambda: B.linear_backward(t, small, t, None, "none", None, None, None, None),
+                     lambda: B._ld("gradient", t)):
+            with pytest.raises(ValueError, match="less than 2"):
+                call()
