@@ -112,14 +112,12 @@ __device__ __forceinline__ DenseTile dense_decode(const DenseParams<P> &prm, int
         while (cursor + 1 < prm.n_prob && tile >= prm.prob[cursor + 1].tile0) ++cursor;
     t.p = cursor;
     const DenseProblem &q = prm.prob[cursor];
-    constexpr int kUnits = DenseShape<TALL>::kTileRows / TN;      // column tiles as wide as a row tile is high
     int local = tile - q.tile0, mb, nb;
-    bool below = false;                          // symmetric: the second half lies below the diagonal
-    if (q.flags & kDenseSym) {
+    if (!TALL && (q.flags & kDenseSym)) {
+        constexpr int kUnits = DenseShape<TALL>::kTileRows / TN;  // column tiles as wide as a row tile is high
         mb = 0;                                  // row by row of the upper triangle; squares on the diagonal are whole
         while (local >= q.nt - kUnits * mb) { local -= q.nt - kUnits * mb; ++mb; }
         nb = kUnits * mb + local;
-        below = TALL && local == 0;
     } else {
         const int per = kDenseGroupRows * q.nt, g = local / per, rem = local - g * per;
         const int rows = min(kDenseGroupRows, q.mt - g * kDenseGroupRows);
@@ -128,7 +126,7 @@ __device__ __forceinline__ DenseTile dense_decode(const DenseParams<P> &prm, int
     }
     t.m0 = mb * DenseShape<TALL>::kTileRows;
     t.n0 = nb * TN;
-    t.two = TALL && !below && t.m0 + 256 < q.M;
+    t.two = TALL && t.m0 + 256 < q.M;
     t.skip = false;
     if (half >= 0) {
         t.skip = half == 1 && !t.two;
@@ -905,16 +903,17 @@ struct DensePlan {
 
 int dense_nk(DenseType type, long long k) { return (int)((k + (type == DenseE4m3 ? 127 : 63)) / (type == DenseE4m3 ? 128 : 64)); }
 
+// (A symmetric output has no tall form.)
 long long dense_tiles(const DenseProblem &p, bool tall, int tn)
 {
     const long long mt = (p.M + (tall ? 511 : 255)) / (tall ? 512 : 256), nt = (p.N + tn - 1) / tn;
     if (!(p.flags & kDenseSym)) return mt * nt;
     long long c = 0;
-    for (long long m = 0; m < mt; ++m) c += nt - (tall ? 512 : 256) / tn * m;
+    for (long long m = 0; m < mt; ++m) c += nt - 256 / tn * m;
     return c;
 }
 
-DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int n, bool light, int sms, size_t partial_capacity)
+DensePlan dense_plan(DenseType type, const DenseItem *items, int n, bool light, int sms, size_t partial_capacity)
 {
     const int pairs = std::max(1, sms / 2);
     auto count = [&](bool tall, int tn) {
@@ -929,7 +928,7 @@ DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int
     // of 256-row tiles 585 a k-block.  Measured, tall against not: dx and dw of 16384 x 2048 -> 5632 504 against 580 us,
     // the product alone 250 against 262, with K 5632 273 against 283; but 350 against 303 with bias, gelu and z, 293
     // against 282 with a residual, 205 against 148 from 8-bit rows, 56 against 58 with 16 k-blocks.
-    const long long talls = count(true, 256), squares = count(false, 256);
+    const long long talls = light ? count(true, 256) : 0, squares = count(false, 256);
     const long long whole = talls / pairs, rest = talls % pairs;
     const double tall_rounds = (double)whole + (rest == 0 ? 0.0 : 2 * rest <= pairs ? 0.57 : 1.0);
     const double square_rounds = (double)((squares + pairs - 1) / pairs);
@@ -980,6 +979,7 @@ DensePlan dense_plan(DenseMode mode, DenseType type, const DenseItem *items, int
 template <int MODE, int TYPE, int TN, bool TALL, bool SHARED, int P>
 cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const LinearEpilogue *lin, const DenseColumnSum *sum, void *ws, int head, cudaStream_t s)
 {
+    static_assert(!TALL || MODE == DensePlain || MODE == DenseLinear, "dense_decode has no tall form of symmetric outputs");
     DenseParams<P> prm;
     int tiles = 0;
     for (int i = 0; i < n; ++i) {
@@ -1054,7 +1054,7 @@ cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin
 {
     if (n > P) return cudaErrorInvalidValue;
     const bool light = MODE == DensePlain || (MODE == DenseLinear && TYPE == DenseBf16 && !lin->residual && !lin->z && lin->act <= MODSE_ACT_RELU);
-    const DensePlan pl = dense_plan((DenseMode)MODE, (DenseType)TYPE, items, n, light, device_sms(), cap);
+    const DensePlan pl = dense_plan((DenseType)TYPE, items, n, light, device_sms(), cap);
     if constexpr (MODE == DensePlain || (MODE == DenseLinear && TYPE == DenseBf16))
         if (pl.tall) return launch_tn<MODE, TYPE, 256, true, false, P>(pl, items, n, lin, sum, ws, head, s);
     if (pl.share > 1)       // so few tiles are 128 columns wide
@@ -1065,9 +1065,9 @@ cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin
 
 }  // namespace
 
-size_t dense_partial_bytes(DenseMode mode, DenseType type, const DenseItem *items, int n)
+size_t dense_partial_bytes(DenseType type, const DenseItem *items, int n)
 {
-    const DensePlan pl = dense_plan(mode, type, items, n, false, kDenseSms, ~(size_t)0 >> 1);
+    const DensePlan pl = dense_plan(type, items, n, false, kDenseSms, ~(size_t)0 >> 1);
     return !pl.tall && pl.splits > 1 ? (size_t)(pl.items - pl.full) * 256 * pl.tn * 4 : 0;
 }
 

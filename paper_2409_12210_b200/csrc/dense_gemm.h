@@ -75,7 +75,7 @@ constexpr size_t kDenseZeroBytes = kDenseCounterOffset + (size_t)kDenseMaxSplitI
 constexpr size_t kDenseHead = (kDenseZeroBytes + 255) / 256 * 256;
 
 // Bytes behind the head that a launch of these products (extents and flags of p, k) can use for pieces.
-size_t dense_partial_bytes(DenseMode mode, DenseType type, const DenseItem *items, int n);
+size_t dense_partial_bytes(DenseType type, const DenseItem *items, int n);
 // Bytes that hold the pieces of these products and of any set with smaller extents or contractions: it never falls when an
 // extent grows, as the exact figure does (2048 -> 5632: 14.7 MB for 2048 tokens, none for 8192).
 size_t dense_partial_bound(DenseType type, const DenseItem *items, int n);

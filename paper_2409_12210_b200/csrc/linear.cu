@@ -17,7 +17,7 @@ bool extents_ok(int T, int k, int n, int k_step)
 // tiles of 256 x 128 have to be countable in 31 bits
 bool countable(long long m, long long n) { return ((m + 255) / 256) * ((n + 127) / 128) < (1ll << 30); }
 
-DenseItem forward_item(DenseType type, int T, int k, int n, const void *x, const void *w)
+DenseItem forward_item(int T, int k, int n, const void *x, const void *w)
 {
     DenseItem it{};
     it.a = {x, T, k, k};
@@ -25,7 +25,6 @@ DenseItem forward_item(DenseType type, int T, int k, int n, const void *x, const
     it.p.M = T;
     it.p.N = n;
     it.k = k;
-    (void)type;
     return it;
 }
 
@@ -138,7 +137,7 @@ linear_dz_kernel(const __nv_bfloat16 *dy, const __nv_bfloat16 *z, __nv_bfloat16 
     }
 }
 
-// Strips of rows of the dz kernel: 64 rows, more where the launch's second grid extent would pass 65535.
+// Strips of 64 rows of the dz kernel, its second grid extent: at most 65535 of them, so at most 4194240 tokens a call.
 int dz_strips(int T) { return (int)(((long long)T + kDzRows - 1) / kDzRows); }
 
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -202,7 +201,7 @@ size_t modse_linear_workspace_bytes(modse_dtype_t dtype, int n_tokens, int d_in,
         return 0;
     const DenseType type = dtype == MODSE_E4M3 ? DenseE4m3 : DenseBf16;
     if (n_tokens <= kLinearRowsMax) return kDenseHead;
-    const DenseItem it = forward_item(type, n_tokens, d_in, d_out, nullptr, nullptr);
+    const DenseItem it = forward_item(n_tokens, d_in, d_out, nullptr, nullptr);
     return kDenseHead + up256(dense_partial_bound(type, &it, 1));
 }
 
@@ -234,7 +233,7 @@ modse_status_t modse_linear(modse_dtype_t dtype, int n_tokens, int d_in, int d_o
         MODSE_CUDA(launch_linear_rows(type, a.x, a.w, n_tokens, d_in, d_out, lin, (int *)workspace, s));
         return MODSE_OK;
     }
-    const DenseItem it = forward_item(type, n_tokens, d_in, d_out, a.x, a.w);
+    const DenseItem it = forward_item(n_tokens, d_in, d_out, a.x, a.w);
     MODSE_CUDA(dense_launch(DenseLinear, type, &it, 1, &lin, nullptr, workspace, need - kDenseHead, kDenseHeadRaw, s));
     return MODSE_OK;
 }

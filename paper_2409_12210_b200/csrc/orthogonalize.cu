@@ -238,8 +238,8 @@ void group_layout(const modse_matrix_t *m, int n, GroupLayout &L)
 {
     DenseItem gram[kGroup], poly[kGroup], step[kGroup];
     for (int i = 0; i < n; ++i) step_items(m[i], nullptr, nullptr, nullptr, gram[i], poly[i], step[i]);
-    size_t need = dense_partial_bytes(DenseGram, DenseF16, gram, n);
-    const size_t p2 = dense_partial_bytes(DensePoly, DenseF16, poly, n), p3 = dense_partial_bytes(DenseStep, DenseF16, step, n);
+    size_t need = dense_partial_bytes(DenseF16, gram, n);
+    const size_t p2 = dense_partial_bytes(DenseF16, poly, n), p3 = dense_partial_bytes(DenseF16, step, n);
     need = need > p2 ? need : p2;
     need = need > p3 ? need : p3;
     L.partials = kDenseHead;

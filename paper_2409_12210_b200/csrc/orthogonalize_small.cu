@@ -8,7 +8,7 @@
 //   B = aI + bA + cA^2  computed by every block for itself (a 128 x 128 product is cheaper than another meeting);
 //   X <- B hi + a lo   every block on its own columns.
 // Of the longest matrices the step replaces hi in place instead of writing a second copy: a warp then takes all rows of
-// sixteen columns.  Sixteen blocks and the step in place hold 64 x 12544 to 128 x 3840, eight blocks 64 x 3968 to 128 x 1792
+// sixteen columns.  Eight blocks hold 64 x 3968 to 128 x 896, sixteen 64 x 7936 to 128 x 1792 and in place 64 x 12544 to 128 x 3840
 // (75 x 3499, 114 x 75 and 1345 x 75: 63 us against 175 as grouped products; 64 x 8448 97 against 141; 99 x 5000, near the
 // end of the range, 115 against 133).
 // The roundings are those of the grouped form (orthogonalize.cu): fp16 factors scaled by powers of two, X in 22 bits.

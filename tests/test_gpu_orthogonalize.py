@@ -362,3 +362,18 @@ def test_refusals_need_no_gpu():
     assert f(layer._h, B.MODSE_F32, B._WGrads(None, p, None, p), g, None, 5, k3, 1e-7, p, full) == inv
     assert f(layer._h, B.MODSE_F32, g, g, None, 5, k3, 1e-7, p, full - 1) == B.MODSE_ERR_WORKSPACE_TOO_SMALL
     layer.destroy()
+
+
+def test_what_the_one_kernel_form_holds():
+    """Sets in the one-kernel form need the head of the workspace alone: sixteen blocks a matrix for up to seven matrices,
+    eight for more; columns in steps of sixteen a block."""
+    from paper_2409_12210_b200 import binding as B
+    from paper_2409_12210_b200 import build
+    build.build()
+    head = B.orthogonalize_workspace_bytes([(1, 1)])
+    for count, ends in [(8, {64: 3968, 96: 2048, 112: 1408, 128: 896}), (7, {64: 12544, 96: 6912, 112: 5376, 128: 3840})]:
+        for short, long in ends.items():
+            for shape in ((short, long), (long, short)):
+                assert B.orthogonalize_workspace_bytes([shape] * count) == head, shape
+            assert B.orthogonalize_workspace_bytes([(short, long + 1)] * count) > head
+        assert B.orthogonalize_workspace_bytes([(129, 130)] * count) > head
