@@ -312,8 +312,8 @@ const char *modse_stage_name(int stage);
  * None of them uses a layer object; tensors are row-major and contiguous unless
  * said otherwise, every pointer 16-byte aligned unless said otherwise, every
  * workspace 256-byte aligned and in use by one call at a time (two calls that may
- * overlap, or two captured graphs that may, need one each).  Results do not
- * depend on the order in which blocks run.  (The paper fixes none of them: its
+ * overlap, or two captured graphs that may, need one each).  Outputs of a call do
+ * not overlap one another.  Results do not depend on the order in which blocks run.  (The paper fixes none of them: its
  * blocks are Llama-2's, Sec. 4.1, whose pre-norm residual form this is.)      */
 
 /* Residual addition and root-mean-square norm, the step that makes a sub-layer's

@@ -4,9 +4,10 @@
 // copy rate), so the kernel is built around loads in flight, not around the tensor cores' peak: a block of eight warps
 // owns 16 rows of w, each warp takes every eighth 128-byte column block of them straight from global memory into
 // mma.sync fragments, and the eight partial sums meet in shared memory in a fixed order.  A 128-row tcgen05 tile would
-// spend its time on filling and draining itself.  Measured, weights from HBM (launch included, an empty one is 2.3 us):
-// one token on 2048 x 5632 bf16 7.4 us (23 MB: 3.5 us at the measured copy rate), on 8448 x 8448 27.2 us (143 MB: 21.8);
-// 24 tokens on 2048 x 5632 e4m3 6 us (11.5 MB: 1.8); the tcgen05 form takes 12 to 46 us on these.
+// spend its time on filling and draining itself.  Measured on rows of calls in a graph, each with weights of its own, so
+// that they come from HBM (in brackets the weights' time at the measured copy rate): one token on 2048 x 5632 bf16 7.1 us
+// (3.5), on 8448 x 8448 26.7 (21.8); 24 tokens on 2048 x 5632 e4m3 6.1 (1.8), 4.9 where the calls share weights that stay
+// in L2.  A call by itself, cold and with all of its launch, takes 3 to 5 us more.  The tcgen05 form takes 12 to 46 us on these.
 //
 // Fragments without shared memory: a sum over k may be taken in any order as long as both operands agree on it.  Thread
 // t of a group of four loads 16 contiguous bytes of its row of w and the same 16 bytes of its row of x; the k-th pair of
