@@ -358,6 +358,7 @@ modse_status_t modse_add_rms_norm_backward(modse_dtype_t dtype, int n_tokens, in
  * modse_linear_backward reads, is rounded once from the fp32 value, and y, from
  * the unrounded z, once.  Products are accumulated in fp32.
  * relu, gelu (z Phi(z), Phi the normal distribution function), silu (z / (1 + e^-z)).
+ * Infinities give the functions' limits, a NaN gives NaN.
  * The workspace's first bytes hold a status word that modse_check_workspace_status
  * reads (a bounded wait inside a kernel may expire, as in modse_forward).  Its size,
  * and that of the gradient's, never falls with n_tokens: one that serves a batch
