@@ -437,9 +437,37 @@ modse_status_t modse_orthogonalize_wgrads(const modse_layer_t *layer, modse_dtyp
                                           const float *coefficients, float eps, void *workspace, size_t workspace_bytes,
                                           void *cuda_stream);
 
+/* Embedding lookup with scaling, what the first block's residual stream is made of:
+ *   y_t = scale table[id_t].
+ * ids [T], of 4 or 8 bytes each (id_bytes; int32 or int64, aligned to that), table
+ * [vocabulary, d] and y [T, d] in `dtype`, y not overlapping the table; d a multiple
+ * of 8, at most 32768 (else MODSE_ERR_UNSUPPORTED); at most 2^30 tokens and rows.  A
+ * negative id is padding: its row of y is zeros.  So is that of an id past the table,
+ * which is an error: `status` (a device word, or NULL) then becomes nonzero, as
+ * modse_check_workspace_status reads it.  No call clears it, so one word may serve many.
+ * The product is formed in fp32 and rounded once.                             */
+modse_status_t modse_embedding(modse_dtype_t dtype, int n_tokens, int d_model, int vocabulary, const void *ids, int id_bytes,
+                               const void *table, float scale, void *y, int *status, void *cuda_stream);
+
+/* Gradient of the above: from dy [T, d] in `dtype`, into dtable [vocabulary, d] in
+ * grad_dtype,
+ *   dtable_v = scale sum of dy_t over all t with id_t = v,
+ * overwritten (rows that no id names are zeros), or, with accumulate, added to what is
+ * there (rows that no id names are not touched): to the gradient of a head that shares
+ * the table, or of earlier micro-batches.  Sums are fp32, over ascending t, in an order
+ * that does not depend on the run; each element is rounded once a call.  Ids as above: padding
+ * and ids past the table give nothing, the latter leave MODSE_ERR_DEVICE_BOUNDS in the
+ * workspace's status word.  dtable overlaps no input.  The workspace's size never falls
+ * with n_tokens.                                                              */
+size_t modse_embedding_backward_workspace_bytes(int n_tokens, int d_model, int vocabulary);
+modse_status_t modse_embedding_backward(modse_dtype_t dtype, int n_tokens, int d_model, int vocabulary, const void *ids,
+                                        int id_bytes, const void *dy, float scale, modse_dtype_t grad_dtype, int accumulate,
+                                        void *dtable, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 /* Synchronises the stream and reads the status word of the last call that used this
- * workspace (modse_linear, modse_linear_backward, modse_orthogonalize): MODSE_OK or
- * MODSE_ERR_DEVICE_TIMEOUT.  A call without tokens or matrices leaves MODSE_OK there. */
+ * workspace (modse_linear, modse_linear_backward, modse_orthogonalize,
+ * modse_embedding_backward): MODSE_OK, MODSE_ERR_DEVICE_TIMEOUT or
+ * MODSE_ERR_DEVICE_BOUNDS.  A call without tokens or matrices leaves MODSE_OK there. */
 modse_status_t modse_check_workspace_status(const void *workspace, void *cuda_stream);
 
 /* Debugging aid, process-wide: when on, bf16 layers run their grouped GEMMs on

@@ -181,6 +181,12 @@ def load():
     lib.modse_orthogonalize_wgrads.restype = ci
     lib.modse_orthogonalize_wgrads.argtypes = [vp, ci, ctypes.POINTER(_WGrads), ctypes.POINTER(_WGrads), fp, ci, fp, cf, vp,
                                                sz, vp]
+    lib.modse_embedding.restype = ci
+    lib.modse_embedding.argtypes = [ci, ci, ci, ci, vp, ci, vp, cf, vp, vp, vp]
+    lib.modse_embedding_backward_workspace_bytes.restype = sz
+    lib.modse_embedding_backward_workspace_bytes.argtypes = [ci, ci, ci]
+    lib.modse_embedding_backward.restype = ci
+    lib.modse_embedding_backward.argtypes = [ci, ci, ci, ci, vp, ci, vp, cf, ci, ci, vp, vp, sz, vp]
     lib.modse_check_workspace_status.restype = ci
     lib.modse_check_workspace_status.argtypes = [vp, vp]
     lib.modse_debug_use_fma_path.restype = None
@@ -435,6 +441,49 @@ def orthogonalize(grads, updates, workspace, *, scales=None, steps: int = 5, coe
                                     *_workspace(workspace, dev), stream)
     if st != MODSE_OK:
         raise ModseError(st, "modse_orthogonalize")
+
+
+def _tokens(name, t, n, device):
+    """(device address, bytes a number) of a tensor of n whole numbers."""
+    if torch is None:
+        _bind_torch()
+    if t.dtype not in (torch.int32, torch.int64):
+        raise TypeError(f"{name}: expected int32 or int64, got {t.dtype}")
+    return _buffer(name, t, (n,), t.dtype, device), t.element_size()
+
+
+def embedding(ids, table, y, *, scale: float = 1.0, status=None) -> None:
+    """modse_embedding on the current stream: ``y[t] = scale * table[ids[t]]``, zeros where the id is negative.  ids [T]
+    int32 or int64, table [vocabulary, d] and y [T, d] bf16 or fp32.  ``status``: None or one int32 that becomes nonzero
+    where an id lies past the table (see :func:`check_workspace_status`)."""
+    v, d = _rows("table", table)
+    T = _rows("y", y)[0]
+    dt, code = table.dtype, _dtype_code(table)
+    stream, dev = _current_stream("table", table)
+    address, width = _tokens("ids", ids, T, dev)
+    st = load().modse_embedding(code, T, d, v, address, width, _buffer("table", table, (v, d), dt, dev), scale,
+                                _buffer("y", y, (T, d), dt, dev), _buffer("status", status, (1,), torch.int32, dev), stream)
+    if st != MODSE_OK:
+        raise ModseError(st, "modse_embedding")
+
+
+def embedding_backward_workspace_bytes(n_tokens: int, d_model: int, vocabulary: int) -> int:
+    return int(load().modse_embedding_backward_workspace_bytes(n_tokens, d_model, vocabulary))
+
+
+def embedding_backward(ids, dy, dtable, workspace, *, scale: float = 1.0, accumulate: bool = False) -> None:
+    """modse_embedding_backward: the gradient of :func:`embedding` with respect to its table from ``dy`` [T, d] into
+    ``dtable`` [vocabulary, d] (each bf16 or fp32), overwritten or, with ``accumulate``, added to what is there."""
+    T, d = _rows("dy", dy)
+    v = _rows("dtable", dtable)[0]
+    code, grad_code = _dtype_code(dy), _dtype_code(dtable)
+    stream, dev = _current_stream("dy", dy)
+    address, width = _tokens("ids", ids, T, dev)
+    st = load().modse_embedding_backward(
+        code, T, d, v, address, width, _buffer("dy", dy, (T, d), dy.dtype, dev), scale, grad_code, int(bool(accumulate)),
+        _buffer("dtable", dtable, (v, d), dtable.dtype, dev), *_workspace(workspace, dev), stream)
+    if st != MODSE_OK:
+        raise ModseError(st, "modse_embedding_backward")
 
 
 def check_workspace_status(workspace) -> int:
