@@ -464,10 +464,53 @@ modse_status_t modse_embedding_backward(modse_dtype_t dtype, int n_tokens, int d
                                         int id_bytes, const void *dy, float scale, modse_dtype_t grad_dtype, int accumulate,
                                         void *dtable, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
+/* Softmax cross entropy over a vocabulary, straight from the rows that would be multiplied
+ * by the output matrix: the logits z = x w^T are formed tile by tile and never stored.
+ *   lse_t = log sum_v exp z_tv,   loss_t = lse_t - z_t,label_t.
+ * x [T, d] and w [vocabulary, d] bf16, d a multiple of 8, any vocabulary; labels [T], of
+ * 4 or 8 bytes each (label_bytes, aligned to that); loss and lse [T] fp32.  A token with a negative label is
+ * not counted: its loss is 0 (its lse is written all the same).  So is one with a label
+ * past the vocabulary, which is an error: MODSE_ERR_DEVICE_BOUNDS in the workspace's
+ * status word.  total [2] (or NULL): the sum of the losses and how many tokens were counted,
+ * both fp32; their quotient is the mean loss.  Logits are accumulated in fp32 and enter the
+ * exponentials unrounded.  Infinities and NaN go where the formulas lead; finite logits
+ * are below 2e38.  d at most 2^20, T and vocabulary at most 2^28, and their product at most
+ * 2^45.                                                                       */
+typedef struct {
+    const void *x, *w, *labels;
+    float *loss, *lse, *total;
+    int label_bytes;
+} modse_cross_entropy_t;
+size_t modse_cross_entropy_workspace_bytes(int n_tokens, int d_model, int vocabulary);
+modse_status_t modse_cross_entropy(int n_tokens, int d_model, int vocabulary, const modse_cross_entropy_t *args, void *workspace,
+                                   size_t workspace_bytes, void *cuda_stream);
+
+/* Gradient of sum_t f_t loss_t, from the lse that forward wrote:
+ *   dz_tv = f_t (exp(z_tv - lse_t) - [v = label_t]),  dx = dz w,  dw = dz^T x,
+ *   f_t = scale dloss_t / total[1]   for counted tokens, 0 for the others.
+ * dloss [T] fp32 (NULL: ones), total as forward wrote it (NULL: no division), so that
+ * the gradient of the mean loss takes neither arithmetic nor a copy to the host in between.
+ * A row whose f is 0 gives nothing, whatever its logits are.  dx [T, d] and dw
+ * [vocabulary, d] bf16; either may be NULL; both are overwritten and overlap no input.  The
+ * logits are formed again, a piece of the vocabulary at a time (the workspace holds one
+ * piece's dz: at most 128 MB or 2048 columns, whichever is more; and T d fp32 numbers where
+ * there are several pieces); dz enters the products rounded to bf16 once, sums are
+ * fp32.                                                                       */
+typedef struct {
+    const void *x, *w, *labels;
+    const float *lse, *dloss, *total;
+    void *dx, *dw;
+    float scale;
+    int label_bytes;
+} modse_cross_entropy_grads_t;
+size_t modse_cross_entropy_backward_workspace_bytes(int n_tokens, int d_model, int vocabulary);
+modse_status_t modse_cross_entropy_backward(int n_tokens, int d_model, int vocabulary, const modse_cross_entropy_grads_t *args,
+                                            void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 /* Synchronises the stream and reads the status word of the last call that used this
  * workspace (modse_linear, modse_linear_backward, modse_orthogonalize,
- * modse_embedding_backward): MODSE_OK, MODSE_ERR_DEVICE_TIMEOUT or
- * MODSE_ERR_DEVICE_BOUNDS.  A call without tokens or matrices leaves MODSE_OK there. */
+ * modse_embedding_backward, modse_cross_entropy and its gradient): MODSE_OK,
+ * MODSE_ERR_DEVICE_TIMEOUT or MODSE_ERR_DEVICE_BOUNDS.  A call without tokens or matrices leaves MODSE_OK there. */
 modse_status_t modse_check_workspace_status(const void *workspace, void *cuda_stream);
 
 /* Debugging aid, process-wide: when on, bf16 layers run their grouped GEMMs on

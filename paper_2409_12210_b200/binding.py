@@ -57,6 +57,15 @@ class _LinearGrads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("x", "w", "dy", "z", "dx", "dw", "dbias")]
 
 
+class _CrossEntropy(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "w", "labels", "loss", "lse", "total")] + [("label_bytes", ctypes.c_int)]
+
+
+class _CrossEntropyGrads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "w", "labels", "lse", "dloss", "total", "dx", "dw")] + \
+               [("scale", ctypes.c_float), ("label_bytes", ctypes.c_int)]
+
+
 class _Matrix(ctypes.Structure):
     _fields_ = [("grad", ctypes.c_void_p), ("update", ctypes.c_void_p), ("ld_grad", ctypes.c_longlong),
                 ("ld_update", ctypes.c_longlong), ("rows", ctypes.c_int), ("cols", ctypes.c_int), ("scale", ctypes.c_float)]
@@ -187,6 +196,14 @@ def load():
     lib.modse_embedding_backward_workspace_bytes.argtypes = [ci, ci, ci]
     lib.modse_embedding_backward.restype = ci
     lib.modse_embedding_backward.argtypes = [ci, ci, ci, ci, vp, ci, vp, cf, ci, ci, vp, vp, sz, vp]
+    lib.modse_cross_entropy_workspace_bytes.restype = sz
+    lib.modse_cross_entropy_workspace_bytes.argtypes = [ci, ci, ci]
+    lib.modse_cross_entropy.restype = ci
+    lib.modse_cross_entropy.argtypes = [ci, ci, ci, ctypes.POINTER(_CrossEntropy), vp, sz, vp]
+    lib.modse_cross_entropy_backward_workspace_bytes.restype = sz
+    lib.modse_cross_entropy_backward_workspace_bytes.argtypes = [ci, ci, ci]
+    lib.modse_cross_entropy_backward.restype = ci
+    lib.modse_cross_entropy_backward.argtypes = [ci, ci, ci, ctypes.POINTER(_CrossEntropyGrads), vp, sz, vp]
     lib.modse_check_workspace_status.restype = ci
     lib.modse_check_workspace_status.argtypes = [vp, vp]
     lib.modse_debug_use_fma_path.restype = None
@@ -484,6 +501,49 @@ def embedding_backward(ids, dy, dtable, workspace, *, scale: float = 1.0, accumu
         _buffer("dtable", dtable, (v, d), dtable.dtype, dev), *_workspace(workspace, dev), stream)
     if st != MODSE_OK:
         raise ModseError(st, "modse_embedding_backward")
+
+
+def cross_entropy_workspace_bytes(n_tokens: int, d_model: int, vocabulary: int) -> int:
+    return int(load().modse_cross_entropy_workspace_bytes(n_tokens, d_model, vocabulary))
+
+
+def cross_entropy(x, w, labels, loss, lse, workspace, *, total=None) -> None:
+    """modse_cross_entropy on the current stream: ``loss`` and ``lse`` [T] fp32 of the softmax over the rows of ``w``
+    [vocabulary, d] for the hidden rows ``x`` [T, d] (bf16) and ``labels`` [T] (int32 or int64, negative: not counted).
+    ``total``: None or two fp32 numbers, the sum of the losses and the number of counted tokens."""
+    T, d = _rows("x", x)
+    v = _rows("w", w)[0]
+    stream, dev = _current_stream("x", x)
+    bf, f32 = torch.bfloat16, torch.float32
+    address, width = _tokens("labels", labels, T, dev)
+    args = _CrossEntropy(_buffer("x", x, (T, d), bf, dev), _buffer("w", w, (v, d), bf, dev), address,
+                         _buffer("loss", loss, (T,), f32, dev), _buffer("lse", lse, (T,), f32, dev),
+                         _buffer("total", total, (2,), f32, dev), width)
+    st = load().modse_cross_entropy(T, d, v, args, *_workspace(workspace, dev), stream)
+    if st != MODSE_OK:
+        raise ModseError(st, "modse_cross_entropy")
+
+
+def cross_entropy_backward_workspace_bytes(n_tokens: int, d_model: int, vocabulary: int) -> int:
+    return int(load().modse_cross_entropy_backward_workspace_bytes(n_tokens, d_model, vocabulary))
+
+
+def cross_entropy_backward(x, w, labels, lse, dx, dw, workspace, *, dloss=None, total=None, scale: float = 1.0) -> None:
+    """modse_cross_entropy_backward: the gradients of :func:`cross_entropy` from the ``lse`` it wrote into ``dx`` [T, d] and
+    ``dw`` [vocabulary, d] (bf16, either may be None), for an objective that weighs a counted token by
+    ``scale * dloss[t] / total[1]`` (``dloss`` None: ones; ``total`` None: no division, otherwise as forward wrote it)."""
+    T, d = _rows("x", x)
+    v = _rows("w", w)[0]
+    stream, dev = _current_stream("x", x)
+    bf, f32 = torch.bfloat16, torch.float32
+    address, width = _tokens("labels", labels, T, dev)
+    args = _CrossEntropyGrads(_buffer("x", x, (T, d), bf, dev), _buffer("w", w, (v, d), bf, dev), address,
+                              _buffer("lse", lse, (T,), f32, dev), _buffer("dloss", dloss, (T,), f32, dev),
+                              _buffer("total", total, (2,), f32, dev), _buffer("dx", dx, (T, d), bf, dev),
+                              _buffer("dw", dw, (v, d), bf, dev), scale, width)
+    st = load().modse_cross_entropy_backward(T, d, v, args, *_workspace(workspace, dev), stream)
+    if st != MODSE_OK:
+        raise ModseError(st, "modse_cross_entropy_backward")
 
 
 def check_workspace_status(workspace) -> int:

@@ -71,6 +71,7 @@ template <int P> struct DenseParams {
     int clear_status;
     int skip_item;       // debugging: the producers that get this item stop without loading it (-1: none)
     DenseColumnSum sum;
+    LossEpilogue loss;
 };
 
 struct DenseTile {
@@ -260,7 +261,8 @@ __device__ __forceinline__ void activate_all(float (&v)[32], int act)
 // accumulator is waited for, the next one's as soon as the registers of the present one are free.  Plain loads all: scales
 // and bias may come from the kernel ahead, which may still be writing them when this one starts.
 template <int MODE, bool F8> struct ChunkInputs {
-    uint4 raw[MODE == DensePlain || MODE == DenseGram ? 1 : 4];      // residual, or the first input
+    // residual, or the first input
+    uint4 raw[MODE == DensePlain || MODE == DenseGram || MODE == DenseLse || MODE == DenseSoftmax ? 1 : MODE == DenseSum ? 8 : 4];
     uint4 bias[MODE == DenseLinear ? 4 : 1];
     float sx;
 };
@@ -286,15 +288,57 @@ __device__ __forceinline__ void chunk_load(ChunkInputs<MODE, F8> &in, const Dens
         const long long at = (long long)r0 * q.ld_in + c0;
         if constexpr ((WHAT & kLoadFirst) != 0)
             rows_load(lane, (const unsigned char *)((const __half *)q.in0 + at), 2 * q.ld_in, rows, pieces, in.raw);
+    } else if constexpr (MODE == DenseSum) {
+        if constexpr ((WHAT & kLoadFirst) != 0)
+            if ((q.flags & kDenseAdd) && pieces > 0) {
+                const uint4 *at = static_cast<const uint4 *>(q.in0) + ((long long)(r0 >> 5) * ((q.N + 31) >> 5) + (c0 >> 5)) * 256 + lane;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) in.raw[j] = __ldcg(at + 32 * j);
+            }
     }
+}
+
+// What a lane keeps of its row from one chunk of a tile to the next.
+template <int MODE> struct RowState {};
+template <> struct RowState<DenseLse> {
+    float top, sum;        // see LossEpilogue::part
+    long long label;       // column of the label, negative: none
+};
+template <> struct RowState<DenseSoftmax> {
+    float lse2, factor;
+    long long label;
+};
+constexpr float kLog2e = 1.4426950408889634f;
+template <int MODE>
+__device__ __forceinline__ void row_begin(RowState<MODE> &rs, const LossEpilogue &loss, const DenseProblem &q, int r0, int lane)
+{
+    if constexpr (MODE == DenseLse || MODE == DenseSoftmax) {
+        const bool in = r0 + lane < q.M;
+        rs.label = in ? loss.labels.at(r0 + lane) : -1;
+        rs.label = rs.label < 0 ? -1 : rs.label - loss.first;
+        if constexpr (MODE == DenseLse) {
+            rs.top = -3.402823466e38f;
+            rs.sum = 0.f;
+        } else {
+            rs.lse2 = in ? __ldcg(loss.lse2 + r0 + lane) : 0.f;
+            rs.factor = in ? __ldcg(loss.factor + r0 + lane) : 0.f;
+        }
+    }
+}
+// ... and what it leaves behind when the run of columns from c0 is done
+template <int MODE>
+__device__ __forceinline__ void row_end(const RowState<MODE> &rs, const LossEpilogue &loss, const DenseProblem &q, int r0, int c0, int lane)
+{
+    if constexpr (MODE == DenseLse)
+        if (r0 + lane < q.M) __stcg(loss.part + (c0 / kDenseLseCols) * loss.rows + r0 + lane, make_float2(rs.top, rs.sum));
 }
 
 // Finishes the chunk and requests the inputs of the one that starts at column `next` (an outside column: of none); v: this
 // lane's row.
 template <int MODE, bool F8>
-__device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const DenseProblem &q, const LinearEpilogue &lin,
-                                             const CUtensorMap *o0, const CUtensorMap *o1, int r0, int c0, int next, int lane,
-                                             Staging &stg, float (&v)[32])
+__device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, RowState<MODE> &rs, const DenseProblem &q,
+                                             const LinearEpilogue &lin, const LossEpilogue &loss, const CUtensorMap *o0,
+                                             const CUtensorMap *o1, int r0, int c0, int next, int lane, Staging &stg, float (&v)[32])
 {
     const int rows = min(32, q.M - r0), cols = min(32, q.N - c0);
     uint4 w[4];
@@ -342,6 +386,77 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, const De
     } else if constexpr (MODE == DensePlain) {
         pack_bf16(v, w);
         tile_out(stg.take(lane), lane, o0, c0, r0, w);
+    } else if constexpr (MODE == DenseLse) {
+        const long long at = rs.label - c0;
+        if (at >= 0 && at < cols) {
+            float z = 0.f;        // (written as an index or a choice, this puts v into local memory)
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                asm("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %2, %3;\n\t@p mov.f32 %0, %1;\n\t}" : "+f"(z) : "f"(v[i]), "r"((int)at), "r"(i));
+            loss.picked[r0 + lane] = z;
+        }
+        if (cols < 32) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = i < cols ? v[i] : -INFINITY;
+        }
+        // 2^(z log2(e) - M): M is rounded, but one and the same for all terms and for the logarithm at the end.  It stays
+        // finite, so that an infinite logit gives an infinite sum, a row of -infinity a sum of zero, and a NaN a NaN.
+        float top[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top[i] = v[i];
+#pragma unroll
+        for (int i = 4; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], v[i]);
+        const float m = fmaxf(rs.top, fminf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * kLog2e, 3.402823466e38f));
+        f32x2 sum = pack2(rs.sum * ex2_approx(rs.top - m), 0.f);
+        rs.top = m;
+        const f32x2 scale = both(kLog2e), shift = both(-m);
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            float a, b;
+            unpack2(fma2(pack2(v[i], v[i + 1]), scale, shift), a, b);
+            sum = add2(sum, pack2(ex2_approx(a), ex2_approx(b)));
+        }
+        float a, b;
+        unpack2(sum, a, b);
+        rs.sum = a + b;
+    } else if constexpr (MODE == DenseSoftmax) {
+        const f32x2 scale = both(kLog2e), shift = both(-rs.lse2);
+        const long long at = rs.label - c0;
+        const bool here = at >= 0 && at < cols;
+#pragma unroll
+        for (int i = 0; i < 32; i += 2) {
+            unpack2(fma2(pack2(v[i], v[i + 1]), scale, shift), v[i], v[i + 1]);
+            v[i] = ex2_approx(v[i]);
+            v[i + 1] = ex2_approx(v[i + 1]);
+        }
+        if (here) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] -= i == (int)at ? 1.f : 0.f;
+        }
+        // a row that does not count has a factor of zero and no gradient, whatever its logits are
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = rs.factor != 0.f ? rs.factor * v[i] : 0.f;
+        pack_bf16(v, w);
+        tile_out(stg.take(lane), lane, o0, c0, r0, w);
+    } else if constexpr (MODE == DenseSum) {
+        if (q.flags & kDenseAdd) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[4 * j] += __uint_as_float(in.raw[j].x);
+                v[4 * j + 1] += __uint_as_float(in.raw[j].y);
+                v[4 * j + 2] += __uint_as_float(in.raw[j].z);
+                v[4 * j + 3] += __uint_as_float(in.raw[j].w);
+            }
+            chunk_load<kLoadFirst>(in, q, lin, r0, next, lane);
+        }
+        if (q.flags & kDenseKeep) {
+            float4 *to = static_cast<float4 *>(q.out1) + ((long long)(r0 >> 5) * ((q.N + 31) >> 5) + (c0 >> 5)) * 256 + lane;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) __stcg(to + 32 * j, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+        } else {
+            pack_bf16(v, w);
+            tile_out(stg.take(lane), lane, o0, c0, r0, w);
+        }
     } else if constexpr (MODE == DenseGram || MODE == DensePoly) {
         unsigned char *buf = stg.take(lane);
         if constexpr (MODE == DensePoly) {
@@ -525,7 +640,9 @@ __device__ __forceinline__ void finish_shared(const DenseParams<P> &prm, unsigne
             }
         }
     }
-    chunk_finish(in, q, prm.lin, &prm.o0[t.p], &prm.o1[t.p], r0, c0 + 32 * own, q.N, lane, stg, v);
+    RowState<MODE> rs;
+    row_begin(rs, prm.loss, q, r0, lane);
+    chunk_finish(in, rs, q, prm.lin, prm.loss, &prm.o0[t.p], &prm.o1[t.p], r0, c0 + 32 * own, q.N, lane, stg, v);
     if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 
@@ -581,6 +698,7 @@ __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
     allow_next_kernel();
     // the first block clears the status word; a wait can expire a millisecond later at the earliest
     if (prm.clear_status && blockIdx.x == 0 && tid == 0) *prm.status = kDevOk;
+    if (MODE == DenseLse && blockIdx.x == 0 && tid == 0) *prm.loss.counter = 0;
     const uint32_t tmem_base = st->tmem_base;
     const WaitCtx wc{&st->abort_flag, prm.status, prm.wait_limit_ns};
 
@@ -764,7 +882,11 @@ __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
                 const int acc = TALL ? h : first, r0 = t.m0 + 256 * h + rank * 128 + quad * 32;
                 const bool any = r0 < q.M && c0 < q.N;
                 ChunkInputs<MODE, kF8> in;
-                if (any && t.tail < 0) chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
+                RowState<MODE> rs;
+                if (any && t.tail < 0) {
+                    chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
+                    row_begin(rs, prm.loss, q, r0, lane);
+                }
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&st->tmem_full[acc]), (acc ? used1 : used0) & 1u, wc))) { ok = false; break; }
                 if (acc) ++used1; else ++used0;
                 tc_fence_after();
@@ -786,13 +908,14 @@ __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(w[i]);
                         if (t.tail < 0) {
-                            chunk_finish(in, q, prm.lin, o0, o1, r0, c0 + 32 * c, c + 1 < kChunks ? c0 + 32 * c + 32 : q.N, lane, stg, v);
+                            chunk_finish(in, rs, q, prm.lin, prm.loss, o0, o1, r0, c0 + 32 * c, c + 1 < kChunks ? c0 + 32 * c + 32 : q.N, lane, stg, v);
                         } else {
                             float4 *dst = strip + (size_t)t.split * kPiece + (size_t)c * 256;
 #pragma unroll
                             for (int j = 0; j < 8; ++j) __stcg(dst + 32 * j, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
                         }
                     }
+                    if (t.tail < 0) row_end(rs, prm.loss, q, r0, c0, lane);
                 }
                 tc_fence_before();
                 __syncwarp();
@@ -808,6 +931,7 @@ __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
                         __threadfence();
                         if (lane == 0) *counter = 0;               // for the next launch
                         chunk_load<kLoadAll>(in, q, prm.lin, r0, c0, lane);
+                        row_begin(rs, prm.loss, q, r0, lane);
 #pragma unroll 1
                         for (int c = 0; c < kChunks; ++c) {
                             if (c0 + 32 * c >= q.N) break;
@@ -823,8 +947,9 @@ __device__ __forceinline__ void dense_gemm_body(const DenseParams<P> &prm)
                                     v[4 * j] += f.x; v[4 * j + 1] += f.y; v[4 * j + 2] += f.z; v[4 * j + 3] += f.w;
                                 }
                             }
-                            chunk_finish(in, q, prm.lin, o0, o1, r0, c0 + 32 * c, c + 1 < kChunks ? c0 + 32 * c + 32 : q.N, lane, stg, v);
+                            chunk_finish(in, rs, q, prm.lin, prm.loss, o0, o1, r0, c0 + 32 * c, c + 1 < kChunks ? c0 + 32 * c + 32 : q.N, lane, stg, v);
                         }
+                        row_end(rs, prm.loss, q, r0, c0, lane);
                     }
                 }
             }
@@ -913,7 +1038,8 @@ long long dense_tiles(const DenseProblem &p, bool tall, int tn)
     return c;
 }
 
-DensePlan dense_plan(DenseType type, const DenseItem *items, int n, bool light, int sms, size_t partial_capacity)
+// `wide`: tiles of 256 columns and none shared, so that a warp sees a run of 128 columns of its rows.
+DensePlan dense_plan(DenseType type, const DenseItem *items, int n, bool light, int sms, size_t partial_capacity, bool wide = false)
 {
     const int pairs = std::max(1, sms / 2);
     auto count = [&](bool tall, int tn) {
@@ -945,7 +1071,7 @@ DensePlan dense_plan(DenseType type, const DenseItem *items, int n, bool light, 
     }
     // 256-column tiles unless the whole output has less than half a tile for each CTA pair: then 128-column tiles, whose
     // epilogue, which shows in a launch of one round, is half as long
-    pl.tn = squares * 2 <= pairs ? 128 : 256;
+    pl.tn = squares * 2 <= pairs && !wide ? 128 : 256;
     pl.tiles = (int)count(false, pl.tn);
     pl.full = pl.tiles / pairs * pairs;
     const int left = pl.tiles - pl.full;
@@ -977,9 +1103,10 @@ DensePlan dense_plan(DenseType type, const DenseItem *items, int n, bool light, 
 }
 
 template <int MODE, int TYPE, int TN, bool TALL, bool SHARED, int P>
-cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const LinearEpilogue *lin, const DenseColumnSum *sum, void *ws, int head, cudaStream_t s)
+cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const LinearEpilogue *lin, const DenseColumnSum *sum,
+                      const LossEpilogue *loss, void *ws, int head, cudaStream_t s)
 {
-    static_assert(!TALL || MODE == DensePlain || MODE == DenseLinear, "dense_decode has no tall form of symmetric outputs");
+    static_assert(!TALL || MODE == DensePlain || MODE == DenseLinear || MODE == DenseSum, "dense_decode has no tall form of symmetric outputs");
     DenseParams<P> prm;
     int tiles = 0;
     for (int i = 0; i < n; ++i) {
@@ -1009,7 +1136,7 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
             } else {
                 ok = encode_output(&prm.o0[i], q.out0, q.M, q.N, q.ld_in) && encode_output(&prm.o1[i], q.out1, q.M, q.N, q.ld_in);
             }
-        } else {
+        } else if (MODE != DenseLse && !(MODE == DenseSum && (q.flags & kDenseKeep))) {
             ok = encode_output(&prm.o0[i], q.out0, q.M, q.N, q.ld_out);
         }
         if (!ok) return cudaErrorInvalidValue;
@@ -1027,6 +1154,7 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
     prm.wait_limit_ns = tc_wait_limit_ns();
     prm.clear_status = head == kDenseHeadRaw;
     prm.sum = sum ? *sum : DenseColumnSum{};
+    prm.loss = loss ? *loss : LossEpilogue{};
     prm.skip_item = tc_skip_tile(kTcDenseProducts);
 
     void (*kern)(DenseParams<P>);
@@ -1050,17 +1178,21 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
 }
 
 template <int MODE, int TYPE, int P>
-cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin, const DenseColumnSum *sum, void *ws, size_t cap, int head, cudaStream_t s)
+cudaError_t launch_mode(const DenseItem *items, int n, const LinearEpilogue *lin, const DenseColumnSum *sum, const LossEpilogue *loss,
+                        void *ws, size_t cap, int head, cudaStream_t s)
 {
     if (n > P) return cudaErrorInvalidValue;
-    const bool light = MODE == DensePlain || (MODE == DenseLinear && TYPE == DenseBf16 && !lin->residual && !lin->z && lin->act <= MODSE_ACT_RELU);
-    const DensePlan pl = dense_plan((DenseType)TYPE, items, n, light, device_sms(), cap);
-    if constexpr (MODE == DensePlain || (MODE == DenseLinear && TYPE == DenseBf16))
-        if (pl.tall) return launch_tn<MODE, TYPE, 256, true, false, P>(pl, items, n, lin, sum, ws, head, s);
-    if (pl.share > 1)       // so few tiles are 128 columns wide
-        return launch_tn<MODE, TYPE, 128, false, true, P>(pl, items, n, lin, sum, ws, head, s);
-    if (pl.tn == 128) return launch_tn<MODE, TYPE, 128, false, false, P>(pl, items, n, lin, sum, ws, head, s);
-    return launch_tn<MODE, TYPE, 256, false, false, P>(pl, items, n, lin, sum, ws, head, s);
+    const bool light = MODE == DensePlain || MODE == DenseSum ||
+                       (MODE == DenseLinear && TYPE == DenseBf16 && !lin->residual && !lin->z && lin->act <= MODSE_ACT_RELU);
+    const DensePlan pl = dense_plan((DenseType)TYPE, items, n, light, device_sms(), cap, MODE == DenseLse);
+    if constexpr (MODE == DensePlain || MODE == DenseSum || (MODE == DenseLinear && TYPE == DenseBf16))
+        if (pl.tall) return launch_tn<MODE, TYPE, 256, true, false, P>(pl, items, n, lin, sum, loss, ws, head, s);
+    if constexpr (MODE != DenseLse) {
+        if (pl.share > 1)       // so few tiles are 128 columns wide
+            return launch_tn<MODE, TYPE, 128, false, true, P>(pl, items, n, lin, sum, loss, ws, head, s);
+        if (pl.tn == 128) return launch_tn<MODE, TYPE, 128, false, false, P>(pl, items, n, lin, sum, loss, ws, head, s);
+    }
+    return launch_tn<MODE, TYPE, 256, false, false, P>(pl, items, n, lin, sum, loss, ws, head, s);
 }
 
 }  // namespace
@@ -1095,16 +1227,23 @@ cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *list, 
     DenseItem items[kDenseMaxProblems];
     std::copy(list, list + n, items);
     std::stable_sort(items, items + n, [](const DenseItem &a, const DenseItem &b) { return a.k > b.k; });
+    const auto run = [&](auto launch) { return launch(items, n, lin, sum, nullptr, ws, partial_capacity, head, s); };
     switch (mode) {
-    case DenseLinear:
-        return type == DenseE4m3 ? launch_mode<DenseLinear, DenseE4m3, 1>(items, n, lin, sum, ws, partial_capacity, head, s)
-                                 : launch_mode<DenseLinear, DenseBf16, 1>(items, n, lin, sum, ws, partial_capacity, head, s);
-    case DensePlain: return launch_mode<DensePlain, DenseBf16, 2>(items, n, lin, sum, ws, partial_capacity, head, s);
-    case DenseGram: return launch_mode<DenseGram, DenseF16, kDenseMaxProblems>(items, n, lin, sum, ws, partial_capacity, head, s);
-    case DensePoly: return launch_mode<DensePoly, DenseF16, kDenseMaxProblems>(items, n, lin, sum, ws, partial_capacity, head, s);
-    case DenseStep: return launch_mode<DenseStep, DenseF16, kDenseMaxProblems>(items, n, lin, sum, ws, partial_capacity, head, s);
+    case DenseLinear: return type == DenseE4m3 ? run(launch_mode<DenseLinear, DenseE4m3, 1>) : run(launch_mode<DenseLinear, DenseBf16, 1>);
+    case DensePlain: return run(launch_mode<DensePlain, DenseBf16, 2>);
+    case DenseGram: return run(launch_mode<DenseGram, DenseF16, kDenseMaxProblems>);
+    case DensePoly: return run(launch_mode<DensePoly, DenseF16, kDenseMaxProblems>);
+    case DenseStep: return run(launch_mode<DenseStep, DenseF16, kDenseMaxProblems>);
+    case DenseSum: return run(launch_mode<DenseSum, DenseBf16, 2>);
+    default: return cudaErrorInvalidValue;
     }
-    return cudaErrorInvalidValue;
+}
+
+cudaError_t dense_launch_loss(DenseMode mode, const DenseItem &item, const LossEpilogue &loss, void *ws, size_t partial_capacity,
+                              int head, cudaStream_t s)
+{
+    return mode == DenseLse ? launch_mode<DenseLse, DenseBf16, 1>(&item, 1, nullptr, nullptr, &loss, ws, partial_capacity, head, s)
+                            : launch_mode<DenseSoftmax, DenseBf16, 1>(&item, 1, nullptr, nullptr, &loss, ws, partial_capacity, head, s);
 }
 
 }  // namespace modse

@@ -1,5 +1,5 @@
 // Dense matrix products on CTA pairs (tcgen05, cta_group::2) with fused epilogues: the products of modse_linear, its
-// gradients and modse_orthogonalize.
+// gradients, modse_orthogonalize and modse_cross_entropy.
 #pragma once
 
 #include <cuda.h>
@@ -14,7 +14,10 @@ enum DenseMode : int {
     DensePlain = 1,    // out = acc (bf16)
     DenseGram = 2,     // out = alpha acc (fp16), symmetric
     DensePoly = 3,     // out = alpha acc + beta in0 + scale I (fp16), symmetric
-    DenseStep = 4      // x = alpha acc + beta in0: its two fp16 halves, or the final bf16 result times scale
+    DenseStep = 4,     // x = alpha acc + beta in0: its two fp16 halves, or the final bf16 result times scale
+    DenseLse = 5,      // rows of logits: largest and sum of exponentials of each run of 128 columns, the label's logit
+    DenseSoftmax = 6,  // logits to their gradient: factor (exp(acc - lse) - [column is the label]) (bf16)
+    DenseSum = 7       // out = acc + in0: a running fp32 sum (kDenseAdd, kDenseKeep) whose last part leaves as bf16
 };
 enum DenseType : int { DenseBf16 = 0, DenseF16 = 1, DenseE4m3 = 2 };
 enum : int {
@@ -22,6 +25,8 @@ enum : int {
     kDenseBMn = 2,     // same for the column operand ([K, N], not [N, K])
     kDenseSym = 4,     // out is symmetric: tiles below the diagonal are not computed but mirrored
     kDenseLast = 8,    // DenseStep: write the final result
+    kDenseAdd = 32,    // DenseSum: in0 is added
+    kDenseKeep = 64,   // DenseSum: the sum goes to out1 in fp32, not to out0
     kDenseTmaOut = 16  // set by the launch: the final result's rows are aligned for TMA and whole 16-byte pieces long
 };
 
@@ -43,6 +48,34 @@ struct LinearEpilogue {
     __nv_bfloat16 *z, *y;
     int act;
 };
+
+// Token ids as the caller holds them; read from L2, where everything the stream held before the call has arrived.
+struct TokenIds {
+    const void *p;
+    int wide;          // 64-bit
+#ifdef __CUDACC__
+    __device__ __forceinline__ long long at(long long i) const
+    {
+        return wide ? __ldcg(static_cast<const long long *>(p) + i) : (long long)__ldcg(static_cast<const int *>(p) + i);
+    }
+#endif
+};
+
+// The rows of DenseLse and DenseSoftmax.  DenseLse writes, for run c of 128 columns and row t, part[c * rows + t] =
+// (M, sum over the run of 2^(z log2(e) - M)), M the run's largest z log2(e) (rounded) held to finite numbers.
+struct LossEpilogue {
+    TokenIds labels;
+    long long first;       // vocabulary index of column 0
+    long long rows;
+    float2 *part;
+    float *picked;         // [rows] the label's logit
+    int *counter;          // cleared by DenseLse for the kernel behind it
+    const float *lse2, *factor;     // [rows] lse log2(e), factor
+};
+constexpr int kDenseLseCols = 128;
+// A running sum of DenseSum: blocks of 32 rows x 32 columns, row by row of blocks, block element (r, c) at
+// (c / 4) * 128 + r * 4 + c % 4, so that a warp that holds a row a lane moves 512 contiguous bytes at a time.
+inline size_t dense_sum_bytes(long long rows, long long cols) { return (size_t)((rows + 31) / 32) * (size_t)((cols + 31) / 32) * 4096; }
 
 // out[c] = sum over r of part[r][c], in order, done beside the products of a DensePlain launch (cols 0: none).
 struct DenseColumnSum {
@@ -83,5 +116,8 @@ size_t dense_partial_bound(DenseType type, const DenseItem *items, int n);
 // Launches n products of one mode and type as one kernel on a workspace whose head is `ws`.
 cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *list, int n, const LinearEpilogue *lin,
                          const DenseColumnSum *sum, void *ws, size_t partial_capacity, int head, cudaStream_t s);
+// ... of DenseLse and DenseSoftmax: one product
+cudaError_t dense_launch_loss(DenseMode mode, const DenseItem &item, const LossEpilogue &loss, void *ws, size_t partial_capacity,
+                              int head, cudaStream_t s);
 
 }  // namespace modse

@@ -14,6 +14,7 @@
 // chunks' order.
 #include <algorithm>
 
+#include "dense_gemm.h"
 #include "launch.h"
 #include "modse_internal.h"
 #include "tc_device.h"
@@ -64,23 +65,13 @@ __device__ __forceinline__ void store_piece(float *p, const float (&f)[8])
     *reinterpret_cast<float4 *>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
 }
 
-struct Ids {
-    const void *p;
-    int wide;          // 64-bit
-    // from L2, where everything the stream held before the call has arrived
-    __device__ __forceinline__ long long at(long long i) const
-    {
-        return wide ? __ldcg(static_cast<const long long *>(p) + i) : (long long)__ldcg(static_cast<const int *>(p) + i);
-    }
-};
-
 // ---- lookup ----
 constexpr int kLookupThreads = 256, kLookupFlight = 4;
 
 // A row belongs to `tpr` threads (a power of two); each has kLookupFlight pieces of 8 elements of it in flight.
 template <typename T>
 __global__ void __launch_bounds__(kLookupThreads)
-embedding_kernel(const Ids ids, const T *table, float scale, T *y, int *status, int n, int d, int vocabulary, int tpr)
+embedding_kernel(const TokenIds ids, const T *table, float scale, T *y, int *status, int n, int d, int vocabulary, int tpr)
 {
     wait_for_earlier_kernels();
     allow_next_kernel();
@@ -114,7 +105,7 @@ embedding_kernel(const Ids ids, const T *table, float scale, T *y, int *status, 
 }
 
 template <typename T>
-cudaError_t launch_lookup(const Ids &ids, const void *table, float scale, void *y, int *status, int n, int d, int vocabulary,
+cudaError_t launch_lookup(const TokenIds &ids, const void *table, float scale, void *y, int *status, int n, int d, int vocabulary,
                           cudaStream_t s)
 {
     int tpr = 8;       // threads of a row: as few as leave each of them at most kLookupFlight pieces
@@ -129,7 +120,7 @@ cudaError_t launch_lookup(const Ids &ids, const void *table, float scale, void *
 constexpr int kSortBlocks = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortMaxBits = 10;
 
 struct SortArgs {
-    Ids ids;
+    TokenIds ids;
     uint2 *a, *b;          // (token, position) pairs; pass p writes a where p is even, b where it is odd
     int *status, *counters;
     int n, vocabulary, bits, passes, n_counters;
@@ -232,7 +223,7 @@ constexpr int kSumThreads = 64, kSumCols = 8 * kSumThreads, kSumFlight = 8, kMax
 constexpr int kFillBits = 65536;
 
 struct GradArgs {
-    Ids ids;
+    TokenIds ids;
     const uint2 *sorted;
     const void *dy;
     void *out;
@@ -515,7 +506,7 @@ modse_status_t modse_embedding(modse_dtype_t dtype, int n_tokens, int d_model, i
     if (ids == nullptr || table == nullptr || y == nullptr || !aligned(ids, id_bytes) || !aligned(table, 16) ||
         !aligned(y, 16) || !aligned(status, 4))
         return MODSE_ERR_INVALID_ARG;
-    const Ids in{ids, id_bytes == 8};
+    const TokenIds in{ids, id_bytes == 8};
     const cudaStream_t s = (cudaStream_t)cuda_stream;
     if (dtype == MODSE_F32) MODSE_CUDA(launch_lookup<float>(in, table, scale, y, status, n_tokens, d_model, vocabulary, s));
     else MODSE_CUDA(launch_lookup<__nv_bfloat16>(in, table, scale, y, status, n_tokens, d_model, vocabulary, s));
@@ -550,7 +541,7 @@ modse_status_t modse_embedding_backward(modse_dtype_t dtype, int n_tokens, int d
     const GradLayout L = grad_layout(n_tokens, d_model);
     if (workspace_bytes < L.total) return MODSE_ERR_WORKSPACE_TOO_SMALL;
     unsigned char *ws = (unsigned char *)workspace;
-    const Ids in{ids, id_bytes == 8};
+    const TokenIds in{ids, id_bytes == 8};
     const int chunk = chunk_of(n_tokens), chunks = (n_tokens + chunk - 1) / chunk, slabs = slabs_of(d_model);
     int bits = 1;
     while (vocabulary >> bits) ++bits;
