@@ -114,6 +114,24 @@ modse_status_t modse_forward(modse_layer_t *layer, modse_dtype_t dtype, const mo
                              const void *x, int n_tokens, void *y, void *workspace,
                              size_t workspace_bytes, int save_for_backward, void *cuda_stream);
 
+/* The same function for the few tokens of a generation step, at most
+ * MODSE_DECODE_MAX_TOKENS (more: MODSE_ERR_UNSUPPORTED; modse_forward takes any number):
+ * two kernels that stream the weights of the experts met once, where modse_forward lays
+ * tokens out in groups of 128 rows.  Any layer that modse_create accepts (d and widths to 2^26), in either dtype;
+ * the second router term (modse_set_noise_gate) and fp32 outputs (modse_set_output_f32) as
+ * in modse_forward.  topk_idx and topk_gate [T, k] (each may be NULL) receive the routing.
+ * Sums are fp32, in an order that does not depend on the run but is not modse_forward's: values agree to
+ * rounding, and so do the logits, so that a token whose k-th and k+1-st logits are equal to their last
+ * bits may be routed differently (equal logits: the lower index in both).
+ * The layer object is only read: calls on several streams may share it, with a workspace
+ * each (256-byte aligned; its size never falls with n_tokens).  It takes no part in
+ * modse_backward, modse_get_routing, stage timing and launch counts.  y overlaps no input. */
+#define MODSE_DECODE_MAX_TOKENS 32
+size_t modse_decode_workspace_bytes(const modse_layer_t *layer, modse_dtype_t dtype, int n_tokens);
+modse_status_t modse_decode(const modse_layer_t *layer, modse_dtype_t dtype, const modse_weights_t *weights, const void *x,
+                            int n_tokens, void *y, int *topk_idx, float *topk_gate, void *workspace, size_t workspace_bytes,
+                            void *cuda_stream);
+
 /* Exact gradient of modse_forward with the top-k selection held fixed (the
  * selection is piecewise constant in x).  Needs the workspace of a preceding
  * modse_forward(..., save_for_backward=1) on the same layer object, dtype and

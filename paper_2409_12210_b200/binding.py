@@ -26,6 +26,7 @@ MODSE_BF16 = 1
 MODSE_E4M3 = 2
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 N_STAGES = 12
+DECODE_MAX_TOKENS = 32
 MODSE_FUSE_GATHER = 1
 MODSE_FUSE_DG_ROWDOT = 2
 MODSE_FUSE_SCATTER = 4
@@ -111,6 +112,10 @@ def load():
     lib.modse_backward.restype = ci
     lib.modse_backward.argtypes = [vp, ci, ctypes.POINTER(_Weights), vp, vp, ci, vp, ctypes.POINTER(_WGrads), vp, sz,
                                    vp]
+    lib.modse_decode_workspace_bytes.restype = sz
+    lib.modse_decode_workspace_bytes.argtypes = [vp, ci, ci]
+    lib.modse_decode.restype = ci
+    lib.modse_decode.argtypes = [vp, ci, ctypes.POINTER(_Weights), vp, ci, vp, vp, vp, vp, sz, vp]
     pp = ctypes.POINTER(ctypes.c_void_p)
     lib.modse_get_routing.restype = ci
     lib.modse_get_routing.argtypes = [vp, vp, ci, pp, pp, pp, pp, pp, pp, pp]
@@ -568,7 +573,7 @@ class ModseLayer:
     def __init__(self, d_model: int, ffn_sizes, top_k: int):
         lib = load()
         self.d_model, self.ffn_sizes, self.top_k = int(d_model), [int(h) for h in ffn_sizes], int(top_k)
-        self.n_experts = len(self.ffn_sizes)
+        self.n_experts, self.total_width, self.output_f32 = len(self.ffn_sizes), sum(self.ffn_sizes), False
         arr = (ctypes.c_int * self.n_experts)(*self.ffn_sizes)
         self._h = lib.modse_create(self.d_model, self.n_experts, arr, self.top_k)
         if not self._h:
@@ -607,6 +612,34 @@ class ModseLayer:
                                   workspace.data_ptr(), workspace.numel(), int(save_for_backward), self._stream())
         if st != MODSE_OK:
             raise ModseError(st, "modse_forward")
+
+    def decode_workspace_bytes(self, dtype_code: int, n_tokens: int) -> int:
+        return int(load().modse_decode_workspace_bytes(self._h, dtype_code, n_tokens))
+
+    def alloc_decode_workspace(self, dtype, n_tokens: int = DECODE_MAX_TOKENS, device="cuda"):
+        """A workspace for :meth:`decode` with up to this many tokens."""
+        import torch
+        code = MODSE_F32 if dtype == torch.float32 else MODSE_BF16
+        return torch.empty(max(self.decode_workspace_bytes(code, n_tokens), 256), dtype=torch.uint8, device=device)
+
+    def decode(self, w_router, w_gate, w_up, w_down, x, y, workspace, *, topk_idx=None, topk_gate=None) -> None:
+        """modse_decode on the current stream: the layer on the few rows of ``x`` [T, d], T at most DECODE_MAX_TOKENS, into
+        ``y`` [T, d] (fp32 with :meth:`set_output_f32`); ``topk_idx`` int32 and ``topk_gate`` fp32 [T, k] receive the
+        routing if given."""
+        T, d = _rows("x", x)
+        if d != self.d_model:
+            raise ValueError(f"x: expected rows of {self.d_model} elements, got {d}")
+        dt, code = x.dtype, _dtype_code(x)
+        stream, dev = _current_stream("x", x)
+        N, S, k = self.n_experts, self.total_width, self.top_k
+        w = _Weights(_buffer("w_router", w_router, (N, d), dt, dev), _buffer("w_gate", w_gate, (S, d), dt, dev),
+                     _buffer("w_up", w_up, (S, d), dt, dev), _buffer("w_down", w_down, (d, S), dt, dev))
+        st = load().modse_decode(self._h, code, w, _buffer("x", x, (T, d), dt, dev), T,
+                                 _buffer("y", y, (T, d), torch.float32 if self.output_f32 else dt, dev),
+                                 _buffer("topk_idx", topk_idx, (T, k), torch.int32, dev),
+                                 _buffer("topk_gate", topk_gate, (T, k), torch.float32, dev), *_workspace(workspace, dev), stream)
+        if st != MODSE_OK:
+            raise ModseError(st, "modse_decode")
 
     def tune_forward(self, w_router, w_gate, w_up, w_down, x, y, workspace, save_for_backward: bool) -> int:
         """Time the kernel shapes of the forward products on this device (synchronises) and keep the fastest;
@@ -763,6 +796,7 @@ class ModseLayer:
         st = load().modse_set_output_f32(self._h, int(bool(on)))
         if st != MODSE_OK:
             raise ModseError(st, "modse_set_output_f32")
+        self.output_f32 = bool(on)
 
     def stage_timing_begin(self, max_calls: int) -> None:
         st = load().modse_stage_timing_begin(self._h, int(max_calls))

@@ -8,11 +8,6 @@
 // that they come from HBM (in brackets the weights' time at the measured copy rate): one token on 2048 x 5632 bf16 7.1 us
 // (3.5), on 8448 x 8448 26.7 (21.8); 24 tokens on 2048 x 5632 e4m3 6.1 (1.8), 4.9 where the calls share weights that stay
 // in L2.  A call by itself, cold and with all of its launch, takes 3 to 5 us more.  The tcgen05 form takes 12 to 46 us on these.
-//
-// Fragments without shared memory: a sum over k may be taken in any order as long as both operands agree on it.  Thread
-// t of a group of four loads 16 contiguous bytes of its row of w and the same 16 bytes of its row of x; the k-th pair of
-// 16-bit numbers in them plays the part of the fragment's columns 2t, 2t+1 (+8).  Four such loads of neighbouring threads
-// cover 64 contiguous bytes of a row.  8-bit operands are widened to fp16 on the way (exact) and use the fp16 form.
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
@@ -20,23 +15,12 @@
 #include "dense_gemm.h"
 #include "launch.h"
 #include "linear_rows.h"
+#include "rows_mma.h"
 
 namespace modse {
 namespace {
 
 constexpr int kWarps = 8;
-
-__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool f16)
-{
-    if (f16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 
 // four e4m3 bytes as two pairs of fp16
 __device__ __forceinline__ void widen(uint32_t v, uint32_t &lo, uint32_t &hi)
@@ -44,28 +28,6 @@ __device__ __forceinline__ void widen(uint32_t v, uint32_t &lo, uint32_t &hi)
     asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
         : "=r"(lo), "=r"(hi) : "r"(v));
 }
-
-// 16 bytes, or zeros where there are none.  volatile: the loads of a step stay ahead of its products.  Not the read-only
-// path: the kernel ahead may still be writing x when this one starts, and that path promises nothing for such data, even
-// where it is read after wait_for_earlier_kernels.
-__device__ __forceinline__ uint4 load_stream(const unsigned char *p, bool in)
-{
-    uint4 v;
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\t"
-                 "mov.b32 %3, 0;\n\t@q ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
-                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((int)in));
-    return v;
-}
-__device__ __forceinline__ uint4 load_shared_rows(const unsigned char *p, bool in)      // x: every block reads it, L1 may keep it
-{
-    uint4 v;
-    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\t"
-                 "mov.b32 %3, 0;\n\t@q ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
-                 : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(p), "r"((int)in));
-    return v;
-}
-
-__device__ __forceinline__ uint32_t word_at(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // products of 16 bytes of two rows of w (rows g and g + 8) with 16 bytes of NT rows of x
 template <bool F8, int NT>

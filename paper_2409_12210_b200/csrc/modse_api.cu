@@ -167,6 +167,9 @@ void layer_expert(const modse_layer_t *layer, int e, int *d, int *S, int *offset
     *offset = layer->meta.hoff[e];
     *width = layer->h[e];
 }
+const LayerMeta *layer_meta(const modse_layer_t *layer) { return &layer->meta; }
+const NoiseGate *layer_noise(const modse_layer_t *layer) { return &layer->noise; }
+int layer_out_f32(const modse_layer_t *layer) { return layer->out_f32; }
 
 }  // namespace modse
 

@@ -111,6 +111,9 @@ cudaError_t launch_aux_loss(const LayerMeta &m, int T, int nblk_bwd, const WsPtr
 // Experts of a layer object, and where expert e lies: d_model, total width, width offset, width (modse_api.cu).
 int layer_experts(const modse_layer_t *layer);
 void layer_expert(const modse_layer_t *layer, int e, int *d, int *S, int *offset, int *width);
+const LayerMeta *layer_meta(const modse_layer_t *layer);
+const NoiseGate *layer_noise(const modse_layer_t *layer);
+int layer_out_f32(const modse_layer_t *layer);
 
 // ---- shared by the operators around the layer (norm_kernels.cu) ----
 int device_sms();      // SMs of the current device (148 where the question fails)
