@@ -125,7 +125,8 @@ modse_status_t modse_forward(modse_layer_t *layer, modse_dtype_t dtype, const mo
  * bits may be routed differently (equal logits: the lower index in both).
  * The layer object is only read: calls on several streams may share it, with a workspace
  * each (256-byte aligned; its size never falls with n_tokens).  It takes no part in
- * modse_backward, modse_get_routing, stage timing and launch counts.  y overlaps no input. */
+ * modse_backward, modse_get_routing, stage timing and launch counts.  y overlaps no input.
+ * The workspace's first bytes hold a status word that modse_check_workspace_status reads. */
 #define MODSE_DECODE_MAX_TOKENS 32
 size_t modse_decode_workspace_bytes(const modse_layer_t *layer, modse_dtype_t dtype, int n_tokens);
 modse_status_t modse_decode(const modse_layer_t *layer, modse_dtype_t dtype, const modse_weights_t *weights, const void *x,
@@ -527,7 +528,7 @@ modse_status_t modse_cross_entropy_backward(int n_tokens, int d_model, int vocab
 
 /* Synchronises the stream and reads the status word of the last call that used this
  * workspace (modse_linear, modse_linear_backward, modse_orthogonalize,
- * modse_embedding_backward, modse_cross_entropy and its gradient): MODSE_OK,
+ * modse_embedding_backward, modse_cross_entropy and its gradient, modse_decode): MODSE_OK,
  * MODSE_ERR_DEVICE_TIMEOUT or MODSE_ERR_DEVICE_BOUNDS.  A call without tokens or matrices leaves MODSE_OK there. */
 modse_status_t modse_check_workspace_status(const void *workspace, void *cuda_stream);
 
@@ -558,8 +559,9 @@ void modse_debug_set_epilogue_warps(int mask_128, int mask_256, int mask_pair);
  * records MODSE_ERR_DEVICE_TIMEOUT in the status word, lets its copies in flight land, frees its tensor
  * memory and returns; modse_debug_set_wait_limit_ms changes the limit (1..60000).
  * modse_debug_skip_tile_loads(product, tile) makes the CTA that is handed tile `tile` of grouped product
- * `product` (0..5; 6: the products of modse_linear, its gradient and modse_orthogonalize, whose `tile` counts
- * a launch's work items) issue no loads for it and stop producing, so that its consumers run into that limit
+ * `product` (0..5; 6: the products of modse_linear, its gradient, modse_orthogonalize and modse_cross_entropy, whose
+ * `tile` counts a launch's work items; 7: modse_decode on bf16 layers whose extents are multiples of 64, whose
+ * `tile` is a block of its first kernel) issue no loads for it and stop producing, so that its consumers run into that limit
  * with nothing in flight; (-1, -1) switches it off.  For tests of the time-out path on tiny inputs.          */
 void modse_debug_set_wait_limit_ms(int ms);
 void modse_debug_skip_tile_loads(int product, int tile);

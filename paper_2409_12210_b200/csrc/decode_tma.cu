@@ -1,0 +1,699 @@
+// modse_decode for bf16 layers whose extents are multiples of 64: weights come by TMA, column blocks of 64 elements (128
+// bytes) of several rows at a time, and nothing that the inner loops read comes from global memory.
+//
+// The last point is what counts.  With 130 to 190 KB of weights in flight to an SM a row of x asked for beside them arrives
+// only behind them, and the warps wait for it longer than for anything else.  So the rows of x of an expert lie in shared
+// memory while a block works on it (a block's units are neighbours, so that is one expert or two), and the gated hidden
+// rows, which are used once by each group of 128 rows of W_down, come by TMA in the same stage as the weights.
+//
+// First kernel: units of eight hidden columns, whose rows of W_gate and W_up are one mma.sync fragment; the eight warps split the
+// contraction, each with a ring that it fills for itself, and sums meet once a unit.  So there are enough units to go round
+// 148 SMs evenly, and a block reads whole rows, 64 KB side by side, at a time.
+// Second kernel: 128 rows of W_down and 16 or 32 hidden rows are the operands of tcgen05 instructions as TMA leaves them, so no
+// warp touches them.  What a block asks for is 128 bytes of each of 128 rows that lie far apart, so the blocks of a group of
+// rows take its column blocks in turn: together they read a few KB of each row at a time.
+// MEASURED
+//
+// A fragment's rows lie 128 bytes apart in a stage, swizzled by TMA in 16-byte pieces.  Row i of a fragment's half plays row
+// row_of(i) of the stage, so that the two rows that eight neighbouring lanes read lie in opposite halves of the banks.
+#include <algorithm>
+
+#include "decode.h"
+#include "tc_device.h"
+
+namespace modse {
+namespace decode {
+namespace {
+
+constexpr int kGroupRows = 128;                  // of W_down, and the rows of W_gate and W_up of a unit together
+constexpr int kBlockBytes = kGroupRows * 128;    // a column block of them
+constexpr int kSmemMost = 232448 - 6 * 1024;     // dynamic shared memory, beside what the kernels declare
+
+struct Maps {
+    CUtensorMap gate, up;        // [column block][row][64 elements], boxes of 8 rows and up_blocks blocks
+    CUtensorMap gate64, up64;    // boxes of 64 rows x 64 elements
+    CUtensorMap down;            // boxes of 128 rows x 64 elements
+    CUtensorMap hidden;          // boxes of 16 rows x 64 elements
+};
+
+__device__ __forceinline__ int row_of(int g) { return (g >> 1) | ((g & 1) << 2); }
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ uint4 lds(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+// A warp's sums of one fragment of rows with NTM groups of eight columns (tokens).
+template <int NTM> struct Sums {
+    float acc[NTM][4];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int n = 0; n < NTM; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
+    }
+    // A column block.  rows: of the fragment's rows 0 .. 7 (unswizzled row 0), `second` bytes ahead of rows 8 .. 15;
+    // column(n, h): the lane's 16 bytes of unit h of its column in group n; `some` groups of columns.
+    template <typename Column>
+    __device__ __forceinline__ void add(uint32_t rows, uint32_t second, int some, const Column &column)
+    {
+        const int lane = threadIdx.x & 31, t = lane & 3, row = row_of(lane >> 2);
+        uint4 a[2], b[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t at = rows + row * 128 + (((4 * h + t) ^ row) << 4);
+            a[h] = lds(at);
+            b[h] = lds(at + second);
+        }
+#pragma unroll
+        for (int n = 0; n < NTM; ++n)
+            if (n < some)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint4 x = column(n, h);
+                    const uint32_t lo[4] = {a[h].x, b[h].x, a[h].y, b[h].y}, hi[4] = {a[h].z, b[h].z, a[h].w, b[h].w};
+                    mma_16816(acc[n], lo, x.x, x.y, false);
+                    mma_16816(acc[n], hi, x.z, x.w, false);
+                }
+    }
+};
+
+// The rows of x of an expert, in shared memory where they fit: rows 64 bytes more than a multiple of 128 apart, so that the two
+// rows that eight neighbouring lanes read lie in opposite halves of the banks.
+struct Tokens {
+    uint32_t at;
+    int pitch, room;                     // bytes a row, rows
+    bool held;
+    // Every thread of the team calls it; what was held before is no longer needed.
+    __device__ __forceinline__ void hold(const DecodeArgs &p, const Routing &r, int s)
+    {
+        const int count = r.first[s + 1] - r.first[s], row = 2 * p.m.d, pieces = row / 16;
+        held = count <= room;
+        team_sync();
+        if (held)
+            for (int i = threadIdx.x; i < count * pieces; i += kThreads) {
+                const int c = i / pieces, at16 = (i - c * pieces) * 16;
+                const uint4 v = *reinterpret_cast<const uint4 *>(p.x + (size_t)(r.pick[r.first[s] + c] / p.m.k) * row + at16);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + c * pitch + at16), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+            }
+        team_sync();
+    }
+};
+
+// ---- first kernel ----
+constexpr int kUpBlocks = 4 /* at most, of a stage */, kUpBytes = kUpBlocks * kRows * 128, kUpDepth = 2;
+constexpr int kUpRing = kWarps * kUpDepth * kUpBytes;
+
+template <int NTM> struct UpShared {
+    unsigned long long full[kWarps][kUpDepth];
+    float part[NTM == 1 ? 2 : 1][kWarps][NTM * 8][kRows + 1];      // two where there is room: then one meeting a unit is enough
+    Routing r;
+    float z[NTM * 8 * kInBlockExperts];
+    __align__(16) int idx[kMaxPicks], scan[kMaxPicks];
+    int abort_flag;
+};
+
+template <int NTM>
+__global__ void __launch_bounds__(kThreads, 1) decode_up_tma(const __grid_constant__ DecodeArgs p, const __grid_constant__ Maps maps)
+{
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ UpShared<NTM> sh;
+    Routing &r = sh.r;
+    const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int k = p.m.k, row = 2 * p.m.d, blocks = p.m.d / 64;
+    if (threadIdx.x < kWarps * kUpDepth) mbar_init(smem_u32(&sh.full[0][0] + threadIdx.x), 1);
+    if (threadIdx.x == 0) sh.abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    wait_for_earlier_kernels();
+    allow_next_kernel();
+    route<__nv_bfloat16, NTM>(p, sh.z, sh.part[0], sh.idx, sh.scan, r);
+    if (blockIdx.x == 0) publish(p, r, sh.idx);
+    const WaitCtx wc{&sh.abort_flag, p.status, p.wait_limit_ns};
+    int all = 0;
+    for (int s = 0; s < r.met; ++s) all += (p.m.hoff[r.expert[s] + 1] - p.m.hoff[r.expert[s]]) / kUnitCols;
+    const int begin = (int)((long long)all * blockIdx.x / gridDim.x), end = (int)((long long)all * (blockIdx.x + 1) / gridDim.x);
+    // the warp's blocks of a unit's rows, in stages of stage_blocks; lane 0 starts the copies
+    const int lo = blocks * warp / kWarps, hi = blocks * (warp + 1) / kWarps, stage_blocks = p.up_blocks;
+    const uint32_t ring = stages + warp * (kUpDepth * kUpBytes), bar = smem_u32(sh.full[warp]);
+    int in = 0, out = 0, pending = 0, step = lo;
+    uint32_t phase = 0;
+    bool ok = true;
+    UnitCursor ahead{begin, 0, 0, 0}, at = ahead;
+    bool more = lo < hi && begin < end && (int)blockIdx.x != p.skip_block && ahead.settle(p, r);
+    auto push = [&] {                            // every lane is done with the stage
+        if (!more || !ok) return;
+        __syncwarp();
+        if (lane == 0) {
+            const int first = p.m.hoff[r.expert[ahead.s]] + ahead.c0;
+            const uint32_t to = ring + in * kUpBytes, on = bar + 8 * in;
+            mbar_arrive_expect_tx(on, stage_blocks * (kRows * 128));
+            tma_load_3d(to, &maps.gate, on, 0, first, step);
+            tma_load_3d(to + stage_blocks * 1024, &maps.up, on, 0, first, step);
+        }
+        in = in + 1 == kUpDepth ? 0 : in + 1;
+        ++pending;
+        step += stage_blocks;
+        if (step >= hi) {
+            step = lo;
+            more = ++ahead.u < end && ahead.settle(p, r);
+        }
+    };
+    for (int i = 0; i < kUpDepth; ++i) push();
+    const int pitch = row + 64;
+    Tokens x{stages + kUpRing, pitch, p.x_room / pitch, false};
+    Sums<NTM> sums;
+    int held = -1, count = 0, some = 0;
+    const unsigned char *mine[NTM];              // the lane's rows of x, where they are not held
+    uint32_t cols[NTM];
+    for (int round = 0; at.u < end && at.settle(p, r); ++at.u, ++round) {
+        if (at.s != held) {
+            held = at.s;
+            count = r.first[at.s + 1] - r.first[at.s];
+            some = (count + 7) / 8;
+#pragma unroll
+            for (int n = 0; n < NTM; ++n) {
+                const int q = min(8 * n + g, count - 1);
+                mine[n] = p.x + (size_t)(r.pick[r.first[at.s] + q] / k) * row + t * 16;
+                cols[n] = x.at + q * pitch + t * 16;
+            }
+            x.hold(p, r, at.s);
+        }
+        sums.clear();
+        for (int b = lo; b < hi && ok; b += stage_blocks) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar + 8 * out, phase, wc));
+            if (!ok) break;
+            const uint32_t rows = ring + out * kUpBytes;
+#pragma unroll
+            for (int i = 0; i < kUpBlocks; ++i)
+                if (i < stage_blocks && b + i < hi)
+                    sums.add(rows + i * 1024, stage_blocks * 1024, some, [&](int n, int h) {
+                        const int from = (b + i) * 128 + h * kUnit;
+                        return x.held ? lds(cols[n] + from) : load_shared_rows(mine[n] + from, true);
+                    });
+            --pending;
+            if (++out == kUpDepth) {
+                out = 0;
+                phase ^= 1u;
+            }
+            push();
+        }
+        auto &part = sh.part[NTM == 1 ? round & 1 : 0];
+        if constexpr (NTM > 1) team_sync();      // the unit before has been read
+        const int row8 = row_of(g);
+#pragma unroll
+        for (int n = 0; n < NTM; ++n)
+            if (n < some)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) part[warp][8 * n + 2 * t + (i & 1)][row8 + 8 * (i >> 1)] = sums.acc[n][i];
+        team_sync();
+        if (threadIdx.x < count * kUnitCols) {
+            const int i = threadIdx.x / kUnitCols, c = threadIdx.x % kUnitCols, q = r.first[at.s] + i;
+            float a = 0.f, b = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                a += part[w][i][c];
+                b += part[w][i][c + kUnitCols];
+            }
+            // one rounding of the gated hidden value, as in modse_forward
+            reinterpret_cast<__nv_bfloat16 *>(p.hidden + q * p.ld)[at.c0 + c] = __float2bfloat16_rn(gated(r.gate[r.pick[q]], a, b));
+        }
+    }
+    // after a wait that expired the copies in flight land before the warp leaves, or the limit passes again
+    for (; !ok && pending > 0; --pending) {
+        const unsigned long long t0 = global_ns();
+        while (!mbar_try_wait(bar + 8 * out, phase) && global_ns() - t0 < p.wait_limit_ns) {}
+        if (++out == kUpDepth) {
+            out = 0;
+            phase ^= 1u;
+        }
+    }
+}
+
+// ---- tensor cores fed from shared memory: one ring for a block, multiplied by one thread ----
+// A stage is a column block of 128 rows of weights and the same columns of up to N rows of tokens, and as such the two
+// operands of four tcgen05 instructions: the weights' rows are the rows of the product, the tokens its columns.
+// Four threads fill the ring, every fourth stage each: waiting for a place and starting the copies takes one of them 0.3 us, in
+// which HBM delivers 12 KB to an SM.
+constexpr int kLoaders = 4, kLoader = kWarps, kIssuer = kWarps + kLoaders;
+constexpr int kTcThreads = kThreads + 32 * (kLoaders + 1);      // eight warps for routing and results
+constexpr int kMostStages = 5;
+// Two column blocks a stage, as far as there are two: handing a stage over costs the multiplying thread 0.2 us, as long as half a
+// stage of weights takes to arrive.
+constexpr int kPair = 2;
+template <int N> struct Tc {
+    static constexpr int kTokens = kPair * kBlockBytes;           // where a stage's rows of tokens begin
+    static constexpr int kStage = kPair * (kBlockBytes + N * 128);
+    static constexpr int kStages = N == 16 ? 5 : 5;
+    static constexpr int kTmemCols = 2 * N;      // two accumulators: one is drained while the next is summed up
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage;
+};
+
+struct Ring {
+    unsigned long long full[kMostStages], empty[kMostStages], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    int abort_flag;
+};
+struct Place {                                   // of a role in a ring of `n`
+    int n, at = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ explicit Place(int size) : n(size) {}
+    __device__ __forceinline__ void skip(int steps)
+    {
+        for (int i = 0; i < steps; ++i) next();
+    }
+    __device__ __forceinline__ void next()
+    {
+        if (++at == n) {
+            at = 0;
+            phase ^= 1u;
+        }
+    }
+};
+
+// fills: what has to arrive for a stage to be full beside the copies' bytes
+template <int N> __device__ __forceinline__ void tc_begin(Ring &ring, int fills)
+{
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < Tc<N>::kStages; ++i) {
+            mbar_init(smem_u32(&ring.full[i]), fills);
+            mbar_init(smem_u32(&ring.empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&ring.acc_full[i]), 1);
+            mbar_init(smem_u32(&ring.acc_empty[i]), 4);
+        }
+        ring.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (threadIdx.x >> 5 == kIssuer) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ring.tmem)), "r"(Tc<N>::kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+}
+template <int N> __device__ __forceinline__ void tc_end(const Ring &ring)
+{
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x >> 5 == kIssuer) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(ring.tmem), "r"(Tc<N>::kTmemCols) : "memory");
+    }
+}
+
+// One thread's part of a run of `length` column blocks, `count` tokens, that are summed up in one accumulator: false if a wait
+// expired.
+template <int N>
+__device__ __forceinline__ bool tc_multiply(Ring &ring, Place &st, Place &acc, uint32_t stages, int length, int count, const WaitCtx &wc)
+{
+    if (!mbar_wait(smem_u32(&ring.acc_empty[acc.at]), acc.phase ^ 1u, wc)) return false;
+    tc_fence_after();
+    const uint32_t idesc = make_idesc(false, false, count <= 16 ? 16 : N), to = ring.tmem + (uint32_t)(acc.at * N);
+    for (int i = 0; i < length; i += kPair) {
+        if (!mbar_wait(smem_u32(&ring.full[st.at]), st.phase, wc)) return false;
+        tc_fence_after();
+        const uint32_t at = stages + st.at * Tc<N>::kStage;
+#pragma unroll
+        for (int c = 0; c < kPair; ++c) {
+            if (i + c >= length) break;
+            const uint64_t a = make_desc(at + c * kBlockBytes, false), b = make_desc(at + Tc<N>::kTokens + c * N * 128, false);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) umma_bf16(to, a + 2 * q, b + 2 * q, idesc, i + c > 0 || q > 0);
+        }
+        umma_commit(smem_u32(&ring.empty[st.at]));
+        st.next();
+    }
+    umma_commit(smem_u32(&ring.acc_full[acc.at]));
+    acc.next();
+    return true;
+}
+// One of the team's first four warps takes its 32 rows of an accumulator: a row a lane.
+template <int N>
+__device__ __forceinline__ bool tc_take(Ring &ring, Place &acc, uint32_t (&v)[N], const WaitCtx &wc)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&ring.acc_full[acc.at]), acc.phase, wc))) return false;
+    tc_fence_after();
+    const uint32_t from = ring.tmem + ((uint32_t)(32 * warp) << 16) + (uint32_t)(acc.at * N);
+    if constexpr (N == 16) tmem_ld16(from, v);
+    else tmem_ld32(from, v);
+    tmem_ld_wait();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&ring.acc_empty[acc.at]));
+    acc.next();
+    return true;
+}
+// After a wait of a loading thread that expired: its copies in flight land before it leaves, or the limit passes again.
+// st: the place that it waited for.
+__device__ __forceinline__ void drain(Ring &ring, Place st, int issued, unsigned long long limit_ns)
+{
+    for (int i = 0; i < issued && i * kLoaders < st.n; ++i) {
+        for (int j = 0; j < kLoaders; ++j)
+            if (--st.at < 0) {
+                st.at = st.n - 1;
+                st.phase ^= 1u;
+            }
+        const unsigned long long t0 = global_ns();
+        while (!mbar_try_wait(smem_u32(&ring.full[st.at]), st.phase) && global_ns() - t0 < limit_ns) {}
+    }
+}
+
+// Meeting of the team's first four warps; true if all say so.
+__device__ __forceinline__ bool half_sync(bool v)
+{
+    int all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 2, %2, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+                 : "=r"(all) : "r"((int)v), "n"(kThreads / 2) : "memory");
+    return all != 0;
+}
+
+constexpr int kManyCols = 64;                    // hidden columns of a unit: 64 rows of W_gate over 64 of W_up
+
+template <int N>
+__global__ void __launch_bounds__(kTcThreads, 1) decode_up_many(const __grid_constant__ DecodeArgs p, const __grid_constant__ Maps maps)
+{
+    constexpr int NTM = N / 8;
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ Routing r;
+    __shared__ Ring ring;
+    __shared__ __align__(16) float out[N][kGroupRows];
+    __shared__ __align__(16) int idx[kMaxPicks], scan[kMaxPicks];
+    const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int k = p.m.k, blocks = p.m.d / 64;
+    tc_begin<N>(ring, 2);
+    wait_for_earlier_kernels();
+    allow_next_kernel();
+    if (warp < kWarps) {
+        // the logits and their partial sums, where the ring will be
+        typedef float Part[kWarps][NTM * 8][kRows + 1];
+        unsigned char *scratch = smem_raw + (stages - smem_u32(smem_raw));
+        route<__nv_bfloat16, NTM>(p, reinterpret_cast<float *>(scratch + sizeof(Part)), *reinterpret_cast<Part *>(scratch), idx, scan, r);
+        if (blockIdx.x == 0) publish(p, r, idx);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    const WaitCtx wc{&ring.abort_flag, p.status, p.wait_limit_ns};
+    int all = 0;
+    for (int s = 0; s < r.met; ++s) all += (p.m.hoff[r.expert[s] + 1] - p.m.hoff[r.expert[s]]) / kManyCols;
+    const int begin = (int)((long long)all * blockIdx.x / gridDim.x), end = (int)((long long)all * (blockIdx.x + 1) / gridDim.x);
+    Place st(Tc<N>::kStages), acc(2);
+    int s = 0, base = 0;                         // the expert that unit u lies in, units ahead of it
+    auto settle = [&](int u) {
+        while (true) {
+            const int units = (p.m.hoff[r.expert[s] + 1] - p.m.hoff[r.expert[s]]) / kManyCols;
+            if (u - base < units) return (u - base) * kManyCols;
+            base += units;
+            ++s;
+        }
+    };
+    if (warp >= kLoader && warp < kIssuer) {
+        // The weights come by TMA, the rows of x by the loading warp's lanes: 16 bytes a lane and piece, swizzled as TMA would (its
+        // row gather takes 0.25 us for four rows).  The next stage's pieces are requested before this one's place is waited for.
+        constexpr int P = N / 4;                 // pieces of a lane and column block: rows lane / 8 + 4 j
+        const int piece = lane & 7, mine = warp - kLoader, pairs = (blocks + kPair - 1) / kPair;
+        const int total = (int)blockIdx.x == p.skip_block ? 0 : (end - begin) * pairs;
+        uint4 v[kPair][P];
+        int count = 0, held = -1, c0 = 0, u = begin, b = mine;       // of the stage whose pieces are on their way: unit, pair of blocks
+        const unsigned char *from[P];
+        auto request = [&] {
+            while (b >= pairs) {
+                b -= pairs;
+                ++u;
+            }
+            if (u >= end) return;
+            c0 = settle(u);
+            if (s != held) {
+                held = s;
+                count = r.first[s + 1] - r.first[s];
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const int q = min((lane >> 3) + 4 * j, count - 1);
+                    from[j] = p.x + (size_t)(r.pick[r.first[s] + q] / k) * (2 * p.m.d) + piece * 16;
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kPair; ++c)
+#pragma unroll
+                for (int j = 0; j < P; ++j)
+                    if (4 * j < count) v[c][j] = load_shared_rows(from[j] + (kPair * b + c) * 128, kPair * b + c < blocks);
+        };
+        st.skip(mine);
+        request();
+        int issued = 0;
+        for (int i = mine; i < total; i += kLoaders) {
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&ring.empty[st.at]), st.phase ^ 1u, wc))) {
+                if (lane == 0) drain(ring, st, issued, p.wait_limit_ns);
+                break;
+            }
+            const uint32_t bar = smem_u32(&ring.full[st.at]), to = stages + st.at * Tc<N>::kStage;
+            const int n = min(kPair, blocks - kPair * b);
+            if (lane == 0) {
+                const int first = p.m.hoff[r.expert[s]] + c0;
+                mbar_arrive_expect_tx(bar, n * kBlockBytes);
+                for (int c = 0; c < n; ++c) {
+                    tma_load_2d(to + c * kBlockBytes, &maps.gate64, bar, (kPair * b + c) * 64, first);
+                    tma_load_2d(to + c * kBlockBytes + kBlockBytes / 2, &maps.up64, bar, (kPair * b + c) * 64, first);
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < kPair; ++c)
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    const int q = (lane >> 3) + 4 * j;
+                    if (c < n && 4 * j < count)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};"
+                                     ::"r"(to + Tc<N>::kTokens + c * N * 128 + q * 128 + ((piece ^ (q & 7)) << 4)), "r"(v[c][j].x), "r"(v[c][j].y),
+                                       "r"(v[c][j].z), "r"(v[c][j].w) : "memory");
+                }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+            st.skip(kLoaders);
+            ++issued;
+            b += kLoaders;
+            request();
+        }
+    } else if (warp == kIssuer) {
+        if (lane == 0)
+            for (int u = begin; u < end; ++u) {
+                settle(u);
+                if (!tc_multiply<N>(ring, st, acc, stages, blocks, r.first[s + 1] - r.first[s], wc)) break;
+            }
+    } else if (warp < kWarps / 2) {
+        constexpr int kHalf = kThreads / 2;
+        for (int u = begin; u < end; ++u) {
+            const int c0 = settle(u), count = r.first[s + 1] - r.first[s];
+            uint32_t v[N];
+            const bool ok = tc_take<N>(ring, acc, v, wc);
+            if (ok)
+#pragma unroll
+                for (int n = 0; n < N; ++n) out[n][32 * warp + lane] = __uint_as_float(v[n]);
+            if (!half_sync(ok)) break;
+            for (int i = threadIdx.x; i < count * kManyCols; i += kHalf) {
+                const int q = i / kManyCols, c = i % kManyCols, at = r.first[s] + q;
+                // one rounding of the gated hidden value, as in modse_forward
+                reinterpret_cast<__nv_bfloat16 *>(p.hidden + at * p.ld)[c0 + c] =
+                    __float2bfloat16_rn(gated(r.gate[r.pick[at]], out[q][c], out[q][c + kManyCols]));
+            }
+            half_sync(true);
+        }
+    }
+    tc_end<N>(ring);
+}
+
+// ---- second kernel ----
+template <int N>
+__global__ void __launch_bounds__(kTcThreads, 1) decode_down_tma(const __grid_constant__ DecodeArgs p, const __grid_constant__ Maps maps)
+{
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ Routing r;
+    __shared__ Ring ring;
+    __shared__ int upto[kMaxPicks + 1];                       // column blocks ahead of each expert met
+    __shared__ __align__(16) float out[N][kGroupRows];
+    __shared__ int last;
+    const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
+    tc_begin<N>(ring, 1);
+    wait_for_earlier_kernels();
+    allow_next_kernel();
+    for (int i = tid; i < (int)(sizeof(Routing) / 4); i += kTcThreads) ((int *)&r)[i] = __ldcg((const int *)p.routing + i);
+    __syncthreads();
+    if (tid <= r.met) {
+        int n = 0;
+        for (int s = 0; s < tid; ++s) n += (p.m.hoff[r.expert[s] + 1] - p.m.hoff[r.expert[s]]) / 64;
+        upto[tid] = n;
+    }
+    __syncthreads();
+    const int per = upto[r.met], groups = (p.m.d + kGroupRows - 1) / kGroupRows;
+    // `share` blocks a group of rows, which take its column blocks in turn: what they ask for at a time lies side by side
+    const int share = max(1, min((int)gridDim.x / groups, per / 2)), step = max(1, (int)gridDim.x / share), member = blockIdx.x % share;
+    const WaitCtx wc{&ring.abort_flag, p.status, p.wait_limit_ns};
+    Place st(Tc<N>::kStages), acc(2);
+    const int first_group = (int)blockIdx.x / share < step ? (int)blockIdx.x / share : groups;
+    // the block's column blocks of expert s: from upto[s] on the first that is `member` modulo `share`
+    auto first_of = [&](int s) { return upto[s] + (member - upto[s] % share + share) % share; };
+    auto length_of = [&](int s) { return (upto[s + 1] - first_of(s) + share - 1) / share; };      // 0 or less: none
+    if (warp >= kLoader && warp < kIssuer) {
+        if (lane == 0) {
+            bool ok = true;
+            int issued = 0, turn = warp - kLoader;       // the next of an expert's stages that is this thread's
+            st.skip(turn);
+            for (int group = first_group; ok && group < groups; group += step)
+                for (int s = 0; ok && s < r.met; ++s) {
+                    const int first = first_of(s), n = length_of(s), boxes = (r.first[s + 1] - r.first[s] + 15) / 16, col0 = p.m.hoff[r.expert[s]];
+                    const int pairs = (max(n, 0) + kPair - 1) / kPair;
+                    for (; turn < pairs; turn += kLoaders) {
+                        if (!mbar_wait(smem_u32(&ring.empty[st.at]), st.phase ^ 1u, wc)) { ok = false; break; }
+                        const uint32_t bar = smem_u32(&ring.full[st.at]), to = stages + st.at * Tc<N>::kStage;
+                        const int held = min(kPair, n - kPair * turn);
+                        mbar_arrive_expect_tx(bar, held * (kBlockBytes + boxes * 2048));
+                        for (int c = 0; c < held; ++c) {
+                            const int col = (first + (kPair * turn + c) * share - upto[s]) * 64;
+                            tma_load_2d(to + c * kBlockBytes, &maps.down, bar, col0 + col, group * kGroupRows);
+                            for (int i = 0; i < boxes; ++i)
+                                tma_load_2d(to + Tc<N>::kTokens + c * N * 128 + i * 2048, &maps.hidden, bar, col, r.first[s] + 16 * i);
+                        }
+                        st.skip(kLoaders);
+                        ++issued;
+                    }
+                    turn -= pairs;
+                }
+            if (!ok) drain(ring, st, issued, p.wait_limit_ns);
+        }
+    } else if (warp == kIssuer) {
+        if (lane == 0) {
+            bool ok = true;
+            for (int group = first_group; ok && group < groups; group += step)
+                for (int s = 0; ok && s < r.met; ++s)
+                    if (length_of(s) > 0) ok = tc_multiply<N>(ring, st, acc, stages, length_of(s), r.first[s + 1] - r.first[s], wc);
+        }
+    } else {
+        bool ok = true;
+        for (int group = first_group; group < groups; group += step) {
+            if (warp < 4) {
+                // a lane's own row of `out`: nobody else touches it before the meeting below
+                float (*mine)[kGroupRows] = reinterpret_cast<float (*)[kGroupRows]>(&out[0][32 * warp + lane]);
+                for (int tok = 0; tok < p.T; ++tok) mine[tok][0] = 0.f;
+                for (int s = 0; s < r.met; ++s) {
+                    if (length_of(s) <= 0) continue;
+                    uint32_t v[N];
+                    if (ok) ok = tc_take<N>(ring, acc, v, wc);
+                    const int count = r.first[s + 1] - r.first[s];
+                    if (ok)
+#pragma unroll
+                        for (int q = 0; q < N; ++q)
+                            if (q < count) mine[r.pick[r.first[s] + q] / p.m.k][0] += __uint_as_float(v[q]);
+                }
+            }
+            team_sync();
+            leave_rows<kGroupRows>(p, group, &out[0][0], member, share, group * share, &last, p.y_f32 != 0);
+            team_sync();                     // `out` and `last` have been read
+        }
+    }
+    tc_end<N>(ring);
+}
+
+// ---- host ----
+bool encode(CUtensorMap *map, int rank, const void *base, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box)
+{
+    EncodeTiledFn fn = get_encode();
+    if (fn == nullptr) return false;
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool encode_2d(CUtensorMap *map, const void *base, long long rows, long long cols, long long ld_bytes, int box_rows)
+{
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld_bytes};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    return encode(map, 2, base, dims, strides, box);
+}
+bool encode_3d(CUtensorMap *map, const void *base, long long rows, int d, int blocks)
+{
+    const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(d / 64)}, strides[2] = {(cuuint64_t)d * 2, 128};
+    const cuuint32_t box[3] = {64, kUnitCols, (cuuint32_t)blocks};
+    return encode(map, 3, base, dims, strides, box);
+}
+
+template <typename K>
+cudaError_t allow_smem(K kern, size_t bytes, unsigned long long &done)
+{
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev <= 63 && ((done >> dev) & 1ull)) return cudaSuccess;      // a bit a device; those beyond 63 set it every time
+    if (dev <= 63) done |= 1ull << dev;
+    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+
+// One group of eight tokens: the first kernel on mma.sync, whose small units go round the SMs evenly; more: on tcgen05.
+constexpr int kFewTokens = 8;
+
+cudaError_t launch_up_few(DecodeArgs &a, const Maps &maps, int blocks, cudaStream_t s)
+{
+    constexpr size_t bytes = kSmemMost - sizeof(UpShared<1>);
+    static unsigned long long done = 0;
+    a.x_room = (int)(bytes - 1024 - kUpRing);
+    const cudaError_t e = allow_smem(decode_up_tma<1>, bytes, done);
+    return e != cudaSuccess ? e : launch_overlapped(decode_up_tma<1>, blocks, kThreads, bytes, s, a, maps);
+}
+template <int N>
+cudaError_t launch(DecodeArgs &a, const Maps &maps, int blocks, cudaStream_t s)
+{
+    static unsigned long long done_up = 0, done_down = 0;
+    cudaError_t e = cudaSuccess;
+    if (a.T <= kFewTokens) {
+        e = launch_up_few(a, maps, blocks, s);
+    } else {
+        e = allow_smem(decode_up_many<N>, Tc<N>::kSmem, done_up);
+        if (e == cudaSuccess) e = launch_overlapped(decode_up_many<N>, blocks, kTcThreads, Tc<N>::kSmem, s, a, maps);
+    }
+    if (e == cudaSuccess) e = allow_smem(decode_down_tma<N>, Tc<N>::kSmem, done_down);
+    return e != cudaSuccess ? e : launch_overlapped(decode_down_tma<N>, blocks, kTcThreads, Tc<N>::kSmem, s, a, maps);
+}
+
+}  // namespace
+
+bool tma_takes(const LayerMeta &m)
+{
+    if (m.d % 64 != 0) return false;
+    for (int e = 0; e <= m.N; ++e)
+        if (m.hoff[e] % 64 != 0) return false;
+    return true;
+}
+
+cudaError_t launch_tma(const DecodeArgs &args, int sms, cudaStream_t s)
+{
+    DecodeArgs a = args;
+    Maps maps;
+    // a warp's share of a row, up to kUpBlocks blocks at a time, as evenly as it goes
+    const int share = (a.m.d / 64 + kWarps - 1) / kWarps, steps = (share + kUpBlocks - 1) / kUpBlocks;
+    a.up_blocks = (share + steps - 1) / steps;
+    const bool rows = a.T <= kFewTokens ? encode_3d(&maps.gate, a.w_gate, a.m.S, a.m.d, a.up_blocks) && encode_3d(&maps.up, a.w_up, a.m.S, a.m.d, a.up_blocks)
+                                        : encode_2d(&maps.gate64, a.w_gate, a.m.S, a.m.d, 2ll * a.m.d, kManyCols) &&
+                                          encode_2d(&maps.up64, a.w_up, a.m.S, a.m.d, 2ll * a.m.d, kManyCols);
+    if (!rows || !encode_2d(&maps.down, a.w_down, a.m.d, a.m.S, 2ll * a.m.S, kGroupRows) ||
+        !encode_2d(&maps.hidden, a.hidden, (long long)a.T * a.m.k, a.ld / 2, a.ld, 16))
+        return cudaErrorInvalidValue;
+    const int blocks = std::min(sms, kTmaBlocks);
+    return a.T <= 16 ? launch<16>(a, maps, blocks, s) : launch<32>(a, maps, blocks, s);
+}
+
+}  // namespace decode
+}  // namespace modse

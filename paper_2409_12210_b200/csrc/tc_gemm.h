@@ -79,6 +79,7 @@ void tc_set_dynamic_tiles(int on);    // 1 (default): CTAs take tiles from a sha
 void tc_set_wait_limit_ms(int ms);    // limit of every bounded wait inside the kernels (default 2000)
 unsigned long long tc_wait_limit_ns();
 constexpr int kTcDenseProducts = 6;  // the number by which the switch below names the dense products around the layer
+constexpr int kTcDecode = 7;         // ... and the blocks of modse_decode
 int tc_skip_tile(int kind);          // the tile to skip of a product, -1: none
 // bit per product: sixteen epilogue warps on 128-row tiles / one-CTA 256-row tiles / CTA-pair tiles
 void tc_set_epilogue_warps16(int narrow_mask, int wide_mask, int pair_mask);
