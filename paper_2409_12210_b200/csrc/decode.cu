@@ -50,15 +50,16 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(NTM)) decode_up_kernel
     __shared__ __align__(16) int idx[kMaxPicks], scan[kMaxPicks];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int k = p.m.k, row = p.m.d * (int)sizeof(T), units = (row + kUnit - 1) / kUnit;
+    fetch_router(p, row);
     wait_for_earlier_kernels();
     allow_next_kernel();
     route<T, NTM>(p, z, part[0], idx, scan, r);
     if (blockIdx.x == 0) publish(p, r, idx);
     int round = 0;
-    for (UnitCursor at{(int)blockIdx.x, 0, 0, 0}; at.settle(p, r); at.u += gridDim.x, ++round) {
+    for (UnitCursor at{(int)blockIdx.x, 0, 0, 0}; at.settle(r); at.u += gridDim.x, ++round) {
         const int count = r.first[at.s + 1] - r.first[at.s];
         const int *pick = r.pick + r.first[at.s];
-        const size_t w = ((size_t)p.m.hoff[r.expert[at.s]] + at.c0 + g) * row + t * 16;
+        const size_t w = ((size_t)r.offset[at.s] + at.c0 + g) * row + t * 16;
         const unsigned char *x[NTM];
 #pragma unroll
         for (int n = 0; n < NTM; ++n) x[n] = p.x + (size_t)(pick[min(8 * n + g, count - 1)] / k) * row + t * 16;
@@ -99,7 +100,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(NTM)) decode_down_kern
     __syncthreads();
     if (tid <= r.met) {
         int n = 0;
-        for (int s = 0; s < tid; ++s) n += ((p.m.hoff[r.expert[s] + 1] - p.m.hoff[r.expert[s]]) * esz + kUnit - 1) / kUnit;
+        for (int s = 0; s < tid; ++s) n += (r.width[s] * esz + kUnit - 1) / kUnit;
         upto[tid] = n;
     }
     __syncthreads();
@@ -118,7 +119,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(NTM)) decode_down_kern
         int s = 0;
         while (upto[s + 1] <= lo) ++s;
         for (; s < r.met && upto[s] < hi; ++s, ++round) {
-            const int off = p.m.hoff[r.expert[s]], bytes = (p.m.hoff[r.expert[s] + 1] - off) * esz;
+            const int off = r.offset[s], bytes = r.width[s] * esz;
             const int count = r.first[s + 1] - r.first[s];
             const int *pick = r.pick + r.first[s];
             const unsigned char *x[NTM];

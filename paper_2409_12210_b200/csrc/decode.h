@@ -17,6 +17,7 @@ constexpr int kInBlockExperts = 32;       // rows of router matrices that every 
 struct Routing {
     int met;
     int expert[kMaxPicks];                // ascending
+    int offset[kMaxPicks], width[kMaxPicks];      // theirs
     int first[kMaxPicks + 1];             // of each expert's picks in `pick`
     int pick[kMaxPicks];                  // ascending within an expert
     float gate[kMaxPicks];                // by pick
@@ -38,7 +39,7 @@ struct DecodeArgs {
     int *status;
     unsigned long long wait_limit_ns;
     int x_room;                           // bytes of shared memory for rows of x
-    int up_blocks;                        // column blocks of a stage of decode_up_tma
+    int up_blocks;                        // column blocks of a stage of decode_up_few
     int skip_block;                       // debugging: the block that stops loading weights (-1: none)
     int T, y_f32;
 };
@@ -142,8 +143,8 @@ template <> struct Dot<float> {
     }
 };
 
-// ... with as many groups of eight tokens as there are
-template <typename T, int NTM>
+// ... with as many groups of eight tokens as there are, U1 units in flight with one of them.
+template <typename T, int NTM, int U1 = 4>
 __device__ __forceinline__ void dot(int nt, const unsigned char *w0, const unsigned char *w1, const unsigned char *const (&x)[NTM],
                                     int u0, int u1, int row_bytes, float (*part)[kRows + 1])
 {
@@ -153,7 +154,7 @@ __device__ __forceinline__ void dot(int nt, const unsigned char *w0, const unsig
     }
     if constexpr (NTM >= 2)
         if (nt == 2) return Dot<T>::template run<2, 4>(w0, w1, x, u0, u1, row_bytes, part);
-    Dot<T>::template run<1, 4>(w0, w1, x, u0, u1, row_bytes, part);
+    Dot<T>::template run<1, U1>(w0, w1, x, u0, u1, row_bytes, part);
 }
 
 __device__ __forceinline__ float softplus(float u) { return u > 0.f ? u + log1pf(expf(-u)) : log1pf(expf(u)); }
@@ -175,7 +176,7 @@ __device__ __forceinline__ void router_tile(const DecodeArgs &p, int tile, float
 #pragma unroll
     for (int n = 0; n < NTM; ++n) x[n] = p.x + (size_t)min(8 * n + g, p.T - 1) * row + t * 16;
     team_sync();
-    dot<T, NTM>((p.T + 7) / 8, w + (size_t)min(e0 + g, last) * row + t * 16, w + (size_t)min(e0 + g + 8, last) * row + t * 16, x, 0,
+    dot<T, NTM, 8>((p.T + 7) / 8, w + (size_t)min(e0 + g, last) * row + t * 16, w + (size_t)min(e0 + g + 8, last) * row + t * 16, x, 0,
                 (row + kUnit - 1) / kUnit, row, part[warp]);
     team_sync();
     z += tile < tiles ? 0 : p.T * p.m.N;
@@ -247,15 +248,24 @@ __device__ __forceinline__ void route(const DecodeArgs &p, float *mem, float (&p
             }
             float best[2] = {-INFINITY, -INFINITY}, raw[2] = {0.f, 0.f};
             int at[2] = {-1, -1};
-#pragma unroll 4
-            for (int e = 0; e < N; ++e) {
-                const float v = p.w_noise ? fmaf(softplus(ut[e]), scale, zt[e]) : zt[e];
-                const float c = isnan(v) ? -INFINITY : v;
-                if (at[0] < 0 || c > best[0]) {
-                    best[1] = best[0], raw[1] = raw[0], at[1] = at[0];
-                    best[0] = c, raw[0] = v, at[0] = e;
-                } else if (at[1] < 0 || c > best[1]) {
-                    best[1] = c, raw[1] = v, at[1] = e;
+            for (int e0 = 0; e0 < N; e0 += 8) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = e0 + i < N ? zt[e0 + i] : 0.f;
+                if (p.w_noise)
+                    for (int i = 0; i < 8; ++i)
+                        if (e0 + i < N) v[i] = fmaf(softplus(ut[e0 + i]), scale, v[i]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (e0 + i >= N) break;
+                    const float c = isnan(v[i]) ? -INFINITY : v[i];
+                    const bool top = at[0] < 0 || c > best[0], next = !top && (at[1] < 0 || c > best[1]);
+                    best[1] = top ? best[0] : next ? c : best[1];
+                    raw[1] = top ? raw[0] : next ? v[i] : raw[1];
+                    at[1] = top ? at[0] : next ? e0 + i : at[1];
+                    best[0] = top ? c : best[0];
+                    raw[0] = top ? v[i] : raw[0];
+                    at[0] = top ? e0 + i : at[0];
                 }
             }
             gates(tid, at[0], at[1], raw[0], raw[1]);
@@ -335,6 +345,8 @@ __device__ __forceinline__ void route(const DecodeArgs &p, float *mem, float (&p
         }
         if (mine == 0) {
             r.expert[place] = e;
+            r.offset[place] = p.m.hoff[e];
+            r.width[place] = p.m.hoff[e + 1] - p.m.hoff[e];
             r.first[place] = before;
         }
         if (tid == 0) {
@@ -343,6 +355,21 @@ __device__ __forceinline__ void route(const DecodeArgs &p, float *mem, float (&p
         }
     }
     team_sync();
+}
+
+// Before the kernels ahead have ended: the router matrix on its way to L2, where every block reads it a moment later.
+__device__ __forceinline__ void fetch_router(const DecodeArgs &p, int row_bytes)
+{
+    const size_t bytes = (size_t)p.m.N * row_bytes, at = ((size_t)blockIdx.x * blockDim.x + threadIdx.x) * 128;
+    if (at < bytes) asm volatile("prefetch.global.L2 [%0];" ::"l"(p.w_router + at));
+}
+
+// Block b's even share [begin, end) of n units.
+__device__ __forceinline__ void share_of(int n, int &begin, int &end)
+{
+    const int b = blockIdx.x, each = n / (int)gridDim.x, more = n - each * (int)gridDim.x;
+    begin = each * b + min(b, more);
+    end = begin + each + (b < more);
 }
 
 // For the second kernel and the caller, by one block of the first.
@@ -360,10 +387,10 @@ __device__ __forceinline__ void publish(const DecodeArgs &p, const Routing &r, c
 // A unit of the first kernel: eight hidden columns of an expert met.
 struct UnitCursor {
     int u, s, base, c0;                   // unit, its expert's place among those met, units ahead of that expert, first column
-    __device__ __forceinline__ bool settle(const DecodeArgs &p, const Routing &r)
+    __device__ __forceinline__ bool settle(const Routing &r)
     {
         while (s < r.met) {
-            const int e = r.expert[s], units = (p.m.hoff[e + 1] - p.m.hoff[e]) / kUnitCols;
+            const int units = r.width[s] / kUnitCols;
             if (u - base < units) {
                 c0 = (u - base) * kUnitCols;
                 return true;

@@ -43,6 +43,7 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
 }
+__device__ __forceinline__ void prefetch(const CUtensorMap &map) { asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory"); }
 __device__ __forceinline__ uint4 lds(uint32_t at)
 {
     uint4 v;
@@ -50,41 +51,25 @@ __device__ __forceinline__ uint4 lds(uint32_t at)
     return v;
 }
 
-// A warp's sums of one fragment of rows with NTM groups of eight columns (tokens).
-template <int NTM> struct Sums {
-    float acc[NTM][4];
-    __device__ __forceinline__ void clear()
-    {
+// A column block of a fragment's sixteen rows times eight tokens.  rows: of the fragment's rows 0 .. 7 (unswizzled row 0), `second`
+// bytes ahead of rows 8 .. 15; x: the lane's 16 bytes of both units of its token's row.
+__device__ __forceinline__ void add_block(float (&acc)[4], uint32_t rows, uint32_t second, const uint4 (&x)[2])
+{
+    const int lane = threadIdx.x & 31, t = lane & 3, row = row_of(lane >> 2);
+    uint4 a[2], b[2];
 #pragma unroll
-        for (int n = 0; n < NTM; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t at = rows + row * 128 + (((4 * h + t) ^ row) << 4);
+        a[h] = lds(at);
+        b[h] = lds(at + second);
     }
-    // A column block.  rows: of the fragment's rows 0 .. 7 (unswizzled row 0), `second` bytes ahead of rows 8 .. 15;
-    // column(n, h): the lane's 16 bytes of unit h of its column in group n; `some` groups of columns.
-    template <typename Column>
-    __device__ __forceinline__ void add(uint32_t rows, uint32_t second, int some, const Column &column)
-    {
-        const int lane = threadIdx.x & 31, t = lane & 3, row = row_of(lane >> 2);
-        uint4 a[2], b[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t at = rows + row * 128 + (((4 * h + t) ^ row) << 4);
-            a[h] = lds(at);
-            b[h] = lds(at + second);
-        }
-#pragma unroll
-        for (int n = 0; n < NTM; ++n)
-            if (n < some)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint4 x = column(n, h);
-                    const uint32_t lo[4] = {a[h].x, b[h].x, a[h].y, b[h].y}, hi[4] = {a[h].z, b[h].z, a[h].w, b[h].w};
-                    mma_16816(acc[n], lo, x.x, x.y, false);
-                    mma_16816(acc[n], hi, x.z, x.w, false);
-                }
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t lo[4] = {a[h].x, b[h].x, a[h].y, b[h].y}, hi[4] = {a[h].z, b[h].z, a[h].w, b[h].w};
+        mma_16816(acc, lo, x[h].x, x[h].y, false);
+        mma_16816(acc, hi, x[h].z, x[h].w, false);
     }
-};
+}
 
 // The rows of x of an expert, in shared memory where they fit: rows 64 bytes more than a multiple of 128 apart, so that the two
 // rows that eight neighbouring lanes read lie in opposite halves of the banks.
@@ -112,36 +97,41 @@ struct Tokens {
 constexpr int kUpBlocks = 4 /* at most, of a stage */, kUpBytes = kUpBlocks * kRows * 128, kUpDepth = 2;
 constexpr int kUpRing = kWarps * kUpDepth * kUpBytes;
 
-template <int NTM> struct UpShared {
+struct UpShared {
     unsigned long long full[kWarps][kUpDepth];
-    float part[NTM == 1 ? 2 : 1][kWarps][NTM * 8][kRows + 1];      // two where there is room: then one meeting a unit is enough
+    float part[2][kWarps][8][kRows + 1];          // two of them, so that one meeting a unit is enough
     Routing r;
-    float z[NTM * 8 * kInBlockExperts];
+    float z[8 * kInBlockExperts];
     __align__(16) int idx[kMaxPicks], scan[kMaxPicks];
     int abort_flag;
 };
 
-template <int NTM>
-__global__ void __launch_bounds__(kThreads, 1) decode_up_tma(const __grid_constant__ DecodeArgs p, const __grid_constant__ Maps maps)
+__global__ void __launch_bounds__(kThreads, 1) decode_up_few(const __grid_constant__ DecodeArgs p, const __grid_constant__ Maps maps)
 {
     extern __shared__ unsigned char smem_raw[];
-    __shared__ UpShared<NTM> sh;
+    __shared__ UpShared sh;
     Routing &r = sh.r;
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int k = p.m.k, row = 2 * p.m.d, blocks = p.m.d / 64;
     if (threadIdx.x < kWarps * kUpDepth) mbar_init(smem_u32(&sh.full[0][0] + threadIdx.x), 1);
-    if (threadIdx.x == 0) sh.abort_flag = 0;
+    if (threadIdx.x == 0) {
+        sh.abort_flag = 0;
+        prefetch(maps.gate);
+        prefetch(maps.up);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    fetch_router(p, row);
     wait_for_earlier_kernels();
     allow_next_kernel();
-    route<__nv_bfloat16, NTM>(p, sh.z, sh.part[0], sh.idx, sh.scan, r);
+    route<__nv_bfloat16, 1>(p, sh.z, sh.part[0], sh.idx, sh.scan, r);
     if (blockIdx.x == 0) publish(p, r, sh.idx);
     const WaitCtx wc{&sh.abort_flag, p.status, p.wait_limit_ns};
     int all = 0;
-    for (int s = 0; s < r.met; ++s) all += (p.m.hoff[r.expert[s] + 1] - p.m.hoff[r.expert[s]]) / kUnitCols;
-    const int begin = (int)((long long)all * blockIdx.x / gridDim.x), end = (int)((long long)all * (blockIdx.x + 1) / gridDim.x);
+    for (int s = 0; s < r.met; ++s) all += r.width[s] / kUnitCols;
+    int begin, end;
+    share_of(all, begin, end);
     // the warp's blocks of a unit's rows, in stages of stage_blocks; lane 0 starts the copies
     const int lo = blocks * warp / kWarps, hi = blocks * (warp + 1) / kWarps, stage_blocks = p.up_blocks;
     const uint32_t ring = stages + warp * (kUpDepth * kUpBytes), bar = smem_u32(sh.full[warp]);
@@ -149,12 +139,12 @@ __global__ void __launch_bounds__(kThreads, 1) decode_up_tma(const __grid_consta
     uint32_t phase = 0;
     bool ok = true;
     UnitCursor ahead{begin, 0, 0, 0}, at = ahead;
-    bool more = lo < hi && begin < end && (int)blockIdx.x != p.skip_block && ahead.settle(p, r);
+    bool more = lo < hi && begin < end && (int)blockIdx.x != p.skip_block && ahead.settle(r);
     auto push = [&] {                            // every lane is done with the stage
         if (!more || !ok) return;
         __syncwarp();
         if (lane == 0) {
-            const int first = p.m.hoff[r.expert[ahead.s]] + ahead.c0;
+            const int first = r.offset[ahead.s] + ahead.c0;
             const uint32_t to = ring + in * kUpBytes, on = bar + 8 * in;
             mbar_arrive_expect_tx(on, stage_blocks * (kRows * 128));
             tma_load_3d(to, &maps.gate, on, 0, first, step);
@@ -165,41 +155,41 @@ __global__ void __launch_bounds__(kThreads, 1) decode_up_tma(const __grid_consta
         step += stage_blocks;
         if (step >= hi) {
             step = lo;
-            more = ++ahead.u < end && ahead.settle(p, r);
+            more = ++ahead.u < end && ahead.settle(r);
         }
     };
     for (int i = 0; i < kUpDepth; ++i) push();
     const int pitch = row + 64;
     Tokens x{stages + kUpRing, pitch, p.x_room / pitch, false};
-    Sums<NTM> sums;
-    int held = -1, count = 0, some = 0;
-    const unsigned char *mine[NTM];              // the lane's rows of x, where they are not held
-    uint32_t cols[NTM];
-    for (int round = 0; at.u < end && at.settle(p, r); ++at.u, ++round) {
+    float acc[4];
+    int held = -1, count = 0;
+    const unsigned char *mine = nullptr;         // the lane's row of x, where the rows are not held
+    uint32_t cols = 0;                           // ... and where they are
+    for (int round = 0; at.u < end && at.settle(r); ++at.u, ++round) {
         if (at.s != held) {
             held = at.s;
             count = r.first[at.s + 1] - r.first[at.s];
-            some = (count + 7) / 8;
-#pragma unroll
-            for (int n = 0; n < NTM; ++n) {
-                const int q = min(8 * n + g, count - 1);
-                mine[n] = p.x + (size_t)(r.pick[r.first[at.s] + q] / k) * row + t * 16;
-                cols[n] = x.at + q * pitch + t * 16;
-            }
+            const int q = min(g, count - 1);
+            mine = p.x + (size_t)(r.pick[r.first[at.s] + q] / k) * row + t * 16;
+            cols = x.at + q * pitch + t * 16;
             x.hold(p, r, at.s);
         }
-        sums.clear();
+        acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
         for (int b = lo; b < hi && ok; b += stage_blocks) {
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar + 8 * out, phase, wc));
             if (!ok) break;
             const uint32_t rows = ring + out * kUpBytes;
 #pragma unroll
             for (int i = 0; i < kUpBlocks; ++i)
-                if (i < stage_blocks && b + i < hi)
-                    sums.add(rows + i * 1024, stage_blocks * 1024, some, [&](int n, int h) {
+                if (i < stage_blocks && b + i < hi) {
+                    uint4 v[2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
                         const int from = (b + i) * 128 + h * kUnit;
-                        return x.held ? lds(cols[n] + from) : load_shared_rows(mine[n] + from, true);
-                    });
+                        v[h] = x.held ? lds(cols + from) : load_shared_rows(mine + from, true);
+                    }
+                    add_block(acc, rows + i * 1024, stage_blocks * 1024, v);
+                }
             --pending;
             if (++out == kUpDepth) {
                 out = 0;
@@ -207,14 +197,10 @@ __global__ void __launch_bounds__(kThreads, 1) decode_up_tma(const __grid_consta
             }
             push();
         }
-        auto &part = sh.part[NTM == 1 ? round & 1 : 0];
-        if constexpr (NTM > 1) team_sync();      // the unit before has been read
+        auto &part = sh.part[round & 1];
         const int row8 = row_of(g);
 #pragma unroll
-        for (int n = 0; n < NTM; ++n)
-            if (n < some)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) part[warp][8 * n + 2 * t + (i & 1)][row8 + 8 * (i >> 1)] = sums.acc[n][i];
+        for (int i = 0; i < 4; ++i) part[warp][2 * t + (i & 1)][row8 + 8 * (i >> 1)] = acc[i];
         team_sync();
         if (threadIdx.x < count * kUnitCols) {
             const int i = threadIdx.x / kUnitCols, c = threadIdx.x % kUnitCols, q = r.first[at.s] + i;
@@ -244,22 +230,23 @@ __global__ void __launch_bounds__(kThreads, 1) decode_up_tma(const __grid_consta
 // operands of four tcgen05 instructions: the weights' rows are the rows of the product, the tokens its columns.
 // Four threads fill the ring, every fourth stage each: waiting for a place and starting the copies takes one of them 0.3 us, in
 // which HBM delivers 12 KB to an SM.
-constexpr int kLoaders = 4, kLoader = kWarps, kIssuer = kWarps + kLoaders;
-constexpr int kTcThreads = kThreads + 32 * (kLoaders + 1);      // eight warps for routing and results
-constexpr int kMostStages = 5;
+constexpr int kLoaders = 4, kIssuer = kWarps, kLoader = kWarps + 1;
+constexpr int kTcThreads = kThreads + 32 * (1 + kLoaders);      // eight warps for routing and results
 // Two column blocks a stage, as far as there are two: handing a stage over costs the multiplying thread 0.2 us, as long as half a
 // stage of weights takes to arrive.
 constexpr int kPair = 2;
 template <int N> struct Tc {
-    static constexpr int kTokens = kPair * kBlockBytes;           // where a stage's rows of tokens begin
+    static constexpr int kTokens = kPair * kBlockBytes;            // where a stage's rows of tokens begin
     static constexpr int kStage = kPair * (kBlockBytes + N * 128);
-    static constexpr int kStages = N == 16 ? 5 : 5;
-    static constexpr int kTmemCols = 2 * N;      // two accumulators: one is drained while the next is summed up
-    static constexpr size_t kSmem = 1024 + (size_t)kStages * kStage;
 };
+constexpr int kTcStages = 5;
+template <int N> constexpr size_t kTcSmem = 1024 + (size_t)kTcStages * Tc<N>::kStage;
+// A loading thread that waits for a place has seen the one `loaders` stages ahead of its own emptied; it must not be two fills
+// ahead of it, which the one bit of a barrier's phase cannot tell from none.
+static_assert(kTcStages >= kLoaders, "stages per loading thread");
 
 struct Ring {
-    unsigned long long full[kMostStages], empty[kMostStages], acc_full[2], acc_empty[2];
+    unsigned long long full[kTcStages], empty[kTcStages], acc_full[2], acc_empty[2];
     uint32_t tmem;
     int abort_flag;
 };
@@ -284,7 +271,7 @@ struct Place {                                   // of a role in a ring of `n`
 template <int N> __device__ __forceinline__ void tc_begin(Ring &ring, int fills)
 {
     if (threadIdx.x == 0) {
-        for (int i = 0; i < Tc<N>::kStages; ++i) {
+        for (int i = 0; i < kTcStages; ++i) {
             mbar_init(smem_u32(&ring.full[i]), fills);
             mbar_init(smem_u32(&ring.empty[i]), 1);
         }
@@ -297,7 +284,7 @@ template <int N> __device__ __forceinline__ void tc_begin(Ring &ring, int fills)
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (threadIdx.x >> 5 == kIssuer) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ring.tmem)), "r"(Tc<N>::kTmemCols) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ring.tmem)), "r"(2 * N) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -311,7 +298,7 @@ template <int N> __device__ __forceinline__ void tc_end(const Ring &ring)
     __syncthreads();
     if (threadIdx.x >> 5 == kIssuer) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(ring.tmem), "r"(Tc<N>::kTmemCols) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(ring.tmem), "r"(2 * N) : "memory");
     }
 }
 
@@ -396,7 +383,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) decode_up_many(const __grid_con
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int k = p.m.k, blocks = p.m.d / 64;
+    if (threadIdx.x == 0) {
+        prefetch(maps.gate64);
+        prefetch(maps.up64);
+    }
     tc_begin<N>(ring, 2);
+    fetch_router(p, 2 * p.m.d);
     wait_for_earlier_kernels();
     allow_next_kernel();
     if (warp < kWarps) {
@@ -410,19 +402,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) decode_up_many(const __grid_con
     __syncthreads();
     const WaitCtx wc{&ring.abort_flag, p.status, p.wait_limit_ns};
     int all = 0;
-    for (int s = 0; s < r.met; ++s) all += (p.m.hoff[r.expert[s] + 1] - p.m.hoff[r.expert[s]]) / kManyCols;
-    const int begin = (int)((long long)all * blockIdx.x / gridDim.x), end = (int)((long long)all * (blockIdx.x + 1) / gridDim.x);
-    Place st(Tc<N>::kStages), acc(2);
+    for (int s = 0; s < r.met; ++s) all += r.width[s] / kManyCols;
+    int begin, end;
+    share_of(all, begin, end);
+    Place st(kTcStages), acc(2);
     int s = 0, base = 0;                         // the expert that unit u lies in, units ahead of it
     auto settle = [&](int u) {
         while (true) {
-            const int units = (p.m.hoff[r.expert[s] + 1] - p.m.hoff[r.expert[s]]) / kManyCols;
+            const int units = r.width[s] / kManyCols;
             if (u - base < units) return (u - base) * kManyCols;
             base += units;
             ++s;
         }
     };
-    if (warp >= kLoader && warp < kIssuer) {
+    if (warp >= kLoader) {
         // The weights come by TMA, the rows of x by the loading warp's lanes: 16 bytes a lane and piece, swizzled as TMA would (its
         // row gather takes 0.25 us for four rows).  The next stage's pieces are requested before this one's place is waited for.
         constexpr int P = N / 4;                 // pieces of a lane and column block: rows lane / 8 + 4 j
@@ -464,7 +457,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) decode_up_many(const __grid_con
             const uint32_t bar = smem_u32(&ring.full[st.at]), to = stages + st.at * Tc<N>::kStage;
             const int n = min(kPair, blocks - kPair * b);
             if (lane == 0) {
-                const int first = p.m.hoff[r.expert[s]] + c0;
+                const int first = r.offset[s] + c0;
                 mbar_arrive_expect_tx(bar, n * kBlockBytes);
                 for (int c = 0; c < n; ++c) {
                     tma_load_2d(to + c * kBlockBytes, &maps.gate64, bar, (kPair * b + c) * 64, first);
@@ -518,6 +511,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) decode_up_many(const __grid_con
 }
 
 // ---- second kernel ----
+// `share` blocks take the column blocks of all experts met, one after the other, of a group of rows in turn: what they ask for
+// at a time lies side by side.
+struct DownShare {
+    int groups, share, member, first, step;      // the block's groups: first, first + step, ..
+    __device__ __forceinline__ DownShare(int d, int per)
+    {
+        groups = (d + kGroupRows - 1) / kGroupRows;
+        share = max(1, min((int)gridDim.x / groups, per / 2));
+        step = max(1, (int)gridDim.x / share);
+        member = blockIdx.x % share;
+        first = (int)blockIdx.x / share < step ? (int)blockIdx.x / share : groups;
+    }
+    // the first of the column blocks from `upto` on that is the block's
+    __device__ __forceinline__ int from(int upto) const { return upto + (member - upto % share + share) % share; }
+};
+
 template <int N>
 __global__ void __launch_bounds__(kTcThreads, 1) decode_down_tma(const __grid_constant__ DecodeArgs p, const __grid_constant__ Maps maps)
 {
@@ -529,6 +538,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) decode_down_tma(const __grid_co
     __shared__ int last;
     const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
+    if (tid == 0) {
+        prefetch(maps.down);
+        prefetch(maps.hidden);
+    }
     tc_begin<N>(ring, 1);
     wait_for_earlier_kernels();
     allow_next_kernel();
@@ -536,27 +549,25 @@ __global__ void __launch_bounds__(kTcThreads, 1) decode_down_tma(const __grid_co
     __syncthreads();
     if (tid <= r.met) {
         int n = 0;
-        for (int s = 0; s < tid; ++s) n += (p.m.hoff[r.expert[s] + 1] - p.m.hoff[r.expert[s]]) / 64;
+        for (int s = 0; s < tid; ++s) n += r.width[s] / 64;
         upto[tid] = n;
     }
     __syncthreads();
-    const int per = upto[r.met], groups = (p.m.d + kGroupRows - 1) / kGroupRows;
-    // `share` blocks a group of rows, which take its column blocks in turn: what they ask for at a time lies side by side
-    const int share = max(1, min((int)gridDim.x / groups, per / 2)), step = max(1, (int)gridDim.x / share), member = blockIdx.x % share;
+    const DownShare mine(p.m.d, upto[r.met]);
+    const int groups = mine.groups, share = mine.share, step = mine.step, member = mine.member, first_group = mine.first;
     const WaitCtx wc{&ring.abort_flag, p.status, p.wait_limit_ns};
-    Place st(Tc<N>::kStages), acc(2);
-    const int first_group = (int)blockIdx.x / share < step ? (int)blockIdx.x / share : groups;
-    // the block's column blocks of expert s: from upto[s] on the first that is `member` modulo `share`
-    auto first_of = [&](int s) { return upto[s] + (member - upto[s] % share + share) % share; };
+    Place st(kTcStages), acc(2);
+    // the block's column blocks of expert s
+    auto first_of = [&](int s) { return mine.from(upto[s]); };
     auto length_of = [&](int s) { return (upto[s + 1] - first_of(s) + share - 1) / share; };      // 0 or less: none
-    if (warp >= kLoader && warp < kIssuer) {
+    if (warp >= kLoader) {
         if (lane == 0) {
             bool ok = true;
             int issued = 0, turn = warp - kLoader;       // the next of an expert's stages that is this thread's
             st.skip(turn);
             for (int group = first_group; ok && group < groups; group += step)
                 for (int s = 0; ok && s < r.met; ++s) {
-                    const int first = first_of(s), n = length_of(s), boxes = (r.first[s + 1] - r.first[s] + 15) / 16, col0 = p.m.hoff[r.expert[s]];
+                    const int first = first_of(s), n = length_of(s), boxes = (r.first[s + 1] - r.first[s] + 15) / 16, col0 = r.offset[s];
                     const int pairs = (max(n, 0) + kPair - 1) / kPair;
                     for (; turn < pairs; turn += kLoaders) {
                         if (!mbar_wait(smem_u32(&ring.empty[st.at]), st.phase ^ 1u, wc)) { ok = false; break; }
@@ -635,37 +646,33 @@ template <typename K>
 cudaError_t allow_smem(K kern, size_t bytes, unsigned long long &done)
 {
     int dev = 0;
-    const cudaError_t e = cudaGetDevice(&dev);
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev <= 63 && ((done >> dev) & 1ull)) return cudaSuccess;      // a bit a device; those beyond 63 set it every time
-    if (dev <= 63) done |= 1ull << dev;
-    return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess && dev <= 63) done |= 1ull << dev;
+    return e;
 }
 
 // One group of eight tokens: the first kernel on mma.sync, whose small units go round the SMs evenly; more: on tcgen05.
 constexpr int kFewTokens = 8;
 
-cudaError_t launch_up_few(DecodeArgs &a, const Maps &maps, int blocks, cudaStream_t s)
-{
-    constexpr size_t bytes = kSmemMost - sizeof(UpShared<1>);
-    static unsigned long long done = 0;
-    a.x_room = (int)(bytes - 1024 - kUpRing);
-    const cudaError_t e = allow_smem(decode_up_tma<1>, bytes, done);
-    return e != cudaSuccess ? e : launch_overlapped(decode_up_tma<1>, blocks, kThreads, bytes, s, a, maps);
-}
 template <int N>
 cudaError_t launch(DecodeArgs &a, const Maps &maps, int blocks, cudaStream_t s)
 {
-    static unsigned long long done_up = 0, done_down = 0;
-    cudaError_t e = cudaSuccess;
-    if (a.T <= kFewTokens) {
-        e = launch_up_few(a, maps, blocks, s);
+    static unsigned long long done_few = 0, done_up = 0, done_down = 0;
+    cudaError_t e = allow_smem(decode_down_tma<N>, kTcSmem<N>, done_down);
+    if (e != cudaSuccess) return e;
+    if (N == 16 && a.T <= kFewTokens) {
+        constexpr size_t most = kSmemMost - sizeof(UpShared);
+        a.x_room = (int)(most - 1024 - kUpRing);
+        e = allow_smem(decode_up_few, most, done_few);
+        if (e == cudaSuccess) e = launch_overlapped(decode_up_few, blocks, kThreads, most, s, a, maps);
     } else {
-        e = allow_smem(decode_up_many<N>, Tc<N>::kSmem, done_up);
-        if (e == cudaSuccess) e = launch_overlapped(decode_up_many<N>, blocks, kTcThreads, Tc<N>::kSmem, s, a, maps);
+        e = allow_smem(decode_up_many<N>, kTcSmem<N>, done_up);
+        if (e == cudaSuccess) e = launch_overlapped(decode_up_many<N>, blocks, kTcThreads, kTcSmem<N>, s, a, maps);
     }
-    if (e == cudaSuccess) e = allow_smem(decode_down_tma<N>, Tc<N>::kSmem, done_down);
-    return e != cudaSuccess ? e : launch_overlapped(decode_down_tma<N>, blocks, kTcThreads, Tc<N>::kSmem, s, a, maps);
+    return e != cudaSuccess ? e : launch_overlapped(decode_down_tma<N>, blocks, kTcThreads, kTcSmem<N>, s, a, maps);
 }
 
 }  // namespace
