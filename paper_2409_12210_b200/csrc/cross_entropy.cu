@@ -8,6 +8,10 @@
 // Gradient: the logits are formed again, a piece of the vocabulary at a time, and leave the product as dz in bf16
 // (DenseSoftmax); dx and dw of the piece follow as one launch, dx on top of the sum of the pieces before (DenseSum).  That
 // is 8 T d V operations with the forward's 2, against 6 of a form that keeps T x V logits.
+//
+// dz is rounded to bf16 once, because the products read 16-bit operands.  A factor that all rows share - the 1 / count of a
+// mean - would be rounded with it, by the same amount everywhere (0.0033 off in norm where the count was 7372, 0.0023 without), so
+// rows enter with their weight over the largest one and the rest multiplies the sums in fp32.
 #include <algorithm>
 
 #include "dense_gemm.h"
@@ -120,6 +124,7 @@ struct FactorArgs {
     TokenIds labels;
     const float *lse, *dloss, *total;
     float *lse2, *factor;
+    float *scalars;          // 1 / the largest factor, and what the sums are multiplied by: scale / total[1] times the largest factor
     int *head;               // status word and counters of the products that follow
     float scale;
     int n, vocabulary;
@@ -129,36 +134,84 @@ constexpr int kFactorThreads = 1024;
 __global__ void __launch_bounds__(kFactorThreads) loss_factor_kernel(const FactorArgs p)
 {
     __shared__ int bad;
+    __shared__ float most[32];
     if (threadIdx.x == 0) bad = 0;
     wait_for_earlier_kernels();
     allow_next_kernel();
+    auto factor_of = [&](long long label, long long t) {
+        return label >= 0 && label < p.vocabulary ? (p.dloss ? __ldcg(p.dloss + t) : 1.f) : 0.f;
+    };
     const long long t = (long long)blockIdx.x * kFactorThreads + threadIdx.x;
     if (t < p.n) {
-        const long long label = p.labels.at(t);
-        float f = 0.f;
-        if (label >= 0 && label < p.vocabulary) {
-            f = p.scale;
-            if (p.dloss) f *= __ldcg(p.dloss + t);
-            if (p.total) f /= __ldcg(p.total + 1);
-        }
-        p.factor[t] = f;
+        p.factor[t] = factor_of(p.labels.at(t), t);
         p.lse2[t] = __ldcg(p.lse + t) * kLog2e;
     }
     if (blockIdx.x != 0) return;
-    // the first block clears the head and, having looked at all labels, says whether one lies past the vocabulary
+    // the first block clears the head and, having looked at all rows, says whether a label lies past the vocabulary and how
+    // large the largest factor is
     for (int i = threadIdx.x; i < (int)(kDenseZeroBytes / 4); i += kFactorThreads) p.head[i] = 0;
     __syncthreads();
+    float m = 0.f;
     for (long long t0 = threadIdx.x; t0 < p.n; t0 += 8 * kFactorThreads) {
+        long long label[8];
         bool past = false;
 #pragma unroll
+        for (int u = 0; u < 8; ++u) label[u] = t0 + u * kFactorThreads < p.n ? p.labels.at(t0 + u * kFactorThreads) : -1;
+#pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const long long i = t0 + u * kFactorThreads;
-            past |= (i < p.n ? p.labels.at(i) : -1) >= p.vocabulary;
+            past |= label[u] >= p.vocabulary;
+            const float f = fabsf(factor_of(label[u], t0 + u * kFactorThreads));
+            if (f < INFINITY) m = fmaxf(m, f);           // an infinity or a NaN is no measure for the others
         }
         if (past) bad = 1;
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = m;
     __syncthreads();
-    if (threadIdx.x == 0 && bad) p.head[0] = kDevBounds;
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 32; ++w) m = fmaxf(m, most[w]);
+        if (bad) p.head[0] = kDevBounds;
+        // (below 2^-126 the quotient would be infinite; without a row that counts nothing is multiplied, by no count either)
+        const bool some = m >= 1.17549435e-38f;
+        const float rest = p.total ? p.scale / __ldcg(p.total + 1) : p.scale;
+        p.scalars[0] = some ? 1.f / m : 1.f;
+        p.scalars[1] = some ? rest * m : m == 0.f ? 0.f : rest;
+    }
+}
+
+// dx = gain times the sum of `parts` running sums (see dense_sum_bytes), where dx was summed up in parts.
+__global__ void __launch_bounds__(256) loss_join_kernel(const float *sums, long long part_floats, int parts, const float *gain, __nv_bfloat16 *dx,
+                                                        int n, int d)
+{
+    wait_for_earlier_kernels();
+    allow_next_kernel();
+    const int lane = threadIdx.x & 31, across = (d + 31) / 32;
+    const long long block = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (block >= (long long)((n + 31) / 32) * across) return;
+    const float g = __ldcg(gain);
+    const int r = (int)(block / across) * 32 + lane, c0 = (int)(block % across) * 32;
+    float4 v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int q = 0; q < parts; ++q) {
+        const float4 *at = reinterpret_cast<const float4 *>(sums + q * part_floats + block * 1024) + lane;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float4 u = __ldcg(at + 32 * j);
+            v[j].x += u.x; v[j].y += u.y; v[j].z += u.z; v[j].w += u.w;
+        }
+    }
+    if (r >= n) return;
+    auto pack = [g](float a, float b) {
+        __nv_bfloat162 t = __floats2bfloat162_rn(a * g, b * g);
+        return *reinterpret_cast<uint32_t *>(&t);
+    };
+#pragma unroll
+    for (int j = 0; j < 8; j += 2)
+        if (c0 + 4 * j < d)                              // (d is a multiple of 8)
+            *reinterpret_cast<uint4 *>(dx + (size_t)r * d + c0 + 4 * j) =
+                make_uint4(pack(v[j].x, v[j].y), pack(v[j].z, v[j].w), pack(v[j + 1].x, v[j + 1].y), pack(v[j + 1].z, v[j + 1].w));
 }
 
 // ---- host ----
@@ -198,8 +251,8 @@ ForwardLayout forward_layout(int n, int d, int vocabulary)
     return L;
 }
 
-// dx = dz w and dw = dz^T x of a piece of the vocabulary
-DenseItem dx_item(int n, int d, int cols, int ld, const void *dz, const void *w, void *dx, float *sum, bool add, bool keep)
+// dx = dz w of a piece of the vocabulary (or of a part of its columns), on top of `sum` or into it, and dw = dz^T x
+DenseItem dx_item(int n, int d, int cols, int ld, const void *dz, const void *w, void *dx, float *sum, bool add, bool keep, const float *gain)
 {
     DenseItem it{};
     it.a = {dz, n, cols, ld};
@@ -211,10 +264,11 @@ DenseItem dx_item(int n, int d, int cols, int ld, const void *dz, const void *w,
     it.p.out0 = dx;
     it.p.out1 = sum;
     it.p.ld_out = d;
+    it.p.gain = gain;
     it.k = cols;
     return it;
 }
-DenseItem dw_item(int n, int d, int cols, int ld, const void *dz, const void *x, void *dw)
+DenseItem dw_item(int n, int d, int cols, int ld, const void *dz, const void *x, void *dw, const float *gain)
 {
     DenseItem it{};
     it.a = {dz, n, cols, ld};
@@ -224,6 +278,7 @@ DenseItem dw_item(int n, int d, int cols, int ld, const void *dz, const void *x,
     it.p.flags = kDenseAMn | kDenseBMn;
     it.p.out0 = dw;
     it.p.ld_out = d;
+    it.p.gain = gain;
     it.k = n;
     return it;
 }
@@ -239,36 +294,60 @@ int piece_cols(int n, int vocabulary)
 }
 int up64(int v) { return (v + 63) / 64 * 64; }
 
-// One launch for both products unless dx's few long tiles would outlast all the others: then dx is cut along the vocabulary
-// in a launch of its own.
-bool together(int n, int d, int cols)
+// Parts into which dx's contraction over a piece's columns is cut, each with a running sum of its own: as many as keep one of its
+// tiles below a quarter of what a CTA pair has to do in all (2051 x 1536 over pieces of 25088: 54 tiles of 392 k-blocks beside 588 of
+// 33; in one part 333 us a piece, in four JOINED), but not below 24 k-blocks.
+int parts_of(int n, int d, int cols)
 {
     const long long tn = (n + 255) / 256, td = (d + 255) / 256, tv = (cols + 255) / 256, kn = (n + 63) / 64, kv = (cols + 63) / 64;
-    return kv * (kDenseSms / 2) <= tn * td * kv + tv * td * kn;
+    const long long each = (tn * td * kv + tv * td * kn) / (kDenseSms / 2);
+    int parts = 1;
+    while (2 * parts < kDenseMaxSums && kv * 4 > each * parts && kv >= 48 * parts) parts *= 2;
+    return parts;
+}
+int part_cols(int cols, int parts) { return up64((cols + parts - 1) / parts); }
+
+// The products of one piece; *n_dx is how many of them are parts of dx.
+int piece_items(DenseItem *items, int n, int d, int cols, int ld, int parts, unsigned char *dz, const unsigned char *w, const void *x, void *dx,
+                void *dw, float *sums, size_t part_floats, bool add, bool keep, const float *gain, int *n_dx)
+{
+    int c = 0;
+    if (dx) {
+        const int each = part_cols(cols, parts);
+        for (int at = 0; at < cols; at += each, ++c)
+            items[c] = dx_item(n, d, std::min(each, cols - at), ld, dz + (size_t)at * 2, w + (size_t)at * d * 2, dx, sums + c * part_floats, add, keep, gain);
+    }
+    *n_dx = c;
+    if (dw) items[c++] = dw_item(n, d, cols, ld, dz, x, dw, gain);
+    return c;
 }
 
-struct BackwardLayout { size_t partials, partial_bytes, lse2, factor, dz, sum, total; int cols; };
+struct BackwardLayout { size_t partials, partial_bytes, scalars, lse2, factor, dz, sum, total; int cols, parts; };
 BackwardLayout backward_layout(int n, int d, int vocabulary)
 {
     BackwardLayout L;
     L.cols = piece_cols(n, vocabulary);
+    L.parts = parts_of(n, d, L.cols);
     size_t need = 0;
     auto more = [&](const DenseItem *items, int c) { need = std::max(need, dense_partial_bound(DenseBf16, items, c)); };
     // the last piece may be narrower, and the bound does not fall with an extent
     const DenseItem z = logits_item(n, d, L.cols, nullptr, nullptr);
     more(&z, 1);
-    const DenseItem both[2] = {dx_item(n, d, L.cols, up64(L.cols), nullptr, nullptr, nullptr, nullptr, false, false),
-                               dw_item(n, d, L.cols, up64(L.cols), nullptr, nullptr, nullptr)};
-    more(both, 2);
-    more(both, 1);
-    more(both + 1, 1);
+    unsigned char *const some = reinterpret_cast<unsigned char *>(16);
+    DenseItem items[kDenseMaxSums];
+    int n_dx;
+    const int c = piece_items(items, n, d, L.cols, up64(L.cols), L.parts, some, some, some, some, some, nullptr, 0, false, false, nullptr, &n_dx);
+    more(items, c);
+    more(items, n_dx);
+    more(items + n_dx, 1);
     L.partials = kDenseHead;
     L.partial_bytes = need;
-    L.lse2 = up256(L.partials + need);
+    L.scalars = up256(L.partials + need);
+    L.lse2 = L.scalars + 256;
     L.factor = up256(L.lse2 + (size_t)n * 4);
     L.dz = up256(L.factor + (size_t)n * 4);
     L.sum = up256(L.dz + (size_t)n * up64(L.cols) * 2);
-    L.total = L.sum + (L.cols < vocabulary ? dense_sum_bytes(n, d) : 0);
+    L.total = L.sum + (L.cols < vocabulary || L.parts > 1 ? L.parts * dense_sum_bytes(n, d) : 0);
     return L;
 }
 
@@ -353,27 +432,35 @@ modse_status_t modse_cross_entropy_backward(int n_tokens, int d_model, int vocab
     loss.rows = n_tokens;
     loss.lse2 = (float *)(ws + L.lse2);
     loss.factor = (float *)(ws + L.factor);
-    const FactorArgs f{labels, a.lse, a.dloss, a.total, (float *)(ws + L.lse2), (float *)(ws + L.factor), (int *)ws, a.scale,
-                       n_tokens, vocabulary};
+    loss.factor_scale = (float *)(ws + L.scalars);
+    const float *gain = loss.factor_scale + 1;
+    const FactorArgs f{labels, a.lse, a.dloss, a.total, (float *)(ws + L.lse2), (float *)(ws + L.factor), (float *)(ws + L.scalars), (int *)ws,
+                       a.scale, n_tokens, vocabulary};
     MODSE_CUDA(launch_overlapped(loss_factor_kernel, (unsigned)((n_tokens + kFactorThreads - 1) / kFactorThreads), kFactorThreads, 0, s, f));
     float *sum = (float *)(ws + L.sum);
-    void *dz = ws + L.dz;
+    unsigned char *dz = ws + L.dz;
+    const size_t part_floats = dense_sum_bytes(n_tokens, d_model) / 4;
     for (int first = 0; first < vocabulary; first += L.cols) {
         const int cols = std::min(L.cols, vocabulary - first), ld = up64(cols);
         const size_t at = (size_t)first * d_model * 2;
-        const void *w = (const unsigned char *)a.w + at;
+        const unsigned char *w = (const unsigned char *)a.w + at;
         DenseItem z = logits_item(n_tokens, d_model, cols, a.x, w);
         z.p.out0 = dz;
         z.p.ld_out = ld;
         loss.first = first;
         MODSE_CUDA(dense_launch_loss(DenseSoftmax, z, loss, ws, L.partial_bytes, kDenseHeadZero, s));
-        DenseItem items[2];
-        int c = 0;
-        if (a.dx) items[c++] = dx_item(n_tokens, d_model, cols, ld, dz, w, a.dx, sum, first > 0, first + cols < vocabulary);
-        if (a.dw) items[c++] = dw_item(n_tokens, d_model, cols, ld, dz, a.x, (unsigned char *)a.dw + at);
-        const bool one = c < 2 || together(n_tokens, d_model, cols);
-        MODSE_CUDA(dense_launch(DenseSum, DenseBf16, items, one ? c : 1, nullptr, nullptr, ws, L.partial_bytes, kDenseHeadZero, s));
-        if (!one) MODSE_CUDA(dense_launch(DenseSum, DenseBf16, items + 1, 1, nullptr, nullptr, ws, L.partial_bytes, kDenseHeadZero, s));
+        DenseItem items[kDenseMaxSums];
+        int n_dx;
+        const bool keep = L.parts > 1 || first + cols < vocabulary;
+        const int c = piece_items(items, n_tokens, d_model, cols, ld, L.parts, dz, w, a.x, a.dx, a.dw ? (unsigned char *)a.dw + at : nullptr, sum,
+                                  part_floats, first > 0, keep, gain, &n_dx);
+        MODSE_CUDA(dense_launch(DenseSum, DenseBf16, items, c, nullptr, nullptr, ws, L.partial_bytes, kDenseHeadZero, s));
+    }
+    if (a.dx && L.parts > 1) {
+        const int parts = (L.cols + part_cols(L.cols, L.parts) - 1) / part_cols(L.cols, L.parts);
+        const long long blocks = (long long)((n_tokens + 31) / 32) * ((d_model + 31) / 32);
+        MODSE_CUDA(launch_overlapped(loss_join_kernel, (unsigned)((blocks + 7) / 8), 256, 0, s, (const float *)sum, (long long)part_floats, parts, gain,
+                                     (__nv_bfloat16 *)a.dx, n_tokens, d_model));
     }
     return MODSE_OK;
 }

@@ -321,7 +321,7 @@ __device__ __forceinline__ void row_begin(RowState<MODE> &rs, const LossEpilogue
             rs.sum = 0.f;
         } else {
             rs.lse2 = in ? __ldcg(loss.lse2 + r0 + lane) : 0.f;
-            rs.factor = in ? __ldcg(loss.factor + r0 + lane) : 0.f;
+            rs.factor = in ? __ldcg(loss.factor + r0 + lane) * __ldcg(loss.factor_scale) : 0.f;
         }
     }
 }
@@ -454,6 +454,11 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, RowState
 #pragma unroll
             for (int j = 0; j < 8; ++j) __stcg(to + 32 * j, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
         } else {
+            if (q.gain) {
+                const float gain = __ldcg(q.gain);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] *= gain;
+            }
             pack_bf16(v, w);
             tile_out(stg.take(lane), lane, o0, c0, r0, w);
         }
@@ -1234,7 +1239,7 @@ cudaError_t dense_launch(DenseMode mode, DenseType type, const DenseItem *list, 
     case DenseGram: return run(launch_mode<DenseGram, DenseF16, kDenseMaxProblems>);
     case DensePoly: return run(launch_mode<DensePoly, DenseF16, kDenseMaxProblems>);
     case DenseStep: return run(launch_mode<DenseStep, DenseF16, kDenseMaxProblems>);
-    case DenseSum: return run(launch_mode<DenseSum, DenseBf16, 2>);
+    case DenseSum: return run(launch_mode<DenseSum, DenseBf16, kDenseMaxSums>);
     default: return cudaErrorInvalidValue;
     }
 }

@@ -40,6 +40,7 @@ struct DenseProblem {
     const void *in0;
     void *out0, *out1;
     long long ld_in, ld_out; // elements
+    const float *gain;       // DenseSum: what leaves as bf16 is multiplied by this number (null: 1)
 };
 
 struct LinearEpilogue {
@@ -70,7 +71,7 @@ struct LossEpilogue {
     float2 *part;
     float *picked;         // [rows] the label's logit
     int *counter;          // cleared by DenseLse for the kernel behind it
-    const float *lse2, *factor;     // [rows] lse log2(e), factor
+    const float *lse2, *factor, *factor_scale;     // [rows] lse log2(e), factor; and a number that all factors are multiplied by
 };
 constexpr int kDenseLseCols = 128;
 // A running sum of DenseSum: blocks of 32 rows x 32 columns, row by row of blocks, block element (r, c) at
@@ -84,7 +85,7 @@ struct DenseColumnSum {
     int rows, cols;
 };
 
-constexpr int kDenseMaxProblems = 16;
+constexpr int kDenseMaxProblems = 16, kDenseMaxSums = 9;      // of a launch; of one in the mode DenseSum
 // An operand as it lies in memory: rows x cols elements, ld elements from row to row (a multiple of 16 bytes).
 struct DenseOperand {
     const void *base;
