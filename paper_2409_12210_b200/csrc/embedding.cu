@@ -2,7 +2,8 @@
 //
 //   y_t = scale E[id_t];     dE_v = scale sum over t with id_t = v, ascending, of dy_t
 //
-// Both are bound by HBM: a row of the table or of dy is read once, a row of the result written once.
+// Both are bound by HBM: a row of the table or of dy is read once, a row of the result written once.  Lookup of 65536 rows of
+// 2048 bf16 numbers out of 32000: 55 us, 7.3 TB/s, some of the table out of L2.
 //
 // Gradient, two kernels.  Atomic additions would make the result depend on the order of arrival, so the positions are
 // sorted by token first (stable, least significant digit first): one cluster of eight blocks does all passes, each of its
@@ -11,7 +12,8 @@
 // first write zeros into the rows that no token names, which needs no sorted order, so they start beside the sort.  The
 // others each take a chunk of sorted positions and a slab of columns and add up the rows of a token in order; sums of a
 // token whose positions lie in several chunks meet in the workspace, where the block that arrives last adds them in the
-// chunks' order.
+// chunks' order.  16384 rows of dy of 2048 bf16 numbers into 32000 (fp32) rows: 70 us for 329 MB, 4.7 TB/s; about 15 us are
+// the sort, beside which the zeros are written.
 #include <algorithm>
 
 #include "dense_gemm.h"
@@ -220,7 +222,7 @@ sort_kernel(const SortArgs p)
 
 // ---- zeros and sums ----
 constexpr int kSumThreads = 64, kSumCols = 8 * kSumThreads, kSumFlight = 8, kMaxChunk = 128, kJoinFlight = 8;
-constexpr int kFillBits = 65536;
+constexpr int kFillBits = 65536, kIdFlight = 16;
 
 struct GradArgs {
     TokenIds ids;
@@ -245,15 +247,15 @@ __device__ void fill_rows(const GradArgs &p, int block, unsigned *named)
         const int rows = (int)min((long long)kFillBits, end - v0);
         for (int i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) named[i] = 0;
         __syncthreads();
-        for (long long i0 = threadIdx.x; i0 < p.n; i0 += 8 * blockDim.x) {
-            long long id[8];
+        for (long long i0 = threadIdx.x; i0 < p.n; i0 += kIdFlight * blockDim.x) {
+            long long id[kIdFlight];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < kIdFlight; ++u) {
                 const long long i = i0 + u * blockDim.x;
                 id[u] = i < p.n ? p.ids.at(i) : -1;
             }
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < kIdFlight; ++u) {
                 const unsigned long long r = (unsigned long long)(id[u] - v0);
                 if (r < (unsigned long long)rows) atomicOr(named + (r >> 5), 1u << (r & 31));
             }
@@ -409,10 +411,10 @@ __device__ void sum_rows(const GradArgs &p, int chunk, int slab, int group, SumS
     }
 }
 
-constexpr int kGradThreads = 512, kGroups = kGradThreads / kSumThreads;
+constexpr int kGradThreads = 256, kGroups = kGradThreads / kSumThreads;
 
 template <typename T, typename G>
-__global__ void __launch_bounds__(kGradThreads)
+__global__ void __launch_bounds__(kGradThreads, sizeof(T) == 2 ? 3 : 2)
 embedding_grad_kernel(const GradArgs p)
 {
     __shared__ union {
