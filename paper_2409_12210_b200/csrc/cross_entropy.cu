@@ -4,10 +4,12 @@
 //   dz_t = f_t (exp(z_t - lse_t) - [v = label]);  dx = dz w;  dw = dz^T x
 //
 // Forward: the product's epilogue turns every run of 128 logits of a row into their largest and the sum of exponentials
-// over it (DenseLse), 8 bytes for 256; a second kernel joins the runs of a row.  What bounds it is the product.
+// over it (DenseLse), 8 bytes for 256; a second kernel joins the runs of a row.  What bounds it is the product (16384 x 2048
+// over 32000: 1366 to 1451 us, 1.48 to 1.57 PFLOP/s), and the weights' way from HBM where there are few rows (24: 36 us, 3.6 TB/s).
 // Gradient: the logits are formed again, a piece of the vocabulary at a time, and leave the product as dz in bf16
 // (DenseSoftmax); dx and dw of the piece follow as one launch, dx on top of the sum of the pieces before (DenseSum).  That
-// is 8 T d V operations with the forward's 2, against 6 of a form that keeps T x V logits.
+// is 8 T d V operations with the forward's 2, against 6 of a form that keeps T x V logits.  8192 x 2048 over 32000: 2163 to 2250
+// us, 1.43 to 1.49 PFLOP/s; 2051 x 1536 over 100003: 1551 us, 1.22.
 //
 // dz is rounded to bf16 once, because the products read 16-bit operands.  A factor that all rows share - the 1 / count of a
 // mean - would be rounded with it, by the same amount everywhere (0.0033 off in norm where the count was 7372, 0.0023 without), so
@@ -36,41 +38,50 @@ struct RowsArgs {
     int n, runs, vocabulary;
 };
 
-// 32 rows a block, one a lane; warp w joins an even share of their runs, the first warp the 32 shares.
+// 32 rows a block.  First warp w joins an even share of the runs of all rows, one a lane; then the 32 shares of row w, one a lane.
 __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowsArgs p)
 {
     __shared__ float2 share[32][33];
     __shared__ double2 sum[32];
     __shared__ int last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long t = (long long)blockIdx.x * 32 + lane;
+    const long long row0 = (long long)blockIdx.x * 32;
     wait_for_earlier_kernels();
     allow_next_kernel();
-    // largest first, then the sums brought to it: 2^(m - M) is 0 for a run of nothing and must not meet an infinite sum
-    auto join = [](float2 a, float2 b) {
-        const float m = fmaxf(a.x, b.x);
-        auto to = [m](float2 v) { return v.y == INFINITY ? v.y : v.y * exp2f(v.x - m); };
-        return make_float2(m, to(a) + to(b));
-    };
+    // a sum brought to another largest number: 2^(m - M) is 0 for a run of nothing and must not meet an infinite sum
+    auto to = [](float2 v, float m) { return v.y == INFINITY ? v.y : v.y * exp2f(v.x - m); };
     const int lo = (int)((long long)p.runs * warp / 32), hi = (int)((long long)p.runs * (warp + 1) / 32);
-    float2 v = make_float2(-3.402823466e38f, 0.f);
-    if (t < p.n) {
+    const float2 none = make_float2(-3.402823466e38f, 0.f);
+    float2 v = none;
+    if (row0 + lane < p.n) {
         for (int c0 = lo; c0 < hi; c0 += 8) {
             float2 r[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) r[u] = c0 + u < hi ? __ldcg(p.part + (long long)(c0 + u) * p.n + t) : make_float2(-3.402823466e38f, 0.f);
+            for (int u = 0; u < 8; ++u) r[u] = c0 + u < hi ? __ldcg(p.part + (long long)(c0 + u) * p.n + row0 + lane) : none;
+            float m = v.x;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v = join(v, r[u]);
+            for (int u = 0; u < 8; ++u) m = fmaxf(m, r[u].x);
+            float s = to(v, m);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += to(r[u], m);
+            v = make_float2(m, s);
         }
     }
     share[warp][lane] = v;
     __syncthreads();
-    if (warp == 0) {
+    v = share[lane][warp];
+    float m = v.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    float s = to(v, m);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (lane == 0) {
+        const long long t = row0 + warp;
         float loss = 0.f;
         bool counted = false;
         if (t < p.n) {
-            for (int w = 1; w < 32; ++w) v = join(v, share[w][lane]);
-            const float lse = (v.x + log2f(v.y)) * kLog2;
+            const float lse = (m + log2f(s)) * kLog2;
             const long long label = p.labels.at(t);
             counted = label >= 0 && label < p.vocabulary;
             if (label >= p.vocabulary) atomicMax(p.status, kDevBounds);
@@ -78,43 +89,53 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowsArgs p)
             p.loss[t] = loss;
             p.lse[t] = lse;
         }
-        double s = loss, k = counted ? 1.0 : 0.0;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-            k += __shfl_xor_sync(0xFFFFFFFFu, k, o);
-        }
-        if (lane == 0 && p.total != nullptr) {
-            __stcg(p.sums + blockIdx.x, make_double2(s, k));
-            __threadfence();
-            last = atomicAdd(p.counter, 1) == (int)gridDim.x - 1;
-        }
+        sum[warp] = make_double2(loss, counted ? 1.0 : 0.0);
     }
     if (p.total == nullptr) return;
+    __syncthreads();
+    if (warp == 0) {
+        double a = sum[lane].x, k = sum[lane].y;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+            k += __shfl_xor_sync(0xFFFFFFFFu, k, o);
+        }
+        if (lane == 0) {
+            if (gridDim.x == 1) {
+                p.total[0] = (float)a;
+                p.total[1] = (float)k;
+                last = 0;
+            } else {
+                __stcg(p.sums + blockIdx.x, make_double2(a, k));
+                __threadfence();
+                last = atomicAdd(p.counter, 1) == (int)gridDim.x - 1;
+            }
+        }
+    }
     __syncthreads();
     if (!last) return;
     // whichever block is last, the order of the additions is the same
     __threadfence();
-    double s = 0.0, k = 0.0;
+    double a = 0.0, k = 0.0;
     for (int i = threadIdx.x; i < (int)gridDim.x; i += 1024) {
         const double2 b = __ldcg(p.sums + i);
-        s += b.x;
+        a += b.x;
         k += b.y;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
         k += __shfl_xor_sync(0xFFFFFFFFu, k, o);
     }
-    if (lane == 0) sum[warp] = make_double2(s, k);
+    if (lane == 0) sum[warp] = make_double2(a, k);
     __syncthreads();
     if (threadIdx.x == 0) {
-        s = k = 0.0;
+        a = k = 0.0;
         for (int w = 0; w < 32; ++w) {
-            s += sum[w].x;
+            a += sum[w].x;
             k += sum[w].y;
         }
-        p.total[0] = (float)s;
+        p.total[0] = (float)a;
         p.total[1] = (float)k;
     }
 }
@@ -296,7 +317,7 @@ int up64(int v) { return (v + 63) / 64 * 64; }
 
 // Parts into which dx's contraction over a piece's columns is cut, each with a running sum of its own: as many as keep one of its
 // tiles below a quarter of what a CTA pair has to do in all (2051 x 1536 over pieces of 25088: 54 tiles of 392 k-blocks beside 588 of
-// 33; in one part 333 us a piece, in four JOINED), but not below 24 k-blocks.
+// 33; the whole gradient over four pieces takes 1862 us in one part, 1551 in four), but not below 24 k-blocks.
 int parts_of(int n, int d, int cols)
 {
     const long long tn = (n + 255) / 256, td = (d + 255) / 256, tv = (cols + 255) / 256, kn = (n + 63) / 64, kv = (cols + 63) / 64;
