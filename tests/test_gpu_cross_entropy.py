@@ -395,3 +395,88 @@ def test_wrong_tensors_are_refused():
             call()
     with pytest.raises(TypeError):
         B.cross_entropy(x, w, lab.float(), v, v, ws)
+
+
+@pytest.mark.gpu
+def test_a_vocabulary_past_32_bits():
+    """More than 2^31 elements in w and dw: logits of zero but for the last rows."""
+    from paper_2409_12210_b200 import binding as B
+    T, d, V = 6, 2048, 1_100_003
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w = torch.zeros(V, d, dtype=torch.bfloat16, device="cuda")
+    w[-3:] = torch.randn(3, d, generator=g, device="cuda").bfloat16() * 0.1
+    x = torch.randn(T, d, generator=g, device="cuda").bfloat16()
+    labels = torch.tensor([V - 1, V - 2, V - 3, 0, -1, V - 1], device="cuda")
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    ws, _ = workspace(B.cross_entropy_workspace_bytes(T, d, V))
+    B.cross_entropy(x, w, labels, loss, lse, ws)
+    z = x.double() @ w[-3:].double().T
+    ref = torch.logsumexp(torch.cat([z, torch.full((T, 1), float(np.log(V - 3)), dtype=torch.float64, device="cuda")], 1), 1)
+    own = torch.stack([z[0, 2], z[1, 1], z[2, 0], z[3, 0] * 0, z[4, 0] * 0, z[5, 2]])
+    want = torch.where(labels >= 0, ref - own, 0.0)
+    # logits of at most 30, each off by (d + 8) 2^-23 of a sum of magnitudes below 200
+    assert float((lse.double() - ref).abs().max()) <= 0.06 and float((loss.double() - want).abs().max()) <= 0.1
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    ws, _ = workspace(B.cross_entropy_backward_workspace_bytes(T, d, V))
+    B.cross_entropy_backward(x, w, labels, lse, dx, dw, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    dz = torch.exp(z - ref[:, None]) * (labels >= 0)[:, None]
+    for t, c in ((0, 2), (1, 1), (2, 0), (5, 2)):
+        dz[t, c] -= 1
+    got, exact = dw[-3:].double(), dz.T @ x.double()
+    assert float((got - exact).norm()) <= 0.02 * float(exact.norm())
+    exact = dz @ w[-3:].double()
+    assert float((dx.double() - exact).norm()) <= 0.02 * float(exact.norm())
+    # the row of token 3's label, and one that nobody names: p x summed over the counted rows
+    p0 = torch.exp(-ref) * (labels >= 0)
+    far = dw[V // 2].double()
+    assert float((far - p0 @ x.double()).norm()) <= 0.02 * float(far.norm())
+
+
+@pytest.mark.gpu
+def test_an_expired_wait_is_reported():
+    from paper_2409_12210_b200 import binding as B
+    T, d, V = 40, 64, 300
+    x, w, labels = problem(T, d, V, 7)
+    lab = torch.from_numpy(labels).cuda()
+    loss, lse, dx, dw = torch.empty(T, device="cuda"), torch.zeros(T, device="cuda"), torch.empty_like(x), torch.empty_like(w)
+    ws, _ = workspace(B.cross_entropy_workspace_bytes(T, d, V))
+    wsb, _ = workspace(B.cross_entropy_backward_workspace_bytes(T, d, V))
+    B.debug_set_wait_limit_ms(50)
+    B.debug_skip_tile_loads(6, 0)
+    try:
+        B.cross_entropy(x, w, lab, loss, lse, ws)
+        assert B.check_workspace_status(ws) == B.MODSE_ERR_DEVICE_TIMEOUT
+        B.cross_entropy_backward(x, w, lab, lse, dx, dw, wsb)
+        assert B.check_workspace_status(wsb) == B.MODSE_ERR_DEVICE_TIMEOUT
+    finally:
+        B.debug_skip_tile_loads(-1, -1)
+        B.debug_set_wait_limit_ms(2000)
+    B.cross_entropy(x, w, lab, loss, lse, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    rloss, _, _, e_loss = forward64(x, w, labels)
+    assert bool(((loss.double() - rloss).abs() <= e_loss).all())
+
+
+@pytest.mark.gpu
+def test_a_factor_that_all_rows_share_costs_no_precision():
+    """A mean over 7372 tokens, or weights that are all 1 / 3: the gradient is as exact as that of the sum."""
+    from paper_2409_12210_b200 import binding as B
+    T, d, V = 500, 128, 900
+    x, w, labels = problem(T, d, V, 13)
+    lab = torch.from_numpy(labels).cuda()
+    _, rlse, _, _ = forward64(x, w, labels)
+    ws, _ = workspace(B.cross_entropy_backward_workspace_bytes(T, d, V))
+    z, _ = logits64(x, w)
+    p = torch.exp(z - rlse[:, None])
+    at = np.nonzero(labels >= 0)[0]
+    p[torch.from_numpy(at).cuda(), torch.from_numpy(labels[at]).cuda()] -= 1
+    p *= torch.from_numpy((labels >= 0).astype(np.float64)).cuda()[:, None]
+    third = torch.full((T,), 1 / 3, device="cuda")
+    for kw, f in ((dict(total=torch.tensor([1.0, 7372.0], device="cuda")), 1 / 7372), (dict(dloss=third), float(third[0])), (dict(scale=0.1), float(np.float32(0.1)))):
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        B.cross_entropy_backward(x, w, lab, rlse.float(), dx, dw, ws, **kw)
+        for got, ref in ((dx, f * p @ w.double()), (dw, f * p.T @ x.double())):
+            # dz and the output are rounded to bf16 once each, 2^-8 / sqrt(3) of a typical element at most: together 0.0032, on
+            # average over the positions inside a binade 0.0024; a shared factor's own rounding would come on top, up to 0.0039
+            assert float((got.double() - ref).norm()) <= 0.0028 * float(ref.norm())

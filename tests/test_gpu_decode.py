@@ -318,3 +318,91 @@ def test_wrong_tensors_are_refused():
         big = torch.zeros(33, 64, dtype=BF, device="cuda")
         layer.decode(wr, wg, wu, wd, big, torch.empty_like(big), ws)
     layer.destroy()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [3, 12, 25])
+def test_an_expired_wait_is_reported_and_the_next_call_is_right(T):
+    """One block of the first kernel asks for no weights: nothing is in flight when its warps give up."""
+    from paper_2409_12210_b200 import binding as B
+    p = Problem(256, (128, 384, 192, 320), 2, BF)
+    layer = p.layer()
+    y, ws = torch.empty_like(p.x[:T]), layer.alloc_decode_workspace(BF)
+    good = torch.empty_like(y)
+    layer.decode(*p.w, p.x[:T], good, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    B.debug_set_wait_limit_ms(50)
+    B.debug_skip_tile_loads(7, 0)
+    try:
+        layer.decode(*p.w, p.x[:T], y, ws)
+        assert B.check_workspace_status(ws) == B.MODSE_ERR_DEVICE_TIMEOUT
+    finally:
+        B.debug_skip_tile_loads(-1, -1)
+        B.debug_set_wait_limit_ms(2000)
+    layer.decode(*p.w, p.x[:T], y, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK and torch.equal(y, good)
+    layer.destroy()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 20])
+def test_weights_past_32_bits(T):
+    """An expert whose weights begin behind 2^31 elements of the three matrices."""
+    d, widths = 2048, (1_060_864, 64)
+    p = Problem(d, (64, 64), 1, BF, seed=T)
+    small = p.w
+    S = sum(widths)
+    wg, wu, wd = torch.zeros(S, d, dtype=BF, device="cuda"), torch.zeros(S, d, dtype=BF, device="cuda"), torch.zeros(d, S, dtype=BF, device="cuda")
+    wg[-64:], wu[-64:], wd[:, -64:] = small[1][-64:], small[2][-64:], small[3][:, -64:]
+    wr = torch.zeros(2, d, dtype=BF, device="cuda")
+    wr[1] = p.x[0].sign()
+    x = (p.x.abs() * p.x[0].sign())[:T].contiguous()
+    from paper_2409_12210_b200 import binding as B
+    big, little = B.ModseLayer(d, widths, 1), B.ModseLayer(d, (64, 64), 1)
+    y, ref = torch.empty_like(x), torch.empty_like(x)
+    idx = torch.empty(T, 1, dtype=torch.int32, device="cuda")
+    big.decode(wr, wg, wu, wd, x, y, big.alloc_decode_workspace(BF, T), topk_idx=idx)
+    little.decode(wr, *small[1:], x, ref, little.alloc_decode_workspace(BF, T))
+    assert bool((idx == 1).all())
+    # the same products in runs of other lengths: fp32 sums of 64 terms, then one rounding to bf16
+    assert bool(((y.float() - ref.float()).abs() <= 2.0 ** -7 * ref.float().abs() + 1e-5).all()) and bool(ref.any())
+    big.destroy()
+    little.destroy()
+
+
+# Extents that are multiples of 64: d of one, three and an odd number of column blocks, more experts than a block's own routing
+# takes, experts narrower and wider than others by far, rows of x too long to be held
+BLOCKED = [(64, (64,), 1), (64, (64, 128), 2), (192, (320, 64, 128), 2), (320, (64,) * 9, 2), (128, (64,) * 40, 2), (576, (64, 1984), 1),
+           (8192, (64, 128), 2), (16384, (64, 192), 2), (1088, (704, 64, 128, 960), 1)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,widths,k", BLOCKED)
+def test_layers_of_whole_column_blocks(d, widths, k):
+    p = Problem(d, widths, k, BF, seed=d + len(widths))
+    for T in (1, 3, 8, 9, 16, 17, 32):
+        check(p, T, out_f32=T % 2 == 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("widths", [(64, 128, 192), (64,) * 40])
+def test_second_router_term_of_whole_column_blocks(widths):
+    p = Problem(192, widths, 2, BF, seed=len(widths), noise=(0.7, 1e-6))
+    for T in (1, 8, 10, 32):
+        check(p, T)
+
+
+@pytest.mark.gpu
+def test_tokens_past_the_last_row_are_left_alone():
+    """Fewer tokens than the workspace was sized for, with the hidden rows of an earlier, larger call still in it."""
+    from paper_2409_12210_b200 import binding as B
+    p = Problem(256, (128, 384, 192, 320), 2, BF, seed=3)
+    layer, ws = p.layer(), None
+    ws = layer.alloc_decode_workspace(BF)
+    for T in (32, 5, 20, 1, 32):
+        y, fresh = torch.full((32, p.d), 9.0, dtype=BF, device="cuda"), torch.empty(T, p.d, dtype=BF, device="cuda")
+        layer.decode(*p.w, p.x[:T], y[:T], ws)
+        layer.decode(*p.w, p.x[:T], fresh, layer.alloc_decode_workspace(BF, T))
+        assert torch.equal(y[:T], fresh) and bool((y[T:] == 9).all())
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    layer.destroy()
