@@ -5,7 +5,8 @@
 //
 // Forward: the product's epilogue turns every run of 128 logits of a row into their largest and the sum of exponentials
 // over it (DenseLse), 8 bytes for 256; a second kernel joins the runs of a row.  What bounds it is the product (16384 x 2048
-// over 32000: 1366 to 1451 us, 1.48 to 1.57 PFLOP/s), and the weights' way from HBM where there are few rows (24: 36 us, 3.6 TB/s).
+// over 32000: 1366 to 1451 us, 1.48 to 1.57 PFLOP/s).  Up to 32 rows, which are bound by
+// reading w, go through the kernel in cross_entropy_few.cu instead.
 // Gradient: the logits are formed again, a piece of the vocabulary at a time, and leave the product as dz in bf16
 // (DenseSoftmax); dx and dw of the piece follow as one launch, dx on top of the sum of the pieces before (DenseSum).  That
 // is 8 T d V operations with the forward's 2, against 6 of a form that keeps T x V logits.  8192 x 2048 over 32000: 2163 to 2250
@@ -16,7 +17,7 @@
 // rows enter with their weight over the largest one and the rest multiplies the sums in fp32.
 #include <algorithm>
 
-#include "dense_gemm.h"
+#include "cross_entropy.h"
 #include "launch.h"
 
 namespace modse {
@@ -261,13 +262,15 @@ ForwardLayout forward_layout(int n, int d, int vocabulary)
 {
     ForwardLayout L;
     const DenseItem it = logits_item(n, d, vocabulary, nullptr, nullptr);
-    L.runs = (vocabulary + kDenseLseCols - 1) / kDenseLseCols;
+    const int wide = (vocabulary + kDenseLseCols - 1) / kDenseLseCols, few = few_tiles(vocabulary).count;
+    L.runs = few_takes(n, d, vocabulary) ? few : wide;
     // twice the bound of 128-column tiles holds that of the 256-column ones this product takes
     L.partial_bytes = 2 * dense_partial_bound(DenseBf16, &it, 1);
     L.counter = up256(kDenseHead + L.partial_bytes);
     L.picked = L.counter + 256;
     L.part = up256(L.picked + (size_t)n * 4);
-    L.sums = up256(L.part + (size_t)L.runs * n * 8);
+    // (what holds more rows holds fewer)
+    L.sums = up256(L.part + std::max((size_t)few * std::min(n, kFewRows), (size_t)wide * n) * 8);
     L.total = up256(L.sums + ((size_t)n + 31) / 32 * 16);
     return L;
 }
@@ -415,8 +418,8 @@ modse_status_t modse_cross_entropy(int n_tokens, int d_model, int vocabulary, co
     loss.part = (float2 *)(ws + L.part);
     loss.picked = (float *)(ws + L.picked);
     loss.counter = (int *)(ws + L.counter);
-    MODSE_CUDA(dense_launch_loss(DenseLse, logits_item(n_tokens, d_model, vocabulary, a.x, a.w), loss, ws, L.partial_bytes,
-                                 kDenseHeadRaw, s));
+    if (few_takes(n_tokens, d_model, vocabulary)) MODSE_CUDA(launch_loss_few(n_tokens, d_model, vocabulary, a.x, a.w, loss, (int *)ws, s));
+    else MODSE_CUDA(dense_launch_loss(DenseLse, logits_item(n_tokens, d_model, vocabulary, a.x, a.w), loss, ws, L.partial_bytes, kDenseHeadRaw, s));
     const RowsArgs r{labels, loss.part, loss.picked, a.loss, a.lse, a.total, (double2 *)(ws + L.sums), loss.counter, (int *)ws,
                      n_tokens, L.runs, vocabulary};
     MODSE_CUDA(launch_overlapped(loss_rows_kernel, (unsigned)((n_tokens + 31) / 32), 1024, 0, s, r));

@@ -480,3 +480,56 @@ def test_a_factor_that_all_rows_share_costs_no_precision():
             # dz and the output are rounded to bf16 once each, 2^-8 / sqrt(3) of a typical element at most: together 0.0032, on
             # average over the positions inside a binade 0.0024; a shared factor's own rounding would come on top, up to 0.0039
             assert float((got.double() - ref).norm()) <= 0.0028 * float(ref.norm())
+
+
+# Few rows go through a kernel of their own: tiles of 8 rows of w to 128, one or several a block, the last one cut; one to many
+# column blocks, odd numbers of them and a last one that is cut
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,V", [(8, 1), (64, 9), (72, 1184), (1000, 1185), (192, 18944), (64, 18945), (136, 40003), (4096, 700)])
+def test_forward_of_few_rows(d, V):
+    for T in (1, 2, 15, 16, 17, 32, 33):
+        check_forward(T, d, V, torch.int32 if T % 2 else torch.int64, seed=T)
+
+
+@pytest.mark.gpu
+def test_few_rows_in_the_workspace_of_many():
+    from paper_2409_12210_b200 import binding as B
+    for d, V in ((64, 1184), (256, 3001)):
+        sizes = [B.cross_entropy_workspace_bytes(T, d, V) for T in range(1, 80)]
+        assert sizes == sorted(sizes)
+        x, w, labels = problem(79, d, V, V)
+        lab, (ws, guard) = torch.from_numpy(labels).cuda(), workspace(sizes[-1])
+        rloss, rlse, e_lse, e_loss = forward64(x, w, labels)
+        for T in (79, 20, 64, 1, 33, 32):
+            loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+            B.cross_entropy(x[:T], w, lab[:T], loss, lse, ws)
+            assert bool(((loss.double() - rloss[:T]).abs() <= e_loss[:T]).all()) and bool(((lse.double() - rlse[:T]).abs() <= e_lse[:T]).all())
+        assert bool((guard == 0xA5).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [4, 30])
+def test_an_expired_wait_of_few_rows_is_reported(T):
+    """One tile is not asked for: nothing is in flight when its block gives up."""
+    from paper_2409_12210_b200 import binding as B
+    x, w, labels = problem(T, 640, 40000, 7)
+    lab, (ws, _) = torch.from_numpy(labels).cuda(), workspace(B.cross_entropy_workspace_bytes(T, 640, 40000))
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    B.debug_set_wait_limit_ms(50)
+    B.debug_skip_tile_loads(6, 200)
+    try:
+        B.cross_entropy(x, w, lab, loss, lse, ws)
+        assert B.check_workspace_status(ws) == B.MODSE_ERR_DEVICE_TIMEOUT
+    finally:
+        B.debug_skip_tile_loads(-1, -1)
+        B.debug_set_wait_limit_ms(2000)
+    B.cross_entropy(x, w, lab, loss, lse, ws)
+    rloss, _, _, e_loss = forward64(x, w, labels)
+    assert B.check_workspace_status(ws) == B.MODSE_OK and bool(((loss.double() - rloss).abs() <= e_loss).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,V", [(8192, 300), (5000, 7200), (8192, 7000)])       # long rows: either way, by the tiles' height
+def test_forward_of_few_long_rows(d, V):
+    for T in (1, 32):
+        check_forward(T, d, V, seed=T)
