@@ -155,9 +155,9 @@ struct FactorArgs {
 constexpr int kFactorThreads = 1024;
 __global__ void __launch_bounds__(kFactorThreads) loss_factor_kernel(const FactorArgs p)
 {
-    __shared__ int bad;
+    __shared__ int bad, wild;
     __shared__ float most[32];
-    if (threadIdx.x == 0) bad = 0;
+    if (threadIdx.x == 0) bad = wild = 0;
     wait_for_earlier_kernels();
     allow_next_kernel();
     auto factor_of = [&](long long label, long long t) {
@@ -184,6 +184,7 @@ __global__ void __launch_bounds__(kFactorThreads) loss_factor_kernel(const Facto
             past |= label[u] >= p.vocabulary;
             const float f = fabsf(factor_of(label[u], t0 + u * kFactorThreads));
             if (f < INFINITY) m = fmaxf(m, f);           // an infinity or a NaN is no measure for the others
+            else wild = 1;
         }
         if (past) bad = 1;
     }
@@ -194,11 +195,12 @@ __global__ void __launch_bounds__(kFactorThreads) loss_factor_kernel(const Facto
     if (threadIdx.x == 0) {
         for (int w = 1; w < 32; ++w) m = fmaxf(m, most[w]);
         if (bad) p.head[0] = kDevBounds;
-        // (below 2^-126 the quotient would be infinite; without a row that counts nothing is multiplied, by no count either)
+        // (below 2^-126 the quotient would be infinite; without a row that counts nothing is multiplied, by no count either, unless
+        // an infinity or a NaN is to be seen)
         const bool some = m >= 1.17549435e-38f;
         const float rest = p.total ? p.scale / __ldcg(p.total + 1) : p.scale;
         p.scalars[0] = some ? 1.f / m : 1.f;
-        p.scalars[1] = some ? rest * m : m == 0.f ? 0.f : rest;
+        p.scalars[1] = some ? rest * m : m == 0.f && !wild ? 0.f : rest;
     }
 }
 

@@ -44,7 +44,6 @@ struct DecodeArgs {
     int T, y_f32;
 };
 
-
 // Meeting of the first kThreads threads of a block.
 __device__ __forceinline__ void team_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); }
 
@@ -407,7 +406,6 @@ __device__ __forceinline__ float gated(float gate, float a, float b) { return ga
 // The block that position `at` of a line of `length` positions belongs to, when `blocks` share it evenly.
 __device__ __forceinline__ int owner_of(long long at, long long length, int blocks) { return (int)(((at + 1) * blocks - 1) / length); }
 
-
 // The second kernel's line: for every group of rows of W_down (sixteen, or more) the units of the contraction over all experts met.  The
 // blocks take even spans of it, wherever the cuts fall.
 struct Line {
@@ -423,7 +421,7 @@ struct Line {
 
 // out[token][row], one of `share` blocks' part of the sums of a group of ROWS rows, to y; where there are several it goes to place
 // slot + member of the workspace, and the block that arrives last adds the parts in order.  All threads of the team.
-// second: places beside slot + member that parts 0 of a group take instead (see leave_group).
+// first_slot: the place that part 0 takes instead (negative: none).
 template <int ROWS>
 __device__ __forceinline__ void leave_rows(const DecodeArgs &p, int group, const float *out, int member, int share, long long slot, int *last,
                                            bool f32, long long first_slot = -1)

@@ -471,10 +471,10 @@ GradLayout grad_layout(int n, int d)
 
 cudaError_t launch_sort(const SortArgs &a, cudaStream_t s)
 {
-    const size_t bins = (size_t)1 << a.bits, smem = ((kSortWarps + 2) * bins + kSortWarps) * 4;
-    const cudaError_t e = cudaFuncSetAttribute(sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    return launch_clusters(sort_kernel, kSortBlocks, kSortBlocks, kSortThreads, smem, s, a);
+    auto smem = [](int bits) { return (((kSortWarps + 2) << bits) + kSortWarps) * sizeof(int); };
+    static unsigned long long done = 0;
+    const cudaError_t e = allow_smem(sort_kernel, smem(kSortMaxBits), done);
+    return e != cudaSuccess ? e : launch_clusters(sort_kernel, kSortBlocks, kSortBlocks, kSortThreads, smem(a.bits), s, a);
 }
 
 template <typename T, typename G>

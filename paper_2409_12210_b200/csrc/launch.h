@@ -40,4 +40,17 @@ cudaError_t launch_overlapped(void (*kern)(P...), dim3 grid, dim3 block, size_t 
     return launch_clusters(kern, 1, grid, block, smem, s, args...);
 }
 
+// Lets a kernel have so much dynamic shared memory; `done`: of that kernel, a bit a device (those beyond 63 are asked every time).
+template <typename K>
+cudaError_t allow_smem(K kern, size_t bytes, unsigned long long &done)
+{
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev <= 63 && ((done >> dev) & 1ull)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess && dev <= 63) done |= 1ull << dev;
+    return e;
+}
+
 }  // namespace modse

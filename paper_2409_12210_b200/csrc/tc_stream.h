@@ -168,17 +168,6 @@ inline bool encode_2d(CUtensorMap *map, const void *base, long long rows, long l
     const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
     return encode(map, 2, base, dims, strides, box);
 }
-template <typename K>
-inline cudaError_t allow_smem(K kern, size_t bytes, unsigned long long &done)
-{
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (dev <= 63 && ((done >> dev) & 1ull)) return cudaSuccess;      // a bit a device; those beyond 63 set it every time
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == cudaSuccess && dev <= 63) done |= 1ull << dev;
-    return e;
-}
 
 }  // namespace stream
 }  // namespace modse

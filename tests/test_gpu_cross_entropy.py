@@ -533,3 +533,26 @@ def test_an_expired_wait_of_few_rows_is_reported(T):
 def test_forward_of_few_long_rows(d, V):
     for T in (1, 32):
         check_forward(T, d, V, seed=T)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("weight", [float("inf"), float("nan")])
+def test_a_weight_without_measure_is_seen_where_it_belongs(weight):
+    """One row weighs infinitely much or NaN and the others nothing, or as ever: its own gradient shows it, theirs do not."""
+    from paper_2409_12210_b200 import binding as B
+    T, d, V = 40, 64, 300
+    x, w, labels = problem(T, d, V, 3)
+    labels[:] = np.arange(T) % V
+    lab = torch.from_numpy(labels).cuda()
+    _, rlse, _, _ = forward64(x, w, labels)
+    ws, _ = workspace(B.cross_entropy_backward_workspace_bytes(T, d, V))
+    for others in (0.0, 0.5):
+        dloss = torch.full((T,), others, device="cuda")
+        dloss[7] = weight
+        dx, dw, ref = torch.empty_like(x), torch.empty_like(w), torch.empty_like(x)
+        B.cross_entropy_backward(x, w, lab, rlse.float(), dx, dw, ws, dloss=dloss)
+        assert not bool(torch.isfinite(dx[7]).any()) and not bool(torch.isfinite(dw.float()).any())
+        dloss[7] = 0
+        B.cross_entropy_backward(x, w, lab, rlse.float(), ref, None, ws, dloss=dloss)
+        keep = torch.arange(T, device="cuda") != 7
+        assert torch.equal(dx[keep], ref[keep]) and bool(torch.isfinite(ref.float()).all())
