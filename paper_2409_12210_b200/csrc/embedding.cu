@@ -12,8 +12,8 @@
 // first write zeros into the rows that no token names, which needs no sorted order, so they start beside the sort.  The
 // others each take a chunk of sorted positions and a slab of columns and add up the rows of a token in order; sums of a
 // token whose positions lie in several chunks meet in the workspace, where the block that arrives last adds them in the
-// chunks' order.  16384 rows of dy of 2048 bf16 numbers into 32000 (fp32) rows: 70 us for 329 MB, 4.7 TB/s; about 15 us are
-// the sort, beside which the zeros are written.
+// chunks' order.  16384 rows of dy of 2048 bf16 numbers into 32000 (fp32) rows: 70 us for 329 MB, 4.7 TB/s; the
+// 14 us of the sort are hidden by the zeros.
 #include <algorithm>
 
 #include "dense_gemm.h"
@@ -221,8 +221,8 @@ sort_kernel(const SortArgs p)
 }
 
 // ---- zeros and sums ----
-constexpr int kSumThreads = 64, kSumCols = 8 * kSumThreads, kSumFlight = 8, kMaxChunk = 128, kJoinFlight = 8;
-constexpr int kFillBits = 65536, kIdFlight = 16;
+constexpr int kSumThreads = 64, kSumCols = 8 * kSumThreads, kSumFlight = 8, kMaxChunk = 64, kJoinFlight = 8;
+constexpr int kFillBits = 65536, kIdFlight = 16, kZeroBytes = 8192;
 
 struct GradArgs {
     TokenIds ids;
@@ -235,14 +235,17 @@ struct GradArgs {
     int n, d, vocabulary, chunk, chunks, slabs, fill_blocks, accumulate;
 };
 
-// Zeros into the rows of a range of the vocabulary that no id names.
+// Zeros into the rows of a range of the vocabulary that no id names: bulk copies out of shared memory, which occupy a lane a
+// warp (1000 positions into 32000 x 2048 in fp32, 46 us; by stores of all threads 51, a memset of the same bytes 67).
 template <typename G>
-__device__ void fill_rows(const GradArgs &p, int block, unsigned *named)
+__device__ void fill_rows(const GradArgs &p, int block, unsigned *named, uint4 *zero)
 {
+    for (int i = threadIdx.x; i < kZeroBytes / 16; i += blockDim.x) zero[i] = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     const int per = (p.vocabulary + p.fill_blocks - 1) / p.fill_blocks;
     const long long end = min((long long)p.vocabulary, (long long)per * (block + 1));
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    const int quads = p.d * (int)sizeof(G) / 16;
+    const int bytes = p.d * (int)sizeof(G);
     for (long long v0 = (long long)per * block; v0 < end; v0 += kFillBits) {
         const int rows = (int)min((long long)kFillBits, end - v0);
         for (int i = threadIdx.x; i < (rows + 31) / 32; i += blockDim.x) named[i] = 0;
@@ -261,12 +264,20 @@ __device__ void fill_rows(const GradArgs &p, int block, unsigned *named)
             }
         }
         __syncthreads();
-        for (int r = warp; r < rows; r += warps) {
-            if ((named[r >> 5] >> (r & 31)) & 1u) continue;
-            uint4 *dst = reinterpret_cast<uint4 *>(static_cast<G *>(p.out) + (v0 + r) * p.d);
-            for (int c = lane; c < quads; c += 32) dst[c] = make_uint4(0, 0, 0, 0);
-        }
+        // a warp's first lane asks for its rows, a copy of kZeroBytes zeros after the other
+        if (lane == 0)
+            for (int r = warp; r < rows; r += warps) {
+                if ((named[r >> 5] >> (r & 31)) & 1u) continue;
+                unsigned char *dst = reinterpret_cast<unsigned char *>(static_cast<G *>(p.out) + (v0 + r) * p.d);
+                for (int at = 0; at < bytes; at += kZeroBytes)
+                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;"
+                                 ::"l"(dst + at), "r"(smem_u32(zero)), "r"(min(kZeroBytes, bytes - at)) : "memory");
+            }
         __syncthreads();
+    }
+    if (lane == 0) {
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
 }
 
@@ -418,14 +429,14 @@ __global__ void __launch_bounds__(kGradThreads, sizeof(T) == 2 ? 3 : 2)
 embedding_grad_kernel(const GradArgs p)
 {
     __shared__ union {
-        unsigned named[kFillBits / 32];
+        struct { unsigned named[kFillBits / 32]; uint4 zero[kZeroBytes / 16]; } fill;
         SumShared sum[kGroups];
     } sh;
     // The blocks that write zeros wait for nothing: the sort lets this kernel start when all that came before the sort has
     // completed, and it writes neither the ids nor the result.
     if ((int)blockIdx.x < p.fill_blocks) {
         allow_next_kernel();
-        fill_rows<G>(p, blockIdx.x, sh.named);
+        fill_rows<G>(p, blockIdx.x, sh.fill.named, sh.fill.zero);
         return;
     }
     wait_for_earlier_kernels();
@@ -446,7 +457,8 @@ bool shape_ok(int n, int d, int vocabulary)
 int slabs_of(int d) { return (d + kSumCols - 1) / kSumCols; }
 
 // Positions of a chunk: short ones where there are few positions, so that every SM has rows to read, and at most 512
-// chunks up to 65536 positions: that many parts are added up in a row where all positions hold one token.
+// chunks up to 32768 positions: that many parts are added up in a row where all positions hold one token (65536 rows of 2048:
+// chunks of 64 132 us, of 128 142; if all hold one token, 65536 of 1024 take 215 and 138).
 int chunk_of(int n)
 {
     int c = 8;
@@ -551,8 +563,9 @@ modse_status_t modse_embedding_backward(modse_dtype_t dtype, int n_tokens, int d
     const SortArgs sort{in, (uint2 *)(ws + L.a), (uint2 *)(ws + L.b), (int *)ws, (int *)(ws + L.counters), n_tokens, vocabulary,
                         (bits + passes - 1) / passes, passes, chunks * slabs};
     MODSE_CUDA(launch_sort(sort, s));
-    // two blocks an SM write zeros, at least 16 rows each
-    const int fill = accumulate ? 0 : std::max(1, std::min(2 * device_sms(), vocabulary / 16));
+    // three blocks an SM write zeros, as many as fit while the positions are sorted, at least 16 rows each (5003 positions into
+    // 100003 x 1536 in bf16: one an SM 79 us, two 64 to 71, three 61, four 64, six 65)
+    const int fill = accumulate ? 0 : std::max(1, std::min(3 * device_sms(), vocabulary / 16));
     const GradArgs g{in, (passes & 1) ? sort.a : sort.b, dy, dtable, (float *)(ws + L.part), sort.counters, scale, n_tokens,
                      d_model, vocabulary, chunk, chunks, slabs, fill, accumulate != 0};
     const bool f32 = dtype == MODSE_F32;
