@@ -556,3 +556,23 @@ def test_a_weight_without_measure_is_seen_where_it_belongs(weight):
         B.cross_entropy_backward(x, w, lab, rlse.float(), ref, None, ws, dloss=dloss)
         keep = torch.arange(T, device="cuda") != 7
         assert torch.equal(dx[keep], ref[keep]) and bool(torch.isfinite(ref.float()).all())
+
+
+@pytest.mark.gpu
+def test_forward_of_many_rows_past_32_bits():
+    from paper_2409_12210_b200 import binding as B
+    T, d, V = 300, 2048, 1_050_001
+    g = torch.Generator(device="cuda").manual_seed(4)
+    w = torch.zeros(V, d, dtype=torch.bfloat16, device="cuda")
+    w[-5:] = (torch.randn(5, d, generator=g, device="cuda") * 0.1).bfloat16()
+    x = torch.randn(T, d, generator=g, device="cuda").bfloat16()
+    labels = V - 1 - torch.arange(T, device="cuda") % 5
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    ws, _ = workspace(B.cross_entropy_workspace_bytes(T, d, V))
+    B.cross_entropy(x, w, labels, loss, lse, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    z = x.double() @ w[-5:].double().T
+    ref = torch.logsumexp(torch.cat([z, torch.full((T, 1), float(np.log(V - 5)), dtype=torch.float64, device="cuda")], 1), 1)
+    want = ref - z.gather(1, (labels - (V - 5))[:, None])[:, 0]
+    # a logit is off by (d + 8) 2^-23 of its magnitudes' sum, which is below 200 here, twice; the sum of V / 128 runs by (160 + V / 128) 2^-24
+    assert float((lse.double() - ref).abs().max()) <= 0.06 and float((loss.double() - want).abs().max()) <= 0.1
