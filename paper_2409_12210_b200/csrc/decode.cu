@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(NTM)) decode_up_kernel
 #pragma unroll
         for (int n = 0; n < NTM; ++n) x[n] = p.x + (size_t)(pick[min(8 * n + g, count - 1)] / k) * row + t * 16;
         auto &sums = part[round & 1];
-        dot<T, NTM>((count + 7) / 8, p.w_gate + w, p.w_up + w, x, 0, units, row, sums[warp]);
+        dot<T, NTM>(count, p.w_gate + w, p.w_up + w, x, 0, units, row, sums[warp]);
         __syncthreads();
         if (threadIdx.x < count * kUnitCols) {
             const int i = threadIdx.x / kUnitCols, c = threadIdx.x % kUnitCols;
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(NTM)) decode_down_kern
             for (int n = 0; n < NTM; ++n) x[n] = p.hidden + pick[min(8 * n + g, count - 1)] * p.ld + t * 16;
             auto &sums = part[round & 1];
             const size_t col = (size_t)off * esz + t * 16;
-            dot<T, NTM>((count + 7) / 8, w0 + col, w1 + col, x, max(lo, upto[s]) - upto[s], min(hi, upto[s + 1]) - upto[s], bytes, sums[warp]);
+            dot<T, NTM>(count, w0 + col, w1 + col, x, max(lo, upto[s]) - upto[s], min(hi, upto[s + 1]) - upto[s], bytes, sums[warp]);
             __syncthreads();
             for (int i = tid; i < count * kRows; i += kThreads) {
                 const int q = i / kRows, c = i % kRows;
@@ -174,9 +174,14 @@ cudaError_t launch(const DecodeArgs &a, bool tma, int sms, cudaStream_t s)
         if (e != cudaSuccess) return e;
     }
     if (tma) return launch_tma(a, sms, s);
+    // no more blocks than there is work for if all experts are met
     const int blocks = std::min(kMaxBlocks, blocks_per_sm(NTM) * sms);
-    const cudaError_t e = launch_overlapped(decode_up_kernel<T, NTM>, blocks, kThreads, 0, s, a);
-    return e != cudaSuccess ? e : launch_overlapped(decode_down_kernel<T, NTM>, blocks, kThreads, 0, s, a);
+    long long line = 0;
+    for (int e = 0; e < a.m.N; ++e) line += ((long long)(a.m.hoff[e + 1] - a.m.hoff[e]) * (int)sizeof(T) + kUnit - 1) / kUnit;
+    const int groups = (a.m.d + kRows - 1) / kRows;
+    line = std::max<long long>(groups, line * groups / kLeastSpan);
+    const cudaError_t e = launch_overlapped(decode_up_kernel<T, NTM>, std::min(blocks, a.m.S / kUnitCols), kThreads, 0, s, a);
+    return e != cudaSuccess ? e : launch_overlapped(decode_down_kernel<T, NTM>, (int)std::min<long long>(blocks, line), kThreads, 0, s, a);
 }
 template <typename T>
 cudaError_t launch_tokens(const DecodeArgs &a, bool tma, int sms, cudaStream_t s)
