@@ -26,8 +26,6 @@ namespace {
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-constexpr float kLog2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
-
 // ---- the runs of a row joined ----
 struct RowsArgs {
     TokenIds labels;
@@ -49,8 +47,8 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowsArgs p)
     const long long row0 = (long long)blockIdx.x * 32;
     wait_for_earlier_kernels();
     allow_next_kernel();
-    // a sum brought to another largest number: 2^(m - M) is 0 for a run of nothing and must not meet an infinite sum
-    auto to = [](float2 v, float m) { return v.y == INFINITY ? v.y : v.y * exp2f(v.x - m); };
+    // a sum brought to another largest number: exp(m - M) is 0 for a run of nothing and must not meet an infinite sum
+    auto to = [](float2 v, float m) { return v.y == INFINITY ? v.y : v.y * expf(v.x - m); };
     const int lo = (int)((long long)p.runs * warp / 32), hi = (int)((long long)p.runs * (warp + 1) / 32);
     const float2 none = make_float2(-3.402823466e38f, 0.f);
     float2 v = none;
@@ -82,7 +80,7 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowsArgs p)
         float loss = 0.f;
         bool counted = false;
         if (t < p.n) {
-            const float lse = (m + log2f(s)) * kLog2;
+            const float lse = m + logf(s);
             const long long label = p.labels.at(t);
             counted = label >= 0 && label < p.vocabulary;
             if (label >= p.vocabulary) atomicMax(p.status, kDevBounds);
@@ -144,8 +142,8 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowsArgs p)
 // ---- what a row of the gradient is multiplied by ----
 struct FactorArgs {
     TokenIds labels;
-    const float *lse, *dloss, *total;
-    float *lse2, *factor;
+    const float *dloss, *total;
+    float *factor;
     float *scalars;          // 1 / the largest factor, and what the sums are multiplied by: scale / total[1] times the largest factor
     int *head;               // status word and counters of the products that follow
     float scale;
@@ -164,10 +162,7 @@ __global__ void __launch_bounds__(kFactorThreads) loss_factor_kernel(const Facto
         return label >= 0 && label < p.vocabulary ? (p.dloss ? __ldcg(p.dloss + t) : 1.f) : 0.f;
     };
     const long long t = (long long)blockIdx.x * kFactorThreads + threadIdx.x;
-    if (t < p.n) {
-        p.factor[t] = factor_of(p.labels.at(t), t);
-        p.lse2[t] = __ldcg(p.lse + t) * kLog2e;
-    }
+    if (t < p.n) p.factor[t] = factor_of(p.labels.at(t), t);
     if (blockIdx.x != 0) return;
     // the first block clears the head and, having looked at all rows, says whether a label lies past the vocabulary and how
     // large the largest factor is
@@ -348,7 +343,7 @@ int piece_items(DenseItem *items, int n, int d, int cols, int ld, int parts, uns
     return c;
 }
 
-struct BackwardLayout { size_t partials, partial_bytes, scalars, lse2, factor, dz, sum, total; int cols, parts; };
+struct BackwardLayout { size_t partials, partial_bytes, scalars, factor, dz, sum, total; int cols, parts; };
 BackwardLayout backward_layout(int n, int d, int vocabulary)
 {
     BackwardLayout L;
@@ -369,8 +364,7 @@ BackwardLayout backward_layout(int n, int d, int vocabulary)
     L.partials = kDenseHead;
     L.partial_bytes = need;
     L.scalars = up256(L.partials + need);
-    L.lse2 = L.scalars + 256;
-    L.factor = up256(L.lse2 + (size_t)n * 4);
+    L.factor = L.scalars + 256;
     L.dz = up256(L.factor + (size_t)n * 4);
     L.sum = up256(L.dz + (size_t)n * up64(L.cols) * 2);
     L.total = L.sum + (L.cols < vocabulary || L.parts > 1 ? L.parts * dense_sum_bytes(n, d) : 0);
@@ -456,12 +450,11 @@ modse_status_t modse_cross_entropy_backward(int n_tokens, int d_model, int vocab
     LossEpilogue loss{};
     loss.labels = labels;
     loss.rows = n_tokens;
-    loss.lse2 = (float *)(ws + L.lse2);
+    loss.lse = a.lse;
     loss.factor = (float *)(ws + L.factor);
     loss.factor_scale = (float *)(ws + L.scalars);
     const float *gain = loss.factor_scale + 1;
-    const FactorArgs f{labels, a.lse, a.dloss, a.total, (float *)(ws + L.lse2), (float *)(ws + L.factor), (float *)(ws + L.scalars), (int *)ws,
-                       a.scale, n_tokens, vocabulary};
+    const FactorArgs f{labels, a.dloss, a.total, (float *)(ws + L.factor), (float *)(ws + L.scalars), (int *)ws, a.scale, n_tokens, vocabulary};
     MODSE_CUDA(launch_overlapped(loss_factor_kernel, (unsigned)((n_tokens + kFactorThreads - 1) / kFactorThreads), kFactorThreads, 0, s, f));
     float *sum = (float *)(ws + L.sum);
     unsigned char *dz = ws + L.dz;

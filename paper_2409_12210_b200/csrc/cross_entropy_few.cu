@@ -100,11 +100,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) loss_few_kernel(const __grid_co
                 float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-                // M as LossEpilogue::part has it: one rounded, finite number for all terms and for the logarithm at the end
-                const float m = fmaxf(fminf(top * kLog2e, 3.402823466e38f), -3.402823466e38f);
+                // M as LossEpilogue::part has it
+                const float m = fmaxf(fminf(top, 3.402823466e38f), -3.402823466e38f);
                 float sum = 0.f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum += ex2_approx(fmaf(z[i], kLog2e, -m));
+                for (int i = 0; i < 4; ++i) sum += ex2_approx((z[i] - m) * kLog2e);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
                 if (lane == 0) {

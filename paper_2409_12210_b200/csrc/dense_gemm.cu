@@ -305,7 +305,7 @@ template <> struct RowState<DenseLse> {
     long long label;       // column of the label, negative: none
 };
 template <> struct RowState<DenseSoftmax> {
-    float lse2, factor;
+    float lse, factor;
     long long label;
 };
 constexpr float kLog2e = 1.4426950408889634f;
@@ -320,7 +320,7 @@ __device__ __forceinline__ void row_begin(RowState<MODE> &rs, const LossEpilogue
             rs.top = -3.402823466e38f;
             rs.sum = 0.f;
         } else {
-            rs.lse2 = in ? __ldcg(loss.lse2 + r0 + lane) : 0.f;
+            rs.lse = in ? __ldcg(loss.lse + r0 + lane) : 0.f;
             rs.factor = in ? __ldcg(loss.factor + r0 + lane) * __ldcg(loss.factor_scale) : 0.f;
         }
     }
@@ -399,33 +399,33 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, RowState
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = i < cols ? v[i] : -INFINITY;
         }
-        // 2^(z log2(e) - M): M is rounded, but one and the same for all terms and for the logarithm at the end.  It stays
-        // finite, so that an infinite logit gives an infinite sum, a row of -infinity a sum of zero, and a NaN a NaN.
+        // exp(z - M): M stays finite, so that an infinite logit gives an infinite sum, a row of -infinity a sum of zero, and a
+        // NaN a NaN.
         float top[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) top[i] = v[i];
 #pragma unroll
         for (int i = 4; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], v[i]);
-        const float m = fmaxf(rs.top, fminf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * kLog2e, 3.402823466e38f));
-        f32x2 sum = pack2(rs.sum * ex2_approx(rs.top - m), 0.f);
+        const float m = fmaxf(rs.top, fminf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), 3.402823466e38f));
+        f32x2 sum = pack2(rs.sum * ex2_approx((rs.top - m) * kLog2e), 0.f);
         rs.top = m;
         const f32x2 scale = both(kLog2e), shift = both(-m);
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
             float a, b;
-            unpack2(fma2(pack2(v[i], v[i + 1]), scale, shift), a, b);
+            unpack2(mul2(add2(pack2(v[i], v[i + 1]), shift), scale), a, b);
             sum = add2(sum, pack2(ex2_approx(a), ex2_approx(b)));
         }
         float a, b;
         unpack2(sum, a, b);
         rs.sum = a + b;
     } else if constexpr (MODE == DenseSoftmax) {
-        const f32x2 scale = both(kLog2e), shift = both(-rs.lse2);
+        const f32x2 scale = both(kLog2e), shift = both(-rs.lse);
         const long long at = rs.label - c0;
         const bool here = at >= 0 && at < cols;
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-            unpack2(fma2(pack2(v[i], v[i + 1]), scale, shift), v[i], v[i + 1]);
+            unpack2(mul2(add2(pack2(v[i], v[i + 1]), shift), scale), v[i], v[i + 1]);
             v[i] = ex2_approx(v[i]);
             v[i + 1] = ex2_approx(v[i + 1]);
         }

@@ -63,7 +63,9 @@ struct TokenIds {
 };
 
 // The rows of DenseLse and DenseSoftmax.  DenseLse writes, for run c of 128 columns and row t, part[c * rows + t] =
-// (M, sum over the run of 2^(z log2(e) - M)), M the run's largest z log2(e) (rounded) held to finite numbers.
+// (M, sum over the run of exp(z - M)), M the run's largest logit held to finite numbers.  Both subtract before they multiply
+// by log2(e): a difference from the largest logit is exact where it is small, however large the logits are, while the
+// product's rounding grows with them (1e5 log2(e) is off by up to 2^-8).
 struct LossEpilogue {
     TokenIds labels;
     long long first;       // vocabulary index of column 0
@@ -71,7 +73,7 @@ struct LossEpilogue {
     float2 *part;
     float *picked;         // [rows] the label's logit
     int *counter;          // cleared by DenseLse for the kernel behind it
-    const float *lse2, *factor, *factor_scale;     // [rows] lse log2(e), factor; and a number that all factors are multiplied by
+    const float *lse, *factor, *factor_scale;      // [rows] lse, factor; and a number that all factors are multiplied by
 };
 constexpr int kDenseLseCols = 128;
 // A running sum of DenseSum: blocks of 32 rows x 32 columns, row by row of blocks, block element (r, c) at

@@ -1,0 +1,100 @@
+"""The cross entropy and its gradient over the range of logits that the header promises, against 64 bits.
+
+Rows of x and w with one number that is not zero make logits that are one exact product, whatever order sums take: nothing is
+left but the softmax's own arithmetic.  Bounds.  z - top is rounded once, 2^-24 of it; where the exponential is not all but zero
+(2^-130) it is below 130 / log2 e, and so is its product with log2 e, rounded once more: 2 2^-24 130 of the exponential, whose
+own arithmetic takes 2^-21; the runs add (160 + V / 128) 2^-24, the logarithm 2^-22 of at most 13.  lse and loss are one rounded sum each on
+top, 2^-24 of themselves.  A probability of the gradient is exp(z - lse) of the lse handed over: off by the same of itself."""
+import numpy as np
+import pytest
+
+from test_gpu_cross_entropy import workspace
+
+torch = pytest.importorskip("torch")
+
+U, BF = 2.0 ** -24, 2.0 ** -8
+EXPONENT = 2 * U * 130 + 2.0 ** -21
+
+
+def exact_problem(T, V, size, seed=0, d=8):
+    """Logits x[t, 0] w[v, 0] of magnitudes up to `size`, of either sign."""
+    rng = np.random.default_rng(seed)
+    x, w = torch.zeros(T, d, dtype=torch.bfloat16), torch.zeros(V, d, dtype=torch.bfloat16)
+    x[:, 0] = torch.from_numpy((size ** 0.5 * rng.choice([-1, 1], T)).astype(np.float32)).bfloat16()
+    w[:, 0] = torch.from_numpy((size ** 0.5 * rng.uniform(0.5, 1, V)).astype(np.float32)).bfloat16()
+    return x.cuda(), w.cuda(), torch.from_numpy(rng.integers(0, V, T)).cuda()
+
+
+def forward(x, w, labels):
+    from paper_2409_12210_b200 import binding as B
+    T, d, V = *x.shape, w.shape[0]
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    ws, _ = workspace(B.cross_entropy_workspace_bytes(T, d, V))
+    B.cross_entropy(x, w, labels, loss, lse, ws)
+    assert B.check_workspace_status(ws) == B.MODSE_OK
+    return loss, lse
+
+
+# A few rows and many go through kernels of their own.
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [5, 30, 70, 300])
+@pytest.mark.parametrize("V", [3, 1000])
+@pytest.mark.parametrize("size", [1.0, 200.0, 1e5, 1e7, 1.5e9, 3.1e9, 8657043456.0, 1e20, 1.9e38])
+def test_forward_of_exact_logits(T, V, size):
+    x, w, labels = exact_problem(T, V, size, T + V)
+    z = x.double() @ w.double().T
+    top, at = z.max(1)
+    labels[::2] = at[::2]                            # the right answer, or any other
+    loss, lse = forward(x, w, labels)
+    rlse = torch.logsumexp(z, 1)
+    rloss = rlse - z.gather(1, labels[:, None])[:, 0]
+    e = EXPONENT + (160 + V / 128) * U + 2.0 ** -22 * 13
+    assert bool(((lse.double() - rlse).abs() <= e + U * rlse.abs()).all())
+    assert bool(((loss.double() - rloss).abs() <= e + U * rlse.abs() + U * rloss.abs()).all())
+    # where one word has all the weight, lse is its logit, and so is the loss of another word their distance
+    alone = ((top[:, None] - z) > 110).sum(1) == V - 1
+    assert torch.equal(lse[alone].double(), top.float()[alone].double())
+    assert not bool(loss[alone & (labels == at)].any())
+    assert bool(alone.any()) or size < 1e5 or V > 3      # (among many words the largest number comes more than once)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d", [(1, 8), (24, 200), (70, 200), (500, 1032)])
+def test_a_vocabulary_of_one_word_has_no_loss(T, d):
+    from paper_2409_12210_b200 import binding as B
+    g = torch.Generator(device="cuda").manual_seed(T)
+    for std in (1.0, 15.0):
+        x = (torch.randn(T, d, generator=g, device="cuda") * std).bfloat16()
+        w = torch.randn(1, d, generator=g, device="cuda").bfloat16()
+        labels = torch.zeros(T, dtype=torch.int64, device="cuda")
+        loss, lse = forward(x, w, labels)
+        assert not bool(loss.any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,V", [(5, 3), (40, 1000), (300, 1000), (9000, 9001)])
+@pytest.mark.parametrize("size", [1.0, 200.0, 1e5, 1e7, 1e8, 3.1e9, 1e20])
+def test_gradient_of_exact_logits(T, V, size):
+    """dx alone, against probabilities of the lse handed over; the columns behind the first one are there to be zeros."""
+    from paper_2409_12210_b200 import binding as B
+    x, w, labels = exact_problem(T, V, size, T + V)
+    w[:, 1] = 1.0                                    # x[:, 1] is 0, so that dx[:, 1] is the sum of dz, of moderate terms
+    d = x.shape[1]
+    z = x.double() @ w.double().T
+    _, lse = forward(x, w, labels)
+    top, at = z.max(1)
+    labels[::2] = at[::2]
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    ws, _ = workspace(B.cross_entropy_backward_workspace_bytes(T, d, V))
+    B.cross_entropy_backward(x, w, labels, lse, dx, dw, ws)
+    p = torch.exp(z - lse.double()[:, None])
+    assert float(p.max()) <= 1.0
+    dz = p.scatter_add(1, labels[:, None], torch.full((T, 1), -1.0, dtype=torch.float64, device="cuda"))
+    edz = p * EXPONENT + U * dz.abs()
+    edz = edz + BF * (dz.abs() + edz) + 2.0 ** -126
+    for got, ref, tol in ((dx, dz @ w.double(), edz @ w.double().abs() + (V + 64) * 2.0 ** -23 * (dz.abs() @ w.double().abs())),
+                          (dw, dz.T @ x.double(), edz.T @ x.double().abs() + (T + 64) * 2.0 ** -23 * (dz.abs().T @ x.double().abs()))):
+        assert bool(((got.double() - ref).abs() <= tol + BF * (ref.abs() + tol)).all())
+    # one word has all the weight and is the right one: nothing to learn
+    alone = (((top[:, None] - z) > 130).sum(1) == V - 1) & (labels == at)
+    assert not bool(dx[alone].any())
