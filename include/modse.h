@@ -509,7 +509,9 @@ modse_status_t modse_cross_entropy(int n_tokens, int d_model, int vocabulary, co
  *   f_t = scale dloss_t / total[1]   for counted tokens, 0 for the others.
  * dloss [T] fp32 (NULL: ones), total as forward wrote it (NULL: no division), so that
  * the gradient of the mean loss takes neither arithmetic nor a copy to the host in between.
- * A row whose f is 0 gives nothing, whatever its logits are.  dx [T, d] and dw
+ * A row whose f is 0 gives nothing, whatever its logits are.  No exponential is above 1.  The logits are formed again,
+ * in fp32 sums that may be cut at other places than forward's: an exponential is off by as much of itself as the rounding of
+ * the two sums moves its logit.  dx [T, d] and dw
  * [vocabulary, d] bf16; either may be NULL; both are overwritten and overlap no input.  The
  * logits are formed again, a piece of the vocabulary at a time (the workspace holds one
  * piece's dz: at most 128 MB or 2048 columns, whichever is more; and one to eight sums of

@@ -425,9 +425,11 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, RowState
         const bool here = at >= 0 && at < cols;
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
+            // no probability is above 1: lse comes from logits whose sums were perhaps cut at other places, so that z may be
+            // above it by both roundings, which grow with the logits
             unpack2(mul2(add2(pack2(v[i], v[i + 1]), shift), scale), v[i], v[i + 1]);
-            v[i] = ex2_approx(v[i]);
-            v[i + 1] = ex2_approx(v[i + 1]);
+            v[i] = ex2_approx(min_nan(v[i], 0.f));
+            v[i + 1] = ex2_approx(min_nan(v[i + 1], 0.f));
         }
         if (here) {
 #pragma unroll

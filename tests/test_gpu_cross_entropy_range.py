@@ -98,3 +98,29 @@ def test_gradient_of_exact_logits(T, V, size):
     # one word has all the weight and is the right one: nothing to learn
     alone = (((top[:, None] - z) > 130).sum(1) == V - 1) & (labels == at)
     assert not bool(dx[alone].any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,V", [(8, 2048, 1000), (24, 4096, 1000), (70, 2048, 1), (2051, 4096, 1000), (300, 648, 1)])
+@pytest.mark.parametrize("size", [30.0, 3e5, 3e12])
+def test_no_probability_is_above_one(T, d, V, size):
+    """Logits of 1e5 to 1e26 out of sums that round: forward and backward cut them at different places in some of these shapes.
+    For the word that has all the weight, and is the right one, dz is p - 1, between -1 and 0; dx is that times its row of w."""
+    from paper_2409_12210_b200 import binding as B
+    g = torch.Generator(device="cuda").manual_seed(T + d)
+    x, w = ((torch.randn(n, d, generator=g, device="cuda") * size).bfloat16() for n in (T, V))
+    z = x.double() @ w.double().T
+    top, at = z.max(1)
+    # alone by more than the rounding of any sum
+    S = x.double().abs() @ w.double().abs().T
+    alone = (((top[:, None] - z) > 110 + 2 * (d + 8) * 2.0 ** -23 * S).sum(1) == V - 1)
+    assert bool(alone.any())
+    _, lse = forward(x, w, at)
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    ws, _ = workspace(B.cross_entropy_backward_workspace_bytes(T, d, V))
+    B.cross_entropy_backward(x, w, at, lse, dx, dw, ws)
+    row = w[at].double()
+    dz = (dx.double() * row).sum(1) / row.square().sum(1)
+    assert bool(torch.isfinite(dx.float()).all()) and bool(torch.isfinite(dw.float()).all())
+    # dz and the elements of dx are rounded to bf16 once each
+    assert bool((dz[alone] <= 0).all()) and bool((dz[alone] >= -1 - 2 * BF).all())
