@@ -122,7 +122,8 @@ modse_status_t modse_forward(modse_layer_t *layer, modse_dtype_t dtype, const mo
  * in modse_forward.  topk_idx and topk_gate [T, k] (each may be NULL) receive the routing.
  * Sums are fp32, in an order that does not depend on the run but is not modse_forward's: values agree to
  * rounding, and so do the logits, so that a token whose k-th and k+1-st logits are equal to their last
- * bits may be routed differently (equal logits: the lower index in both).
+ * bits may be routed differently (equal logits: the lower index in both).  A logit that is NaN counts as the largest, the
+ * lower index first: the token's gates and its row of y are NaN (modse_forward may pass such an expert over).
  * The layer object is only read: calls on several streams may share it, with a workspace
  * each (256-byte aligned; its size never falls with n_tokens).  It takes no part in
  * modse_backward, modse_get_routing, stage timing and launch counts.  y overlaps no input.

@@ -200,19 +200,27 @@ __device__ __forceinline__ void router_tile(const DecodeArgs &p, int tile, float
     }
 }
 
-// Larger z first, then the lower index.
-__device__ __forceinline__ void take_better(float v, int i, float &bv, int &bi)
+// Integers in the order of logits: -0 and 0 are equal, and a NaN is larger than any number, so that it is kept and shows in the
+// gates.  (As comparisons of floats, with the questions after a NaN in the chain of selections, 7 tokens through four experts
+// took 45.0 us instead of 44.)
+__device__ __forceinline__ int rank_of(float z)
+{
+    const int bits = __float_as_int(z + 0.f);
+    return isnan(z) ? 0x7FFFFFFF : bits ^ ((bits >> 31) & 0x7FFFFFFF);
+}
+// Larger rank first, then the lower index.
+__device__ __forceinline__ void take_better(int v, int i, int &bv, int &bi)
 {
     if (v > bv || (v == bv && i < bi)) {
         bv = v;
         bi = i;
     }
 }
-__device__ __forceinline__ void warp_best(float &bv, int &bi)
+__device__ __forceinline__ void warp_best(int &bv, int &bi)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-        const float v = __shfl_xor_sync(0xFFFFFFFFu, bv, o);
+        const int v = __shfl_xor_sync(0xFFFFFFFFu, bv, o);
         const int i = __shfl_xor_sync(0xFFFFFFFFu, bi, o);
         take_better(v, i, bv, bi);
     }
@@ -234,7 +242,7 @@ __device__ __forceinline__ void route(const DecodeArgs &p, float *mem, float (&p
     auto gates = [&](int t, int e0, int e1, float z0, float z1) {
         if (k == 1) {
             idx[t] = e0;
-            r.gate[t] = 1.f;
+            r.gate[t] = isnan(z0) ? z0 : 1.f;
         } else {
             const float e = expf(z1 - z0), den = 1.f + e;
             idx[2 * t] = e0;
@@ -243,7 +251,6 @@ __device__ __forceinline__ void route(const DecodeArgs &p, float *mem, float (&p
             r.gate[2 * t + 1] = e / den;
         }
     };
-    // Larger first, then the lower index; a NaN counts as the least of all.
     if (N <= 32) {
         // few experts: a thread a token, which looks at one logit after the other
         if (tid < p.T) {
@@ -257,7 +264,8 @@ __device__ __forceinline__ void route(const DecodeArgs &p, float *mem, float (&p
                 }
                 scale = p.gamma / sqrtf(ss / (float)N + p.eps);
             }
-            float best[2] = {-INFINITY, -INFINITY}, raw[2] = {0.f, 0.f};
+            int best[2] = {0, 0};
+            float raw[2] = {0.f, 0.f};
             int at[2] = {-1, -1};
             for (int e0 = 0; e0 < N; e0 += 8) {
                 float v[8];
@@ -269,7 +277,7 @@ __device__ __forceinline__ void route(const DecodeArgs &p, float *mem, float (&p
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     if (e0 + i >= N) break;
-                    const float c = isnan(v[i]) ? -INFINITY : v[i];
+                    const int c = rank_of(v[i]);
                     const bool top = at[0] < 0 || c > best[0], next = !top && (at[1] < 0 || c > best[1]);
                     best[1] = top ? best[0] : next ? c : best[1];
                     raw[1] = top ? raw[0] : next ? v[i] : raw[1];
@@ -302,12 +310,12 @@ __device__ __forceinline__ void route(const DecodeArgs &p, float *mem, float (&p
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 if (j >= k) break;
-                float bv = -INFINITY;
+                int bv = -0x7FFFFFFF - 1;
                 int bi = 1 << 30;
 #pragma unroll
                 for (int i = 0; i < kPer; ++i) {
                     const int e = lane + 32 * i;
-                    if (e < N && e != at[0]) take_better(isnan(v[i]) ? -INFINITY : v[i], e, bv, bi);
+                    if (e < N && e != at[0]) take_better(rank_of(v[i]), e, bv, bi);
                 }
                 warp_best(bv, bi);
                 at[j] = bi;
