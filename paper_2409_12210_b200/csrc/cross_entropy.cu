@@ -194,8 +194,9 @@ __global__ void __launch_bounds__(kFactorThreads) loss_factor_kernel(const Facto
         // an infinity or a NaN is to be seen)
         const bool some = m >= 1.17549435e-38f;
         const float rest = p.total ? p.scale / __ldcg(p.total + 1) : p.scale;
-        p.scalars[0] = some ? 1.f / m : 1.f;
-        p.scalars[1] = some ? rest * m : m == 0.f && !wild ? 0.f : rest;
+        const float gain = some ? rest * m : m == 0.f && !wild ? 0.f : rest;
+        p.scalars[0] = gain == 0.f ? 0.f : some ? 1.f / m : 1.f;      // (where the gain is 0 no row counts, whatever its logits are)
+        p.scalars[1] = gain;
     }
 }
 

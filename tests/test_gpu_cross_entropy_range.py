@@ -124,3 +124,22 @@ def test_no_probability_is_above_one(T, d, V, size):
     assert bool(torch.isfinite(dx.float()).all()) and bool(torch.isfinite(dw.float()).all())
     # dz and the elements of dx are rounded to bf16 once each
     assert bool((dz[alone] <= 0).all()) and bool((dz[alone] >= -1 - 2 * BF).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [40, 9000])
+def test_a_scale_of_zero_gives_nothing(T):
+    """f is 0 in every row, so that NaN and infinite logits give nothing either."""
+    from paper_2409_12210_b200 import binding as B
+    d, V = 64, 9001
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x, w = torch.randn(T, d, generator=g, device="cuda").bfloat16(), torch.randn(V, d, generator=g, device="cuda").bfloat16()
+    labels = torch.arange(T, device="cuda") % V
+    _, lse = forward(x, w, labels)
+    lse[3], lse[4], lse[5] = float("nan"), float("inf"), float("-inf")
+    ws, _ = workspace(B.cross_entropy_backward_workspace_bytes(T, d, V))
+    total = torch.tensor([1.0, T], device="cuda")
+    for kw in (dict(), dict(total=total), dict(dloss=torch.rand(T, device="cuda"))):
+        dx, dw = torch.ones_like(x), torch.ones_like(w)
+        B.cross_entropy_backward(x, w, labels, lse, dx, dw, ws, scale=0.0, **kw)
+        assert not bool(dx.any()) and not bool(dw.any())
