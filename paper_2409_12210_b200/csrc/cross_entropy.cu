@@ -344,31 +344,55 @@ int piece_items(DenseItem *items, int n, int d, int cols, int ld, int parts, uns
     return c;
 }
 
+// What the products of pieces of `cols` columns, dx in `parts`, can use for tiles that they cut.
+size_t partials_of(int n, int d, int cols, int parts)
+{
+    size_t need = 0;
+    auto more = [&](const DenseItem *items, int c) { need = std::max(need, dense_partial_bound(DenseBf16, items, c)); };
+    // the last piece may be narrower, and the bound does not fall with an extent
+    const DenseItem z = logits_item(n, d, cols, nullptr, nullptr);
+    more(&z, 1);
+    unsigned char *const some = reinterpret_cast<unsigned char *>(16);
+    DenseItem items[kDenseMaxSums];
+    int n_dx;
+    const int c = piece_items(items, n, d, cols, up64(cols), parts, some, some, some, some, some, nullptr, 0, false, false, nullptr, &n_dx);
+    more(items, c);
+    more(items, n_dx);
+    more(items + n_dx, 1);
+    return need;
+}
+
+// More rows are worked off in narrower pieces and fewer parts, so that what a call needs may fall as n grows (2048 columns,
+// 32000 words: 222.7 MB for 2097 rows, 156.3 for 2098).  A workspace for many rows is to serve fewer, so room is made for
+// bounds that do not fall:
+// dz: n rows of the whole vocabulary, or of the widest piece that n makes;
+// sums: parts_of doubles from p to 2 p only where kv 4 > each p, and each >= tn td kv / 74, so 2 p < 592 / (tn td); a sum is at
+// most tn td tiles of 256 KB;
+// pieces of cut tiles: those of products as long as the vocabulary, a sum as many as there can be.
+constexpr size_t kMostSums = (size_t)8 * (kDenseSms / 2) * 256 * 256 * 4;
 struct BackwardLayout { size_t partials, partial_bytes, scalars, factor, dz, sum, total; int cols, parts; };
 BackwardLayout backward_layout(int n, int d, int vocabulary)
 {
     BackwardLayout L;
     L.cols = piece_cols(n, vocabulary);
     L.parts = parts_of(n, d, L.cols);
-    size_t need = 0;
-    auto more = [&](const DenseItem *items, int c) { need = std::max(need, dense_partial_bound(DenseBf16, items, c)); };
-    // the last piece may be narrower, and the bound does not fall with an extent
-    const DenseItem z = logits_item(n, d, L.cols, nullptr, nullptr);
-    more(&z, 1);
-    unsigned char *const some = reinterpret_cast<unsigned char *>(16);
+    int most_parts = 1;
+    while (2 * most_parts < kDenseMaxSums && (vocabulary + 63) / 64 >= 48 * most_parts) most_parts *= 2;
+    const size_t widest = std::max((size_t)n * 2048, ((size_t)1 << 26) + (size_t)n * 255), one = dense_sum_bytes(n, d);
+    const size_t dz = std::min((size_t)n * up64(vocabulary), widest);
+    const size_t sums = L.cols == vocabulary && most_parts == 1 ? 0 : std::max(one, std::min(most_parts * one, kMostSums));
     DenseItem items[kDenseMaxSums];
-    int n_dx;
-    const int c = piece_items(items, n, d, L.cols, up64(L.cols), L.parts, some, some, some, some, some, nullptr, 0, false, false, nullptr, &n_dx);
-    more(items, c);
-    more(items, n_dx);
-    more(items + n_dx, 1);
+    for (int i = 0; i < most_parts; ++i) items[i] = dx_item(n, d, vocabulary, up64(vocabulary), nullptr, nullptr, nullptr, nullptr, false, false, nullptr);
+    items[most_parts] = dw_item(n, d, vocabulary, up64(vocabulary), nullptr, nullptr, nullptr, nullptr);
+    const size_t partials = std::max({partials_of(n, d, vocabulary, 1), dense_partial_bound(DenseBf16, items, most_parts),
+                                      dense_partial_bound(DenseBf16, items, most_parts + 1)});
+    L.partial_bytes = partials_of(n, d, L.cols, L.parts);
     L.partials = kDenseHead;
-    L.partial_bytes = need;
-    L.scalars = up256(L.partials + need);
+    L.scalars = up256(L.partials + partials);
     L.factor = L.scalars + 256;
     L.dz = up256(L.factor + (size_t)n * 4);
-    L.sum = up256(L.dz + (size_t)n * up64(L.cols) * 2);
-    L.total = L.sum + (L.cols < vocabulary || L.parts > 1 ? L.parts * dense_sum_bytes(n, d) : 0);
+    L.sum = up256(L.dz + dz * 2);
+    L.total = L.sum + sums;
     return L;
 }
 

@@ -143,3 +143,38 @@ def test_a_scale_of_zero_gives_nothing(T):
         dx, dw = torch.ones_like(x), torch.ones_like(w)
         B.cross_entropy_backward(x, w, labels, lse, dx, dw, ws, scale=0.0, **kw)
         assert not bool(dx.any()) and not bool(dw.any())
+
+
+# More rows are worked off in narrower pieces, which need less; the sizes do not fall all the same.
+@pytest.mark.parametrize("d,V", [(2048, 32000), (1536, 100003), (64, 9001), (520, 3100), (4096, 1000), (8, 1)])
+def test_workspace_sizes_never_fall_with_the_rows(d, V):
+    from paper_2409_12210_b200 import binding as B, build
+    build.build()
+    rows = list(range(0, 400)) + list(range(400, 9000, 7)) + list(range(9000, 70000, 331)) + [670, 671, 672, 2096, 2097, 2098, 4096]
+    for size in (B.cross_entropy_workspace_bytes, B.cross_entropy_backward_workspace_bytes):
+        sizes = [size(T, d, V) for T in sorted(rows)]
+        assert sizes == sorted(sizes) and sizes[0] > 0
+    # what the header says of the gradient's: a piece's dz and up to eight sums of dx, beside cut tiles and a number a row
+    for T in (1, 300, 2097, 8192, 30000):
+        sums = 8 * ((T + 31) // 32 * 32) * ((d + 31) // 32 * 32) * 4
+        most = 2 * max(2 ** 26 + 255 * T, 2048 * T) + sums + 128 * 2 ** 18 + 4 * T + 2 ** 16
+        assert B.cross_entropy_backward_workspace_bytes(T, d, V) <= most
+
+
+@pytest.mark.gpu
+def test_few_rows_of_the_gradient_in_the_workspace_of_many():
+    from paper_2409_12210_b200 import binding as B
+    d, V, most = 72, 32000, 4096
+    x, w, labels = (t.contiguous() for t in exact_problem(most, V, 200.0, 1, d))
+    _, lse = forward(x, w, labels)
+    ws, guard = workspace(B.cross_entropy_backward_workspace_bytes(most, d, V))
+    for T in (4096, 2097, 2098, 1, 33, 700):
+        own, _ = workspace(B.cross_entropy_backward_workspace_bytes(T, d, V))
+        outs = []
+        for buf in (ws, own):
+            dx, dw = torch.empty_like(x[:T]), torch.empty_like(w)
+            B.cross_entropy_backward(x[:T], w, labels[:T], lse[:T], dx, dw, buf)
+            assert B.check_workspace_status(buf) == B.MODSE_OK
+            outs.append((dx, dw))
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+    assert bool((guard == 0xA5).all())
