@@ -515,7 +515,7 @@ modse_status_t modse_cross_entropy(int n_tokens, int d_model, int vocabulary, co
  * the two sums moves its logit.  dx [T, d] and dw
  * [vocabulary, d] bf16; either may be NULL; both are overwritten and overlap no input.  The
  * logits are formed again, a piece of the vocabulary at a time (the workspace holds one
- * piece's dz: at most 128 MB or 2048 columns, whichever is more; and one to eight sums of
+ * piece's dz: at most 128 MB or 2048 columns, whichever is more, and 255 columns; and one to eight sums of
  * T d fp32 numbers where dx is summed up in several pieces or parts); dz enters the products rounded to bf16 once, sums are
  * fp32.  The workspaces' sizes, forward's and the gradient's, never fall with n_tokens.  */
 typedef struct {

@@ -305,8 +305,8 @@ DenseItem dw_item(int n, int d, int cols, int ld, const void *dz, const void *x,
     return it;
 }
 
-// Columns of a piece: dz of a piece is at most 2^26 elements (128 MB, about what L2 holds) or 2048 columns, whichever is more, the pieces
-// evenly long and whole tiles wide.
+// Columns of a piece: dz of a piece is about 2^26 elements (128 MB, about what L2 holds) or 2048 columns, whichever is more, the pieces
+// evenly long and whole tiles wide, which makes them at most 255 columns wider than that.
 int piece_cols(int n, int vocabulary)
 {
     const long long most = std::max<long long>(2048, (1ll << 26) / std::max(n, 1));
