@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) loss_few_kernel(const __grid_co
 template <int N>
 cudaError_t launch(const FewArgs &a, const CUtensorMap &w, const CUtensorMap &x, cudaStream_t s)
 {
-    static unsigned long long done = 0;
+    static DeviceFlags done;
     const cudaError_t e = allow_smem(loss_few_kernel<N>, kTcSmem<N>, done);
     return e != cudaSuccess ? e : launch_overlapped(loss_few_kernel<N>, std::min(a.tiles, kDenseSms), kTcThreads, kTcSmem<N>, s, a, w, x);
 }

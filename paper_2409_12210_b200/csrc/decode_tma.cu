@@ -498,7 +498,7 @@ constexpr int kFewTokens = 8;
 template <int N>
 cudaError_t launch(DecodeArgs &a, const Maps &maps, int blocks, cudaStream_t s)
 {
-    static unsigned long long done_few = 0, done_up = 0, done_down = 0;
+    static DeviceFlags done_few, done_up, done_down;
     cudaError_t e = allow_smem(decode_down_tma<N>, kTcSmem<N>, done_down);
     if (e != cudaSuccess) return e;
     if (N == 16 && a.T <= kFewTokens) {

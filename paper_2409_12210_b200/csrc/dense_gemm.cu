@@ -1167,15 +1167,9 @@ cudaError_t launch_tn(const DensePlan &pl, const DenseItem *items, int n, const 
     void (*kern)(DenseParams<P>);
     if constexpr (SHARED) kern = dense_gemm_shared<MODE, TYPE, TN, P>;
     else kern = dense_gemm_pair<MODE, TYPE, TN, TALL, P>;
-    static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    static DeviceFlags done;
+    cudaError_t e = allow_smem(kern, kDenseSmem, done);
     if (e != cudaSuccess) return e;
-    if (dev > 63 || !((attr_done >> dev) & 1ull)) {
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDenseSmem);
-        if (e != cudaSuccess) return e;
-        if (dev <= 63) attr_done |= 1ull << dev;
-    }
     if (head == kDenseHeadRaw && !TALL && pl.splits > 1) {      // only cut tiles count arrivals
         e = cudaMemsetAsync(ws, 0, kDenseZeroBytes, s);
         if (e != cudaSuccess) return e;

@@ -484,7 +484,7 @@ GradLayout grad_layout(int n, int d)
 cudaError_t launch_sort(const SortArgs &a, cudaStream_t s)
 {
     auto smem = [](int bits) { return (((kSortWarps + 2) << bits) + kSortWarps) * sizeof(int); };
-    static unsigned long long done = 0;
+    static DeviceFlags done;
     const cudaError_t e = allow_smem(sort_kernel, smem(kSortMaxBits), done);
     return e != cudaSuccess ? e : launch_clusters(sort_kernel, kSortBlocks, kSortBlocks, kSortThreads, smem(a.bits), s, a);
 }

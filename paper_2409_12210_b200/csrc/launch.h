@@ -3,6 +3,8 @@
 
 #include <cuda_runtime.h>
 
+#include "device_flags.h"
+
 namespace modse {
 
 // A kernel launched by launch_overlapped or launch_clusters sets itself up (barriers, tensor memory, address arithmetic)
@@ -40,16 +42,16 @@ cudaError_t launch_overlapped(void (*kern)(P...), dim3 grid, dim3 block, size_t 
     return launch_clusters(kern, 1, grid, block, smem, s, args...);
 }
 
-// Lets a kernel have so much dynamic shared memory; `done`: of that kernel, a bit a device (those beyond 63 are asked every time).
+// Lets a kernel have so much dynamic shared memory; `done`: that kernel's.
 template <typename K>
-cudaError_t allow_smem(K kern, size_t bytes, unsigned long long &done)
+cudaError_t allow_smem(K kern, size_t bytes, DeviceFlags &done)
 {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev <= 63 && ((done >> dev) & 1ull)) return cudaSuccess;
+    if (done.has(dev)) return cudaSuccess;
     e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == cudaSuccess && dev <= 63) done |= 1ull << dev;
+    if (e == cudaSuccess) done.set(dev);
     return e;
 }
 

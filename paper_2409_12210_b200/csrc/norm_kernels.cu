@@ -8,6 +8,8 @@
 // block, VPT vectors each; the choice of (TPR, VPT) is in pick_shape.  All sums are fp32 of fp32 terms.
 #include <cuda_fp8.h>
 
+#include <atomic>
+
 #include "f32x2.h"
 #include "launch.h"
 #include "modse_internal.h"
@@ -491,14 +493,10 @@ cudaError_t launch_bwd_form(const NormBwdArgs &a, int blocks, cudaStream_t s)
     auto kern = add_rms_norm_bwd_kernel<T, TPR, VPT, WEIGHT, SUM>;
     constexpr int threads = TPR == 1024 ? 1024 : kBwdThreads;
     constexpr int smem = TPR == 1024 ? 0 : kBwdThreads * kSlots * 3 * VPT * 8 * (int)sizeof(T);
-    static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    if (smem > 0 && (dev > 63 || !((attr_done >> dev) & 1ull))) {
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static DeviceFlags done;
+    if (smem > 0) {
+        const cudaError_t e = allow_smem(kern, smem, done);
         if (e != cudaSuccess) return e;
-        if (dev <= 63) attr_done |= 1ull << dev;
     }
     return launch_overlapped(kern, blocks, threads, smem, s, a);
 }
@@ -544,13 +542,13 @@ bool norm_shape_ok(int T, int d) { return T >= 0 && T <= (1 << 30) && d >= 8 && 
 
 int device_sms()
 {
-    static int cached[64];                         // by device ordinal; a lost race writes the same value
+    static std::atomic<int> cached[64];            // by device ordinal
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 148;
-    if (dev >= 0 && dev < 64 && cached[dev] > 0) return cached[dev];
-    int n = 0;
+    int n = dev >= 0 && dev < 64 ? cached[dev].load(std::memory_order_relaxed) : 0;
+    if (n > 0) return n;
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 148;
-    if (dev >= 0 && dev < 64) cached[dev] = n;
+    if (dev >= 0 && dev < 64) cached[dev].store(n, std::memory_order_relaxed);
     return n;
 }
 

@@ -396,15 +396,15 @@ template <typename T, bool IN_PLACE>
 cudaError_t launch(const SmallArgs &a, int n, int cluster, size_t smem, cudaStream_t s)
 {
     auto kern = orthogonalize_small_kernel<T, IN_PLACE>;
-    static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
+    static DeviceFlags done;
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if (dev > 63 || !((attr_done >> dev) & 1ull)) {
+    if (!done.has(dev)) {
         e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
-        if (dev <= 63) attr_done |= 1ull << dev;
+        done.set(dev);
     }
     return launch_clusters(kern, cluster, n * cluster, kThreads, smem, s, a);
 }

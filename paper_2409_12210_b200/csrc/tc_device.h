@@ -4,6 +4,8 @@
 
 #include <cuda.h>
 
+#include <atomic>
+
 #include "modse_internal.h"
 
 namespace modse {
@@ -260,13 +262,14 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t
 
 inline EncodeTiledFn get_encode()
 {
-    static EncodeTiledFn fn = nullptr;
+    static std::atomic<EncodeTiledFn> found{nullptr};      // host threads may ask at any time
+    EncodeTiledFn fn = found.load(std::memory_order_relaxed);
     if (fn == nullptr) {
         void *p = nullptr;
         cudaDriverEntryPointQueryResult q;
         if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
             q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<EncodeTiledFn>(p);
+            found.store(fn = reinterpret_cast<EncodeTiledFn>(p), std::memory_order_relaxed);
     }
     return fn;
 }

@@ -66,6 +66,7 @@
 // word and the CTA drains and exits.
 #include <cuda.h>
 
+#include "launch.h"
 #include "tc_device.h"
 #include "tc_gemm.h"
 
@@ -1390,16 +1391,9 @@ cudaError_t launch_one(const TcMaps &maps, const TcParams &prm, int grid, cudaSt
 {
     auto kern = tc_grouped_gemm<KIND, WIDE, VAR, EPI>;
     constexpr size_t smem = smem_bytes<WIDE, EPI>();
-    // the shared-memory attribute of a kernel is set once per process and device
-    static unsigned long long attr_done = 0;      // bit per device ordinal (devices beyond 63 set it every time)
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    static DeviceFlags done;
+    cudaError_t e = allow_smem(kern, smem, done);
     if (e != cudaSuccess) return e;
-    if (dev < 0 || dev > 63 || !((attr_done >> dev) & 1ull)) {
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-        if (dev >= 0 && dev <= 63) attr_done |= 1ull << dev;
-    }
     kern<<<grid, threads_of<EPI>(), smem, s>>>(maps, prm);
     e = cudaGetLastError();
     if (e == cudaSuccess && launches) ++*launches;
@@ -1431,15 +1425,9 @@ cudaError_t launch_pair_one(const TcMaps &maps, const TcParams &prm, int grid, c
 {
     auto kern = tc_grouped_gemm_pair<KIND, VAR, EPI>;
     constexpr size_t smem = pair_smem_bytes<EPI>();
-    static unsigned long long attr_done = 0;
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    static DeviceFlags done;
+    cudaError_t e = allow_smem(kern, smem, done);
     if (e != cudaSuccess) return e;
-    if (dev < 0 || dev > 63 || !((attr_done >> dev) & 1ull)) {
-        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-        if (dev >= 0 && dev <= 63) attr_done |= 1ull << dev;
-    }
     kern<<<grid & ~1, threads_of<EPI>(), smem, s>>>(maps, prm);     // whole clusters of two
     e = cudaGetLastError();
     if (e == cudaSuccess && launches) ++*launches;
