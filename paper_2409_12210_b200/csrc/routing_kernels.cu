@@ -20,6 +20,7 @@
 // No kernel uses a floating-point atomic; every sum has a fixed order.
 #include <algorithm>
 
+#include "launch.h"
 #include "modse_internal.h"
 
 namespace modse {
@@ -1389,13 +1390,9 @@ cudaError_t launch_router_bwd(modse_dtype_t dt, const LayerMeta &m, const void *
                 sms = 148;
             const int grid_mma = std::max(1, std::min(units, 2 * sms));     // two blocks of 118 registers x 256 threads per SM
             const size_t smem = (size_t)8 * kDwrWarpSmem;
-            static bool attr_done = false;
-            if (!attr_done) {
-                cudaError_t e = cudaFuncSetAttribute(router_dwr_mma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     (int)smem);
-                if (e != cudaSuccess) return e;
-                attr_done = true;
-            }
+            static DeviceFlags done;
+            const cudaError_t e = allow_smem(router_dwr_mma_kernel, smem, done);
+            if (e != cudaSuccess) return e;
             router_dwr_mma_kernel<<<grid_mma, 256, smem, s>>>((const __nv_bfloat16 *)x, T, m.d, m.N, m.k, p.topk_idx, p.dz,
                                                              p.dwr_partial, p.logits, p.counts_slot, ascale, dense,
                                                              nblk_dwr, nslice);

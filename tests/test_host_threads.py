@@ -60,3 +60,12 @@ def test_the_checker_sees_a_plain_word(tmp_path):
     if "ThreadSanitizer" not in out.stderr:
         pytest.skip("no thread checker here")
     assert "data race" in out.stderr
+
+
+def test_no_source_keeps_such_a_word_plain():
+    """Plain statics that a call writes: none beside the debugging switches, which are set between calls."""
+    import re
+    for name in sorted(os.listdir(CSRC)):
+        text = open(os.path.join(CSRC, name)).read()
+        for line in re.findall(r"^ +static (?:unsigned|int|bool|long|size_t|[A-Z]\w*Fn)\b[^(\n]*[;{].*$", text, re.M):
+            assert "constexpr" in line or "const " in line, (name, line)
