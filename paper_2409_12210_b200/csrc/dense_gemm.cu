@@ -997,30 +997,22 @@ __global__ void __launch_bounds__(kDenseThreads, 1) dense_gemm_shared(const __gr
 // A 2-D tensor map: `cols` contiguous elements a row, boxes of 128 bytes x box_rows rows, 128-byte swizzle.
 bool encode_operand(CUtensorMap *map, const DenseOperand &o, int type, int box_rows)
 {
-    EncodeTiledFn fn = get_encode();
-    if (fn == nullptr) return false;
     const int esz = type == DenseE4m3 ? 1 : 2;
     const cuuint64_t dims[2] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows};
     const cuuint64_t strides[1] = {(cuuint64_t)(o.ld * esz)};
     const cuuint32_t box[2] = {(cuuint32_t)(128 / esz), (cuuint32_t)box_rows};
-    const cuuint32_t estr[2] = {1, 1};
     const CUtensorMapDataType dt = type == DenseE4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                    : type == DenseF16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    return fn(map, dt, 2, const_cast<void *>(o.base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return encode_tensor_map(map, dt, 2, o.base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
 // An output of 2-byte elements, written in boxes of 32 rows x 64 bytes with the 64-byte swizzle.
 bool encode_output(CUtensorMap *map, const void *base, long long rows, long long cols, long long ld)
 {
-    EncodeTiledFn fn = get_encode();
-    if (fn == nullptr) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
     const cuuint64_t strides[1] = {(cuuint64_t)(ld * 2)};
-    const cuuint32_t box[2] = {32, 32}, estr[2] = {1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const cuuint32_t box[2] = {32, 32};
+    return encode_tensor_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE);
 }
 
 // Tiles up to which clusters of two and of four pairs all find room at once (with 16 clusters of four the last ones waited

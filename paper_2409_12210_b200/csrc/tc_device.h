@@ -274,4 +274,26 @@ inline EncodeTiledFn get_encode()
     return fn;
 }
 
+// A tensor map of `rank` dimensions over an array in device memory, without interleaving; what lies outside reads as zeros.
+inline bool encode_tensor_map(CUtensorMap *map, CUtensorMapDataType type, int rank, const void *base, const cuuint64_t *dims,
+                              const cuuint64_t *strides, const cuuint32_t *box, CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promotion)
+{
+    EncodeTiledFn fn = get_encode();
+    if (fn == nullptr) return false;
+    const cuuint32_t estr[3] = {1, 1, 1};
+    auto encode = [&] {
+        return fn(map, type, rank, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, promotion,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = encode();
+    if (r == CUDA_ERROR_INVALID_CONTEXT) {
+        // The encoder wants a current context.  A host thread whose first call this is has none yet: it gets its device's, as it
+        // would from a launch.
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return false;
+        r = encode();
+    }
+    return r == CUDA_SUCCESS;
+}
+
 }  // namespace modse
