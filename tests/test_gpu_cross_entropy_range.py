@@ -8,7 +8,7 @@ top, 2^-24 of themselves.  A probability of the gradient is exp(z - lse) of the 
 import numpy as np
 import pytest
 
-from test_gpu_cross_entropy import workspace
+from test_gpu_cross_entropy import check_backward, workspace
 
 torch = pytest.importorskip("torch")
 
@@ -178,3 +178,11 @@ def test_few_rows_of_the_gradient_in_the_workspace_of_many():
             outs.append((dx, dw))
         assert all(torch.equal(a, b) for a, b in zip(*outs))
     assert bool((guard == 0xA5).all())
+
+
+# Gradients of training size: dx and dw come out of tiles of 512 rows, dx on top of the pieces ahead (two pieces, one sum), out of
+# four sums that are joined (one piece), and both (100003 words); rows, words and columns all end inside a tile.
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,V", [(5000, 2056, 20011), (2051, 1544, 30011), (2051, 1536, 100003)])
+def test_gradient_of_training_size(T, d, V):
+    check_backward(T, d, V, weighted=d == 1536, seed=V)
