@@ -510,7 +510,8 @@ modse_status_t modse_cross_entropy(int n_tokens, int d_model, int vocabulary, co
  *   f_t = scale dloss_t / total[1]   for counted tokens, 0 for the others.
  * dloss [T] fp32 (NULL: ones), total as forward wrote it (NULL: no division), so that
  * the gradient of the mean loss takes neither arithmetic nor a copy to the host in between.
- * A row whose f is 0 gives nothing, whatever its logits are.  No exponential is above 1.  The logits are formed again,
+ * A row whose f is 0 has a dz of zeros, whatever its logits are (so that dw has a NaN in the columns where such a row of x is
+ * infinite or NaN, and only there).  No exponential is above 1.  The logits are formed again,
  * in fp32 sums that may be cut at other places than forward's: an exponential is off by as much of itself as the rounding of
  * the two sums moves its logit.  dx [T, d] and dw
  * [vocabulary, d] bf16; either may be NULL; both are overwritten and overlap no input.  The

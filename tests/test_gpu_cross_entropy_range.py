@@ -180,9 +180,38 @@ def test_few_rows_of_the_gradient_in_the_workspace_of_many():
     assert bool((guard == 0xA5).all())
 
 
-# Gradients of training size: dx and dw come out of tiles of 512 rows, dx on top of the pieces ahead (two pieces, one sum), out of
-# four sums that are joined (one piece), and both (100003 words); rows, words and columns all end inside a tile.
+# Gradients of training size: dx and dw come out of tiles of 512 rows, dx on top of the piece ahead (two pieces, a sum each), out of
+# four sums that are joined (one piece), both (two pieces, two sums each), and both in tiles of 256 rows (100003 words); rows, words
+# and columns all end inside a tile, and the last round of tiles is halved in the second and third of them.
 @pytest.mark.gpu
-@pytest.mark.parametrize("T,d,V", [(5000, 2056, 20011), (2051, 1544, 30011), (2051, 1536, 100003)])
+@pytest.mark.parametrize("T,d,V", [(5000, 2056, 20011), (2051, 1544, 30011), (4649, 936, 26151), (2051, 1536, 100003)])
 def test_gradient_of_training_size(T, d, V):
-    check_backward(T, d, V, weighted=d == 1536, seed=V)
+    check_backward(T, d, V, weighted=T == 2051, seed=V)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [40, 3000])
+def test_rows_of_x_that_do_not_count(T):
+    """Their dz is 0 whatever their logits are: nothing reaches dx, and dw = dz^T x is as if they were zeros but for the columns
+    where they hold an infinity or a NaN, which 0 times is a NaN."""
+    from paper_2409_12210_b200 import binding as B
+    d, V = 136, 9001
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x, w = torch.randn(T, d, generator=g, device="cuda").bfloat16(), torch.randn(V, d, generator=g, device="cuda").bfloat16()
+    labels = torch.randint(0, V, (T,), generator=g, device="cuda")
+    labels[[3, 4, T - 1]] = torch.tensor([-1, -100, -1], device="cuda")
+    x[[3, 4, T - 1]] = 0
+    outs = []
+    for bad in (False, True):
+        if bad:
+            x[3, 3], x[4, 0], x[4, 100], x[T - 1, 70] = float("nan"), float("inf"), 1e30, float("-inf")
+        loss, lse = forward(x, w, labels)
+        ws, _ = workspace(B.cross_entropy_backward_workspace_bytes(T, d, V))
+        dx, dw = torch.empty_like(x), torch.empty_like(w)
+        B.cross_entropy_backward(x, w, labels, lse, dx, dw, ws)
+        outs.append((loss, dx, dw))
+    (loss, dx, dw), (loss2, dx2, dw2) = outs
+    assert torch.equal(loss, loss2) and torch.equal(dx, dx2) and not bool(dx2[[3, 4, T - 1]].any())
+    apart = torch.ones(d, dtype=torch.bool, device="cuda")
+    apart[[0, 3, 70]] = False
+    assert torch.equal(dw[:, apart], dw2[:, apart]) and bool(dw2[:, ~apart].isnan().all())
