@@ -16,8 +16,7 @@ constexpr int kInBlockExperts = 32;       // rows of router matrices that every 
 // Which experts the tokens meet.  A pick is a token's slot: pick t * k + j.
 struct Routing {
     int met;
-    int expert[kMaxPicks];                // ascending
-    int offset[kMaxPicks], width[kMaxPicks];      // theirs
+    int offset[kMaxPicks], width[kMaxPicks];      // of the experts met, ascending
     int first[kMaxPicks + 1];             // of each expert's picks in `pick`
     int pick[kMaxPicks];                  // ascending within an expert
     float gate[kMaxPicks];                // by pick
@@ -363,7 +362,6 @@ __device__ __forceinline__ void route(const DecodeArgs &p, float *mem, float (&p
             met += (o.x < kMaxExperts) + (o.y < kMaxExperts) + (o.z < kMaxExperts) + (o.w < kMaxExperts);
         }
         if (mine == 0) {
-            r.expert[place] = e;
             r.offset[place] = p.m.hoff[e];
             r.width[place] = p.m.hoff[e + 1] - p.m.hoff[e];
             r.first[place] = before;
