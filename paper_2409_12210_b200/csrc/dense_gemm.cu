@@ -408,16 +408,18 @@ __device__ __forceinline__ void chunk_finish(ChunkInputs<MODE, F8> &in, RowState
         for (int i = 4; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], v[i]);
         const float m = fmaxf(rs.top, fminf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), 3.402823466e38f));
         f32x2 sum = pack2(rs.sum * ex2_approx((rs.top - m) * kLog2e), 0.f);
+        f32x2 more = both(0.f);
         rs.top = m;
         const f32x2 scale = both(kLog2e), shift = both(-m);
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
             float a, b;
             unpack2(mul2(add2(pack2(v[i], v[i + 1]), shift), scale), a, b);
-            sum = add2(sum, pack2(ex2_approx(a), ex2_approx(b)));
+            f32x2 &to = (i & 2) ? more : sum;
+            to = add2(to, pack2(ex2_approx(a), ex2_approx(b)));
         }
         float a, b;
-        unpack2(sum, a, b);
+        unpack2(add2(sum, more), a, b);
         rs.sum = a + b;
     } else if constexpr (MODE == DenseSoftmax) {
         const f32x2 scale = both(kLog2e), shift = both(-rs.lse);
