@@ -5,12 +5,14 @@
 //
 // Forward: the product's epilogue turns every run of 128 logits of a row into their largest and the sum of exponentials
 // over it (DenseLse), 8 bytes for 256; a second kernel joins the runs of a row.  What bounds it is the product (16384 x 2048
-// over 32000: 1366 to 1451 us, 1.48 to 1.57 PFLOP/s).  Up to 32 rows, which are bound by
+// over 32000: 1.42 to 1.49 ms, 1.44 to 1.51 PFLOP/s, by itself; 1.58 to 1.70 in a long row of calls, which the power limit holds down).  Rows of
+// 64 or 256 columns are bound by the epilogue (5000 x 64 over 9000: 37 us).  Up to 32 rows, which are bound by
 // reading w, go through the kernel in cross_entropy_few.cu instead.
 // Gradient: the logits are formed again, a piece of the vocabulary at a time, and leave the product as dz in bf16
 // (DenseSoftmax); dx and dw of the piece follow as one launch, dx on top of the sum of the pieces before (DenseSum).  That
-// is 8 T d V operations with the forward's 2, against 6 of a form that keeps T x V logits.  8192 x 2048 over 32000: 2163 to 2250
-// us, 1.43 to 1.49 PFLOP/s; 2051 x 1536 over 100003: 1551 us, 1.22.
+// is 8 T d V operations with the forward's 2, against 6 of a form that keeps T x V logits.  8192 x 2048 over 32000: 2.11 to 2.24 ms,
+// 1.44 to 1.53 PFLOP/s, by itself, 2.38 to 2.60 in a long row; 2051 x 1536 over 100003: 1.49 to 1.58 ms, 1.20 to 1.27, and 1.71
+// to 1.81.
 //
 // dz is rounded to bf16 once, because the products read 16-bit operands.  A factor that all rows share - the 1 / count of a
 // mean - would be rounded with it, by the same amount everywhere (0.0033 off in norm where the count was 7372, 0.0023 without), so
@@ -25,6 +27,8 @@ namespace {
 
 bool aligned(const void *p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+constexpr float kLog2e = 1.4426950408889634f;
 
 // ---- the runs of a row joined ----
 struct RowsArgs {
@@ -48,7 +52,7 @@ __global__ void __launch_bounds__(1024) loss_rows_kernel(const RowsArgs p)
     wait_for_earlier_kernels();
     allow_next_kernel();
     // a sum brought to another largest number: exp(m - M) is 0 for a run of nothing and must not meet an infinite sum
-    auto to = [](float2 v, float m) { return v.y == INFINITY ? v.y : v.y * expf(v.x - m); };
+    auto to = [](float2 v, float m) { return v.y == INFINITY ? v.y : v.y * exp2f((v.x - m) * kLog2e); };
     const int lo = (int)((long long)p.runs * warp / 32), hi = (int)((long long)p.runs * (warp + 1) / 32);
     const float2 none = make_float2(-3.402823466e38f, 0.f);
     float2 v = none;

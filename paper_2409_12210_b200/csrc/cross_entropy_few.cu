@@ -3,8 +3,8 @@
 // What bounds it is reading w once.  Tiles of 256 rows by 256 of the vocabulary would multiply zeros most of the time, and
 // there would be too few of them to go round (125 for 32000, on 74 pairs of SMs).  Here rows of w are the rows of a
 // tcgen05 product and the tokens its columns, and a tile is as high as gives each block the same number of them: at most 128
-// rows, a multiple of eight (32000: 286 tiles of 112, two a block).  24 rows of 2048 over 32000: 31.5 us, 35.4 as a dense
-// product; 32 of 4096 over 128000: 170 us, 6.2 TB/s, against 195.
+// rows, a multiple of eight (32000: 286 tiles of 112, two a block).  24 rows of 2048 over 32000: 32 to 33 us, 3 more as a
+// dense product; 32 of 4096 over 128000: 172 us, 6.1 TB/s, against 195.
 #include <algorithm>
 
 #include "activations.h"

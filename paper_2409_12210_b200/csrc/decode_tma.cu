@@ -15,11 +15,11 @@
 // warp touches them.  What a block asks for is 128 bytes of each of 128 rows that lie far apart, so the blocks of a group of
 // rows take its column blocks in turn: together they read a few KB of each row at a time.
 //
-// Both kernels of 32 tokens over eight experts of 5632 x 2048 (554 MB, 84 us at the rate of a plain copy): 118 us.  Fragments
-// straight from global memory 130, 16-byte asynchronous copies into rings 178, bulk copies of 256 bytes 270, one ring that
-// all warps share 198, rows of x gathered by TMA (0.25 us for four rows) 376.  One token of the same layer (138 MB, 21 us): 37 us, of
-// which 4 are the routing, which every block does for itself, and 2 to 3 each the first data's way and the meeting of
-// the blocks that share a group of rows, in both kernels.
+// Both kernels of 32 tokens over eight experts of 5632 x 2048 (554 MB, 84 us at the rate of a plain copy): 118 us (153 as
+// modse_forward).  Fragments straight from global memory 130, 16-byte asynchronous copies into rings 178, bulk copies of 256 bytes
+// 270, one ring that all warps share 198, rows of x gathered by TMA (0.25 us for four rows) 376.  One token of the same layer
+// (138 MB, 21 us): 38 us (91 as modse_forward), of which 4 are the routing, which every block does for itself, and 2 to 3 each the
+// first data's way and the meeting of the blocks that share a group of rows, in both kernels.
 //
 // A fragment's rows lie 128 bytes apart in a stage, swizzled by TMA in 16-byte pieces.  Row i of a fragment's half plays row
 // row_of(i) of the stage, so that the two rows that eight neighbouring lanes read lie in opposite halves of the banks.
