@@ -1,5 +1,5 @@
 """What the library remembers of a device between calls may be asked and set by any host thread: built with the compiler's
-thread checker, on the CPU."""
+thread sanitizer, on the CPU."""
 import os
 import shutil
 import subprocess
@@ -40,7 +40,7 @@ def build(tmp_path, source, name):
     cmd = ["g++", "-std=c++17", "-O1", "-g", "-pthread", "-fsanitize=thread", "-I", CSRC, str(src), "-o", str(exe)]
     made = subprocess.run(cmd, capture_output=True).returncode == 0
     if not made or "FATAL: ThreadSanitizer" in subprocess.run([str(exe)], capture_output=True, text=True, timeout=120).stderr:
-        # where the checker is missing or does not run, the program still has to build
+        # where the sanitizer is missing or does not run, the program still has to build
         subprocess.run([c for c in cmd if c != "-fsanitize=thread"], check=True)
     return str(exe)
 
@@ -50,7 +50,7 @@ def test_flags_of_devices_are_free_of_races(tmp_path):
     assert out.returncode == 0 and out.stdout == "done\n", out.stdout + out.stderr
 
 
-def test_the_checker_sees_a_plain_word(tmp_path):
+def test_the_sanitizer_sees_a_plain_word(tmp_path):
     """The mistake planted: the same program on a class without atomics."""
     plain = PROGRAM.replace('#include "device_flags.h"', """namespace modse { struct DeviceFlags {
         unsigned long long bits = 0;
@@ -58,7 +58,7 @@ def test_the_checker_sees_a_plain_word(tmp_path):
         void set(int d) { if (d >= 0 && d < 64) bits |= 1ull << d; } }; }""")
     out = subprocess.run([build(tmp_path, plain, "plain")], capture_output=True, text=True, timeout=120)
     if "ThreadSanitizer" not in out.stderr:
-        pytest.skip("no thread checker here")
+        pytest.skip("no thread sanitizer here")
     assert "data race" in out.stderr
 
 
